@@ -15,9 +15,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhgemm.so")
 LIB_CHECKED = os.path.join(HERE, "libhgemm_checked.so")      # the same sources with -DHGEMM_CHECKED=1 (see include/hgemm.h)
-SOURCES = ["hgemm_api.cu", "hgemm_static_scratch.cu", "hgemm_planner.cpp", "hgemm_table.cpp"]
-DEPS = SOURCES + ["hgemm_kernel.cuh", "hgemm_light_kernel.cuh", "hgemm_small_kernel.cuh", "ptx_sm100.cuh", "hgemm_planner.h", "hgemm_table.inc",
-                  os.path.join("..", "..", "include", "hgemm.h")]
+SOURCES = ["hgemm_api.cu", "hgemm_static_scratch.cu", "hgemm_planner.cpp", "hgemm_table.cpp", "fp8_api.cu", "routing_api.cu"]
+DEPS = SOURCES + ["hgemm_context.h", "hgemm_device.cuh", "fp8_product_kernel.cuh", "fp8_quantize_kernel.cuh", "routing_kernel.cuh", "hgemm_kernel.cuh", "hgemm_light_kernel.cuh", "hgemm_small_kernel.cuh", "ptx_sm100.cuh", "hgemm_planner.h", "hgemm_table.inc",
+                  os.path.join("..", "..", "include", "hgemm.h"), os.path.join("..", "..", "include", "hgemm_fp8.h"),
+                  os.path.join("..", "..", "include", "hgemm_routing.h")]
 
 
 def _nvcc() -> str:
@@ -40,7 +41,7 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
         return lib
     tmp = lib + f".tmp{os.getpid()}"
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-o", tmp]
+           "--threads", "4", "-shared", "-Xcompiler", "-fPIC", "-o", tmp]
     if checked:
         cmd += ["-DHGEMM_CHECKED=1"]
     if verbose:

@@ -1,0 +1,563 @@
+// The 8-bit product with block scales: D = sum_b sP[., b] sQ[., b] (P_b Q_b^T), b = blocks of 128 of the contraction.
+//
+// fp32 scales rule out letting the tensor cores sum the whole contraction (their own block scales are powers of two), so each
+// block of 128 is a product of its own: four tcgen05.mma (kind::f8f6f4, K = 32) into a fresh tensor-memory accumulator, which
+// eight warps then read, multiply by the block's scales and add to running sums in REGISTERS ("promotion").  One accumulator is
+// read while the next is computed, so the tensor pipe and the promotion overlap; the budget per block and SM of a 256 x 256
+// pair tile is 512 cycles of MMA against 256 cycles of tensor-memory reads and 128 (one scale per row and 128-column block) or
+// 256 (a scale per column) cycles of packed fp32 multiply-adds per scheduler.
+//
+// Roles (384 threads): warp 0 fills a ring of shared-memory stages by TMA (one stage = one block of 128: 128 bytes of every
+// row, or 128 rows of 128 columns where an operand is stored along its own dimension); warp 1 issues the MMAs; warp 2 fetches
+// the blocks' scales into a ring of their own with 4-byte asynchronous copies; warps 4..11 promote and store.
+//
+// Two shapes: CTA pairs with 256 x 256 tiles, results stored by rows through a small staging buffer (large problems); single
+// CTAs with 128 x BN tiles, BN = 16 .. 128, for which P is the WEIGHT (its rows fill the 128 lanes of an accumulator
+// however few tokens there are) and the tile is stored transposed; there the CTAs of a cluster may share one tile's
+// contraction and add their parts through distributed shared memory in rank order.
+//
+// Products over experts: the tiles of all groups are numbered through with prefix sums of the groups' tile counts, which
+// every CTA computes for itself from the offsets.  A tile never crosses a group; the rows it computes beyond its group's end
+// are not stored.  Weight gradients contract over a group's rows, which the column-quantised copy pads with zeros to whole blocks.
+//
+// Every mbarrier wait is bounded (see hgemm_device.cuh): a wait that runs out raises the status word and the CTA's abort flag, and
+// every role falls through to the common teardown.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "hgemm_device.cuh"
+
+namespace hgemm_dev {
+
+constexpr int kFp8Threads = 384;
+constexpr int kFp8Block = 128;                    // the scales' block, and one stage's share of the contraction
+constexpr int kFp8PBytes = 128 * 128;             // P part of a stage: 128 rows of 128 bytes
+constexpr int kFp8MaxStages = 12;
+constexpr int kFp8MaxGroups = 1024;
+constexpr int kFp8CtrlBytes = 512;
+constexpr int kFp8StagingPerWarp = 2048;          // direct stores: 32 rows x 64 bytes
+constexpr uint32_t kRoleFp8Load = 8, kRoleFp8Mma = 9, kRoleFp8Scale = 10, kRoleFp8Promote = 11;
+
+// which side of the tile grid follows the groups' offsets
+enum : int32_t { kRaggedNone = 0, kRaggedP = 1, kRaggedQ = 2, kRaggedK = 3 };
+
+struct Fp8Params {
+    int32_t rows_p, rows_q;        // rows of P and Q (per group, or all of them on the side that follows the offsets)
+    int32_t kblocks;               // blocks of the contraction (not with kRaggedK)
+    int32_t tiles_p, tiles_q;      // tiles per group (unused for the side that follows the offsets)
+    int32_t total;                 // tiles, where the host knows them (kRaggedNone, kRaggedK)
+    int32_t raster;                // tiles of P visited together
+    int32_t groups, ragged, rows_ragged, k_capacity;   // rows_ragged: clamp of the offsets; k_capacity: blocks the padded copy has
+    const int32_t *offsets;
+    const float *sp, *sq;          // scale of row r (or of block r / 128), block b: s[r * _row + b * _kb + group * _group]
+    int64_t sp_row, sp_kb, sp_group, sq_row, sq_kb, sq_group;
+    void *out;
+    int64_t ldc, c_group;
+    int32_t out_type, accumulate, vec_ok;   // out_type: 0 fp32, 1 fp16, 2 bf16; vec_ok: rows of C start at multiples of 16 bytes
+    int32_t split, stages;
+    int32_t p_mn, q_mn;            // operand stored along its own rows' dimension (contraction down the columns)
+    uint32_t idesc;
+    uint32_t *status;
+    long long wait_budget;
+};
+
+struct Fp8Tile {
+    int32_t group, p0, p_end, q0, q_end, kb0, kbn;
+};
+
+// The tile with number w; whole (converged) warp.  pre: prefix sums over the groups (tiles, or blocks for kRaggedK); off: clamped offsets.
+template <int TP, int TQ>
+__device__ __forceinline__ Fp8Tile fp8_tile(int32_t w, const Fp8Params &p, const int32_t *pre, const int32_t *off, uint32_t lane)
+{
+    Fp8Tile t;
+    t.group = 0;
+    t.kb0 = 0;
+    t.kbn = p.kblocks;
+    t.p_end = p.rows_p;
+    t.q_end = p.rows_q;
+    if (p.ragged == kRaggedP || p.ragged == kRaggedQ) {
+        const int32_t other = p.ragged == kRaggedP ? p.tiles_q : p.tiles_p;
+        const int32_t r = w / other, o = w - r * other;
+        int32_t g = 0;                                   // groups whose tiles all come before r
+        for (int32_t base = 0; base < p.groups; base += 32) {
+            const int32_t e = base + static_cast<int32_t>(lane);
+            const uint32_t before = __ballot_sync(0xffffffffu, e < p.groups && pre[e + 1] <= r);
+            g += __popc(before);
+            if (before != 0xffffffffu) break;
+        }
+        t.group = g;
+        const int32_t i = r - pre[g];
+        if (p.ragged == kRaggedP) {
+            t.p0 = off[g] + i * TP;
+            t.p_end = off[g + 1];
+            t.q0 = o * TQ;
+        } else {
+            t.q0 = off[g] + i * TQ;
+            t.q_end = off[g + 1];
+            t.p0 = o * TP;
+        }
+        return t;
+    }
+    if (p.ragged == kRaggedK) {
+        const int32_t per = p.tiles_p * p.tiles_q;
+        t.group = w / per;
+        w -= t.group * per;
+        t.kb0 = pre[t.group];
+        t.kbn = pre[t.group + 1] - t.kb0;
+    }
+    const int32_t per_group = p.raster * p.tiles_q;
+    const int32_t rg = w / per_group, first = rg * p.raster, size = min(p.raster, p.tiles_p - first), rem = w - rg * per_group;
+    const int32_t tq = rem / size;
+    t.p0 = (first + rem - tq * size) * TP;
+    t.q0 = tq * TQ;
+    return t;
+}
+
+// Clamped offsets and the prefix sums fp8_tile reads; one whole warp.
+__device__ __forceinline__ void fp8_scan_groups(const Fp8Params &p, int32_t *pre, int32_t *off, int32_t unit, uint32_t lane)
+{
+    int32_t carry = 0, last = 0;
+    for (int32_t base = 0; base < p.groups; base += 32) {
+        const int32_t e = base + static_cast<int32_t>(lane);
+        int32_t o = p.offsets[min(e, p.groups)];
+        o = min(max(o, 0), p.rows_ragged);
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {               // non-decreasing whatever the caller's values
+            const int32_t x = __shfl_up_sync(0xffffffffu, o, d);
+            if (static_cast<int32_t>(lane) >= d) o = max(o, x);
+        }
+        o = max(o, last);
+        int32_t nxt = __shfl_down_sync(0xffffffffu, o, 1);
+        if (lane == 31) nxt = max(o, min(max(p.offsets[min(e + 1, p.groups)], 0), p.rows_ragged));
+        last = __shfl_sync(0xffffffffu, nxt, 31);
+        int32_t n = e < p.groups ? (nxt - o + unit - 1) / unit : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int32_t x = __shfl_up_sync(0xffffffffu, n, d);
+            if (static_cast<int32_t>(lane) >= d) n += x;
+        }
+        if (e < p.groups) {
+            off[e] = o;
+            off[e + 1] = nxt;
+            pre[e + 1] = p.ragged == kRaggedK ? min(carry + n, p.k_capacity) : carry + n;
+        }
+        carry += __shfl_sync(0xffffffffu, n, 31);
+    }
+    if (lane == 0) pre[0] = 0;
+}
+
+template <class T>
+__device__ __forceinline__ T fp8_to(float v);
+template <>
+__device__ __forceinline__ float fp8_to<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half fp8_to<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 fp8_to<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ uint32_t fp8_pack2(float a, float b, __half)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ uint32_t fp8_pack2(float a, float b, __nv_bfloat16)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// One warp's 32 rows x 128 columns of running sums to C, by rows: 64 bytes of every row at a time through the warp's staging
+// buffer (16-byte pieces XOR-swizzled by row pairs: conflict-free both ways), so that four lanes write 64 consecutive bytes.
+template <class T>
+__device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32_t staging, const Fp8Params &p, T *out, int32_t row0, int32_t row_end,
+                                               int32_t col0, int32_t col_end, uint32_t lane)
+{
+    constexpr int kCols = 64 / static_cast<int>(sizeof(T));     // columns of one pass
+    constexpr int kPer = 16 / static_cast<int>(sizeof(T));      // elements of 16 bytes
+    const uint32_t mine = staging + lane * 64u, swz = (lane >> 1) & 3u;
+#pragma unroll
+    for (int c = 0; c < 128; c += kCols) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(T) == 4) {
+                    float lo, hi;
+                    unpack_f32x2(acc[(c + j * 4 + i) / 2], lo, hi);
+                    v[i] = __float_as_uint((i & 1) ? hi : lo);
+                } else {
+                    float lo, hi;
+                    unpack_f32x2(acc[(c + j * 8) / 2 + i], lo, hi);
+                    v[i] = fp8_pack2(lo, hi, T());
+                }
+            }
+            st_shared_v4(mine + ((static_cast<uint32_t>(j) ^ swz) * 16u), v[0], v[1], v[2], v[3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t r = static_cast<uint32_t>(i) * 8u + lane / 4u, k = lane & 3u;
+            const int32_t row = row0 + static_cast<int32_t>(r), col = col0 + c + static_cast<int32_t>(k) * kPer;
+            float4 v = ld_shared_v4(staging + r * 64u + ((k ^ ((r >> 1) & 3u)) * 16u));
+            if (row < row_end && col < col_end) {
+                T *dst = out + static_cast<int64_t>(row) * p.ldc + col;
+                if (p.vec_ok && col + kPer <= col_end) {
+                    if constexpr (sizeof(T) == 4) {
+                        if (p.accumulate) {
+                            const float4 old = *reinterpret_cast<const float4 *>(dst);
+                            v.x += old.x; v.y += old.y; v.z += old.z; v.w += old.w;
+                        }
+                    }
+                    *reinterpret_cast<float4 *>(dst) = v;
+                } else {
+                    const T *src = reinterpret_cast<const T *>(&v);
+#pragma unroll
+                    for (int x = 0; x < kPer; ++x) {
+                        if (col + x >= col_end) break;
+                        if constexpr (sizeof(T) == 4) dst[x] = p.accumulate ? dst[x] + src[x] : src[x];
+                        else dst[x] = src[x];
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void fp8_store_one(T *dst, float v, int32_t accumulate)
+{
+    if constexpr (sizeof(T) == 4) *dst = accumulate ? *dst + v : v;
+    else *dst = fp8_to<T>(v);
+}
+
+// CG: CTAs per tile.  BN: rows of Q per tile.  P_ROW: P has a scale per row (else one per 128 rows).  Q_COL: Q has a scale per row
+// (else one per 128).  CG == 2 stores by rows, CG == 1 transposed.
+template <int CG, int BN, bool P_ROW, bool Q_COL>
+__global__ void __launch_bounds__(kFp8Threads, 1)
+fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_constant__ CUtensorMap tmap_q, const Fp8Params p)
+{
+    constexpr int TP = 128 * CG, TQ = BN;
+    constexpr int kCols = BN / 2;                                 // columns of the tile a promoting warp holds
+    constexpr int kBufs = BN == 256 ? 2 : 4;                      // accumulators
+    constexpr uint32_t kTmemCols = kBufs * BN;
+    constexpr uint32_t kStageBytes = kFp8PBytes + (BN / CG) * 128;
+    constexpr int kRing = CG == 2 ? 4 : 8;                        // blocks of scales in flight
+    constexpr uint32_t kSlotBytes = (128 + BN) * 4;
+    static_assert(kTmemCols >= 32 && (kTmemCols & (kTmemCols - 1)) == 0 && kTmemCols <= 512, "tensor memory is allocated in powers of two");
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+    uint8_t *smem_gen = smem_raw + (smem_base - smem_addr(smem_raw));
+    const uint32_t staging_base = smem_base + static_cast<uint32_t>(p.stages) * kStageBytes;
+    const uint32_t ring_base = staging_base + (CG == 2 ? 8u * kFp8StagingPerWarp : 0u);
+    const uint32_t ctrl_base = ring_base + kRing * kSlotBytes;
+    uint8_t *ctrl_gen = smem_gen + (ctrl_base - smem_base);
+    const uint32_t bar_full = ctrl_base, bar_empty = bar_full + 8 * kFp8MaxStages, bar_tfull = bar_empty + 8 * kFp8MaxStages, bar_tempty = bar_tfull + 32;
+    const uint32_t bar_sfull = bar_tempty + 32, bar_sempty = bar_sfull + 64;          // ends at 384
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 384);
+    volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 388);
+    int32_t *pre = reinterpret_cast<int32_t *>(ctrl_gen + kFp8CtrlBytes);             // groups + 1 each
+    int32_t *off = pre + (p.groups + 1);
+
+    const uint32_t warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
+    const uint32_t lane = lane_id();
+    const bool in_cluster = CG == 2 || p.split > 1;
+    const uint32_t rank = in_cluster ? cluster_ctarank() : 0u;    // place in the pair, or slice of the contraction
+    const bool is_leader = CG == 1 || rank == 0;
+    const int32_t per_unit = CG == 2 ? 2 : p.split;
+    const int32_t unit = static_cast<int32_t>(blockIdx.x) / per_unit, units = static_cast<int32_t>(gridDim.x) / per_unit;
+    WaitCtl ctl{abort_flag, p.status, p.wait_budget};
+
+    grid_launch_dependents();
+    if (threadIdx.x == 0) {
+        *abort_flag = 0u;
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(bar_full + 8 * s, CG);
+            mbar_init(bar_empty + 8 * s, 1);
+        }
+        for (int b = 0; b < kBufs; ++b) {
+            mbar_init(bar_tfull + 8 * b, 1);
+            mbar_init(bar_tempty + 8 * b, 8 * CG);
+        }
+        for (int s = 0; s < kRing; ++s) {
+            mbar_init(bar_sfull + 8 * s, 32);
+            mbar_init(bar_sempty + 8 * s, 8);
+        }
+        fence_mbar_init();
+        prefetch_tensormap(&tmap_p);
+        prefetch_tensormap(&tmap_q);
+    }
+    if (warp == 1) tmem_alloc<CG>(smem_addr(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
+    // No thread reads or writes global memory before the kernels ahead in the stream are complete.
+    grid_dependency_wait();
+    if (warp == 2 && p.groups > 0) fp8_scan_groups(p, pre, off, p.ragged == kRaggedK ? kFp8Block : p.ragged == kRaggedP ? TP : TQ, lane);
+    tc_fence_before_sync();
+    __syncthreads();
+    if (in_cluster) {
+        cluster_arrive();
+        cluster_wait();
+    }
+    tc_fence_after_sync();
+    const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    const int32_t total = p.ragged == kRaggedP ? pre[p.groups] * p.tiles_q : p.ragged == kRaggedQ ? pre[p.groups] * p.tiles_p : p.total;
+
+    auto tile_of = [&](int32_t w) {
+        Fp8Tile t = fp8_tile<TP, TQ>(w, p, pre, off, lane);
+        if (CG == 1 && p.split > 1) {                              // this CTA's share of the contraction
+            const int32_t b = t.kbn * static_cast<int32_t>(rank) / p.split, e = t.kbn * (static_cast<int32_t>(rank) + 1) / p.split;
+            t.kb0 += b;
+            t.kbn = e - b;
+        }
+        return t;
+    };
+
+    if (warp == 0) {
+        // ===== operands =====
+        if constexpr (CG == 2) regs_lower<56>();
+        int s = 0;
+        uint32_t ph = 0;
+        const uint32_t full_leader = CG == 2 ? mapa(bar_full, 0) : bar_full;
+        bool ok = true;
+        for (int32_t w = unit; ok && w < total; w += units) {
+            const Fp8Tile t = tile_of(w);
+            const int32_t prow = t.p0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * 128, qrow = t.q0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * (BN / CG);
+            const int32_t pz = p.ragged == kRaggedQ ? t.group : 0, qz = p.ragged == kRaggedP ? t.group : 0;      // the operand with one matrix per group
+            for (int32_t kb = 0; kb < t.kbn; ++kb) {
+                ok = mbar_wait(bar_empty + 8 * s, ph ^ 1u, ctl, status_code(kRoleFp8Load, 0, s));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t p_dst = smem_base + static_cast<uint32_t>(s) * kStageBytes, q_dst = p_dst + kFp8PBytes;
+                const int32_t k0 = (t.kb0 + kb) * kFp8Block;
+                const uint32_t fb = full_leader + 8 * s;
+                if constexpr (CG == 1) {
+                    mbar_arrive_expect_tx_elect(bar_full + 8 * s, kStageBytes);
+                    tma_load_3d_elect(p_dst, &tmap_p, p.p_mn ? prow : k0, p.p_mn ? k0 : prow, pz, fb);
+                    tma_load_3d_elect(q_dst, &tmap_q, p.q_mn ? qrow : k0, p.q_mn ? k0 : qrow, qz, fb);
+                } else {
+                    if (is_leader) mbar_arrive_expect_tx_elect(bar_full + 8 * s, kStageBytes);
+                    else mbar_arrive_expect_tx_cluster_relaxed_elect(fb, kStageBytes);
+                    tma_load_3d_pair_elect(p_dst, &tmap_p, p.p_mn ? prow : k0, p.p_mn ? k0 : prow, pz, fb);
+                    tma_load_3d_pair_elect(q_dst, &tmap_q, p.q_mn ? qrow : k0, p.q_mn ? k0 : qrow, qz, fb);
+                }
+                if (++s == p.stages) { s = 0; ph ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {
+        // ===== MMA issuer =====
+        if constexpr (CG == 2) regs_lower<56>();
+        if (is_leader) {
+            int s = 0;
+            uint32_t ph = 0, buf = 0, bph = 0;
+            const uint64_t desc_p0 = p.p_mn ? make_smem_desc_sw128_mn_major(smem_base, kFp8PBytes) : make_smem_desc_sw128(smem_base);
+            const uint64_t desc_q0 = p.q_mn ? make_smem_desc_sw128_mn_major(smem_base + kFp8PBytes, kFp8PBytes) : make_smem_desc_sw128(smem_base + kFp8PBytes);
+            // 32 further along the contraction: 32 bytes inside a swizzled row, or 32 rows of 128 bytes
+            const uint32_t p_step = p.p_mn ? (32u * 128u) >> 4 : 2u, q_step = p.q_mn ? (32u * 128u) >> 4 : 2u;
+            bool ok = true;
+            for (int32_t w = unit; ok && w < total; w += units) {
+                const int32_t kbn = __shfl_sync(0xffffffffu, tile_of(w).kbn, 0);
+                for (int32_t kb = 0; kb < kbn; ++kb) {
+                    ok = mbar_wait(bar_tempty + 8 * buf, bph ^ 1u, ctl, status_code(kRoleFp8Mma, 1, buf));
+                    ok = ok && mbar_wait(bar_full + 8 * s, ph, ctl, status_code(kRoleFp8Mma, 0, s));
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint64_t dp = desc_p0 + static_cast<uint64_t>(static_cast<uint32_t>(s) * (kStageBytes >> 4));
+                    const uint64_t dq = desc_q0 + static_cast<uint64_t>(static_cast<uint32_t>(s) * (kStageBytes >> 4));
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) umma_f8_elect<CG>(tmem_base + buf * BN, dp + k * p_step, dq + k * q_step, p.idesc, k);
+                    umma_commit_elect<CG>(bar_empty + 8 * s, 0);
+                    umma_commit_elect<CG>(bar_tfull + 8 * buf, 0);
+                    if (++s == p.stages) { s = 0; ph ^= 1u; }
+                    if (++buf == kBufs) { buf = 0; bph ^= 1u; }
+                }
+            }
+        }
+    } else if (warp == 2) {
+        // ===== scales =====
+        if constexpr (CG == 2) regs_lower<56>();
+        int s = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        for (int32_t w = unit; ok && w < total; w += units) {
+            const Fp8Tile t = tile_of(w);
+            const int32_t prow = t.p0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * 128;
+            const float *sp = p.sp + t.group * p.sp_group, *sq = p.sq + t.group * p.sq_group;
+            for (int32_t kb = 0; kb < t.kbn; ++kb) {
+                ok = mbar_wait(bar_sempty + 8 * s, ph ^ 1u, ctl, status_code(kRoleFp8Scale, 0, s));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t slot = ring_base + static_cast<uint32_t>(s) * kSlotBytes;
+                const float *spk = sp + (t.kb0 + kb) * p.sp_kb, *sqk = sq + (t.kb0 + kb) * p.sq_kb;
+                if constexpr (P_ROW) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int32_t r = prow + i * 32 + static_cast<int32_t>(lane);
+                        cp_async_4(slot + (i * 32 + lane) * 4u, r < t.p_end ? spk + r * p.sp_row : spk, r < t.p_end ? 4u : 0u);
+                    }
+                } else {
+                    if (lane == 0) cp_async_4(slot, spk + (prow >> 7) * p.sp_row, 4u);
+                }
+                if constexpr (Q_COL) {
+#pragma unroll
+                    for (int i = 0; i < (BN + 31) / 32; ++i) {
+                        const int32_t c = i * 32 + static_cast<int32_t>(lane), r = t.q0 + c;
+                        if (BN >= 32 || c < BN) cp_async_4(slot + 512u + c * 4u, r < t.q_end ? sqk + r * p.sq_row : sqk, r < t.q_end ? 4u : 0u);
+                    }
+                } else {
+                    const int32_t r = t.q0 + static_cast<int32_t>(lane) * 128;
+                    if (lane < BN / 128) cp_async_4(slot + 512u + lane * 4u, r < t.q_end ? sqk + (r >> 7) * p.sq_row : sqk, r < t.q_end ? 4u : 0u);
+                }
+                cp_async_mbar_arrive(bar_sfull + 8 * s);
+                if (++s == kRing) { s = 0; ph ^= 1u; }
+            }
+        }
+        cp_async_wait_all();
+    } else if (warp == 3) {
+        if constexpr (CG == 2) regs_lower<56>();
+    } else {
+        // ===== promotion (warps 4..11) =====
+        if constexpr (CG == 2) regs_raise<224>();
+        const uint32_t ew = warp - 4u, quarter = warp & 3u, half = ew >> 2;         // half: first or second BN / 2 columns
+        const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + half * kCols;
+        const uint32_t row_in_tile = quarter * 32u + lane;
+        const uint32_t tempty_leader = CG == 2 ? mapa(bar_tempty, 0) : bar_tempty;
+        int s = 0;
+        uint32_t ph = 0, buf = 0, bph = 0;
+        bool ok = true;
+        for (int32_t w = unit; ok && w < total; w += units) {
+            const Fp8Tile t = tile_of(w);
+            uint64_t acc[kCols / 2];
+#pragma unroll
+            for (int i = 0; i < kCols / 2; ++i) acc[i] = 0ull;
+            for (int32_t kb = 0; kb < t.kbn; ++kb) {
+                ok = mbar_wait_inline(bar_sfull + 8 * s, ph, ctl, status_code(kRoleFp8Promote, 0, s));
+                const uint32_t slot = ring_base + static_cast<uint32_t>(s) * kSlotBytes;
+                float sc = ld_shared_f32(slot + (P_ROW ? row_in_tile * 4u : 0u));
+                if constexpr (!Q_COL) sc *= ld_shared_f32(slot + 512u + half * 4u);
+                const uint64_t sc2 = pack_f32x2(__float_as_uint(sc), __float_as_uint(sc));
+                const uint32_t sq = slot + 512u + half * kCols * 4u;
+                ok = ok && mbar_wait_inline(bar_tfull + 8 * buf, bph, ctl, status_code(kRoleFp8Promote, 1, buf));
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after_sync();
+                constexpr int kChunk = kCols < 32 ? kCols : 32;
+#pragma unroll
+                for (int c = 0; c < kCols; c += kChunk) {
+                    uint32_t v[kChunk];
+                    if constexpr (kChunk == 32) tmem_ld_32x32b_x32(taddr + buf * BN + c, v);
+                    else if constexpr (kChunk == 16) tmem_ld_32x32b_x16(taddr + buf * BN + c, v);
+                    else tmem_ld_32x32b_x8(taddr + buf * BN + c, v);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < kChunk; i += 4) {
+                        uint64_t s0 = sc2, s1 = sc2;
+                        if constexpr (Q_COL) {
+                            ld_shared_2x64(sq + (c + i) * 4u, s0, s1);
+                            s0 = mul_f32x2(s0, sc2);
+                            s1 = mul_f32x2(s1, sc2);
+                        }
+                        acc[(c + i) / 2] = fma_f32x2(pack_f32x2(v[i], v[i + 1]), s0, acc[(c + i) / 2]);
+                        acc[(c + i) / 2 + 1] = fma_f32x2(pack_f32x2(v[i + 2], v[i + 3]), s1, acc[(c + i) / 2 + 1]);
+                    }
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {
+                    if (is_leader) mbar_arrive(bar_tempty + 8 * buf);
+                    else mbar_arrive_cluster(tempty_leader + 8 * buf);
+                    mbar_arrive(bar_sempty + 8 * s);
+                }
+                if (++s == kRing) { s = 0; ph ^= 1u; }
+                if (++buf == kBufs) { buf = 0; bph ^= 1u; }
+            }
+            if (!ok) break;
+            if constexpr (CG == 2) {
+                const int32_t row0 = t.p0 + static_cast<int32_t>(rank * 128u + quarter * 32u), col0 = t.q0 + static_cast<int32_t>(half) * 128;
+                const uint32_t staging = staging_base + ew * kFp8StagingPerWarp;
+                const int64_t base = t.group * p.c_group;
+                if (p.out_type == 0) fp8_store_rows<float>(acc, staging, p, static_cast<float *>(p.out) + base, row0, t.p_end, col0, t.q_end, lane);
+                else if (p.out_type == 1) fp8_store_rows<__half>(acc, staging, p, static_cast<__half *>(p.out) + base, row0, t.p_end, col0, t.q_end, lane);
+                else fp8_store_rows<__nv_bfloat16>(acc, staging, p, static_cast<__nv_bfloat16 *>(p.out) + base, row0, t.p_end, col0, t.q_end, lane);
+            } else if (p.split > 1) {
+                // this slice's part, columns of 128 rows, where the operand stages were (every MMA that read them is complete)
+#pragma unroll
+                for (int i = 0; i < kCols / 2; ++i) {
+                    float lo, hi;
+                    unpack_f32x2(acc[i], lo, hi);
+                    const uint32_t at = smem_base + ((half * kCols + 2 * i) * 128u + row_in_tile) * 4u;
+                    st_shared_f32(at, lo);
+                    st_shared_f32(at + 512u, hi);
+                }
+            } else {
+                const int32_t row = t.p0 + static_cast<int32_t>(row_in_tile);
+                if (row < t.p_end) {
+                    const int64_t base = t.group * p.c_group + row;
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i) {
+                        const int32_t col = t.q0 + static_cast<int32_t>(half) * kCols + i;
+                        if (col < t.q_end) {
+                            float lo, hi;
+                            unpack_f32x2(acc[i / 2], lo, hi);
+                            const float v = (i & 1) ? hi : lo;
+                            const int64_t at = base + static_cast<int64_t>(col) * p.ldc;
+                            if (p.out_type == 0) fp8_store_one(static_cast<float *>(p.out) + at, v, p.accumulate);
+                            else if (p.out_type == 1) fp8_store_one(static_cast<__half *>(p.out) + at, v, 0);
+                            else fp8_store_one(static_cast<__nv_bfloat16 *>(p.out) + at, v, 0);
+                        }
+                    }
+                }
+            }
+        }
+    }
+
+    // ---- sum over the slices of a tile (one tile per cluster: gridDim.x = split * tiles) --------------------------
+    __syncwarp();
+    if (CG == 1 && p.split > 1) {
+        cluster_arrive();
+        cluster_wait();
+        if (unit < total && !*abort_flag) {
+            const Fp8Tile t = fp8_tile<TP, TQ>(unit, p, pre, off, lane);
+            const int32_t share = BN / p.split, row = t.p0 + static_cast<int32_t>(lane) * 4;
+            for (int32_t c = static_cast<int32_t>(rank) * share + static_cast<int32_t>(warp); c < (static_cast<int32_t>(rank) + 1) * share; c += kFp8Threads / 32) {
+                const int32_t col = t.q0 + c;
+                if (col >= t.q_end) break;
+                float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                for (int32_t r = 0; r < p.split; ++r) {
+                    const float4 x = ld_shared_cluster_v4(mapa(smem_base + (static_cast<uint32_t>(c) * 128u + lane * 4u) * 4u, static_cast<uint32_t>(r)));
+                    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+                }
+                const int64_t at = t.group * p.c_group + static_cast<int64_t>(col) * p.ldc + row;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (row + i < t.p_end) {
+                        if (p.out_type == 0) fp8_store_one(static_cast<float *>(p.out) + at + i, v[i], p.accumulate);
+                        else if (p.out_type == 1) fp8_store_one(static_cast<__half *>(p.out) + at + i, v[i], 0);
+                        else fp8_store_one(static_cast<__nv_bfloat16 *>(p.out) + at + i, v[i], 0);
+                    }
+                }
+            }
+        }
+    }
+
+    // ---- teardown (every thread, also after an abort) -----------------------------------------------------------------
+    tc_fence_before_sync();
+    __syncthreads();
+    if (in_cluster) {                            // no CTA leaves while another may still signal it or read its shared memory
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (warp == 1) {
+        if (*abort_flag)
+            for (int i = 0; i < 200; ++i) __nanosleep(1000);      // loads and MMAs in flight when a wait ran out
+        tc_fence_after_sync();
+        tmem_dealloc<CG>(tmem_base, kTmemCols);
+    }
+}
+
+} // namespace hgemm_dev

@@ -9,37 +9,14 @@
 #include <vector>
 
 #include "../../include/hgemm.h"
+#include "../../include/hgemm_fp8.h"
+#include "hgemm_context.h"
 #include "hgemm_kernel.cuh"
 #include "hgemm_light_kernel.cuh"
 #include "hgemm_small_kernel.cuh"
 #include "hgemm_planner.h"
 
 using hgemm_dev::KernelParams;
-
-typedef CUresult (*encode_tiled_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
-                                    const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
-                                    CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// Device status words: one array per context.  Slot 0 belongs to the context itself (the timeout probe), every
-// plan owns one of the others, so that a wait that ran out names the plan whose launch it was.
-constexpr int kStatusSlots = 4096;
-
-struct hgemm_ctx_s {
-    int device = 0;
-    int num_sms = 0;
-    uint32_t *d_status = nullptr;          // kStatusSlots words
-    std::vector<int> free_status_slots;    // slots no plan owns (never holds 0)
-    int pass_allocs = 0, fail_allocs = 0;  // test hook: after pass_allocs more device allocations, fail_allocs of them report failure
-    long long wait_budget = 2000000000LL;
-    encode_tiled_fn encode = nullptr;
-    int last_cuda_error = 0;
-    bool dependent_launch = true;
-    bool tma_3d = true;
-    std::vector<hgemm_plan_s *> plans;
-    // hgemm_run_host: the operand copies and the result copy run on streams of their own (created by its first call), so that
-    // one call's copies overlap the compute and the opposite-direction copy of the calls around it
-    cudaStream_t copy_in = nullptr, copy_out = nullptr;
-};
 
 struct hgemm_plan_s {
     hgemm_ctx_s *ctx = nullptr;
@@ -80,28 +57,6 @@ struct hgemm_plan_s {
 };
 
 namespace {
-
-hgemm_status_t cuda_fail(hgemm_ctx_s *ctx, cudaError_t e)
-{
-    if (ctx) ctx->last_cuda_error = int(e);
-    (void)cudaGetLastError();
-    return HGEMM_ERR_CUDA;
-}
-
-// Every device allocation of the library goes through here (hgemm_debug_fail_allocs can make it fail).
-cudaError_t ctx_malloc(hgemm_ctx_s *ctx, void **out, size_t bytes)
-{
-    if (ctx && ctx->fail_allocs > 0) {
-        if (ctx->pass_allocs > 0) {
-            --ctx->pass_allocs;
-        } else {
-            --ctx->fail_allocs;
-            *out = nullptr;
-            return cudaErrorMemoryAllocation;
-        }
-    }
-    return cudaMalloc(out, bytes);
-}
 
 int32_t pow2_at_least(int32_t x)
 {
@@ -532,6 +487,7 @@ hgemm_status_t hgemm_destroy(hgemm_ctx_t *ctx)
 {
     if (!ctx) return HGEMM_ERR_INVALID_ARG;
     while (!ctx->plans.empty()) hgemm_plan_destroy(ctx->plans.back());
+    while (!ctx->fp8_plans.empty()) hgemm_fp8_plan_destroy(ctx->fp8_plans.back());
     if (ctx->d_status) cudaFree(ctx->d_status);
     if (ctx->copy_in) cudaStreamDestroy(ctx->copy_in);
     if (ctx->copy_out) cudaStreamDestroy(ctx->copy_out);
@@ -1084,6 +1040,11 @@ hgemm_status_t hgemm_ctx_last_device_status(hgemm_ctx_t *ctx, uint32_t *code)
         if (v == 0) v = w;
         const hgemm_status_t s = reset_counters(pl);
         if (s != HGEMM_OK) return s;
+    }
+    for (const hgemm_fp8_plan_s *pl : ctx->fp8_plans) {
+        const uint32_t w = words[size_t(hgemm_host::status_slot_of(pl))];
+        any = any || w != 0;
+        if (v == 0) v = w;
     }
     if (any) {
         e = cudaMemset(ctx->d_status, 0, words.size() * sizeof(uint32_t));

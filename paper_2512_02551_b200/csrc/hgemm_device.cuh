@@ -1,0 +1,99 @@
+// Device code that the kernels share: bounded waits on mbarriers with a status word, and the shared-memory matrix
+// descriptors of tiles that TMA lays out with the 128-byte swizzle.
+#pragma once
+
+#include <stdint.h>
+
+#include "ptx_sm100.cuh"
+
+namespace hgemm_dev {
+
+using namespace hgemm_ptx;
+
+// -------------------------------------------------------------------------------------
+// bounded wait
+
+struct WaitCtl {
+    volatile uint32_t *abort_flag;  // shared memory
+    uint32_t *status;               // global memory
+    long long budget;
+};
+
+static __device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, const WaitCtl &ctl, uint32_t code)
+{
+    const long long t0 = clock64();
+#pragma unroll 1
+    while (true) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*ctl.abort_flag) return false;
+        if (clock64() - t0 > ctl.budget) {
+            *ctl.abort_flag = 1u;
+            atomicCAS(ctl.status, 0u, code);
+            return false;
+        }
+    }
+}
+
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const WaitCtl &ctl, uint32_t code)
+{
+    if (mbar_test_wait(bar, parity)) return true;      // already complete: the cheap query answers
+#pragma unroll 1
+    for (int i = 0; i < 16; ++i)
+        if (mbar_try_wait(bar, parity)) return true;
+    return mbar_wait_slow(bar, parity, ctl, code);
+}
+
+// The same wait without a call: for code that keeps most of its registers live across it.
+__device__ __forceinline__ bool mbar_wait_inline(uint32_t bar, uint32_t parity, const WaitCtl &ctl, uint32_t code)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+#pragma unroll 1
+    while (!mbar_try_wait(bar, parity)) {
+        if (*ctl.abort_flag) return false;
+        if (clock64() - t0 > ctl.budget) {
+            *ctl.abort_flag = 1u;
+            atomicCAS(ctl.status, 0u, code);
+            return false;
+        }
+    }
+    return true;
+}
+
+__device__ __forceinline__ uint32_t status_code(uint32_t role, uint32_t barrier_index, uint32_t stage)
+{
+    return (role << 24) | ((barrier_index & 0xffffu) << 8) | (stage & 0xffu);
+}
+
+// -------------------------------------------------------------------------------------
+// descriptors
+
+// Shared-memory matrix descriptor of a K-major tile whose rows are 64 fp16 = 128 bytes,
+// laid out by TMA with the 128-byte swizzle: 8-row groups are 1024 bytes apart.
+__device__ __forceinline__ uint64_t make_smem_desc_sw128(uint32_t smem_byte_addr)
+{
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((smem_byte_addr & 0x3ffffu) >> 4);        // [0,14)  start address >> 4
+    d |= static_cast<uint64_t>(1) << 16;                                 // [16,30) leading byte offset (unused here)
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;                         // [32,46) stride byte offset: 8 rows * 128 B
+    d |= static_cast<uint64_t>(1) << 46;                                 // [46,48) descriptor version (sm_100)
+    d |= static_cast<uint64_t>(2) << 61;                                 // [61,64) 128-byte swizzle
+    return d;
+}
+
+// The same for a tile that is contiguous along its M/N dimension (a row-major K x N operand): the tile
+// is stored as blocks of 64 columns, each block 64 k-rows of 128 bytes under the 128-byte swizzle.
+// Leading byte offset = distance between 64-column blocks, stride byte offset = distance between
+// groups of 8 k-rows (1024 bytes); one UMMA (K = 16) spans two such groups.
+__device__ __forceinline__ uint64_t make_smem_desc_sw128_mn_major(uint32_t smem_byte_addr, uint32_t block_bytes)
+{
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((smem_byte_addr & 0x3ffffu) >> 4);
+    d |= static_cast<uint64_t>((block_bytes >> 4) & 0x3fffu) << 16;
+    d |= static_cast<uint64_t>(1024 >> 4) << 32;
+    d |= static_cast<uint64_t>(1) << 46;
+    d |= static_cast<uint64_t>(2) << 61;
+    return d;
+}
+
+} // namespace hgemm_dev

@@ -30,6 +30,7 @@
 
 #include <type_traits>
 
+#include "hgemm_device.cuh"
 #include "ptx_sm100.cuh"
 
 namespace hgemm_dev {
@@ -210,44 +211,6 @@ __device__ __forceinline__ void trace_stamp(const KernelParams &p, int slot)
     }
 }
 
-// -------------------------------------------------------------------------------------
-// bounded wait
-
-struct WaitCtl {
-    volatile uint32_t *abort_flag;  // shared memory
-    uint32_t *status;               // global memory
-    long long budget;
-};
-
-__device__ __noinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, const WaitCtl &ctl, uint32_t code)
-{
-    const long long t0 = clock64();
-#pragma unroll 1
-    while (true) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if (*ctl.abort_flag) return false;
-        if (clock64() - t0 > ctl.budget) {
-            *ctl.abort_flag = 1u;
-            atomicCAS(ctl.status, 0u, code);
-            return false;
-        }
-    }
-}
-
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const WaitCtl &ctl, uint32_t code)
-{
-    if (mbar_test_wait(bar, parity)) return true;      // already complete: the cheap query answers
-#pragma unroll 1
-    for (int i = 0; i < 16; ++i)
-        if (mbar_try_wait(bar, parity)) return true;
-    return mbar_wait_slow(bar, parity, ctl, code);
-}
-
-__device__ __forceinline__ uint32_t status_code(uint32_t role, uint32_t barrier_index, uint32_t stage)
-{
-    return (role << 24) | ((barrier_index & 0xffffu) << 8) | (stage & 0xffu);
-}
-
 // Checked build: `holds` is an invariant of site `site`; false records it and tells the caller to skip the access.
 // Ordinary build: always true, and the test of `holds` is compiled out with it.
 __device__ __forceinline__ bool checked(uint32_t *status, bool holds, uint32_t site)
@@ -259,22 +222,6 @@ __device__ __forceinline__ bool checked(uint32_t *status, bool holds, uint32_t s
     }
 #endif
     return true;
-}
-
-// -------------------------------------------------------------------------------------
-// descriptors
-
-// Shared-memory matrix descriptor of a K-major tile whose rows are 64 fp16 = 128 bytes,
-// laid out by TMA with the 128-byte swizzle: 8-row groups are 1024 bytes apart.
-__device__ __forceinline__ uint64_t make_smem_desc_sw128(uint32_t smem_byte_addr)
-{
-    uint64_t d = 0;
-    d |= static_cast<uint64_t>((smem_byte_addr & 0x3ffffu) >> 4);        // [0,14)  start address >> 4
-    d |= static_cast<uint64_t>(1) << 16;                                 // [16,30) leading byte offset (unused here)
-    d |= static_cast<uint64_t>(1024 >> 4) << 32;                         // [32,46) stride byte offset: 8 rows * 128 B
-    d |= static_cast<uint64_t>(1) << 46;                                 // [46,48) descriptor version (sm_100)
-    d |= static_cast<uint64_t>(2) << 61;                                 // [61,64) 128-byte swizzle
-    return d;
 }
 
 // -------------------------------------------------------------------------------------
@@ -303,21 +250,6 @@ __device__ __noinline__ void store_unit4_slow(__half *C, int32_t M, int32_t N, i
     const float f[4] = {x, y, z, w};
     if (transposed) store_transposed(C, M, N, row, col, f, 4);
     else store_ragged(C, N, row, col, f, 4);
-}
-
-// The same for a tile that is contiguous along its M/N dimension (a row-major K x N operand): the tile
-// is stored as blocks of 64 columns, each block 64 k-rows of 128 bytes under the 128-byte swizzle.
-// Leading byte offset = distance between 64-column blocks, stride byte offset = distance between
-// groups of 8 k-rows (1024 bytes); one UMMA (K = 16) spans two such groups.
-__device__ __forceinline__ uint64_t make_smem_desc_sw128_mn_major(uint32_t smem_byte_addr, uint32_t block_bytes)
-{
-    uint64_t d = 0;
-    d |= static_cast<uint64_t>((smem_byte_addr & 0x3ffffu) >> 4);
-    d |= static_cast<uint64_t>((block_bytes >> 4) & 0x3fffu) << 16;
-    d |= static_cast<uint64_t>(1024 >> 4) << 32;
-    d |= static_cast<uint64_t>(1) << 46;
-    d |= static_cast<uint64_t>(2) << 61;
-    return d;
 }
 
 // -------------------------------------------------------------------------------------

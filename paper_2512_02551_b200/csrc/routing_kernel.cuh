@@ -1,0 +1,329 @@
+// Routing of tokens to experts (see include/hgemm_routing.h).
+//
+// hgemm_route: one warp per token, its experts in registers (expert 32 i + lane in slot i).  A value becomes an unsigned key in the same
+// order, so that a maximum over the warp is one redux instruction, and the lowest index among equals another.  Bound by
+// instruction issue (top_k rounds of two redux and a scan of the lane's slots), not by the logits' bytes.
+//
+// hgemm_route_sort: a stable counting sort in one launch.  The CTAs of one cluster divide the choices into consecutive runs, one per
+// warp; per-warp histograms, prefix sums over warps, CTAs (through distributed shared memory) and experts give every run its
+// first place for every expert, and each warp then places its run in order.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <stdint.h>
+
+#include "hgemm_device.cuh"
+
+namespace hgemm_dev {
+
+constexpr int kRouteThreads = 128;
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+
+struct RouteParams {
+    const void *logits;
+    int64_t tokens, ld, ldd;
+    int32_t experts, top_k, sigmoid, groups, top_groups, group_size, top2, renormalize, by_logit;   // by_logit: v = l
+    float scale, inv_group;
+    const float *bias;
+    float *weights;
+    int32_t *indices;
+    const int32_t *chosen;
+    const float *dweights;
+    void *dlogits;
+};
+
+// Unsigned keys in the order of the floats (-0 as +0, NaN as -infinity); 0 is below all of them.
+__device__ __forceinline__ uint32_t order_key(float v)
+{
+    if (!(v == v)) v = __int_as_float(0xff800000);
+    const uint32_t b = __float_as_uint(v + 0.0f);
+    return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); }
+constexpr uint32_t kKeyLowest = 0x007fffffu;           // -infinity
+
+__device__ __forceinline__ float route_load(const float *p) { return *p; }
+__device__ __forceinline__ float route_load(const __half *p) { return __half2float(*p); }
+__device__ __forceinline__ float route_load(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void route_store(float *p, float v) { *p = v; }
+__device__ __forceinline__ void route_store(__half *p, float v) { *p = __float2half_rn(v); }
+__device__ __forceinline__ void route_store(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ float warp_max(float v)
+{
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+
+// Score of a logit; softmax: m the row's maximum, sum that of the exponentials.
+__device__ __forceinline__ float route_score(float l, bool sigmoid, float m, float sum)
+{
+    if (sigmoid) return 1.0f / (1.0f + expf(-l));
+    return m == __int_as_float(0xff800000) ? 0.0f : expf(l - m) / sum;
+}
+
+// NPL: slots per lane (experts <= 32 NPL).
+template <class T, int NPL>
+__global__ void __launch_bounds__(kRouteThreads)
+route_kernel(const RouteParams p)
+{
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int32_t lane = static_cast<int32_t>(lane_id());
+    const bool sigmoid = p.sigmoid != 0;
+    for (int64_t t = blockIdx.x * static_cast<int64_t>(kRouteThreads / 32) + (threadIdx.x >> 5); t < p.tokens; t += gridDim.x * static_cast<int64_t>(kRouteThreads / 32)) {
+        const T *row = static_cast<const T *>(p.logits) + t * p.ld;
+        float l[NPL];
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) {
+            const int32_t e = i * 32 + lane;
+            l[i] = e < p.experts ? route_load(row + e) : __int_as_float(0xff800000);
+        }
+        float m = 0.0f, sum = 1.0f;
+        if (!sigmoid) {
+            m = __int_as_float(0xff800000);
+#pragma unroll
+            for (int i = 0; i < NPL; ++i) m = fmaxf(m, l[i]);
+            m = warp_max(m);
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NPL; ++i)
+                if (i * 32 + lane < p.experts) sum += expf(l[i] - m);
+            sum = warp_sum(sum);
+        }
+        uint32_t key[NPL];
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) {
+            const int32_t e = i * 32 + lane;
+            float v = l[i];
+            if (!p.by_logit) {
+                v = route_score(l[i], sigmoid, m, sum);
+                if (p.bias != nullptr && e < p.experts) v += p.bias[e];
+            }
+            key[i] = e < p.experts ? order_key(v) : 0u;
+        }
+        if (p.groups > 1) {
+            uint32_t of_lane = 0;                       // lane g: key of group g's value
+            for (int32_t g = 0; g < p.groups; ++g) {
+                uint32_t k1 = 0, k2 = 0;                // this lane's two largest keys in the group
+#pragma unroll
+                for (int i = 0; i < NPL; ++i) {
+                    const int32_t e = i * 32 + lane;
+                    const uint32_t k = e >= g * p.group_size && e < (g + 1) * p.group_size ? key[i] : 0u;
+                    k2 = max(k2, min(k1, k));
+                    k1 = max(k1, k);
+                }
+                uint32_t best = __reduce_max_sync(0xffffffffu, k1);
+                if (p.top2) {
+                    const int owner = __ffs(__ballot_sync(0xffffffffu, k1 == best)) - 1;
+                    const uint32_t second = __reduce_max_sync(0xffffffffu, lane == owner ? k2 : k1);
+                    best = order_key(key_value(best) + key_value(max(second, kKeyLowest)));
+                }
+                if (lane == g) of_lane = best;
+            }
+            uint32_t kept = 0;
+            for (int32_t j = 0; j < p.top_groups; ++j) {
+                const uint32_t best = __reduce_max_sync(0xffffffffu, of_lane);
+                const int g = __ffs(__ballot_sync(0xffffffffu, of_lane == best)) - 1;
+                kept |= 1u << g;
+                if (lane == g) of_lane = 0;
+            }
+#pragma unroll
+            for (int i = 0; i < NPL; ++i) {
+                const int32_t e = i * 32 + lane;
+                const int32_t g = static_cast<int32_t>((static_cast<float>(e) + 0.5f) * p.inv_group);      // e / group_size: e < 512, off by less than half
+                if (e < p.experts && !((kept >> g) & 1u)) key[i] = kKeyLowest;
+            }
+        }
+        int32_t mine = 0;                               // lane j: the j-th choice
+        for (int32_t j = 0; j < p.top_k; ++j) {
+            uint32_t k = key[0];
+            int32_t slot = 0;
+#pragma unroll
+            for (int i = 1; i < NPL; ++i)
+                if (key[i] > k) { k = key[i]; slot = i; }
+            const uint32_t best = __reduce_max_sync(0xffffffffu, k);
+            const uint32_t e = __reduce_min_sync(0xffffffffu, k == best ? static_cast<uint32_t>(slot * 32 + lane) : 0xffffffffu);
+            if (lane == j) mine = static_cast<int32_t>(e);
+            if ((e & 31u) == static_cast<uint32_t>(lane)) {
+#pragma unroll
+                for (int i = 0; i < NPL; ++i)
+                    if (i == static_cast<int>(e >> 5)) key[i] = 0u;
+            }
+        }
+        float s = 0.0f;
+        if (lane < p.top_k) s = route_score(route_load(row + mine), sigmoid, m, sum);
+        if (p.renormalize) s = s / (warp_sum(s) + 1e-20f);
+        if (lane < p.top_k) {
+            p.weights[t * p.top_k + lane] = s * p.scale;
+            p.indices[t * p.top_k + lane] = mine;
+        }
+    }
+}
+
+// dl from dw: with S = sum of the chosen scores + 1e-20 and w = s / S,  ds_j = scale (dw_j - sum_i dw_i w_i) / S  (renormalised)  or
+// scale dw_j;  sigmoid: dl = ds s (1 - s);  softmax: dl = s (ds - sum_i s_i ds_i).  One warp per token; lane j holds choice j.
+template <class T, int NPL>
+__global__ void __launch_bounds__(kRouteThreads)
+route_backward_kernel(const RouteParams p)
+{
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int32_t lane = static_cast<int32_t>(lane_id());
+    const bool sigmoid = p.sigmoid != 0;
+    for (int64_t t = blockIdx.x * static_cast<int64_t>(kRouteThreads / 32) + (threadIdx.x >> 5); t < p.tokens; t += gridDim.x * static_cast<int64_t>(kRouteThreads / 32)) {
+        const T *row = static_cast<const T *>(p.logits) + t * p.ld;
+        T *out = static_cast<T *>(p.dlogits) + t * p.ldd;
+        int32_t e = -1;
+        float dw = 0.0f;
+        if (lane < p.top_k) {
+            e = p.chosen[t * p.top_k + lane];
+            dw = p.dweights[t * p.top_k + lane] * p.scale;
+        }
+        const bool has = e >= 0 && e < p.experts;
+        float x[NPL];                                   // softmax: the scores
+        float m = 0.0f, sum = 1.0f;
+        if (!sigmoid) {
+            m = __int_as_float(0xff800000);
+#pragma unroll
+            for (int i = 0; i < NPL; ++i) {
+                x[i] = i * 32 + lane < p.experts ? route_load(row + i * 32 + lane) : __int_as_float(0xff800000);
+                m = fmaxf(m, x[i]);
+            }
+            m = warp_max(m);
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NPL; ++i) {
+                x[i] = i * 32 + lane < p.experts && m != __int_as_float(0xff800000) ? expf(x[i] - m) : 0.0f;
+                sum += x[i];
+            }
+            sum = warp_sum(sum);
+        }
+        const float s = has ? route_score(route_load(row + e), sigmoid, m, sum) : 0.0f;
+        float d = has ? dw : 0.0f;
+        if (p.renormalize) {
+            const float total = warp_sum(s) + 1e-20f;
+            const float mean = warp_sum(d * s) / total;
+            d = has ? (d - mean) / total : 0.0f;
+        }
+        if (sigmoid) {
+#pragma unroll
+            for (int i = 0; i < NPL; ++i)
+                if (i * 32 + lane < p.experts) route_store(out + i * 32 + lane, 0.0f);
+            __syncwarp();
+            if (has) route_store(out + e, d * s * (1.0f - s));
+        } else {
+            const float dot = warp_sum(s * d), inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+            for (int i = 0; i < NPL; ++i)
+                if (i * 32 + lane < p.experts) route_store(out + i * 32 + lane, -(x[i] * inv) * dot);
+            __syncwarp();
+            if (has) route_store(out + e, s * (d - dot));
+        }
+    }
+}
+
+struct SortParams {
+    const int32_t *indices;
+    int32_t count, experts, run;       // run: choices per warp, a multiple of 32
+    int32_t *offsets, *order, *position;
+};
+
+__global__ void __launch_bounds__(kSortThreads)
+route_sort_kernel(const SortParams p)
+{
+    extern __shared__ int32_t s_sort[];                 // [kSortWarps][experts] histograms, then [experts] totals of this CTA, [experts] first places, [33]
+    int32_t *hist = s_sort, *total = s_sort + kSortWarps * p.experts, *first = total + p.experts, *partial = first + p.experts;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int32_t tid = static_cast<int32_t>(threadIdx.x), warp = tid >> 5, lane = tid & 31;
+    const int32_t rank = static_cast<int32_t>(cluster_ctarank()), ctas = static_cast<int32_t>(gridDim.x);
+    for (int32_t i = tid; i < kSortWarps * p.experts; i += kSortThreads) hist[i] = 0;
+    __syncthreads();
+    int32_t *mine = hist + warp * p.experts;
+    const int64_t begin = (static_cast<int64_t>(rank) * kSortWarps + warp) * p.run, end = min(begin + p.run, static_cast<int64_t>(p.count));
+    for (int64_t i = begin + lane; i < end; i += 32) {
+        const int32_t e = p.indices[i];
+        if (e >= 0 && e < p.experts) atomicAdd(mine + e, 1);       // counts: the order of the additions does not show
+    }
+    __syncthreads();
+    for (int32_t e = tid; e < p.experts; e += kSortThreads) {
+        int32_t sum = 0;
+        for (int32_t w = 0; w < kSortWarps; ++w) {
+            const int32_t n = hist[w * p.experts + e];
+            hist[w * p.experts + e] = sum;
+            sum += n;
+        }
+        total[e] = sum;
+    }
+    cluster_arrive();
+    cluster_wait();
+    // thread e: expert e (experts <= threads); places before it: experts below, then the CTAs before this one
+    int32_t all = 0, before = 0;
+    if (tid < p.experts) {
+        for (int32_t r = 0; r < ctas; ++r) {
+            int32_t n;
+            asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(n) : "r"(mapa(smem_addr(total + tid), static_cast<uint32_t>(r))) : "memory");
+            all += n;
+            if (r < rank) before += n;
+        }
+    }
+    int32_t scan = all;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int32_t x = __shfl_up_sync(0xffffffffu, scan, d);
+        if (lane >= d) scan += x;
+    }
+    if (lane == 31) partial[warp] = scan;
+    __syncthreads();
+    if (warp == 0) {
+        int32_t x = partial[lane];
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int32_t y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
+        }
+        partial[lane] = x;
+    }
+    __syncthreads();
+    const int32_t offset = scan - all + (warp > 0 ? partial[warp - 1] : 0);
+    const int32_t placed = partial[kSortWarps - 1];
+    if (tid < p.experts) {
+        first[tid] = offset + before;
+        if (rank == 0) {
+            p.offsets[tid] = offset;
+            if (tid == p.experts - 1) p.offsets[p.experts] = placed;
+        }
+    }
+    __syncthreads();
+    for (int64_t i = begin; i < end; i += 32) {
+        const int64_t slot = i + lane;
+        const int32_t e = slot < end ? p.indices[slot] : -1;
+        const bool valid = e >= 0 && e < p.experts;
+        const uint32_t peers = __match_any_sync(0xffffffffu, valid ? e : -1);
+        if (valid) {
+            const int32_t place = first[e] + mine[e] + __popc(peers & ((1u << lane) - 1u));
+            p.order[place] = static_cast<int32_t>(slot);
+            p.position[slot] = place;
+        } else if (slot < end) {
+            p.position[slot] = -1;
+        }
+        __syncwarp();
+        if (valid && lane == __ffs(peers) - 1) mine[e] += __popc(peers);
+        __syncwarp();
+    }
+    for (int64_t i = placed + static_cast<int64_t>(rank) * kSortThreads + tid; i < p.count; i += static_cast<int64_t>(ctas) * kSortThreads) p.order[i] = -1;
+    cluster_arrive();                                   // no CTA leaves while another may still read its totals
+    cluster_wait();
+}
+
+} // namespace hgemm_dev

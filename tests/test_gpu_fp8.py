@@ -1,0 +1,481 @@
+"""The 8-bit products with block scales and their quantiser on the GPU, against plain 64-bit forms.
+
+Inputs hold NaN wherever nothing may be read (columns between a matrix's width and its row distance, rows of other groups) and
+results sit inside guard bands; the tolerances follow from the arithmetic (fp8_reference.product_bound)."""
+import zlib
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import fp8_reference as ref  # noqa: E402
+from paper_2512_02551_b200 import fp8, hgemm  # noqa: E402
+
+OUTS = [torch.float32, torch.float16, torch.bfloat16]
+E4M3, E5M2 = torch.float8_e4m3fn, torch.float8_e5m2
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    assert torch.cuda.is_available(), "these tests need a B200"
+    with hgemm.Context(0) as c:
+        yield c
+
+
+def rng(*key):
+    return torch.Generator(device="cuda").manual_seed(zlib.crc32(repr(key).encode()))
+
+
+def bytes8(g, shape, dtype, spread=1.0):
+    """8-bit values over most of the type's range, rows 16 bytes (or more) apart, NaN between them."""
+    pitch = -(-shape[-1] // 16) * 16 + 16
+    wide = torch.full((*shape[:-1], pitch), 0x7F, dtype=torch.uint8, device="cuda").view(dtype)
+    v = (torch.randn(*shape, generator=g, device="cuda") * spread * 20.0).clamp(-400, 400).to(dtype)
+    wide.view(torch.uint8)[..., :shape[-1]] = v.view(torch.uint8)
+    return wide[..., :shape[-1]]
+
+
+def scales(g, *shape):
+    return torch.rand(*shape, generator=g, device="cuda") * 0.01 + 1e-4
+
+
+def guarded(shape, dtype, offset=0, extra=0):
+    """A result inside NaN: `extra` more elements per row, `offset` elements into its buffer."""
+    rows, cols = int(np.prod(shape[:-1])), shape[-1]
+    ld = cols + extra
+    buf = torch.full((offset + rows * ld + 64,), float("nan"), dtype=dtype, device="cuda")
+    out = buf[offset:offset + rows * ld].view(rows, ld)
+    return buf, out[:, :cols] if len(shape) == 2 else out.view(*shape[:-1], ld)[..., :cols]
+
+
+def untouched(buf, out):
+    """Nothing outside `out` was written, everything inside was."""
+    assert not bool(torch.isnan(out).any()), "some element of the result was never written"
+    n = out.numel()
+    assert int(torch.isnan(buf).sum()) == buf.numel() - n, "the kernel wrote outside its result"
+
+
+def blocks(n):
+    return -(-n // 128)
+
+
+def dense_case(ctx, form, M, N, K, out_dtype, a_dtype=E4M3, config=None, offset=0, extra=0, accumulate=False):
+    g = rng(form, M, N, K, str(out_dtype))
+    if form == "weight_grad":
+        a, b = bytes8(g, (M, N), a_dtype), bytes8(g, (M, K), E4M3)
+        sa, sb = scales(g, blocks(M), N), scales(g, blocks(M), K)
+        p, q, nb, shape = ref.values(a, sa, 128, 1).T, ref.values(b, sb, 128, 1).T, blocks(M), (N, K)
+    else:
+        a, b = bytes8(g, (M, K) if form == "forward" else (M, N), a_dtype), bytes8(g, (N, K), E4M3)
+        sa, sb = scales(g, M, blocks(a.shape[1])), scales(g, blocks(N), blocks(K))
+        w = ref.values(b, sb, 128, 128)
+        p, q, nb, shape = ref.values(a, sa, 1, 128), w if form == "forward" else w.T, blocks(a.shape[1]), (M, N) if form == "forward" else (M, K)
+    buf, out = guarded(shape, out_dtype, offset, extra)
+    if accumulate:
+        out.copy_(torch.randn(*shape, generator=g, device="cuda"))
+        before = ref.f64(out)
+    with fp8.Plan(ctx, M, N, K, form=form, a_dtype=a_dtype, out_dtype=out_dtype) as plan:
+        if config is not None:
+            plan.set_config(*config)
+        plan.run(a, sa, b, sb, out, accumulate=accumulate)
+        st, code = ctx.last_device_status()
+        assert st == hgemm.OK, hex(code)
+        untouched(buf, out)
+        if accumulate:
+            exact = p @ q.T
+            bound = ref.product_bound(np.abs(p) @ np.abs(q).T + np.abs(before), nb, out_dtype, exact + before)
+            assert (np.abs(ref.f64(out) - exact - before) <= bound).all()
+        else:
+            ref.check_product(out, p, q, nb, f"{form} {M}x{N}x{K} {out_dtype} {plan.config.as_dict()}")
+
+
+SWAPPED = [(1, bq, s) for bq in (16, 32, 64, 128) for s in (1, 2, 4, 8)]
+SHAPES = [(1, 1, 1), (1, 128, 128), (3, 130, 257), (17, 64, 1000), (64, 300, 128), (129, 257, 384), (300, 520, 1040), (256, 256, 128)]
+
+
+@pytest.mark.parametrize("form", ["forward", "input_grad"])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+@pytest.mark.parametrize("config", [(2, 256, 1)] + SWAPPED, ids=str)
+def test_every_kernel_at_small_and_odd_sizes(ctx, form, M, N, K, config):
+    dense_case(ctx, form, M, N, K, OUTS[(M + N + K) % 3], config=config)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 64, 64), (127, 1, 1), (128, 130, 257), (130, 256, 100), (1000, 129, 384), (700, 520, 300)])
+@pytest.mark.parametrize("config", [(2, 256, 1), (1, 128, 1), (1, 128, 2), (1, 128, 4), (1, 128, 8)], ids=str)
+def test_weight_gradient_kernels(ctx, M, N, K, config):
+    dense_case(ctx, "weight_grad", M, N, K, OUTS[(M + N + K) % 3], config=config)
+
+
+@pytest.mark.parametrize("form", ["forward", "input_grad", "weight_grad"])
+@pytest.mark.parametrize("out_dtype", OUTS, ids=str)
+@pytest.mark.parametrize("a_dtype", [E4M3, E5M2], ids=str)
+def test_types(ctx, form, out_dtype, a_dtype):
+    dense_case(ctx, form, 200, 384, 272, out_dtype, a_dtype=a_dtype)
+    dense_case(ctx, form, 200, 384, 272, out_dtype, a_dtype=a_dtype, config=(2, 256, 1))
+
+
+@pytest.mark.parametrize("form", ["forward", "input_grad", "weight_grad"])
+@pytest.mark.parametrize("config", [(2, 256, 1), (1, 128, 1), (1, 128, 4)], ids=str)
+@pytest.mark.parametrize("offset,extra", [(1, 0), (0, 3), (8, 8), (3, 5)])
+def test_result_strides_and_alignment(ctx, form, config, offset, extra):
+    for out_dtype in OUTS:
+        dense_case(ctx, form, 150, 200, 190, out_dtype, config=config, offset=offset, extra=extra)
+
+
+@pytest.mark.parametrize("form", ["forward", "input_grad", "weight_grad"])
+@pytest.mark.parametrize("config", [(2, 256, 1), (1, 128, 1), (1, 128, 4)], ids=str)
+def test_accumulate(ctx, form, config):
+    dense_case(ctx, form, 260, 300, 390, torch.float32, config=config, accumulate=True)
+
+
+@pytest.mark.parametrize("form", ["forward", "input_grad", "weight_grad"])
+def test_several_waves_of_tiles(ctx, form):
+    """More tiles than CTAs: every role walks on to further tiles; exact integers, so one misplaced element shows."""
+    M, N, K = 2900, 3100, 2700
+    g = rng(form)
+    small = lambda r, c: torch.randint(-2, 3, (r, c), generator=g, device="cuda").float()  # noqa: E731
+    ones = lambda *s: torch.full(s, 0.5, device="cuda")  # noqa: E731
+    x = {"forward": (M, K), "input_grad": (M, N), "weight_grad": (M, N)}[form]
+    w = (M, K) if form == "weight_grad" else (N, K)
+    fa, fb = small(*x), small(*w)
+    a, b = fp8.empty_rows(*x)[0], fp8.empty_rows(*w)[0]
+    a.copy_(fa), b.copy_(fb)
+    if form == "weight_grad":
+        sa, sb, want = ones(blocks(M), N), ones(blocks(M), K), fa.double().t() @ fb.double()
+    else:
+        sa, sb = ones(M, blocks(x[1])), ones(blocks(N), blocks(K))
+        want = fa.double() @ (fb.double().t() if form == "forward" else fb.double())
+    for config in ((2, 256, 1), (1, 128, 1), (1, 128, 2)):
+        buf, out = guarded(tuple(want.shape), torch.float32)
+        with fp8.Plan(ctx, M, N, K, form=form, out_dtype=torch.float32) as plan:
+            plan.set_config(*config)
+            plan.run(a, sa, b, sb, out)
+            assert ctx.last_device_status()[0] == hgemm.OK
+        untouched(buf, out)
+        assert torch.equal(out.double(), want * 0.25), config
+
+
+def test_no_rows(ctx):
+    for form in ("forward", "input_grad", "weight_grad"):
+        for groups in (0, 3):
+            g = (groups,) if groups else ()
+            N, K = 64, 96
+            shape = (*g, N, K) if form == "weight_grad" else (0, N if form == "forward" else K)
+            rows = fp8.padded_rows(0, groups) if groups else 0
+            a = torch.empty(rows if form == "weight_grad" else 0, K if form == "forward" else N, dtype=E4M3, device="cuda")
+            b = torch.empty(*((rows, K) if form == "weight_grad" else (*g, N, K)), dtype=E4M3, device="cuda")
+            sa = torch.empty(blocks(rows), N, device="cuda") if form == "weight_grad" else torch.empty(0, blocks(a.shape[1]), device="cuda")
+            sb = torch.empty(blocks(rows), K, device="cuda") if form == "weight_grad" else torch.empty(*g, 1, 1, device="cuda")
+            out = torch.full(shape, float("nan"), device="cuda")
+            with fp8.Plan(ctx, 0, N, K, form=form, groups=groups, out_dtype=torch.float32) as plan:
+                plan.run(a, sa, b, sb, out, offsets=torch.zeros(groups + 1, dtype=torch.int32, device="cuda") if groups else None)
+            torch.cuda.synchronize()
+            assert form != "weight_grad" or bool((out == 0).all())
+
+
+# ---- products over experts ---------------------------------------------------------------------------
+
+COUNTS = {
+    "one of each": [1, 1, 1, 1],
+    "empty ones": [0, 5, 0, 0, 130, 0],
+    "one has all": [0, 0, 300, 0],
+    "ragged": [128, 127, 129, 1, 0, 256, 255, 257, 16, 17],
+    "many": [(7 * i) % 23 for i in range(70)],
+    "all empty": [0, 0, 0],
+}
+
+
+def grouped_case(ctx, form, counts, N, K, config, out_dtype=torch.float32, spare=0):
+    """`spare`: rows behind the last group, which belong to none."""
+    E, M = len(counts), sum(counts) + spare
+    if M == 0:
+        M = spare = 5
+    g = rng(form, E, M, N, K)
+    offsets = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device="cuda")
+    ends = offsets.tolist()
+    if form == "weight_grad":
+        rows = fp8.padded_rows(M, E)
+        a, b = bytes8(g, (rows, N), E4M3), bytes8(g, (rows, K), E4M3)
+        sa, sb = scales(g, blocks(rows), N), scales(g, blocks(rows), K)
+        at, held = 0, torch.zeros(rows, dtype=torch.bool, device="cuda")
+        want = []
+        for n in counts:
+            held[at:at + n] = True
+            up = blocks(n) * 128
+            if n < up:
+                a.view(torch.uint8)[at + n:at + up] = 0
+                b.view(torch.uint8)[at + n:at + up] = 0
+            want.append((at, n))
+            at += up
+        a.view(torch.uint8)[at:] = 0x7F                     # behind the last group: never read
+        b.view(torch.uint8)[at:] = 0x7F
+        pa, pb = ref.values(a, sa, 128, 1), ref.values(b, sb, 128, 1)
+        pairs = [(pa[s:s + n].T, pb[s:s + n].T, blocks(n)) for s, n in want]
+        shape = (E, N, K)
+    else:
+        a, w = bytes8(g, (M, K if form == "forward" else N), E4M3), bytes8(g, (E, N, K), E4M3)
+        w = w.reshape(E, N, -1) if w.is_contiguous() else w
+        sa, sb = scales(g, M, blocks(a.shape[1])), scales(g, E, blocks(N), blocks(K))
+        va, vw = ref.values(a, sa, 1, 128), ref.values(w, sb, 128, 128)
+        pairs = [(va[ends[e]:ends[e + 1]], vw[e] if form == "forward" else vw[e].T, blocks(a.shape[1])) for e in range(E)]
+        b, shape = w, (M, N if form == "forward" else K)
+    buf, out = guarded(shape, out_dtype)
+    with fp8.Plan(ctx, M, N, K, form=form, groups=E, out_dtype=out_dtype) as plan:
+        if config is not None:
+            plan.set_config(*config)
+        plan.run(a, sa, b, sb, out, offsets=offsets)
+        assert ctx.last_device_status()[0] == hgemm.OK
+        what = f"{form} {counts} {N}x{K} {plan.config.as_dict()}"
+    if form == "weight_grad":
+        untouched(buf, out)
+    else:
+        n = ends[-1]
+        assert bool(torch.isnan(out[n:]).all()), "rows of no group were written"
+        if n:
+            assert not bool(torch.isnan(out[:n]).any()) and int(torch.isnan(buf).sum()) == buf.numel() - n * shape[1]
+    for e, (p, q, nb) in enumerate(pairs):
+        got = out[e] if form == "weight_grad" else out[ends[e]:ends[e + 1]]
+        if got.numel():
+            ref.check_product(got, p, q, nb, f"{what} group {e}")
+
+
+@pytest.mark.parametrize("form", ["forward", "input_grad"])
+@pytest.mark.parametrize("counts", list(COUNTS), ids=str)
+@pytest.mark.parametrize("config", [None, (2, 256, 1), (1, 16, 1), (1, 32, 2), (1, 64, 1), (1, 128, 4)], ids=str)
+def test_experts_rows(ctx, form, counts, config):
+    grouped_case(ctx, form, COUNTS[counts], 272, 200, config, OUTS[len(counts) % 3], spare=3 if counts == "ragged" else 0)
+
+
+@pytest.mark.parametrize("counts", list(COUNTS), ids=str)
+@pytest.mark.parametrize("config", [None, (2, 256, 1), (1, 128, 1), (1, 128, 4)], ids=str)
+def test_experts_weight_gradient(ctx, counts, config):
+    grouped_case(ctx, "weight_grad", COUNTS[counts], 144, 272, config, OUTS[len(counts) % 3])
+
+
+def test_experts_offsets_out_of_range_stay_inside(ctx):
+    """Offsets beyond the rows, negative or falling are clamped: nothing outside the operands is touched."""
+    M, N, K, E = 40, 64, 128, 4
+    g = rng("offsets")
+    a, w = bytes8(g, (M, K), E4M3), bytes8(g, (E, N, K), E4M3)
+    sa, sb = scales(g, M, 1), scales(g, E, 1, 1)
+    for bad in ([0, 10, 5, 2000000000, 50], [-5, -1, 20, 10, 40], [7, 7, 7, 7, 1 << 30]):
+        for config in ((2, 256, 1), (1, 16, 1)):
+            buf, out = guarded((M, N), torch.float32)
+            with fp8.Plan(ctx, M, N, K, groups=E, out_dtype=torch.float32) as plan:
+                plan.set_config(*config)
+                plan.run(a, sa, w, sb, out, offsets=torch.tensor(bad, dtype=torch.int32, device="cuda"))
+                assert ctx.last_device_status()[0] == hgemm.OK
+            assert bool(torch.isnan(buf[M * N:]).all())
+
+
+# ---- order of work ---------------------------------------------------------------------------------------
+
+def test_streams_and_repeats_give_the_same_bits(ctx):
+    """Two streams at once, and calls after one another with other operands between them: the same bits as alone."""
+    M, N, K = 70, 512, 2048
+    g = rng("streams")
+    sets = []
+    for _ in range(3):
+        x, w = torch.randn(M, K, generator=g, device="cuda", dtype=torch.float32), torch.randn(N, K, generator=g, device="cuda")
+        sets.append((x, w, *fp8.empty_rows(M, K), *fp8.empty_tiles(N, K)))
+    plan = fp8.Plan(ctx, M, N, K, out_dtype=torch.float32)
+
+    def chain(s, out, stream=None):
+        x, w, q, sc, wq, ws = s
+        fp8.quantize_rows(ctx, x, q, sc, stream=stream)
+        fp8.quantize_tiles(ctx, w, wq, ws, stream=stream)
+        plan.run(q, sc, wq, ws, out, stream=stream)
+
+    alone = []
+    for s in sets:
+        out = torch.empty(M, N, device="cuda")
+        chain(s, out)
+        torch.cuda.synchronize()
+        alone.append(out)
+    streams = [torch.cuda.Stream() for _ in sets]
+    outs = [torch.empty(M, N, device="cuda") for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, o, st in zip(sets, outs, streams):
+            chain(s, o, st.cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(alone, outs))
+    # captured into a graph
+    graph, out = torch.cuda.CUDAGraph(), torch.empty(M, N, device="cuda")
+    with torch.cuda.graph(graph):
+        chain(sets[1], out)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, alone[1])
+    plan.close()
+
+
+# ---- quantisation --------------------------------------------------------------------------------------------
+
+def check_quantized(q, s, x, rows, cols, name, pow2, what):
+    """Scales within 2^-23 of the definition (powers of two exactly), values those of the definition, one code off only where the
+    three roundings of the factor and the product (2^-23 each) reach across the middle between two codes."""
+    v, want_s = ref.quantize(x, rows, cols, name, pow2)
+    got_s = ref.f64(s)
+    assert got_s.shape == want_s.shape
+    assert (got_s == want_s).all() if pow2 else (np.abs(got_s - want_s) <= 2.0 ** -23 * want_s).all(), what
+    got = ref.f64(q)
+    assert (np.isnan(got) == np.isnan(v)).all(), what
+    ok = ~np.isnan(v)
+    lo, hi = ref.nearest(v[ok] * (1 - 3 * 2.0 ** -23), name), ref.nearest(v[ok] * (1 + 3 * 2.0 ** -23), name)
+    near = (got[ok] == lo) | (got[ok] == hi)
+    assert near.all(), f"{what}: {int((~near).sum())} of {near.size} values"
+
+
+def awkward(g, R, C, dtype):
+    x = torch.randn(R, C, generator=g, device="cuda") * torch.exp(2.0 * torch.randn(R, 1, generator=g, device="cuda"))
+    x[::7, ::5] = 0.0
+    if R > 4:
+        x[3] = 0.0                                          # a row of zeros
+        x[4, :] = 1e-8
+        x[2, C // 2] = 60000.0
+    if C > 140 and R > 2:
+        x[1, 0:128] = 0.0
+        x[1, 130], x[0, 5], x[2, 7] = float("nan"), float("inf"), -float("inf")
+    return x.to(dtype)
+
+
+QSHAPES = [(1, 1), (1, 128), (2, 129), (5, 1000), (128, 128), (130, 300), (257, 96), (300, 513)]
+
+
+@pytest.mark.parametrize("R,C", QSHAPES)
+@pytest.mark.parametrize("dtype", OUTS, ids=str)
+@pytest.mark.parametrize("name", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("pow2", [False, True])
+def test_quantize(ctx, R, C, dtype, name, pow2):
+    x = awkward(rng(R, C, name), R, C, dtype)
+    xs = ref.f64(x)
+    f8 = ref.FP8[name]
+    q, s = fp8.empty_rows(R, C, f8)
+    fp8.quantize_rows(ctx, x, q, s, pow2=pow2)
+    check_quantized(q, s, xs, 1, 128, name, pow2, "rows")
+    t, st = fp8.empty_tiles(R, C, dtype=f8)
+    fp8.quantize_tiles(ctx, x, t, st, pow2=pow2)
+    check_quantized(t, st, xs, 128, 128, name, pow2, "tiles")
+    c, sc = fp8.empty_cols(R, C, dtype=f8)
+    fp8.quantize_cols(ctx, x, c, sc, pow2=pow2)
+    check_quantized(c, sc, xs, 128, 1, name, pow2, "cols")
+    q2, s2 = fp8.empty_rows(R, C, f8)
+    c2, sc2 = fp8.empty_cols(R, C, dtype=f8)
+    fp8.quantize_both(ctx, x, q2, s2, c2, sc2, pow2=pow2)
+    for u, v in ((q, q2), (c, c2)):
+        assert torch.equal(u.contiguous().view(torch.uint8), v.contiguous().view(torch.uint8))
+    assert torch.equal(s, s2) and torch.equal(sc, sc2)
+
+
+def test_quantize_extremes(ctx):
+    x = torch.zeros(6, 256, device="cuda")
+    x[0, 3] = 3.4e38
+    x[1, 4] = 2.0 ** -100
+    x[2, 5] = 2.0 ** -101
+    x[3, :] = float("nan")
+    x[4, :] = float("inf")
+    x[5, 1], x[5, 2] = 1e-40, -0.0
+    for pow2 in (False, True):
+        for name in ("e4m3", "e5m2"):
+            q, s = fp8.empty_rows(6, 256, ref.FP8[name])
+            fp8.quantize_rows(ctx, x, q, s, pow2=pow2)
+            check_quantized(q, s, ref.f64(x), 1, 128, name, pow2, "extremes")
+
+
+def test_quantize_strides_and_guards(ctx):
+    """x with any row distance and any base; the copy's own row distance; nothing written between the rows."""
+    g = rng("strides")
+    for dtype in OUTS:
+        for R, C, extra, shift in ((9, 200, 1, 1), (130, 130, 7, 3), (64, 256, 8, 8)):
+            base = torch.randn(R * (C + extra) + shift, generator=g, device="cuda").to(dtype)
+            x = base[shift:].view(R, C + extra)[:, :C]
+            wide = torch.full((R, 320), 0x55, dtype=torch.uint8, device="cuda")
+            wide_c = wide.clone()
+            q, c = wide.view(E4M3)[:, :C], wide_c.view(E4M3)[:, :C]
+            s, sc = torch.empty(R, blocks(C), device="cuda"), torch.empty(blocks(R), C, device="cuda")
+            fp8.quantize_both(ctx, x, q, s, c, sc)
+            check_quantized(q, s, ref.f64(x), 1, 128, "e4m3", False, "rows")
+            check_quantized(c, sc, ref.f64(x), 128, 1, "e4m3", False, "cols")
+            assert bool((wide[:, C:] == 0x55).all()) and bool((wide_c[:, C:] == 0x55).all())
+
+
+def test_quantize_gather(ctx):
+    g = rng("gather")
+    x = torch.randn(50, 300, generator=g, device="cuda").to(torch.bfloat16)
+    rows = torch.randint(0, 50, (333,), generator=g, device="cuda", dtype=torch.int32)
+    rows[::9] = -1
+    rows[5] = 50                                             # outside: rows of zeros
+    picked = ref.f64(x)[np.clip(rows.cpu().numpy(), 0, 49)]
+    picked[(rows.cpu().numpy() < 0) | (rows.cpu().numpy() > 49)] = 0.0
+    q, s = fp8.empty_rows(333, 300)
+    fp8.quantize_rows(ctx, x, q, s, rows=rows)
+    check_quantized(q, s, picked, 1, 128, "e4m3", False, "gathered rows")
+    c, sc = fp8.empty_cols(333, 300)
+    fp8.quantize_cols(ctx, x, c, sc, rows=rows)
+    check_quantized(c, sc, picked, 128, 1, "e4m3", False, "gathered columns")
+
+
+@pytest.mark.parametrize("counts", list(COUNTS), ids=str)
+def test_quantize_per_group(ctx, counts):
+    counts = COUNTS[counts]
+    E, M, C = len(counts), sum(counts) + 2, 200
+    g = rng("groups", M)
+    x = torch.randn(M, C, generator=g, device="cuda")
+    offsets = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device="cuda")
+    q, s = fp8.empty_rows(M, C)
+    c, sc = fp8.empty_cols(M, C, E)
+    c.view(torch.uint8)[:] = 0x55
+    sc.fill_(-1.0)
+    fp8.quantize_both(ctx, x, q, s, c, sc, offsets=offsets)
+    n = sum(counts)
+    if n:
+        check_quantized(q[:n], s[:n], ref.f64(x)[:n], 1, 128, "e4m3", False, "rows")
+    c1, sc1 = fp8.empty_cols(M, C, E)
+    fp8.quantize_cols(ctx, x, c1, sc1, offsets=offsets)
+    at, start = 0, 0
+    for n in counts:
+        up = blocks(n) * 128
+        if n:
+            check_quantized(c[at:at + n], sc[at // 128:(at + up) // 128], ref.f64(x)[start:start + n], 128, 1, "e4m3", False, "a group's columns")
+            assert bool((c[at + n:at + up].float() == 0).all())
+            assert torch.equal(c[at:at + up].contiguous().view(torch.uint8), c1[at:at + up].contiguous().view(torch.uint8))
+        at, start = at + up, start + n
+    assert bool((c.view(torch.uint8)[at:] == 0x55).all()) and bool((sc[at // 128:] == -1.0).all())
+
+
+# ---- the layer as a whole ---------------------------------------------------------------------------------------
+
+def test_gradients_against_differences(ctx):
+    """loss = sum(Y * G) for Y = X W^T: the gradients through the 8-bit products against differences of the 64-bit loss.  Operands
+    are exact in 8 bits (integers, scale 2^-k), so the products' own errors are those of 32-bit sums."""
+    M, N, K = 12, 20, 24
+    g = rng("differences")
+    X, W, G = (torch.randint(-8, 9, s, generator=g, device="cuda").float() for s in ((M, K), (N, K), (M, N)))
+
+    def rows(t):
+        q, s = fp8.empty_rows(*t.shape)
+        fp8.quantize_rows(ctx, t, q, s, pow2=True)
+        return q, s
+
+    def cols(t):
+        q, s = fp8.empty_cols(*t.shape)
+        fp8.quantize_cols(ctx, t, q, s, pow2=True)
+        return q, s
+
+    wq = fp8.empty_tiles(N, K)
+    fp8.quantize_tiles(ctx, W, *wq, pow2=True)
+    dX, dW = torch.empty(M, K, device="cuda"), torch.empty(N, K, device="cuda")
+    fp8.Plan(ctx, M, N, K, form="input_grad", out_dtype=torch.float32).run(*rows(G), *wq, dX)
+    fp8.Plan(ctx, M, N, K, form="weight_grad", out_dtype=torch.float32).run(*cols(G), *cols(X), dW)
+    x, w, gg = ref.f64(X), ref.f64(W), ref.f64(G)
+    loss = lambda x, w: float(((x @ w.T) * gg).sum())  # noqa: E731
+    h = 0.5                                                  # the loss is linear in each operand: differences are exact for any step
+    for t, d, at in ((0, dX, [(0, 0), (M - 1, K - 1), (5, 7)]), (1, dW, [(0, 0), (N - 1, K - 1), (11, 3)])):
+        for i, j in at:
+            up, down = [x.copy(), w.copy()], [x.copy(), w.copy()]
+            up[t][i, j] += h
+            down[t][i, j] -= h
+            assert float(d[i, j]) == pytest.approx((loss(*up) - loss(*down)) / (2 * h), rel=1e-6)
