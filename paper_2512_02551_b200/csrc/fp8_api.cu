@@ -83,10 +83,11 @@ hgemm_fp8_config_t choose(int32_t form, int64_t M, int64_t N, int64_t K, int32_t
     return c;
 }
 
-int stages_of(const hgemm_fp8_config_t &c, int32_t groups, int *smem)
+int stages_of(int32_t form, const hgemm_fp8_config_t &c, int32_t groups, int *smem)
 {
+    const bool q_col = c.cta_group == 1 || form == HGEMM_FP8_WEIGHT_GRAD;
     const int bn = c.block_q, stage = hgemm_dev::kFp8PBytes + bn / c.cta_group * 128;
-    const int fixed = 1024 + (c.cta_group == 2 ? 8 * hgemm_dev::kFp8StagingPerWarp : 0) + (c.cta_group == 2 ? 4 : 8) * (128 + bn) * 4 + hgemm_dev::kFp8CtrlBytes +
+    const int fixed = 1024 + (c.cta_group == 2 ? 8 * hgemm_dev::kFp8StagingPerWarp : 0) + hgemm_dev::kFp8Ring * hgemm_dev::kFp8Batch * hgemm_dev::fp8_slot_bytes(bn, q_col) + hgemm_dev::kFp8CtrlBytes +
                       (groups > 0 ? 8 * (groups + 1) : 8);
     const int stages = std::min((kSmemOptIn - fixed) / stage, hgemm_dev::kFp8MaxStages);
     *smem = kSmemOptIn;            // all of it: a second CTA on the SM could wait for this one's tensor memory
@@ -332,7 +333,7 @@ hgemm_status_t hgemm_fp8_run(hgemm_fp8_plan_t *plan, const void *A, int64_t lda,
     Fp8Params p;
     std::memset(&p, 0, sizeof(p));
     int smem = 0;
-    p.stages = stages_of(c, groups, &smem);
+    p.stages = stages_of(form, c, groups, &smem);
     if (p.stages < 2) return HGEMM_ERR_UNSUPPORTED;
     p.split = c.split_k;
     p.groups = groups;
@@ -394,7 +395,7 @@ hgemm_status_t hgemm_fp8_run(hgemm_fp8_plan_t *plan, const void *A, int64_t lda,
     p.vec_ok = aligned16(C) && (ldc * es) % 16 == 0 ? 1 : 0;
     // instruction descriptor: fp32 accumulators; formats 0 = e4m3, 1 = e5m2; bits 15 / 16: operand stored along its own rows
     p.idesc = (1u << 4) | (P.type == HGEMM_TYPE_E5M2 ? 1u << 7 : 0u) | (Q.type == HGEMM_TYPE_E5M2 ? 1u << 10 : 0u) | (P.mn ? 1u << 15 : 0u) | (Q.mn ? 1u << 16 : 0u) |
-              (uint32_t(tq >> 3) << 17) | (uint32_t(tp >> 4) << 24);
+              (uint32_t((tq / c.cta_group) >> 3) << 17) | (uint32_t(tp >> 4) << 24);
     p.status = ctx->d_status + plan->status_slot;
     p.wait_budget = ctx->wait_budget;
 

@@ -29,6 +29,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "hgemm_device.cuh"
 
 namespace hgemm_dev {
@@ -41,6 +43,8 @@ constexpr int kFp8MaxGroups = 1024;
 constexpr int kFp8CtrlBytes = 512;
 constexpr int kFp8StagingPerWarp = 2048;          // direct stores: 32 rows x 64 bytes
 constexpr uint32_t kRoleFp8Load = 8, kRoleFp8Mma = 9, kRoleFp8Scale = 10, kRoleFp8Promote = 11;
+constexpr int kFp8Batch = 4, kFp8Ring = 2;        // scales travel in batches of four blocks, two batches in flight (one barrier round per batch)
+__host__ __device__ constexpr int fp8_slot_bytes(int bn, bool q_col) { return (128 + (q_col ? bn : 4)) * 4; }     // one block's scales
 
 // which side of the tile grid follows the groups' offsets
 enum : int32_t { kRaggedNone = 0, kRaggedP = 1, kRaggedQ = 2, kRaggedK = 3 };
@@ -170,7 +174,7 @@ __device__ __forceinline__ uint32_t fp8_pack2(float a, float b, __nv_bfloat16)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// One warp's 32 rows x 128 columns of running sums to C, by rows: 64 bytes of every row at a time through the warp's staging
+// One warp's 32 rows x 128 columns of running sums (64 columns from col0, 64 from col0 + 128) to C, by rows: 64 bytes of every row at a time through the warp's staging
 // buffer (16-byte pieces XOR-swizzled by row pairs: conflict-free both ways), so that four lanes write 64 consecutive bytes.
 template <class T>
 __device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32_t staging, const Fp8Params &p, T *out, int32_t row0, int32_t row_end,
@@ -202,7 +206,7 @@ __device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t r = static_cast<uint32_t>(i) * 8u + lane / 4u, k = lane & 3u;
-            const int32_t row = row0 + static_cast<int32_t>(r), col = col0 + c + static_cast<int32_t>(k) * kPer;
+            const int32_t row = row0 + static_cast<int32_t>(r), col = col0 + (c < 64 ? c : c + 64) + static_cast<int32_t>(k) * kPer;
             float4 v = ld_shared_v4(staging + r * 64u + ((k ^ ((r >> 1) & 3u)) * 16u));
             if (row < row_end && col < col_end) {
                 T *dst = out + static_cast<int64_t>(row) * p.ldc + col;
@@ -244,11 +248,11 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
 {
     constexpr int TP = 128 * CG, TQ = BN;
     constexpr int kCols = BN / 2;                                 // columns of the tile a promoting warp holds
-    constexpr int kBufs = BN == 256 ? 2 : 4;                      // accumulators
-    constexpr uint32_t kTmemCols = kBufs * BN;
+    constexpr int kParts = CG;                                    // accumulators of a block: a pair's columns come in two parts, promoted by four warps each
+    constexpr int kDepth = CG == 2 ? 2 : 4;                       // blocks in tensor memory
+    constexpr uint32_t kTmemCols = kDepth * BN;
     constexpr uint32_t kStageBytes = kFp8PBytes + (BN / CG) * 128;
-    constexpr int kRing = CG == 2 ? 4 : 8;                        // blocks of scales in flight
-    constexpr uint32_t kSlotBytes = (128 + BN) * 4;
+    constexpr uint32_t kSlotBytes = fp8_slot_bytes(BN, Q_COL);
     static_assert(kTmemCols >= 32 && (kTmemCols & (kTmemCols - 1)) == 0 && kTmemCols <= 512, "tensor memory is allocated in powers of two");
 
     extern __shared__ uint8_t smem_raw[];
@@ -256,12 +260,12 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
     uint8_t *smem_gen = smem_raw + (smem_base - smem_addr(smem_raw));
     const uint32_t staging_base = smem_base + static_cast<uint32_t>(p.stages) * kStageBytes;
     const uint32_t ring_base = staging_base + (CG == 2 ? 8u * kFp8StagingPerWarp : 0u);
-    const uint32_t ctrl_base = ring_base + kRing * kSlotBytes;
+    const uint32_t ctrl_base = ring_base + kFp8Ring * kFp8Batch * kSlotBytes;
     uint8_t *ctrl_gen = smem_gen + (ctrl_base - smem_base);
     const uint32_t bar_full = ctrl_base, bar_empty = bar_full + 8 * kFp8MaxStages, bar_tfull = bar_empty + 8 * kFp8MaxStages, bar_tempty = bar_tfull + 32;
-    const uint32_t bar_sfull = bar_tempty + 32, bar_sempty = bar_sfull + 64;          // ends at 384
-    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 384);
-    volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 388);
+    const uint32_t bar_sfull = bar_tempty + 32, bar_sempty = bar_sfull + 8 * kFp8Ring;          // ends at 320
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 320);
+    volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 324);
     int32_t *pre = reinterpret_cast<int32_t *>(ctrl_gen + kFp8CtrlBytes);             // groups + 1 each
     int32_t *off = pre + (p.groups + 1);
 
@@ -281,11 +285,11 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             mbar_init(bar_full + 8 * s, CG);
             mbar_init(bar_empty + 8 * s, 1);
         }
-        for (int b = 0; b < kBufs; ++b) {
+        for (int b = 0; b < kDepth * kParts; ++b) {
             mbar_init(bar_tfull + 8 * b, 1);
-            mbar_init(bar_tempty + 8 * b, 8 * CG);
+            mbar_init(bar_tempty + 8 * b, 8);      // a pair: four warps of each CTA; one CTA: its eight
         }
-        for (int s = 0; s < kRing; ++s) {
+        for (int s = 0; s < kFp8Ring; ++s) {
             mbar_init(bar_sfull + 8 * s, 32);
             mbar_init(bar_sempty + 8 * s, 8);
         }
@@ -329,8 +333,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             const int32_t prow = t.p0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * 128, qrow = t.q0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * (BN / CG);
             const int32_t pz = p.ragged == kRaggedQ ? t.group : 0, qz = p.ragged == kRaggedP ? t.group : 0;      // the operand with one matrix per group
             for (int32_t kb = 0; kb < t.kbn; ++kb) {
-                ok = mbar_wait(bar_empty + 8 * s, ph ^ 1u, ctl, status_code(kRoleFp8Load, 0, s));
-                ok = __all_sync(0xffffffffu, ok);
+                ok = mbar_wait_warp(bar_empty + 8 * s, ph ^ 1u, ctl, status_code(kRoleFp8Load, 0, s));
                 if (!ok) break;
                 const uint32_t p_dst = smem_base + static_cast<uint32_t>(s) * kStageBytes, q_dst = p_dst + kFp8PBytes;
                 const int32_t k0 = (t.kb0 + kb) * kFp8Block;
@@ -353,132 +356,202 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         if constexpr (CG == 2) regs_lower<56>();
         if (is_leader) {
             int s = 0;
-            uint32_t ph = 0, buf = 0, bph = 0;
+            uint32_t ph = 0, par = 0;                             // par: bit d = phase of accumulator d's barriers
             const uint64_t desc_p0 = p.p_mn ? make_smem_desc_sw128_mn_major(smem_base, kFp8PBytes) : make_smem_desc_sw128(smem_base);
             const uint64_t desc_q0 = p.q_mn ? make_smem_desc_sw128_mn_major(smem_base + kFp8PBytes, kFp8PBytes) : make_smem_desc_sw128(smem_base + kFp8PBytes);
             // 32 further along the contraction: 32 bytes inside a swizzled row, or 32 rows of 128 bytes
             const uint32_t p_step = p.p_mn ? (32u * 128u) >> 4 : 2u, q_step = p.q_mn ? (32u * 128u) >> 4 : 2u;
+            const uint32_t q_part = p.q_mn ? 64u >> 4 : (64u * 128u) >> 4;        // a pair's second part: the next 64 of this CTA's 128 rows of Q
+            uint64_t dp = desc_p0, dq = desc_q0;
+            uint32_t full = bar_full;
+            // Each barrier is asked ahead of its use (the answer of a completed one takes some 100 cycles); only a "not yet" waits.
+            bool full_ready = false, acc_ready[kParts] = {};
             bool ok = true;
+            auto block = [&](auto dc) {                            // one block into accumulator dc
+                constexpr uint32_t d = decltype(dc)::value;
+                const uint32_t want = ((par >> d) & 1u) ^ 1u;
+                par ^= 1u << d;
+                if (!__all_sync(0xffffffffu, full_ready)) ok = mbar_wait_warp(full, ph, ctl, status_code(kRoleFp8Mma, 0, s));
+#pragma unroll
+                for (uint32_t h = 0; h < kParts; ++h) {
+                    constexpr uint32_t acc0 = d * kParts;
+                    if (h + 1 < kParts) acc_ready[h + 1] = mbar_test_wait(bar_tempty + 8 * (acc0 + h + 1), want);
+                    if (ok && !__all_sync(0xffffffffu, acc_ready[h])) ok = mbar_wait_warp(bar_tempty + 8 * (acc0 + h), want, ctl, status_code(kRoleFp8Mma, 1, acc0 + h));
+                    if (!ok) return;
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) umma_f8_elect<CG>(tmem_base + d * BN + h * (BN / kParts), dp + k * p_step, dq + h * q_part + k * q_step, p.idesc, k);
+                    if constexpr (CG == 2) {
+                        umma_commit_both_elect(bar_tfull + 8 * (acc0 + h));
+                        if (h + 1 == kParts) umma_commit_both_elect(full + 8 * kFp8MaxStages);
+                    } else {
+                        umma_commit_elect<1>(bar_tfull + 8 * (acc0 + h), 0);
+                        umma_commit_elect<1>(full + 8 * kFp8MaxStages, 0);
+                    }
+                }
+                dp += kStageBytes >> 4;
+                dq += kStageBytes >> 4;
+                full += 8;
+                if (++s == p.stages) { s = 0; ph ^= 1u; dp = desc_p0; dq = desc_q0; full = bar_full; }
+                full_ready = mbar_test_wait(full, ph);
+                constexpr uint32_t nd = (d + 1) % kDepth;
+                acc_ready[0] = mbar_test_wait(bar_tempty + 8 * nd * kParts, ((par >> nd) & 1u) ^ 1u);
+            };
             for (int32_t w = unit; ok && w < total; w += units) {
                 const int32_t kbn = __shfl_sync(0xffffffffu, tile_of(w).kbn, 0);
-                for (int32_t kb = 0; kb < kbn; ++kb) {
-                    ok = mbar_wait(bar_tempty + 8 * buf, bph ^ 1u, ctl, status_code(kRoleFp8Mma, 1, buf));
-                    ok = ok && mbar_wait(bar_full + 8 * s, ph, ctl, status_code(kRoleFp8Mma, 0, s));
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                    tc_fence_after_sync();
-                    const uint64_t dp = desc_p0 + static_cast<uint64_t>(static_cast<uint32_t>(s) * (kStageBytes >> 4));
-                    const uint64_t dq = desc_q0 + static_cast<uint64_t>(static_cast<uint32_t>(s) * (kStageBytes >> 4));
-#pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) umma_f8_elect<CG>(tmem_base + buf * BN, dp + k * p_step, dq + k * q_step, p.idesc, k);
-                    umma_commit_elect<CG>(bar_empty + 8 * s, 0);
-                    umma_commit_elect<CG>(bar_tfull + 8 * buf, 0);
-                    if (++s == p.stages) { s = 0; ph ^= 1u; }
-                    if (++buf == kBufs) { buf = 0; bph ^= 1u; }
+                acc_ready[0] = false;                              // every tile begins with accumulator 0
+                for (int32_t kb = 0; ok && kb < kbn; kb += kDepth) {
+                    block(std::integral_constant<uint32_t, 0>());
+                    if (ok && kb + 1 < kbn) block(std::integral_constant<uint32_t, 1>());
+                    if constexpr (kDepth == 4) {
+                        if (ok && kb + 2 < kbn) block(std::integral_constant<uint32_t, 2>());
+                        if (ok && kb + 3 < kbn) block(std::integral_constant<uint32_t, 3>());
+                    }
                 }
             }
         }
     } else if (warp == 2) {
         // ===== scales =====
         if constexpr (CG == 2) regs_lower<56>();
-        int s = 0;
-        uint32_t ph = 0;
+        uint32_t it = 0;
         bool ok = true;
         for (int32_t w = unit; ok && w < total; w += units) {
             const Fp8Tile t = tile_of(w);
             const int32_t prow = t.p0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * 128;
-            const float *sp = p.sp + t.group * p.sp_group, *sq = p.sq + t.group * p.sq_group;
-            for (int32_t kb = 0; kb < t.kbn; ++kb) {
-                ok = mbar_wait(bar_sempty + 8 * s, ph ^ 1u, ctl, status_code(kRoleFp8Scale, 0, s));
-                ok = __all_sync(0xffffffffu, ok);
+            const float *sp = p.sp + t.group * p.sp_group + t.kb0 * p.sp_kb, *sq = p.sq + t.group * p.sq_group + t.kb0 * p.sq_kb;
+            for (int32_t kb = 0; kb < t.kbn; ++kb, ++it, sp += p.sp_kb, sq += p.sq_kb) {
+                const uint32_t batch = it / kFp8Batch, s = batch % kFp8Ring, slot = ring_base + (it % (kFp8Ring * kFp8Batch)) * kSlotBytes;
+                if (it % kFp8Batch == 0) ok = mbar_wait_warp(bar_sempty + 8 * s, ((batch / kFp8Ring) & 1u) ^ 1u, ctl, status_code(kRoleFp8Scale, 0, s));
                 if (!ok) break;
-                const uint32_t slot = ring_base + static_cast<uint32_t>(s) * kSlotBytes;
-                const float *spk = sp + (t.kb0 + kb) * p.sp_kb, *sqk = sq + (t.kb0 + kb) * p.sq_kb;
                 if constexpr (P_ROW) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int32_t r = prow + i * 32 + static_cast<int32_t>(lane);
-                        cp_async_4(slot + (i * 32 + lane) * 4u, r < t.p_end ? spk + r * p.sp_row : spk, r < t.p_end ? 4u : 0u);
+                        cp_async_4(slot + (i * 32 + lane) * 4u, r < t.p_end ? sp + r * p.sp_row : sp, r < t.p_end ? 4u : 0u);
                     }
                 } else {
-                    if (lane == 0) cp_async_4(slot, spk + (prow >> 7) * p.sp_row, 4u);
+                    if (lane == 0) cp_async_4(slot, sp + (prow >> 7) * p.sp_row, 4u);
                 }
                 if constexpr (Q_COL) {
 #pragma unroll
                     for (int i = 0; i < (BN + 31) / 32; ++i) {
                         const int32_t c = i * 32 + static_cast<int32_t>(lane), r = t.q0 + c;
-                        if (BN >= 32 || c < BN) cp_async_4(slot + 512u + c * 4u, r < t.q_end ? sqk + r * p.sq_row : sqk, r < t.q_end ? 4u : 0u);
+                        if (BN >= 32 || c < BN) cp_async_4(slot + 512u + c * 4u, r < t.q_end ? sq + r * p.sq_row : sq, r < t.q_end ? 4u : 0u);
                     }
                 } else {
                     const int32_t r = t.q0 + static_cast<int32_t>(lane) * 128;
-                    if (lane < BN / 128) cp_async_4(slot + 512u + lane * 4u, r < t.q_end ? sqk + (r >> 7) * p.sq_row : sqk, r < t.q_end ? 4u : 0u);
+                    if (lane < BN / 128) cp_async_4(slot + 512u + lane * 4u, r < t.q_end ? sq + (r >> 7) * p.sq_row : sq, r < t.q_end ? 4u : 0u);
                 }
-                cp_async_mbar_arrive(bar_sfull + 8 * s);
-                if (++s == kRing) { s = 0; ph ^= 1u; }
+                if (it % kFp8Batch == kFp8Batch - 1) cp_async_mbar_arrive(bar_sfull + 8 * s);
             }
         }
+        if (it % kFp8Batch != 0) cp_async_mbar_arrive(bar_sfull + 8 * ((it / kFp8Batch) % kFp8Ring));      // the last, partly filled batch
         cp_async_wait_all();
     } else if (warp == 3) {
         if constexpr (CG == 2) regs_lower<56>();
     } else {
         // ===== promotion (warps 4..11) =====
         if constexpr (CG == 2) regs_raise<224>();
-        const uint32_t ew = warp - 4u, quarter = warp & 3u, half = ew >> 2;         // half: first or second BN / 2 columns
+        const uint32_t ew = warp - 4u, quarter = warp & 3u, half = ew >> 2;         // half: which BN / 2 accumulator columns
         const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + half * kCols;
         const uint32_t row_in_tile = quarter * 32u + lane;
-        const uint32_t tempty_leader = CG == 2 ? mapa(bar_tempty, 0) : bar_tempty;
-        int s = 0;
-        uint32_t ph = 0, buf = 0, bph = 0;
+        const uint32_t tempty = CG == 2 ? mapa(bar_tempty, 0) + half * 8u : bar_tempty, tfull = bar_tfull + (CG == 2 ? half * 8u : 0u);
+        const uint32_t ring_end = ring_base + kFp8Ring * kFp8Batch * kSlotBytes;
+        uint32_t it = 0;                                          // blocks so far (scales)
+        uint32_t slot = ring_base;                                // the next block's scales
+        uint32_t par = 0;                                         // bit d = phase of accumulator d's barriers
         bool ok = true;
         for (int32_t w = unit; ok && w < total; w += units) {
-            const Fp8Tile t = tile_of(w);
+            const int32_t kbn = __shfl_sync(0xffffffffu, tile_of(w).kbn, 0);
             uint64_t acc[kCols / 2];
 #pragma unroll
             for (int i = 0; i < kCols / 2; ++i) acc[i] = 0ull;
-            for (int32_t kb = 0; kb < t.kbn; ++kb) {
-                ok = mbar_wait_inline(bar_sfull + 8 * s, ph, ctl, status_code(kRoleFp8Promote, 0, s));
-                const uint32_t slot = ring_base + static_cast<uint32_t>(s) * kSlotBytes;
-                float sc = ld_shared_f32(slot + (P_ROW ? row_in_tile * 4u : 0u));
-                if constexpr (!Q_COL) sc *= ld_shared_f32(slot + 512u + half * 4u);
-                const uint64_t sc2 = pack_f32x2(__float_as_uint(sc), __float_as_uint(sc));
-                const uint32_t sq = slot + 512u + half * kCols * 4u;
-                ok = ok && mbar_wait_inline(bar_tfull + 8 * buf, bph, ctl, status_code(kRoleFp8Promote, 1, buf));
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
+            // A block's scales -- the row's, and those of the first and the last 64 of a pair's columns -- are read one block
+            // ahead, and its accumulator's barrier is asked ahead too, so that neither round trip lies between two accumulators.
+            float row_s = 0.0f, col_s0 = 1.0f, col_s1 = 1.0f;
+            uint32_t sq_next = 0;                                 // Q_COL: this warp's columns' scales of the block that was read last
+            bool ready = false;
+            auto read_scales = [&](bool first) {
+                const uint32_t batch = it / kFp8Batch;
+                if (it % kFp8Batch == 0 || first) ok = mbar_wait_warp(bar_sfull + 8 * (batch % kFp8Ring), (batch / kFp8Ring) & 1u, ctl, status_code(kRoleFp8Promote, 0, 0));
+                row_s = ld_shared_f32(slot + (P_ROW ? row_in_tile * 4u : 0u));
+                if constexpr (Q_COL) {
+                    sq_next = slot + 512u + (CG == 2 ? half * 64u : half * kCols) * 4u;
+                } else {
+                    col_s0 = ld_shared_f32(slot + 512u);
+                    col_s1 = ld_shared_f32(slot + 516u);
+                }
+                slot += kSlotBytes;
+                if (slot == ring_end) slot = ring_base;
+            };
+            if (kbn > 0) read_scales(true);
+            auto block = [&](auto dc, bool last) {                 // one block from accumulator dc
+                constexpr uint32_t d = decltype(dc)::value, nd = (d + 1) % kDepth;
+                [[maybe_unused]] const uint32_t sq = sq_next;
+                const float sc0 = row_s * col_s0, sc1 = row_s * col_s1;
+                const uint64_t row0 = pack_f32x2(__float_as_uint(sc0), __float_as_uint(sc0)), row1 = pack_f32x2(__float_as_uint(sc1), __float_as_uint(sc1));
+                const uint32_t batch_bar = bar_sempty + 8 * ((it / kFp8Batch) % kFp8Ring);
+                const bool batch_end = it % kFp8Batch == kFp8Batch - 1;
+                if (!Q_COL && batch_end) mbar_arrive_elect(batch_bar);        // the batch's last scales are in registers
+                if (!__all_sync(0xffffffffu, ready)) ok = mbar_wait_warp(tfull + 8 * kParts * d, (par >> d) & 1u, ctl, status_code(kRoleFp8Promote, 1, d));
+                if (!ok) return;
+                par ^= 1u << d;
+                ++it;
                 tc_fence_after_sync();
-                constexpr int kChunk = kCols < 32 ? kCols : 32;
+                constexpr int kChunk = kCols < 16 ? kCols : 16, kChunks = kCols / kChunk;
+                uint32_t v[2][kChunk];
+                auto load = [&](int c) {
+                    if constexpr (kChunk == 16) tmem_ld_32x32b_x16(taddr + d * BN + c * kChunk, v[c & 1]);
+                    else tmem_ld_32x32b_x8(taddr + d * BN + c * kChunk, v[c & 1]);
+                };
+                load(0);
 #pragma unroll
-                for (int c = 0; c < kCols; c += kChunk) {
-                    uint32_t v[kChunk];
-                    if constexpr (kChunk == 32) tmem_ld_32x32b_x32(taddr + buf * BN + c, v);
-                    else if constexpr (kChunk == 16) tmem_ld_32x32b_x16(taddr + buf * BN + c, v);
-                    else tmem_ld_32x32b_x8(taddr + buf * BN + c, v);
-                    tmem_ld_wait();
+                for (int c = 0; c < kChunks; ++c) {
+                    tmem_ld_wait_for(v[c & 1]);
+                    if (c + 1 < kChunks) {
+                        load(c + 1);                               // in flight while this chunk is added up
+                    } else {
+                        tc_fence_before_sync();                    // the accumulator is in registers: a later block may have it
+                        if constexpr (CG == 2) mbar_arrive_cluster_elect(tempty + 8 * kParts * d);
+                        else mbar_arrive_elect(tempty + 8 * kParts * d);
+                        ready = false;
+                        if (!last) {
+                            read_scales(false);
+                            ready = mbar_test_wait(tfull + 8 * kParts * nd, (par >> nd) & 1u);
+                        }
+                    }
 #pragma unroll
                     for (int i = 0; i < kChunk; i += 4) {
-                        uint64_t s0 = sc2, s1 = sc2;
+                        const int col = c * kChunk + i, j = col / 2;
+                        const uint32_t *x = v[c & 1] + i;
+                        uint64_t s0 = (CG == 2 && !Q_COL && col >= 64) ? row1 : row0, s1 = s0;
                         if constexpr (Q_COL) {
-                            ld_shared_2x64(sq + (c + i) * 4u, s0, s1);
-                            s0 = mul_f32x2(s0, sc2);
-                            s1 = mul_f32x2(s1, sc2);
+                            ld_shared_2x64(sq + static_cast<uint32_t>(CG == 2 && col >= 64 ? col + 64 : col) * 4u, s0, s1);
+                            s0 = mul_f32x2(s0, row0);
+                            s1 = mul_f32x2(s1, row0);
                         }
-                        acc[(c + i) / 2] = fma_f32x2(pack_f32x2(v[i], v[i + 1]), s0, acc[(c + i) / 2]);
-                        acc[(c + i) / 2 + 1] = fma_f32x2(pack_f32x2(v[i + 2], v[i + 3]), s1, acc[(c + i) / 2 + 1]);
+                        acc[j] = fma_f32x2(pack_f32x2(x[0], x[1]), s0, acc[j]);
+                        acc[j + 1] = fma_f32x2(pack_f32x2(x[2], x[3]), s1, acc[j + 1]);
                     }
                 }
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) {
-                    if (is_leader) mbar_arrive(bar_tempty + 8 * buf);
-                    else mbar_arrive_cluster(tempty_leader + 8 * buf);
-                    mbar_arrive(bar_sempty + 8 * s);
+                if constexpr (Q_COL) {
+                    __syncwarp();                                  // every lane has read this block's scales
+                    if (batch_end) mbar_arrive_elect(batch_bar);
                 }
-                if (++s == kRing) { s = 0; ph ^= 1u; }
-                if (++buf == kBufs) { buf = 0; bph ^= 1u; }
+            };
+#pragma unroll 1
+            for (int32_t kb = 0; ok && kb < kbn; kb += kDepth) {
+                block(std::integral_constant<uint32_t, 0>(), kb + 1 == kbn);
+                if (ok && kb + 1 < kbn) block(std::integral_constant<uint32_t, 1>(), kb + 2 == kbn);
+                if constexpr (kDepth == 4) {
+                    if (ok && kb + 2 < kbn) block(std::integral_constant<uint32_t, 2>(), kb + 3 == kbn);
+                    if (ok && kb + 3 < kbn) block(std::integral_constant<uint32_t, 3>(), kb + 4 == kbn);
+                }
             }
+            const Fp8Tile t = tile_of(w);
             if (!ok) break;
             if constexpr (CG == 2) {
-                const int32_t row0 = t.p0 + static_cast<int32_t>(rank * 128u + quarter * 32u), col0 = t.q0 + static_cast<int32_t>(half) * 128;
+                const int32_t row0 = t.p0 + static_cast<int32_t>(rank * 128u + quarter * 32u), col0 = t.q0 + static_cast<int32_t>(half) * 64;
                 const uint32_t staging = staging_base + ew * kFp8StagingPerWarp;
                 const int64_t base = t.group * p.c_group;
                 if (p.out_type == 0) fp8_store_rows<float>(acc, staging, p, static_cast<float *>(p.out) + base, row0, t.p_end, col0, t.q_end, lane);

@@ -43,17 +43,21 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
     return mbar_wait_slow(bar, parity, ctl, code);
 }
 
-// The same wait without a call: for code that keeps most of its registers live across it.
-__device__ __forceinline__ bool mbar_wait_inline(uint32_t bar, uint32_t parity, const WaitCtl &ctl, uint32_t code)
+// The same wait for a converged warp, without a call (for code that keeps most of its registers live across it); the result is
+// the same in every lane.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, const WaitCtl &ctl, uint32_t code)
 {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     const long long t0 = clock64();
 #pragma unroll 1
-    while (!mbar_try_wait(bar, parity)) {
-        if (*ctl.abort_flag) return false;
-        if (clock64() - t0 > ctl.budget) {
-            *ctl.abort_flag = 1u;
-            atomicCAS(ctl.status, 0u, code);
+    while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
+        const bool late = clock64() - t0 > ctl.budget;
+        if (__any_sync(0xffffffffu, late || *ctl.abort_flag != 0u)) {
+            if (late && *ctl.abort_flag == 0u) {
+                *ctl.abort_flag = 1u;
+                atomicCAS(ctl.status, 0u, code);
+            }
+            __syncwarp();
             return false;
         }
     }

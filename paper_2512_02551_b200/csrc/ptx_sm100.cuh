@@ -475,6 +475,32 @@ __device__ __forceinline__ void umma_f8_elect(uint32_t d_tmem, uint64_t a_desc, 
             : "memory");
 }
 
+// One lane of the (converged) warp arrives on a barrier of the cluster (address from mapa), or of this CTA.
+__device__ __forceinline__ void mbar_arrive_cluster_elect(uint32_t cluster_bar)
+{
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}"
+        ::"r"(cluster_bar) : "memory");
+}
+
+__device__ __forceinline__ void mbar_arrive_elect(uint32_t bar)
+{
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}"
+        ::"r"(bar) : "memory");
+}
+
+// One commit whose arrival goes to the barrier at the same shared-memory offset in both CTAs of a two-CTA cluster.
+__device__ __forceinline__ void umma_commit_both_elect(uint32_t bar)
+{
+    asm volatile(
+        "{\n\t.reg .pred e;\n\t.reg .b16 m;\n\telect.sync _|e, 0xffffffff;\n\tmov.b16 m, 3;\n\t"
+        "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}"
+        ::"r"(bar) : "memory");
+}
+
 // Whole warp: thread t reads 8 (16) consecutive fp32 columns of tensor-memory lane (base lane + t).
 __device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t *r)
 {
@@ -493,6 +519,20 @@ __device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t *r)
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr)
         : "memory");
+}
+
+// Waits for this thread's tensor-memory loads; the registers pass through, so that nothing that uses them moves ahead of the wait.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])::"memory");
+}
+
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]),
+                   "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
 }
 
 // Two fp32 lanes at once (one 64-bit register pair each): a * b + c and a * b, each lane rounded as fmaf / a product.
