@@ -109,15 +109,16 @@ const void *kernel_of(int32_t form, const hgemm_fp8_config_t &c)
     }
 }
 
-// {inner, outer, matrices} bytes with `ld` between rows; boxes of 128 bytes x box_outer rows of one matrix.
-bool encode(hgemm_ctx_s *ctx, CUtensorMap *map, const void *base, int64_t inner, int64_t outer, int64_t matrices, int64_t ld, uint32_t box_outer)
+// {inner, outer, matrices} elements with `ld` between rows; boxes of 128 bytes x box_outer rows of one matrix.
+bool encode(hgemm_ctx_s *ctx, CUtensorMap *map, CUtensorMapDataType type, int bytes, const void *base, int64_t inner, int64_t outer, int64_t matrices, int64_t ld,
+            uint32_t box_outer)
 {
     cuuint64_t dims[3] = {cuuint64_t(inner), cuuint64_t(outer), cuuint64_t(matrices)};
-    cuuint64_t strides[2] = {cuuint64_t(ld), cuuint64_t(ld) * cuuint64_t(outer)};
-    cuuint32_t box[3] = {128, box_outer, 1};
+    cuuint64_t strides[2] = {cuuint64_t(ld) * unsigned(bytes), cuuint64_t(ld) * unsigned(bytes) * cuuint64_t(outer)};
+    cuuint32_t box[3] = {128u / unsigned(bytes), box_outer, 1};
     cuuint32_t estr[3] = {1, 1, 1};
-    const CUresult r = ctx->encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const CUresult r = ctx->encode(map, type, 3, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
         ctx->last_cuda_error = int(r);
         return false;
@@ -377,6 +378,15 @@ hgemm_status_t hgemm_fp8_run(hgemm_fp8_plan_t *plan, const void *A, int64_t lda,
     if (tiles > (int64_t(1) << 30)) return HGEMM_ERR_UNSUPPORTED;
     p.total = int32_t(tiles);
     p.raster = std::min(8, p.tiles_p);
+    {
+        using hgemm_dev::make_fast_div;
+        const int32_t last = p.tiles_p - (p.tiles_p - 1) / p.raster * p.raster;         // rows of tiles of the last sweep
+        p.fd_other = make_fast_div(uint32_t(p.ragged == hgemm_dev::kRaggedP ? p.tiles_q : p.tiles_p));
+        p.fd_group = make_fast_div(uint32_t(p.tiles_p) * uint32_t(p.tiles_q));
+        p.fd_sweep = make_fast_div(uint32_t(p.raster) * uint32_t(p.tiles_q));
+        p.fd_raster = make_fast_div(uint32_t(p.raster));
+        p.fd_last = make_fast_div(uint32_t(last));
+    }
     p.sp = P.s;
     p.sp_row = P.s_row;
     p.sp_kb = P.s_kb;
@@ -392,21 +402,27 @@ hgemm_status_t hgemm_fp8_run(hgemm_fp8_plan_t *plan, const void *A, int64_t lda,
     p.c_group = wgrad ? N * ldc : 0;
     p.out_type = plan->out_type;
     p.accumulate = accumulate;
-    p.vec_ok = aligned16(C) && (ldc * es) % 16 == 0 ? 1 : 0;
+    p.vec_ok = aligned16(C) && (ldc * es) % 16 == 0 && (out_cols * es) % 16 == 0 ? 1 : 0;      // a tensor store clips at multiples of 16 bytes only
     // instruction descriptor: fp32 accumulators; formats 0 = e4m3, 1 = e5m2; bits 15 / 16: operand stored along its own rows
     p.idesc = (1u << 4) | (P.type == HGEMM_TYPE_E5M2 ? 1u << 7 : 0u) | (Q.type == HGEMM_TYPE_E5M2 ? 1u << 10 : 0u) | (P.mn ? 1u << 15 : 0u) | (Q.mn ? 1u << 16 : 0u) |
               (uint32_t((tq / c.cta_group) >> 3) << 17) | (uint32_t(tp >> 4) << 24);
     p.status = ctx->d_status + plan->status_slot;
     p.wait_budget = ctx->wait_budget;
 
-    CUtensorMap map_p, map_q;
-    if (!encode(ctx, &map_p, P.base, P.inner, P.outer, P.count, P.ld, 128)) return HGEMM_ERR_CUDA;
-    if (!encode(ctx, &map_q, Q.base, Q.inner, Q.outer, Q.count, Q.ld, Q.mn ? 128u : uint32_t(tq / c.cta_group))) return HGEMM_ERR_CUDA;
+    CUtensorMap map_p, map_q, map_c;
+    if (!encode(ctx, &map_p, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, P.base, P.inner, P.outer, P.count, P.ld, 128)) return HGEMM_ERR_CUDA;
+    if (!encode(ctx, &map_q, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Q.base, Q.inner, Q.outer, Q.count, Q.ld, Q.mn ? 128u : uint32_t(tq / c.cta_group))) return HGEMM_ERR_CUDA;
+    map_c = map_p;                                           // not used by the kernels that store through pointers
+    if (c.cta_group == 2 && p.vec_ok && !accumulate) {
+        const CUtensorMapDataType t = plan->out_type == HGEMM_TYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : plan->out_type == HGEMM_TYPE_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                                                                                                        : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+        if (!encode(ctx, &map_c, t, es, C, out_cols, wgrad ? N : M, wgrad ? matrices : 1, ldc, 32)) return HGEMM_ERR_CUDA;
+    }
     const int per_unit = c.cta_group == 2 ? 2 : c.split_k;
     // CTAs that share a tile through a cluster's shared memory take one tile each; the others walk the tiles
     const int64_t units = c.split_k > 1 ? tiles : std::min<int64_t>(tiles, std::max(1, ctx->num_sms / per_unit));
     if (units * per_unit > 0x7fffffff) return HGEMM_ERR_UNSUPPORTED;
-    void *args[3] = {&map_p, &map_q, &p};
+    void *args[4] = {&map_p, &map_q, &map_c, &p};
     return launch(ctx, kernel_of(form, c), dim3(unsigned(units * per_unit), 1, 1), hgemm_dev::kFp8Threads, smem, per_unit, args, stream);
 }
 

@@ -41,7 +41,7 @@ constexpr int kFp8PBytes = 128 * 128;             // P part of a stage: 128 rows
 constexpr int kFp8MaxStages = 12;
 constexpr int kFp8MaxGroups = 1024;
 constexpr int kFp8CtrlBytes = 512;
-constexpr int kFp8StagingPerWarp = 2048;          // direct stores: 32 rows x 64 bytes
+constexpr int kFp8StagingPerWarp = 8192;          // results on their way out: two boxes of 32 rows x 128 bytes
 constexpr uint32_t kRoleFp8Load = 8, kRoleFp8Mma = 9, kRoleFp8Scale = 10, kRoleFp8Promote = 11;
 constexpr int kFp8Batch = 4, kFp8Ring = 2;        // scales travel in batches of four blocks, two batches in flight (one barrier round per batch)
 __host__ __device__ constexpr int fp8_slot_bytes(int bn, bool q_col) { return (128 + (q_col ? bn : 4)) * 4; }     // one block's scales
@@ -55,13 +55,14 @@ struct Fp8Params {
     int32_t tiles_p, tiles_q;      // tiles per group (unused for the side that follows the offsets)
     int32_t total;                 // tiles, where the host knows them (kRaggedNone, kRaggedK)
     int32_t raster;                // tiles of P visited together
+    FastDiv fd_other, fd_group, fd_sweep, fd_raster, fd_last;   // divisors of the tile numbering: see fp8_tile
     int32_t groups, ragged, rows_ragged, k_capacity;   // rows_ragged: clamp of the offsets; k_capacity: blocks the padded copy has
     const int32_t *offsets;
     const float *sp, *sq;          // scale of row r (or of block r / 128), block b: s[r * _row + b * _kb + group * _group]
     int64_t sp_row, sp_kb, sp_group, sq_row, sq_kb, sq_group;
     void *out;
     int64_t ldc, c_group;
-    int32_t out_type, accumulate, vec_ok;   // out_type: 0 fp32, 1 fp16, 2 bf16; vec_ok: rows of C start at multiples of 16 bytes
+    int32_t out_type, accumulate, vec_ok;   // out_type: 0 fp32, 1 fp16, 2 bf16; vec_ok: rows of C start and end at multiples of 16 bytes
     int32_t split, stages;
     int32_t p_mn, q_mn;            // operand stored along its own rows' dimension (contraction down the columns)
     uint32_t idesc;
@@ -85,7 +86,7 @@ __device__ __forceinline__ Fp8Tile fp8_tile(int32_t w, const Fp8Params &p, const
     t.q_end = p.rows_q;
     if (p.ragged == kRaggedP || p.ragged == kRaggedQ) {
         const int32_t other = p.ragged == kRaggedP ? p.tiles_q : p.tiles_p;
-        const int32_t r = w / other, o = w - r * other;
+        const int32_t r = fast_div(w, p.fd_other), o = w - r * other;
         int32_t g = 0;                                   // groups whose tiles all come before r
         for (int32_t base = 0; base < p.groups; base += 32) {
             const int32_t e = base + static_cast<int32_t>(lane);
@@ -108,14 +109,14 @@ __device__ __forceinline__ Fp8Tile fp8_tile(int32_t w, const Fp8Params &p, const
     }
     if (p.ragged == kRaggedK) {
         const int32_t per = p.tiles_p * p.tiles_q;
-        t.group = w / per;
+        t.group = fast_div(w, p.fd_group);
         w -= t.group * per;
         t.kb0 = pre[t.group];
         t.kbn = pre[t.group + 1] - t.kb0;
     }
-    const int32_t per_group = p.raster * p.tiles_q;
-    const int32_t rg = w / per_group, first = rg * p.raster, size = min(p.raster, p.tiles_p - first), rem = w - rg * per_group;
-    const int32_t tq = rem / size;
+    const int32_t sweep = p.raster * p.tiles_q;          // tiles of `raster` rows of tiles
+    const int32_t rg = fast_div(w, p.fd_sweep), first = rg * p.raster, size = min(p.raster, p.tiles_p - first), rem = w - rg * sweep;
+    const int32_t tq = fast_div(rem, size == p.raster ? p.fd_raster : p.fd_last);
     t.p0 = (first + rem - tq * size) * TP;
     t.q0 = tq * TQ;
     return t;
@@ -174,62 +175,70 @@ __device__ __forceinline__ uint32_t fp8_pack2(float a, float b, __nv_bfloat16)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// One warp's 32 rows x 128 columns of running sums (64 columns from col0, 64 from col0 + 128) to C, by rows: 64 bytes of every row at a time through the warp's staging
-// buffer (16-byte pieces XOR-swizzled by row pairs: conflict-free both ways), so that four lanes write 64 consecutive bytes.
+// One warp's 32 rows x 128 columns of running sums (64 columns from col0, 64 from col0 + 128) to C, by rows.  Each lane packs its
+// row into boxes of 32 rows x 128 bytes in shared memory (16-byte pieces swizzled as TMA reads them: conflict-free), which leave as
+// tensor stores while the warp goes on with the next tile; stores by the warp itself kept it for 3500 cycles a tile.  A warp whose
+// rows end inside its 32 (a group's end), rows of C that do not start at multiples of 16 bytes, and C += take ordinary
+// stores of 32 consecutive elements instead.
 template <class T>
-__device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32_t staging, const Fp8Params &p, T *out, int32_t row0, int32_t row_end,
-                                               int32_t col0, int32_t col_end, uint32_t lane)
+__device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32_t staging, const Fp8Params &p, const CUtensorMap *tmap_c, const Fp8Tile &t,
+                                               int32_t row0, int32_t col0, uint32_t lane)
 {
-    constexpr int kCols = 64 / static_cast<int>(sizeof(T));     // columns of one pass
-    constexpr int kPer = 16 / static_cast<int>(sizeof(T));      // elements of 16 bytes
-    const uint32_t mine = staging + lane * 64u, swz = (lane >> 1) & 3u;
+    constexpr int kSize = static_cast<int>(sizeof(T));
+    constexpr int kBox = 128 / kSize;                             // columns of a box
+    constexpr int kPass = 2 * kBox;                               // columns of one pass: two boxes
+    const uint32_t mine = staging + lane * 128u, swz = lane & 7u;
+    const bool whole = p.vec_ok && !p.accumulate && (row0 + 32 <= t.p_end || t.p_end == p.rows_p);   // the map clips at the matrix's own end
 #pragma unroll
-    for (int c = 0; c < 128; c += kCols) {
+    for (int c = 0; c < 128; c += kPass) {
+        bulk_wait_group_read<0>();                                // earlier stores have read the boxes
+        __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 16; ++j) {
             uint32_t v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if constexpr (sizeof(T) == 4) {
-                    float lo, hi;
+                float lo, hi;
+                if constexpr (kSize == 4) {
                     unpack_f32x2(acc[(c + j * 4 + i) / 2], lo, hi);
                     v[i] = __float_as_uint((i & 1) ? hi : lo);
                 } else {
-                    float lo, hi;
-                    unpack_f32x2(acc[(c + j * 8) / 2 + i], lo, hi);
+                    unpack_f32x2(acc[j * 4 + i], lo, hi);
                     v[i] = fp8_pack2(lo, hi, T());
                 }
             }
-            st_shared_v4(mine + ((static_cast<uint32_t>(j) ^ swz) * 16u), v[0], v[1], v[2], v[3]);
+            st_shared_v4(mine + (j / 8) * 4096u + (((j & 7u) ^ swz) * 16u), v[0], v[1], v[2], v[3]);
         }
-        __syncwarp();
+        if (whole) {
+            fence_proxy_async_smem();
+            __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t r = static_cast<uint32_t>(i) * 8u + lane / 4u, k = lane & 3u;
-            const int32_t row = row0 + static_cast<int32_t>(r), col = col0 + (c < 64 ? c : c + 64) + static_cast<int32_t>(k) * kPer;
-            float4 v = ld_shared_v4(staging + r * 64u + ((k ^ ((r >> 1) & 3u)) * 16u));
-            if (row < row_end && col < col_end) {
-                T *dst = out + static_cast<int64_t>(row) * p.ldc + col;
-                if (p.vec_ok && col + kPer <= col_end) {
-                    if constexpr (sizeof(T) == 4) {
-                        if (p.accumulate) {
-                            const float4 old = *reinterpret_cast<const float4 *>(dst);
-                            v.x += old.x; v.y += old.y; v.z += old.z; v.w += old.w;
+            for (int r = 0; r < 2; ++r) {
+                const int at = c + r * kBox, col = col0 + at + (at & 64);
+                if (row0 < t.p_end && col < t.q_end) tma_store_3d_elect(tmap_c, col, row0, p.ragged == kRaggedK ? t.group : 0, staging + r * 4096u);
+            }
+        } else {
+            __syncwarp();
+            T *out = static_cast<T *>(p.out) + t.group * p.c_group;
+#pragma unroll 1
+            for (int32_t i = 0; i < 32 && row0 + i < t.p_end; ++i) {
+                T *dst = out + static_cast<int64_t>(row0 + i) * p.ldc;
+#pragma unroll
+                for (int x = 0; x < kPass; x += 32) {
+                    const int32_t at = x + static_cast<int32_t>(lane), byte = at * kSize, col = col0 + c + at + ((c + at) & 64);
+                    const uint32_t src = staging + (byte / 128) * 4096 + i * 128 + (((byte / 16) ^ i) & 7) * 16 + (byte & 15);
+                    if (col < t.q_end) {
+                        if constexpr (kSize == 4) {
+                            const float v = ld_shared_f32(src);
+                            dst[col] = p.accumulate ? dst[col] + v : v;
+                        } else {
+                            const unsigned short h = ld_shared_u16(src);
+                            dst[col] = *reinterpret_cast<const T *>(&h);
                         }
-                    }
-                    *reinterpret_cast<float4 *>(dst) = v;
-                } else {
-                    const T *src = reinterpret_cast<const T *>(&v);
-#pragma unroll
-                    for (int x = 0; x < kPer; ++x) {
-                        if (col + x >= col_end) break;
-                        if constexpr (sizeof(T) == 4) dst[x] = p.accumulate ? dst[x] + src[x] : src[x];
-                        else dst[x] = src[x];
                     }
                 }
             }
         }
-        __syncwarp();
     }
 }
 
@@ -244,7 +253,7 @@ __device__ __forceinline__ void fp8_store_one(T *dst, float v, int32_t accumulat
 // (else one per 128).  CG == 2 stores by rows, CG == 1 transposed.
 template <int CG, int BN, bool P_ROW, bool Q_COL>
 __global__ void __launch_bounds__(kFp8Threads, 1)
-fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_constant__ CUtensorMap tmap_q, const Fp8Params p)
+fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_c, const Fp8Params p)
 {
     constexpr int TP = 128 * CG, TQ = BN;
     constexpr int kCols = BN / 2;                                 // columns of the tile a promoting warp holds
@@ -504,12 +513,23 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                     if constexpr (kChunk == 16) tmem_ld_32x32b_x16(taddr + d * BN + c * kChunk, v[c & 1]);
                     else tmem_ld_32x32b_x8(taddr + d * BN + c * kChunk, v[c & 1]);
                 };
+                [[maybe_unused]] uint64_t qs[2][kChunk / 2];       // Q_COL: the chunk's column scales, a chunk ahead like the accumulator
+                auto load_q = [&](int c) {
+                    if constexpr (Q_COL) {
+                        const int col = c * kChunk;
+#pragma unroll
+                        for (int i = 0; i < kChunk / 2; i += 2)
+                            ld_shared_2x64(sq + static_cast<uint32_t>((CG == 2 && col >= 64 ? col + 64 : col) + 2 * i) * 4u, qs[c & 1][i], qs[c & 1][i + 1]);
+                    }
+                };
+                load_q(0);
                 load(0);
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) {
                     tmem_ld_wait_for(v[c & 1]);
                     if (c + 1 < kChunks) {
                         load(c + 1);                               // in flight while this chunk is added up
+                        load_q(c + 1);
                     } else {
                         tc_fence_before_sync();                    // the accumulator is in registers: a later block may have it
                         if constexpr (CG == 2) mbar_arrive_cluster_elect(tempty + 8 * kParts * d);
@@ -526,9 +546,8 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                         const uint32_t *x = v[c & 1] + i;
                         uint64_t s0 = (CG == 2 && !Q_COL && col >= 64) ? row1 : row0, s1 = s0;
                         if constexpr (Q_COL) {
-                            ld_shared_2x64(sq + static_cast<uint32_t>(CG == 2 && col >= 64 ? col + 64 : col) * 4u, s0, s1);
-                            s0 = mul_f32x2(s0, row0);
-                            s1 = mul_f32x2(s1, row0);
+                            s0 = mul_f32x2(qs[c & 1][i / 2], row0);
+                            s1 = mul_f32x2(qs[c & 1][i / 2 + 1], row0);
                         }
                         acc[j] = fma_f32x2(pack_f32x2(x[0], x[1]), s0, acc[j]);
                         acc[j + 1] = fma_f32x2(pack_f32x2(x[2], x[3]), s1, acc[j + 1]);
@@ -553,10 +572,9 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             if constexpr (CG == 2) {
                 const int32_t row0 = t.p0 + static_cast<int32_t>(rank * 128u + quarter * 32u), col0 = t.q0 + static_cast<int32_t>(half) * 64;
                 const uint32_t staging = staging_base + ew * kFp8StagingPerWarp;
-                const int64_t base = t.group * p.c_group;
-                if (p.out_type == 0) fp8_store_rows<float>(acc, staging, p, static_cast<float *>(p.out) + base, row0, t.p_end, col0, t.q_end, lane);
-                else if (p.out_type == 1) fp8_store_rows<__half>(acc, staging, p, static_cast<__half *>(p.out) + base, row0, t.p_end, col0, t.q_end, lane);
-                else fp8_store_rows<__nv_bfloat16>(acc, staging, p, static_cast<__nv_bfloat16 *>(p.out) + base, row0, t.p_end, col0, t.q_end, lane);
+                if (p.out_type == 0) fp8_store_rows<float>(acc, staging, p, &tmap_c, t, row0, col0, lane);
+                else if (p.out_type == 1) fp8_store_rows<__half>(acc, staging, p, &tmap_c, t, row0, col0, lane);
+                else fp8_store_rows<__nv_bfloat16>(acc, staging, p, &tmap_c, t, row0, col0, lane);
             } else if (p.split > 1) {
                 // this slice's part, columns of 128 rows, where the operand stages were (every MMA that read them is complete)
 #pragma unroll
@@ -589,6 +607,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         }
     }
 
+    if constexpr (CG == 2) bulk_wait_group<0>();              // the results are in memory
     // ---- sum over the slices of a tile (one tile per cluster: gridDim.x = split * tiles) --------------------------
     __syncwarp();
     if (CG == 1 && p.split > 1) {

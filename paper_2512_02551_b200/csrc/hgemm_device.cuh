@@ -1,4 +1,4 @@
-// Device code that the kernels share: bounded waits on mbarriers with a status word, and the shared-memory matrix
+// Device code that the kernels share: division by run-time constants, bounded waits on mbarriers with a status word, and the shared-memory matrix
 // descriptors of tiles that TMA lays out with the 128-byte swizzle.
 #pragma once
 
@@ -9,6 +9,37 @@
 namespace hgemm_dev {
 
 using namespace hgemm_ptx;
+
+// x / d for x < 2^31 without a division instruction: q = umulhi(x, mul) >> shr (d == 1: q = x).
+// mul = ceil(2^(31 + ceil(log2 d)) / d), shr = ceil(log2 d) - 1.
+struct FastDiv {
+    uint32_t mul, shr, d;
+};
+
+__host__ __device__ inline FastDiv make_fast_div(uint32_t d)
+{
+    FastDiv f;
+    f.d = d < 1u ? 1u : d;
+    f.mul = 0u;
+    f.shr = 0u;
+    if (f.d > 1u) {
+        uint32_t lg = 0;
+        while ((1ull << lg) < f.d) ++lg;                                 // ceil(log2 d) >= 1
+        const unsigned long long pw = 1ull << (31u + lg);
+        f.mul = static_cast<uint32_t>((pw + f.d - 1u) / f.d);
+        f.shr = lg - 1u;
+    }
+    return f;
+}
+
+__host__ __device__ __forceinline__ int32_t fast_div(int32_t x, const FastDiv &f)
+{
+#ifdef __CUDA_ARCH__
+    return f.d == 1u ? x : static_cast<int32_t>(__umulhi(static_cast<uint32_t>(x), f.mul) >> f.shr);
+#else
+    return static_cast<int32_t>(static_cast<uint32_t>(x) / f.d);      // the host's copy (layout computations, tests)
+#endif
+}
 
 // -------------------------------------------------------------------------------------
 // bounded wait

@@ -63,37 +63,6 @@ constexpr uint32_t kRoleCheck = 7;
 constexpr uint32_t kCheckWorkItem = 1, kCheckLoadCoord = 2, kCheckUnitStore = 3, kCheckSlot = 4, kCheckCounter = 5, kCheckStoreCoord = 6,
                    kCheckTmemColumn = 7, kCheckSmallStore = 8, kCheckProbe = 99;
 
-// x / d for x < 2^31 without a division instruction: q = umulhi(x, mul) >> shr (d == 1: q = x).
-// mul = ceil(2^(31 + ceil(log2 d)) / d), shr = ceil(log2 d) - 1.
-struct FastDiv {
-    uint32_t mul, shr, d;
-};
-
-__host__ __device__ inline FastDiv make_fast_div(uint32_t d)
-{
-    FastDiv f;
-    f.d = d < 1u ? 1u : d;
-    f.mul = 0u;
-    f.shr = 0u;
-    if (f.d > 1u) {
-        uint32_t lg = 0;
-        while ((1ull << lg) < f.d) ++lg;                                 // ceil(log2 d) >= 1
-        const unsigned long long pw = 1ull << (31u + lg);
-        f.mul = static_cast<uint32_t>((pw + f.d - 1u) / f.d);
-        f.shr = lg - 1u;
-    }
-    return f;
-}
-
-__host__ __device__ __forceinline__ int32_t fast_div(int32_t x, const FastDiv &f)
-{
-#ifdef __CUDA_ARCH__
-    return f.d == 1u ? x : static_cast<int32_t>(__umulhi(static_cast<uint32_t>(x), f.mul) >> f.shr);
-#else
-    return static_cast<int32_t>(static_cast<uint32_t>(x) / f.d);      // the host's copy (layout computations, tests)
-#endif
-}
-
 // Stream-K tail (paper section 5.2 picks a tile shape per problem; a tile count that does not fill the last wave of
 // SMs is what this evens out): the `rem` tiles that remain after the full waves are `q = rem * kblocks` k-blocks in
 // tile-major order, dealt out as `gs` contiguous ranges [floor(j q / gs), floor((j + 1) q / gs)), one per CTA

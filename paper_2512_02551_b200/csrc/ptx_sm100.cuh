@@ -492,6 +492,17 @@ __device__ __forceinline__ void mbar_arrive_elect(uint32_t bar)
         ::"r"(bar) : "memory");
 }
 
+// 3-D tiled store shared -> global (clipped at the tensor's bounds) by one lane of the converged warp, as a bulk group of that lane.
+__device__ __forceinline__ void tma_store_3d_elect(const void *tmap, int32_t x, int32_t y, int32_t z, uint32_t src)
+{
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];\n\t"
+        "@e cp.async.bulk.commit_group;\n\t}"
+        ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(src), "r"(x), "r"(y), "r"(z)
+        : "memory");
+}
+
 // One commit whose arrival goes to the barrier at the same shared-memory offset in both CTAs of a two-CTA cluster.
 __device__ __forceinline__ void umma_commit_both_elect(uint32_t bar)
 {
