@@ -127,11 +127,13 @@ bool encode(hgemm_ctx_s *ctx, CUtensorMap *map, CUtensorMapDataType type, int by
 }
 
 template <class T>
-const void *quantize_kernel(int32_t blocks)
+const void *quantize_kernel(int32_t blocks, bool many, bool dense)
 {
     using namespace hgemm_dev;
     switch (blocks) {
-    case HGEMM_FP8_ROWS: return reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T>);
+    case HGEMM_FP8_ROWS:
+        if (dense) return many ? reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 4, true>) : reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 1, true>);
+        return many ? reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 4, false>) : reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 1, false>);
     case HGEMM_FP8_COLS: return reinterpret_cast<const void *>(fp8_quantize_tile_kernel<T, 2>);
     case HGEMM_FP8_ROWS | HGEMM_FP8_COLS: return reinterpret_cast<const void *>(fp8_quantize_tile_kernel<T, 3>);
     default: return reinterpret_cast<const void *>(fp8_quantize_tile_kernel<T, 4>);
@@ -221,16 +223,22 @@ hgemm_status_t hgemm_fp8_quantize(hgemm_ctx_t *ctx, const hgemm_fp8_quantize_t *
     p.scales_cols = d->scales_cols;
     const int64_t col_blocks = ceil_div(d->cols, 128);
     dim3 grid(1, 1, 1);
+    p.fd_blocks = hgemm_dev::make_fast_div(uint32_t(col_blocks));
+    // four blocks in flight per group of lanes once that still leaves every SM a full set of warps (128 blocks a CTA, eight CTAs)
+    const int64_t row_work = d->rows * col_blocks;
+    const bool many = row_work >= int64_t(ctx->num_sms) * 8 * 128;
+    const bool dense = !d->row_index && d->cols % 128 == 0 && p.vec_ok && d->ldx == d->cols && d->ldq == d->cols;
+    if (row_work >= (int64_t(1) << 31) - 65536) return HGEMM_ERR_UNSUPPORTED;
     if (d->blocks == HGEMM_FP8_ROWS) {
-        grid.x = unsigned(std::min<int64_t>(ceil_div(d->rows * col_blocks, 16), int64_t(ctx->num_sms) * 32));
+        grid.x = unsigned(std::min<int64_t>(ceil_div(row_work, many ? 128 : 32), int64_t(ctx->num_sms) * 64));
     } else {
         const int64_t row_blocks = d->offsets ? hgemm_fp8_padded_rows(d->rows, d->groups) / 128 : ceil_div(d->rows, 128);
         grid.x = unsigned(col_blocks);
         grid.y = unsigned(std::min<int64_t>(row_blocks, 65535));
         grid.z = unsigned(tiles ? d->groups : 1);
     }
-    const void *fn = d->x_type == HGEMM_TYPE_F32 ? quantize_kernel<float>(d->blocks) : d->x_type == HGEMM_TYPE_F16 ? quantize_kernel<__half>(d->blocks)
-                                                                                                               : quantize_kernel<__nv_bfloat16>(d->blocks);
+    const void *fn = d->x_type == HGEMM_TYPE_F32 ? quantize_kernel<float>(d->blocks, many, dense) : d->x_type == HGEMM_TYPE_F16 ? quantize_kernel<__half>(d->blocks, many, dense)
+                                                                                                               : quantize_kernel<__nv_bfloat16>(d->blocks, many, dense);
     void *args[1] = {&p};
     return launch(ctx, fn, grid, hgemm_dev::kQuantThreads, 0, 1, args, stream);
 }
