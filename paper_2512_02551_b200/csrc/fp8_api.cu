@@ -87,7 +87,7 @@ int stages_of(int32_t form, const hgemm_fp8_config_t &c, int32_t groups, int *sm
 {
     const bool q_col = c.cta_group == 1 || form == HGEMM_FP8_WEIGHT_GRAD;
     const int bn = c.block_q, stage = hgemm_dev::kFp8PBytes + bn / c.cta_group * 128;
-    const int fixed = 1024 + (c.cta_group == 2 ? 8 * hgemm_dev::kFp8StagingPerWarp : 0) + hgemm_dev::kFp8Ring * hgemm_dev::kFp8Batch * hgemm_dev::fp8_slot_bytes(bn, q_col) + hgemm_dev::kFp8CtrlBytes +
+    const int fixed = 1024 + (c.cta_group == 2 ? 8 * hgemm_dev::kFp8StagingPerWarp : 0) + hgemm_dev::fp8_ring(c.cta_group) * hgemm_dev::kFp8Batch * hgemm_dev::fp8_slot_bytes(bn, q_col) + hgemm_dev::kFp8CtrlBytes +
                       (groups > 0 ? 8 * (groups + 1) : 8);
     const int stages = std::min((kSmemOptIn - fixed) / stage, hgemm_dev::kFp8MaxStages);
     *smem = kSmemOptIn;            // all of it: a second CTA on the SM could wait for this one's tensor memory

@@ -43,7 +43,8 @@ constexpr int kFp8MaxGroups = 1024;
 constexpr int kFp8CtrlBytes = 512;
 constexpr int kFp8StagingPerWarp = 8192;          // results on their way out: two boxes of 32 rows x 128 bytes
 constexpr uint32_t kRoleFp8Load = 8, kRoleFp8Mma = 9, kRoleFp8Scale = 10, kRoleFp8Promote = 11;
-constexpr int kFp8Batch = 4, kFp8Ring = 2;        // scales travel in batches of four blocks, two batches in flight (one barrier round per batch)
+constexpr int kFp8Batch = 4;                      // scales travel in batches of four blocks (one barrier round per batch)
+__host__ __device__ constexpr int fp8_ring(int cta_group) { return cta_group == 2 ? 2 : 4; }     // batches in flight: single CTAs go through theirs faster than two arrive
 __host__ __device__ constexpr int fp8_slot_bytes(int bn, bool q_col) { return (128 + (q_col ? bn : 4)) * 4; }     // one block's scales
 
 // which side of the tile grid follows the groups' offsets
@@ -262,6 +263,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
     constexpr uint32_t kTmemCols = kDepth * BN;
     constexpr uint32_t kStageBytes = kFp8PBytes + (BN / CG) * 128;
     constexpr uint32_t kSlotBytes = fp8_slot_bytes(BN, Q_COL);
+    constexpr int kRing = fp8_ring(CG);
     static_assert(kTmemCols >= 32 && (kTmemCols & (kTmemCols - 1)) == 0 && kTmemCols <= 512, "tensor memory is allocated in powers of two");
 
     extern __shared__ uint8_t smem_raw[];
@@ -269,10 +271,10 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
     uint8_t *smem_gen = smem_raw + (smem_base - smem_addr(smem_raw));
     const uint32_t staging_base = smem_base + static_cast<uint32_t>(p.stages) * kStageBytes;
     const uint32_t ring_base = staging_base + (CG == 2 ? 8u * kFp8StagingPerWarp : 0u);
-    const uint32_t ctrl_base = ring_base + kFp8Ring * kFp8Batch * kSlotBytes;
+    const uint32_t ctrl_base = ring_base + kRing * kFp8Batch * kSlotBytes;
     uint8_t *ctrl_gen = smem_gen + (ctrl_base - smem_base);
     const uint32_t bar_full = ctrl_base, bar_empty = bar_full + 8 * kFp8MaxStages, bar_tfull = bar_empty + 8 * kFp8MaxStages, bar_tempty = bar_tfull + 32;
-    const uint32_t bar_sfull = bar_tempty + 32, bar_sempty = bar_sfull + 8 * kFp8Ring;          // ends at 320
+    const uint32_t bar_sfull = bar_tempty + 32, bar_sempty = bar_sfull + 8 * kRing;          // ends at 320
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 320);
     volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 324);
     int32_t *pre = reinterpret_cast<int32_t *>(ctrl_gen + kFp8CtrlBytes);             // groups + 1 each
@@ -298,7 +300,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             mbar_init(bar_tfull + 8 * b, 1);
             mbar_init(bar_tempty + 8 * b, 8);      // a pair: four warps of each CTA; one CTA: its eight
         }
-        for (int s = 0; s < kFp8Ring; ++s) {
+        for (int s = 0; s < kRing; ++s) {
             mbar_init(bar_sfull + 8 * s, 32);
             mbar_init(bar_sempty + 8 * s, 8);
         }
@@ -429,8 +431,8 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             const int32_t prow = t.p0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * 128;
             const float *sp = p.sp + t.group * p.sp_group + t.kb0 * p.sp_kb, *sq = p.sq + t.group * p.sq_group + t.kb0 * p.sq_kb;
             for (int32_t kb = 0; kb < t.kbn; ++kb, ++it, sp += p.sp_kb, sq += p.sq_kb) {
-                const uint32_t batch = it / kFp8Batch, s = batch % kFp8Ring, slot = ring_base + (it % (kFp8Ring * kFp8Batch)) * kSlotBytes;
-                if (it % kFp8Batch == 0) ok = mbar_wait_warp(bar_sempty + 8 * s, ((batch / kFp8Ring) & 1u) ^ 1u, ctl, status_code(kRoleFp8Scale, 0, s));
+                const uint32_t batch = it / kFp8Batch, s = batch % kRing, slot = ring_base + (it % (kRing * kFp8Batch)) * kSlotBytes;
+                if (it % kFp8Batch == 0) ok = mbar_wait_warp(bar_sempty + 8 * s, ((batch / kRing) & 1u) ^ 1u, ctl, status_code(kRoleFp8Scale, 0, s));
                 if (!ok) break;
                 if constexpr (P_ROW) {
 #pragma unroll
@@ -454,7 +456,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                 if (it % kFp8Batch == kFp8Batch - 1) cp_async_mbar_arrive(bar_sfull + 8 * s);
             }
         }
-        if (it % kFp8Batch != 0) cp_async_mbar_arrive(bar_sfull + 8 * ((it / kFp8Batch) % kFp8Ring));      // the last, partly filled batch
+        if (it % kFp8Batch != 0) cp_async_mbar_arrive(bar_sfull + 8 * ((it / kFp8Batch) % kRing));      // the last, partly filled batch
         cp_async_wait_all();
     } else if (warp == 3) {
         if constexpr (CG == 2) regs_lower<56>();
@@ -465,7 +467,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + half * kCols;
         const uint32_t row_in_tile = quarter * 32u + lane;
         const uint32_t tempty = CG == 2 ? mapa(bar_tempty, 0) + half * 8u : bar_tempty, tfull = bar_tfull + (CG == 2 ? half * 8u : 0u);
-        const uint32_t ring_end = ring_base + kFp8Ring * kFp8Batch * kSlotBytes;
+        const uint32_t ring_end = ring_base + kRing * kFp8Batch * kSlotBytes;
         uint32_t it = 0;                                          // blocks so far (scales)
         uint32_t slot = ring_base;                                // the next block's scales
         uint32_t par = 0;                                         // bit d = phase of accumulator d's barriers
@@ -482,7 +484,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             bool ready = false;
             auto read_scales = [&](bool first) {
                 const uint32_t batch = it / kFp8Batch;
-                if (it % kFp8Batch == 0 || first) ok = mbar_wait_warp(bar_sfull + 8 * (batch % kFp8Ring), (batch / kFp8Ring) & 1u, ctl, status_code(kRoleFp8Promote, 0, 0));
+                if (it % kFp8Batch == 0 || first) ok = mbar_wait_warp(bar_sfull + 8 * (batch % kRing), (batch / kRing) & 1u, ctl, status_code(kRoleFp8Promote, 0, 0));
                 row_s = ld_shared_f32(slot + (P_ROW ? row_in_tile * 4u : 0u));
                 if constexpr (Q_COL) {
                     sq_next = slot + 512u + (CG == 2 ? half * 64u : half * kCols) * 4u;
@@ -499,7 +501,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                 [[maybe_unused]] const uint32_t sq = sq_next;
                 const float sc0 = row_s * col_s0, sc1 = row_s * col_s1;
                 const uint64_t row0 = pack_f32x2(__float_as_uint(sc0), __float_as_uint(sc0)), row1 = pack_f32x2(__float_as_uint(sc1), __float_as_uint(sc1));
-                const uint32_t batch_bar = bar_sempty + 8 * ((it / kFp8Batch) % kFp8Ring);
+                const uint32_t batch_bar = bar_sempty + 8 * ((it / kFp8Batch) % kRing);
                 const bool batch_end = it % kFp8Batch == kFp8Batch - 1;
                 if (!Q_COL && batch_end) mbar_arrive_elect(batch_bar);        // the batch's last scales are in registers
                 if (!__all_sync(0xffffffffu, ready)) ok = mbar_wait_warp(tfull + 8 * kParts * d, (par >> d) & 1u, ctl, status_code(kRoleFp8Promote, 1, d));

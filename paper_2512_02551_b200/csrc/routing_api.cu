@@ -42,6 +42,9 @@ void fill(RouteParams *p, const hgemm_routing_t &r, int64_t tokens, const void *
     p->top_groups = r.top_groups;
     p->group_size = r.experts / r.groups;
     p->inv_group = 1.0f / float(p->group_size);
+    p->per_lane = (r.experts + 31) / 32;
+    const int32_t lanes = p->group_size % p->per_lane == 0 ? p->group_size / p->per_lane : 0;
+    p->group_lanes = (lanes & (lanes - 1)) == 0 ? lanes : 0;
     p->top2 = r.group_score == HGEMM_GROUP_TOP2 ? 1 : 0;
     p->renormalize = r.renormalize;
     p->by_logit = r.score == HGEMM_SCORE_SOFTMAX && !bias ? 1 : 0;
@@ -110,6 +113,9 @@ hgemm_status_t hgemm_route(hgemm_ctx_t *ctx, const hgemm_routing_t *routing, int
     RouteParams p;
     fill(&p, *routing, tokens, logits, ld, bias != nullptr);
     p.bias = bias;
+    // vectors of a lane's elements: 32 x 1, 2, 4, 8 or 16 experts (the kernel's slots, exactly filled), rows at multiples of 16 bytes
+    const int32_t per = p.per_lane;
+    p.vec_ok = routing->experts == 32 * per && (per & (per - 1)) == 0 && aligned(logits, 16) && (ld * type_bytes(type)) % 16 == 0 ? 1 : 0;
     p.weights = weights;
     p.indices = indices;
     void *args[1] = {&p};
@@ -138,7 +144,7 @@ hgemm_status_t hgemm_route_sort(hgemm_ctx_t *ctx, const int32_t *indices, int64_
     if (count > 0 && (!aligned(indices, 4) || !aligned(order, 4) || !aligned(position, 4))) return HGEMM_ERR_INVALID_ARG;
     using namespace hgemm_dev;
     int ctas = 1;
-    while (ctas < 16 && count > int64_t(ctas) * 4096) ctas *= 2;
+    while (ctas < kSortMaxCtas && count > int64_t(ctas) * 4096) ctas *= 2;
     SortParams p;
     p.indices = indices;
     p.count = int32_t(count);

@@ -1,8 +1,9 @@
 // Routing of tokens to experts (see include/hgemm_routing.h).
 //
-// hgemm_route: one warp per token, its experts in registers (expert 32 i + lane in slot i).  A value becomes an unsigned key in the same
-// order, so that a maximum over the warp is one redux instruction, and the lowest index among equals another.  Bound by
-// instruction issue (top_k rounds of two redux and a scan of the lane's slots), not by the logits' bytes.
+// hgemm_route: one warp per token, its experts in registers, consecutive ones in one lane.  A value becomes an unsigned key in the same
+// order, so that a maximum over the warp is one redux instruction; the lowest lane that has it holds the lowest index.  Groups that
+// are whole lanes, a power of two of them, find their best values all at once by shuffles among those lanes.  Bound by
+// instruction issue (top_k rounds of redux, ballot and a scan of the lane's slots), not by the logits' bytes.
 //
 // hgemm_route_sort: a stable counting sort in one launch.  The CTAs of one cluster divide the choices into consecutive runs, one per
 // warp; per-warp histograms, prefix sums over warps, CTAs (through distributed shared memory) and experts give every run its
@@ -20,11 +21,14 @@ namespace hgemm_dev {
 constexpr int kRouteThreads = 128;
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortMaxCtas = 16;                   // one cluster
+constexpr int kSortAhead = 4;                      // rounds of 32 choices whose indices a warp fetches together
 
 struct RouteParams {
     const void *logits;
     int64_t tokens, ld, ldd;
     int32_t experts, top_k, sigmoid, groups, top_groups, group_size, top2, renormalize, by_logit;   // by_logit: v = l
+    int32_t per_lane, group_lanes, vec_ok;   // experts of a lane; lanes of a group (0: groups do not consist of a power of two of lanes); rows may be read in vectors
     float scale, inv_group;
     const float *bias;
     float *weights;
@@ -82,11 +86,25 @@ route_kernel(const RouteParams p)
     const bool sigmoid = p.sigmoid != 0;
     for (int64_t t = blockIdx.x * static_cast<int64_t>(kRouteThreads / 32) + (threadIdx.x >> 5); t < p.tokens; t += gridDim.x * static_cast<int64_t>(kRouteThreads / 32)) {
         const T *row = static_cast<const T *>(p.logits) + t * p.ld;
+        const int32_t e0 = lane * p.per_lane, mine_n = min(p.per_lane, p.experts - e0);        // this lane's experts: e0 .. e0 + mine_n - 1 (none: <= 0)
         float l[NPL];
+        if (p.vec_ok) {                                 // rows of NPL elements per lane, aligned
+            constexpr int kBytes = NPL * static_cast<int>(sizeof(T));
+            __align__(16) T t[NPL];
+            if constexpr (kBytes >= 16) {
 #pragma unroll
-        for (int i = 0; i < NPL; ++i) {
-            const int32_t e = i * 32 + lane;
-            l[i] = e < p.experts ? route_load(row + e) : __int_as_float(0xff800000);
+                for (int i = 0; i < kBytes / 16; ++i) reinterpret_cast<uint4 *>(t)[i] = reinterpret_cast<const uint4 *>(row + e0)[i];
+            } else if constexpr (kBytes == 8) {
+                *reinterpret_cast<uint2 *>(t) = *reinterpret_cast<const uint2 *>(row + e0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NPL; ++i) t[i] = row[e0 + i];
+            }
+#pragma unroll
+            for (int i = 0; i < NPL; ++i) l[i] = route_load(t + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NPL; ++i) l[i] = i < mine_n ? route_load(row + e0 + i) : __int_as_float(0xff800000);
         }
         float m = 0.0f, sum = 1.0f;
         if (!sigmoid) {
@@ -97,40 +115,55 @@ route_kernel(const RouteParams p)
             sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < NPL; ++i)
-                if (i * 32 + lane < p.experts) sum += expf(l[i] - m);
+                if (i < mine_n) sum += expf(l[i] - m);
             sum = warp_sum(sum);
         }
         uint32_t key[NPL];
 #pragma unroll
         for (int i = 0; i < NPL; ++i) {
-            const int32_t e = i * 32 + lane;
             float v = l[i];
             if (!p.by_logit) {
                 v = route_score(l[i], sigmoid, m, sum);
-                if (p.bias != nullptr && e < p.experts) v += p.bias[e];
+                if (p.bias != nullptr && i < mine_n) v += p.bias[e0 + i];
             }
-            key[i] = e < p.experts ? order_key(v) : 0u;
+            key[i] = i < mine_n ? order_key(v) : 0u;
         }
         if (p.groups > 1) {
-            uint32_t of_lane = 0;                       // lane g: key of group g's value
-            for (int32_t g = 0; g < p.groups; ++g) {
-                uint32_t k1 = 0, k2 = 0;                // this lane's two largest keys in the group
+            uint32_t of_lane = 0, kept = 0;             // lane g: key of group g's value; bit g: the group stays
+            if (p.group_lanes > 0) {
+                uint32_t k1 = 0, k2 = 0;                // the two largest keys of this lane, then of its group's lanes
 #pragma unroll
                 for (int i = 0; i < NPL; ++i) {
-                    const int32_t e = i * 32 + lane;
-                    const uint32_t k = e >= g * p.group_size && e < (g + 1) * p.group_size ? key[i] : 0u;
-                    k2 = max(k2, min(k1, k));
-                    k1 = max(k1, k);
+                    k2 = max(k2, min(k1, key[i]));
+                    k1 = max(k1, key[i]);
                 }
-                uint32_t best = __reduce_max_sync(0xffffffffu, k1);
-                if (p.top2) {
-                    const int owner = __ffs(__ballot_sync(0xffffffffu, k1 == best)) - 1;
-                    const uint32_t second = __reduce_max_sync(0xffffffffu, lane == owner ? k2 : k1);
-                    best = order_key(key_value(best) + key_value(max(second, kKeyLowest)));
+                for (int d = 1; d < p.group_lanes; d <<= 1) {
+                    const uint32_t o1 = __shfl_xor_sync(0xffffffffu, k1, d), o2 = __shfl_xor_sync(0xffffffffu, k2, d);
+                    k2 = max(min(k1, o1), max(k2, o2));
+                    k1 = max(k1, o1);
                 }
-                if (lane == g) of_lane = best;
+                if (p.top2) k1 = order_key(key_value(k1) + key_value(max(k2, kKeyLowest)));
+                of_lane = __shfl_sync(0xffffffffu, k1, (lane * p.group_lanes) & 31);
+                if (lane >= p.groups) of_lane = 0;
+            } else {
+                for (int32_t g = 0; g < p.groups; ++g) {
+                    uint32_t k1 = 0, k2 = 0;
+#pragma unroll
+                    for (int i = 0; i < NPL; ++i) {
+                        const int32_t e = e0 + i;
+                        const uint32_t k = e >= g * p.group_size && e < (g + 1) * p.group_size ? key[i] : 0u;
+                        k2 = max(k2, min(k1, k));
+                        k1 = max(k1, k);
+                    }
+                    uint32_t best = __reduce_max_sync(0xffffffffu, k1);
+                    if (p.top2) {
+                        const int owner = __ffs(__ballot_sync(0xffffffffu, k1 == best)) - 1;
+                        const uint32_t second = __reduce_max_sync(0xffffffffu, lane == owner ? k2 : k1);
+                        best = order_key(key_value(best) + key_value(max(second, kKeyLowest)));
+                    }
+                    if (lane == g) of_lane = best;
+                }
             }
-            uint32_t kept = 0;
             for (int32_t j = 0; j < p.top_groups; ++j) {
                 const uint32_t best = __reduce_max_sync(0xffffffffu, of_lane);
                 const int g = __ffs(__ballot_sync(0xffffffffu, of_lane == best)) - 1;
@@ -139,9 +172,8 @@ route_kernel(const RouteParams p)
             }
 #pragma unroll
             for (int i = 0; i < NPL; ++i) {
-                const int32_t e = i * 32 + lane;
-                const int32_t g = static_cast<int32_t>((static_cast<float>(e) + 0.5f) * p.inv_group);      // e / group_size: e < 512, off by less than half
-                if (e < p.experts && !((kept >> g) & 1u)) key[i] = kKeyLowest;
+                const int32_t g = static_cast<int32_t>((static_cast<float>(e0 + i) + 0.5f) * p.inv_group);      // (e0 + i) / group_size: below 512, off by less than half
+                if (i < mine_n && !((kept >> g) & 1u)) key[i] = kKeyLowest;
             }
         }
         int32_t mine = 0;                               // lane j: the j-th choice
@@ -152,13 +184,12 @@ route_kernel(const RouteParams p)
             for (int i = 1; i < NPL; ++i)
                 if (key[i] > k) { k = key[i]; slot = i; }
             const uint32_t best = __reduce_max_sync(0xffffffffu, k);
-            const uint32_t e = __reduce_min_sync(0xffffffffu, k == best ? static_cast<uint32_t>(slot * 32 + lane) : 0xffffffffu);
-            if (lane == j) mine = static_cast<int32_t>(e);
-            if ((e & 31u) == static_cast<uint32_t>(lane)) {
+            const int owner = __ffs(__ballot_sync(0xffffffffu, k == best)) - 1;
+            const int32_t e = __shfl_sync(0xffffffffu, e0 + slot, owner);
+            if (lane == j) mine = e;
 #pragma unroll
-                for (int i = 0; i < NPL; ++i)
-                    if (i == static_cast<int>(e >> 5)) key[i] = 0u;
-            }
+            for (int i = 0; i < NPL; ++i)
+                if (lane == owner && i == slot) key[i] = 0u;
         }
         float s = 0.0f;
         if (lane < p.top_k) s = route_score(route_load(row + mine), sigmoid, m, sum);
@@ -251,9 +282,13 @@ route_sort_kernel(const SortParams p)
     __syncthreads();
     int32_t *mine = hist + warp * p.experts;
     const int64_t begin = (static_cast<int64_t>(rank) * kSortWarps + warp) * p.run, end = min(begin + p.run, static_cast<int64_t>(p.count));
-    for (int64_t i = begin + lane; i < end; i += 32) {
-        const int32_t e = p.indices[i];
-        if (e >= 0 && e < p.experts) atomicAdd(mine + e, 1);       // counts: the order of the additions does not show
+    for (int64_t i = begin; i < end; i += 32 * kSortAhead) {
+        int32_t e[kSortAhead];
+#pragma unroll
+        for (int u = 0; u < kSortAhead; ++u) e[u] = i + u * 32 + lane < end ? p.indices[i + u * 32 + lane] : -1;
+#pragma unroll
+        for (int u = 0; u < kSortAhead; ++u)
+            if (e[u] >= 0 && e[u] < p.experts) atomicAdd(mine + e[u], 1);       // counts: the order of the additions does not show
     }
     __syncthreads();
     for (int32_t e = tid; e < p.experts; e += kSortThreads) {
@@ -270,11 +305,14 @@ route_sort_kernel(const SortParams p)
     // thread e: expert e (experts <= threads); places before it: experts below, then the CTAs before this one
     int32_t all = 0, before = 0;
     if (tid < p.experts) {
-        for (int32_t r = 0; r < ctas; ++r) {
-            int32_t n;
-            asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(n) : "r"(mapa(smem_addr(total + tid), static_cast<uint32_t>(r))) : "memory");
-            all += n;
-            if (r < rank) before += n;
+        int32_t n[kSortMaxCtas];
+#pragma unroll
+        for (int r = 0; r < kSortMaxCtas; ++r)
+            asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(n[r]) : "r"(mapa(smem_addr(total + tid), static_cast<uint32_t>(min(r, ctas - 1)))) : "memory");
+#pragma unroll
+        for (int r = 0; r < kSortMaxCtas; ++r) {
+            if (r < ctas) all += n[r];
+            if (r < rank) before += n[r];
         }
     }
     int32_t scan = all;
@@ -305,21 +343,27 @@ route_sort_kernel(const SortParams p)
         }
     }
     __syncthreads();
-    for (int64_t i = begin; i < end; i += 32) {
-        const int64_t slot = i + lane;
-        const int32_t e = slot < end ? p.indices[slot] : -1;
-        const bool valid = e >= 0 && e < p.experts;
-        const uint32_t peers = __match_any_sync(0xffffffffu, valid ? e : -1);
-        if (valid) {
-            const int32_t place = first[e] + mine[e] + __popc(peers & ((1u << lane) - 1u));
-            p.order[place] = static_cast<int32_t>(slot);
-            p.position[slot] = place;
-        } else if (slot < end) {
-            p.position[slot] = -1;
+    for (int64_t i = begin; i < end; i += 32 * kSortAhead) {
+        int32_t es[kSortAhead];
+#pragma unroll
+        for (int u = 0; u < kSortAhead; ++u) es[u] = i + u * 32 + lane < end ? p.indices[i + u * 32 + lane] : -1;
+#pragma unroll
+        for (int u = 0; u < kSortAhead; ++u) {
+            const int64_t slot = i + u * 32 + lane;
+            const bool valid = es[u] >= 0 && es[u] < p.experts;
+            const int32_t e = valid ? es[u] : -1;
+            const uint32_t peers = __match_any_sync(0xffffffffu, e);
+            if (valid) {
+                const int32_t place = first[e] + mine[e] + __popc(peers & ((1u << lane) - 1u));
+                p.order[place] = static_cast<int32_t>(slot);
+                p.position[slot] = place;
+            } else if (slot < end) {
+                p.position[slot] = -1;
+            }
+            __syncwarp();
+            if (valid && lane == __ffs(peers) - 1) mine[e] += __popc(peers);
+            __syncwarp();
         }
-        __syncwarp();
-        if (valid && lane == __ffs(peers) - 1) mine[e] += __popc(peers);
-        __syncwarp();
     }
     for (int64_t i = placed + static_cast<int64_t>(rank) * kSortThreads + tid; i < p.count; i += static_cast<int64_t>(ctas) * kSortThreads) p.order[i] = -1;
     cluster_arrive();                                   // no CTA leaves while another may still read its totals

@@ -78,8 +78,12 @@ def _check(status: int, what: str) -> None:
         raise HgemmError(status, what)
 
 
-def _stream(stream) -> int:
-    return torch.cuda.current_stream().cuda_stream if stream is None else int(stream)
+# the current stream's handle without building a Stream object (which costs more than the rest of a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _stream(ctx, stream) -> int:
+    return _raw_stream(ctx.device) if stream is None else int(stream)
 
 
 def padded_rows(M: int, groups: int) -> int:
@@ -123,18 +127,21 @@ def empty_tiles(*shape, dtype=torch.float8_e4m3fn, device="cuda"):
 # ---- quantisation --------------------------------------------------------------------------------
 
 def _dense(t, shape, dtype, name):
-    if t.dtype != dtype or not t.is_cuda or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of shape {tuple(shape)}")
-    return t.data_ptr()
+    if t.dtype == dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous CUDA {dtype} tensor of shape {tuple(shape)}, not {tuple(t.shape)} {t.dtype}")
 
 
 def _ld(t, shape, dtypes, name):
     """Elements between the rows of a matrix, or of a stack of matrices that follow one another."""
-    if t.dtype not in dtypes or not t.is_cuda or tuple(t.shape) != tuple(shape):
+    if t.dtype not in dtypes or t.shape != shape or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor of shape {tuple(shape)} and type {' / '.join(str(d) for d in dtypes)}, not {tuple(t.shape)} {t.dtype}")
     st = t.stride()
+    if len(st) == 2 and st[1] == 1 and st[0] >= shape[1] and shape[0] > 1:
+        return st[0]
     if st[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}: the elements of a row must be consecutive")
+    # one row: its distance to a next one is free, any that the library accepts
     ld = max(st[-2], shape[-1]) if shape[-2] > 1 else -(-max(st[-2], shape[-1]) // 16) * 16
     if (shape[-2] > 1 and st[-2] < shape[-1]) or (len(shape) == 3 and shape[0] > 1 and st[0] != shape[1] * ld):
         raise ValueError(f"{name}: strides {st} are not those of row-major matrices one after the other")
@@ -152,7 +159,7 @@ def _quantize(ctx, blocks, x, shape, ldx, row_index, x_rows, offsets, groups, po
                  None if row_index is None else row_index.data_ptr(), x_rows, None if offsets is None else offsets.data_ptr(), groups, 0,
                  None if q is None else q.data_ptr(), 0 if q is None else _ld(q, q.shape, _FP8, "q"), None if s is None else s.data_ptr(),
                  None if qc is None else qc.data_ptr(), 0 if qc is None else _ld(qc, qc.shape, _FP8, "q_cols"), None if sc is None else sc.data_ptr())
-    _check(lib().hgemm_fp8_quantize(ctx._h, ctypes.byref(d), _stream(stream)), f"hgemm_fp8_quantize(blocks={blocks}, {rows}x{cols})")
+    _check(lib().hgemm_fp8_quantize(ctx._h, ctypes.byref(d), _stream(ctx, stream)), f"hgemm_fp8_quantize(blocks={blocks}, {rows}x{cols})")
 
 
 def _source(x, rows):
@@ -279,7 +286,7 @@ class Plan:
             off = _dense(offsets, (self.groups + 1,), torch.int32, "offsets")
         elif offsets is not None:
             raise ValueError("offsets belong to a plan with groups")
-        st = self._run(self._h, a.data_ptr(), lda, sa, b.data_ptr(), ldb, sb, out.data_ptr(), ldc, off, 1 if accumulate else 0, _stream(stream))
+        st = self._run(self._h, a.data_ptr(), lda, sa, b.data_ptr(), ldb, sb, out.data_ptr(), ldc, off, 1 if accumulate else 0, _stream(self.ctx, stream))
         if st != OK:
             raise HgemmError(st, f"hgemm_fp8_run({self.form}{self.shape}, groups={self.groups})")
 

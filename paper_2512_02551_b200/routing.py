@@ -77,7 +77,7 @@ class Router:
         ld, T = self._rows(logits, "logits"), logits.shape[0]
         w, i = _dense(weights, (T, self.top_k), torch.float32, "weights"), _dense(indices, (T, self.top_k), torch.int32, "indices")
         b = None if bias is None else _dense(bias, (self.experts,), torch.float32, "bias")
-        _check(lib().hgemm_route(self.ctx._h, self._ref, T, logits.data_ptr(), fp8.TYPES[logits.dtype], ld, b, w, i, _stream(stream)), f"hgemm_route{self.rule}")
+        _check(lib().hgemm_route(self.ctx._h, self._ref, T, logits.data_ptr(), fp8.TYPES[logits.dtype], ld, b, w, i, _stream(self.ctx, stream)), f"hgemm_route{self.rule}")
 
     def backward(self, logits, indices, dweights, dlogits, stream=None) -> None:
         """dlogits (T, experts), of the logits' type, from dweights (T, top_k) fp32."""
@@ -86,7 +86,7 @@ class Router:
         if dlogits.dtype != logits.dtype or dlogits.shape != logits.shape:
             raise ValueError("dlogits must have the shape and type of logits")
         i, d = _dense(indices, (T, self.top_k), torch.int32, "indices"), _dense(dweights, (T, self.top_k), torch.float32, "dweights")
-        _check(lib().hgemm_route_backward(self.ctx._h, self._ref, T, logits.data_ptr(), fp8.TYPES[logits.dtype], ld, i, d, dlogits.data_ptr(), ldd, _stream(stream)),
+        _check(lib().hgemm_route_backward(self.ctx._h, self._ref, T, logits.data_ptr(), fp8.TYPES[logits.dtype], ld, i, d, dlogits.data_ptr(), ldd, _stream(self.ctx, stream)),
                f"hgemm_route_backward{self.rule}")
 
     def sort(self, indices, offsets, order, position, stream=None) -> None:
@@ -94,4 +94,4 @@ class Router:
         n = indices.numel()
         i = _dense(indices, indices.shape, torch.int32, "indices")
         o, r, p = _dense(offsets, (self.experts + 1,), torch.int32, "offsets"), _dense(order, (n,), torch.int32, "order"), _dense(position, (n,), torch.int32, "position")
-        _check(lib().hgemm_route_sort(self.ctx._h, i, n, self.experts, o, r, p, _stream(stream)), f"hgemm_route_sort({n} choices, {self.experts} experts)")
+        _check(lib().hgemm_route_sort(self.ctx._h, i, n, self.experts, o, r, p, _stream(self.ctx, stream)), f"hgemm_route_sort({n} choices, {self.experts} experts)")
