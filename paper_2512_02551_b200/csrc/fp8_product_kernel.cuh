@@ -43,6 +43,7 @@ constexpr int kFp8MaxGroups = 1024;
 constexpr int kFp8CtrlBytes = 512;
 constexpr int kFp8StagingPerWarp = 8192;          // results on their way out: two boxes of 32 rows x 128 bytes
 constexpr uint32_t kRoleFp8Load = 8, kRoleFp8Mma = 9, kRoleFp8Scale = 10, kRoleFp8Promote = 11;
+constexpr uint32_t kFp8PartPitch = 132;            // words between the columns of a slice's part
 constexpr int kFp8Batch = 4;                      // scales travel in batches of four blocks (one barrier round per batch)
 __host__ __device__ constexpr int fp8_ring(int cta_group) { return cta_group == 2 ? 2 : 4; }     // batches in flight: single CTAs go through theirs faster than two arrive
 __host__ __device__ constexpr int fp8_slot_bytes(int bn, bool q_col) { return (128 + (q_col ? bn : 4)) * 4; }     // one block's scales
@@ -176,39 +177,66 @@ __device__ __forceinline__ uint32_t fp8_pack2(float a, float b, __nv_bfloat16)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
+// Where the column-scaled promotion keeps its sums: chunks of 16 rows x 32 columns, rows 0..15 before 16..31, each chunk by eights of
+// columns, each of those as the lane's column pair of row t / 4, then of row t / 4 + 8.  f: eight of columns, hi: eight of rows (0..3).
+template <int REPS = 4>
+__host__ __device__ constexpr int fp8_frag_index(int f, int hi) { return (((f / REPS) * 2 + hi / 2) * REPS + f % REPS) * 2 + hi % 2; }
+
 // One warp's 32 rows x 128 columns of running sums (64 columns from col0, 64 from col0 + 128) to C, by rows.  Each lane packs its
 // row into boxes of 32 rows x 128 bytes in shared memory (16-byte pieces swizzled as TMA reads them: conflict-free), which leave as
 // tensor stores while the warp goes on with the next tile; stores by the warp itself kept it for 3500 cycles a tile.  A warp whose
 // rows end inside its 32 (a group's end), rows of C that do not start at multiples of 16 bytes, and C += take ordinary
 // stores of 32 consecutive elements instead.
-template <class T>
+// FRAG: the sums lie as the fragments of 16 x 8 that the column-scaled promotion reads (see there), else a lane holds its row.
+template <class T, bool FRAG>
 __device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32_t staging, const Fp8Params &p, const CUtensorMap *tmap_c, const Fp8Tile &t,
                                                int32_t row0, int32_t col0, uint32_t lane)
 {
     constexpr int kSize = static_cast<int>(sizeof(T));
     constexpr int kBox = 128 / kSize;                             // columns of a box
     constexpr int kPass = 2 * kBox;                               // columns of one pass: two boxes
-    const uint32_t mine = staging + lane * 128u, swz = lane & 7u;
     const bool whole = p.vec_ok && !p.accumulate && (row0 + 32 <= t.p_end || t.p_end == p.rows_p);   // the map clips at the matrix's own end
 #pragma unroll
     for (int c = 0; c < 128; c += kPass) {
         bulk_wait_group_read<0>();                                // earlier stores have read the boxes
         __syncwarp();
+        if constexpr (FRAG) {
+            const uint32_t fr = lane >> 2, fc = lane & 3u;        // row and column pair of this lane in a fragment
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            uint32_t v[4];
+            for (int n = 0; n < kPass / 8; ++n) {                 // fragments across the pass
+                const int f = c / 8 + n;                          // eight columns 8 f .. 8 f + 7
+                const uint32_t box = staging + static_cast<uint32_t>(n * 8 / kBox) * 4096u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float lo, hi;
-                if constexpr (kSize == 4) {
-                    unpack_f32x2(acc[(c + j * 4 + i) / 2], lo, hi);
-                    v[i] = __float_as_uint((i & 1) ? hi : lo);
-                } else {
-                    unpack_f32x2(acc[j * 4 + i], lo, hi);
-                    v[i] = fp8_pack2(lo, hi, T());
+                for (int hi = 0; hi < 4; ++hi) {                  // rows 8 hi + fr
+                    const uint64_t v = acc[fp8_frag_index(f, hi)];
+                    const uint32_t at = box + (8u * hi + fr) * 128u;
+                    if constexpr (kSize == 4) {
+                        st_shared_u64(at + (((static_cast<uint32_t>(2 * n) & 7u) + (fc >> 1)) ^ fr) * 16u + (fc & 1u) * 8u, v);
+                    } else {
+                        float x, y;
+                        unpack_f32x2(v, x, y);
+                        st_shared_u32(at + ((static_cast<uint32_t>(n) & 7u) ^ fr) * 16u + fc * 4u, fp8_pack2(x, y, T()));
+                    }
                 }
             }
-            st_shared_v4(mine + (j / 8) * 4096u + (((j & 7u) ^ swz) * 16u), v[0], v[1], v[2], v[3]);
+        } else {
+            const uint32_t mine = staging + lane * 128u, swz = lane & 7u;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                uint32_t v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float lo, hi;
+                    if constexpr (kSize == 4) {
+                        unpack_f32x2(acc[(c + j * 4 + i) / 2], lo, hi);
+                        v[i] = __float_as_uint((i & 1) ? hi : lo);
+                    } else {
+                        unpack_f32x2(acc[j * 4 + i], lo, hi);
+                        v[i] = fp8_pack2(lo, hi, T());
+                    }
+                }
+                st_shared_v4(mine + (j / 8) * 4096u + (((j & 7u) ^ swz) * 16u), v[0], v[1], v[2], v[3]);
+            }
         }
         if (whole) {
             fence_proxy_async_smem();
@@ -479,16 +507,22 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             for (int i = 0; i < kCols / 2; ++i) acc[i] = 0ull;
             // A block's scales -- the row's, and those of the first and the last 64 of a pair's columns -- are read one block
             // ahead, and its accumulator's barrier is asked ahead too, so that neither round trip lies between two accumulators.
-            float row_s = 0.0f, col_s0 = 1.0f, col_s1 = 1.0f;
-            uint32_t sq_next = 0;                                 // Q_COL: this warp's columns' scales of the block that was read last
+            float row_s[Q_COL && P_ROW ? 4 : 1] = {}, col_s0 = 1.0f, col_s1 = 1.0f;
+            uint32_t sq_next = 0;                                 // Q_COL: where this lane's column scales of the block that was read last begin
             bool ready = false;
             auto read_scales = [&](bool first) {
                 const uint32_t batch = it / kFp8Batch;
                 if (it % kFp8Batch == 0 || first) ok = mbar_wait_warp(bar_sfull + 8 * (batch % kRing), (batch / kRing) & 1u, ctl, status_code(kRoleFp8Promote, 0, 0));
-                row_s = ld_shared_f32(slot + (P_ROW ? row_in_tile * 4u : 0u));
                 if constexpr (Q_COL) {
-                    sq_next = slot + 512u + (CG == 2 ? half * 64u : half * kCols) * 4u;
+                    if constexpr (P_ROW) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) row_s[i] = ld_shared_f32(slot + (quarter * 32u + 8u * i + (lane >> 2)) * 4u);
+                    } else {
+                        row_s[0] = ld_shared_f32(slot);
+                    }
+                    sq_next = slot + 512u + ((CG == 2 ? half * 64u : half * kCols) + (lane & 3u) * 2u) * 4u;
                 } else {
+                    row_s[0] = ld_shared_f32(slot + (P_ROW ? row_in_tile * 4u : 0u));
                     col_s0 = ld_shared_f32(slot + 512u);
                     col_s1 = ld_shared_f32(slot + 516u);
                 }
@@ -499,8 +533,16 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             auto block = [&](auto dc, bool last) {                 // one block from accumulator dc
                 constexpr uint32_t d = decltype(dc)::value, nd = (d + 1) % kDepth;
                 [[maybe_unused]] const uint32_t sq = sq_next;
-                const float sc0 = row_s * col_s0, sc1 = row_s * col_s1;
-                const uint64_t row0 = pack_f32x2(__float_as_uint(sc0), __float_as_uint(sc0)), row1 = pack_f32x2(__float_as_uint(sc1), __float_as_uint(sc1));
+                // factors of this lane's values: of each row's (FRAG), or of the first and the last 64 columns
+                uint64_t rows2[Q_COL ? (P_ROW ? 4 : 1) : 2];
+                if constexpr (Q_COL) {
+#pragma unroll
+                    for (int i = 0; i < (P_ROW ? 4 : 1); ++i) rows2[i] = pack_f32x2(__float_as_uint(row_s[i]), __float_as_uint(row_s[i]));
+                } else {
+                    const float sc0 = row_s[0] * col_s0, sc1 = row_s[0] * col_s1;
+                    rows2[0] = pack_f32x2(__float_as_uint(sc0), __float_as_uint(sc0));
+                    rows2[1] = pack_f32x2(__float_as_uint(sc1), __float_as_uint(sc1));
+                }
                 const uint32_t batch_bar = bar_sempty + 8 * ((it / kFp8Batch) % kRing);
                 const bool batch_end = it % kFp8Batch == kFp8Batch - 1;
                 if (!Q_COL && batch_end) mbar_arrive_elect(batch_bar);        // the batch's last scales are in registers
@@ -509,19 +551,25 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                 par ^= 1u << d;
                 ++it;
                 tc_fence_after_sync();
-                constexpr int kChunk = kCols < 16 ? kCols : 16, kChunks = kCols / kChunk;
+                // Chunks of 16 registers, the next one in flight while one is added up.  One scale per row: a lane reads 16 columns of its
+                // own row.  A scale per column: fragments of 16 rows x 8 columns, of which a lane holds two columns each; with
+                // whole rows every lane would need every column's scale, and fetching those from shared memory (512 bytes a lane
+                // and block) took twice the MMA's time.
+                constexpr int kReps = kCols >= 32 ? 4 : kCols / 8;         // Q_COL: eights of columns of a chunk
+                constexpr int kChunk = Q_COL ? 4 * kReps : 16, kChunks = 32 * kCols / (32 * kChunk);
                 uint32_t v[2][kChunk];
                 auto load = [&](int c) {
-                    if constexpr (kChunk == 16) tmem_ld_32x32b_x16(taddr + d * BN + c * kChunk, v[c & 1]);
-                    else tmem_ld_32x32b_x8(taddr + d * BN + c * kChunk, v[c & 1]);
+                    if constexpr (Q_COL) tmem_ld_16x256b(taddr + d * BN + (c / 2) * (8 * kReps) + ((c & 1) ? 16u << 16 : 0u), v[c & 1]);
+                    else tmem_ld_32x32b_x16(taddr + d * BN + c * 16, v[c & 1]);
                 };
-                [[maybe_unused]] uint64_t qs[2][kChunk / 2];       // Q_COL: the chunk's column scales, a chunk ahead like the accumulator
-                auto load_q = [&](int c) {
+                [[maybe_unused]] uint64_t qs[2][kReps];            // the column scales of a chunk's eights, one pair of chunks ahead
+                auto load_q = [&](int g) {
                     if constexpr (Q_COL) {
-                        const int col = c * kChunk;
 #pragma unroll
-                        for (int i = 0; i < kChunk / 2; i += 2)
-                            ld_shared_2x64(sq + static_cast<uint32_t>((CG == 2 && col >= 64 ? col + 64 : col) + 2 * i) * 4u, qs[c & 1][i], qs[c & 1][i + 1]);
+                        for (int j = 0; j < kReps; ++j) {
+                            const int col = (g * kReps + j) * 8;
+                            qs[g & 1][j] = ld_shared_u64(sq + static_cast<uint32_t>(CG == 2 && col >= 64 ? col + 64 : col) * 4u);
+                        }
                     }
                 };
                 load_q(0);
@@ -530,8 +578,8 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                 for (int c = 0; c < kChunks; ++c) {
                     tmem_ld_wait_for(v[c & 1]);
                     if (c + 1 < kChunks) {
-                        load(c + 1);                               // in flight while this chunk is added up
-                        load_q(c + 1);
+                        load(c + 1);
+                        if (Q_COL && (c & 1) == 0 && c + 2 < kChunks) load_q(c / 2 + 1);
                     } else {
                         tc_fence_before_sync();                    // the accumulator is in registers: a later block may have it
                         if constexpr (CG == 2) mbar_arrive_cluster_elect(tempty + 8 * kParts * d);
@@ -542,17 +590,23 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                             ready = mbar_test_wait(tfull + 8 * kParts * nd, (par >> nd) & 1u);
                         }
                     }
+                    const uint32_t *x = v[c & 1];
+                    if constexpr (Q_COL) {
 #pragma unroll
-                    for (int i = 0; i < kChunk; i += 4) {
-                        const int col = c * kChunk + i, j = col / 2;
-                        const uint32_t *x = v[c & 1] + i;
-                        uint64_t s0 = (CG == 2 && !Q_COL && col >= 64) ? row1 : row0, s1 = s0;
-                        if constexpr (Q_COL) {
-                            s0 = mul_f32x2(qs[c & 1][i / 2], row0);
-                            s1 = mul_f32x2(qs[c & 1][i / 2 + 1], row0);
+                        for (int j = 0; j < kReps; ++j) {
+                            const uint64_t q = qs[(c / 2) & 1][j];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                uint64_t &a = acc[(c * kReps + j) * 2 + i];
+                                a = fma_f32x2(pack_f32x2(x[4 * j + 2 * i], x[4 * j + 2 * i + 1]), mul_f32x2(q, rows2[P_ROW ? 2 * (c & 1) + i : 0]), a);
+                            }
                         }
-                        acc[j] = fma_f32x2(pack_f32x2(x[0], x[1]), s0, acc[j]);
-                        acc[j + 1] = fma_f32x2(pack_f32x2(x[2], x[3]), s1, acc[j + 1]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            uint64_t &a = acc[(c * 16 + i) / 2];
+                            a = fma_f32x2(pack_f32x2(x[i], x[i + 1]), rows2[c * 16 >= 64 ? 1 : 0], a);
+                        }
                     }
                 }
                 if constexpr (Q_COL) {
@@ -574,34 +628,45 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             if constexpr (CG == 2) {
                 const int32_t row0 = t.p0 + static_cast<int32_t>(rank * 128u + quarter * 32u), col0 = t.q0 + static_cast<int32_t>(half) * 64;
                 const uint32_t staging = staging_base + ew * kFp8StagingPerWarp;
-                if (p.out_type == 0) fp8_store_rows<float>(acc, staging, p, &tmap_c, t, row0, col0, lane);
-                else if (p.out_type == 1) fp8_store_rows<__half>(acc, staging, p, &tmap_c, t, row0, col0, lane);
-                else fp8_store_rows<__nv_bfloat16>(acc, staging, p, &tmap_c, t, row0, col0, lane);
-            } else if (p.split > 1) {
-                // this slice's part, columns of 128 rows, where the operand stages were (every MMA that read them is complete)
-#pragma unroll
-                for (int i = 0; i < kCols / 2; ++i) {
-                    float lo, hi;
-                    unpack_f32x2(acc[i], lo, hi);
-                    const uint32_t at = smem_base + ((half * kCols + 2 * i) * 128u + row_in_tile) * 4u;
-                    st_shared_f32(at, lo);
-                    st_shared_f32(at + 512u, hi);
-                }
+                if (p.out_type == 0) fp8_store_rows<float, Q_COL>(acc, staging, p, &tmap_c, t, row0, col0, lane);
+                else if (p.out_type == 1) fp8_store_rows<__half, Q_COL>(acc, staging, p, &tmap_c, t, row0, col0, lane);
+                else fp8_store_rows<__nv_bfloat16, Q_COL>(acc, staging, p, &tmap_c, t, row0, col0, lane);
             } else {
-                const int32_t row = t.p0 + static_cast<int32_t>(row_in_tile);
-                if (row < t.p_end) {
-                    const int64_t base = t.group * p.c_group + row;
+                constexpr int kReps = kCols >= 32 ? 4 : kCols / 8;
+                if (p.split > 1) {
+                    // this slice's part where the operand stages were (every MMA that read them is complete): columns of 128 rows,
+                    // 132 words apart (conflict-free for fragments)
 #pragma unroll
-                    for (int i = 0; i < kCols; ++i) {
-                        const int32_t col = t.q0 + static_cast<int32_t>(half) * kCols + i;
-                        if (col < t.q_end) {
-                            float lo, hi;
-                            unpack_f32x2(acc[i / 2], lo, hi);
-                            const float v = (i & 1) ? hi : lo;
-                            const int64_t at = base + static_cast<int64_t>(col) * p.ldc;
-                            if (p.out_type == 0) fp8_store_one(static_cast<float *>(p.out) + at, v, p.accumulate);
-                            else if (p.out_type == 1) fp8_store_one(static_cast<__half *>(p.out) + at, v, 0);
-                            else fp8_store_one(static_cast<__nv_bfloat16 *>(p.out) + at, v, 0);
+                    for (int f = 0; f < kCols / 8; ++f) {
+#pragma unroll
+                        for (int hi = 0; hi < 4; ++hi) {
+                            float x, y;
+                            unpack_f32x2(acc[fp8_frag_index<kReps>(f, hi)], x, y);
+                            const uint32_t at = smem_base + ((half * kCols + 8u * f + (lane & 3u) * 2u) * kFp8PartPitch + quarter * 32u + 8u * hi + (lane >> 2)) * 4u;
+                            st_shared_f32(at, x);
+                            st_shared_f32(at + kFp8PartPitch * 4u, y);
+                        }
+                    }
+                } else {
+                    const int64_t base = t.group * p.c_group;
+#pragma unroll
+                    for (int f = 0; f < kCols / 8; ++f) {
+#pragma unroll
+                        for (int hi = 0; hi < 4; ++hi) {
+                            float x, y;
+                            unpack_f32x2(acc[fp8_frag_index<kReps>(f, hi)], x, y);
+                            const int32_t row = t.p0 + static_cast<int32_t>(quarter * 32u + 8u * hi + (lane >> 2)), col = t.q0 + static_cast<int32_t>(half * kCols + 8u * f + (lane & 3u) * 2u);
+                            if (row < t.p_end) {
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    if (col + i >= t.q_end) break;
+                                    const int64_t at = base + static_cast<int64_t>(col + i) * p.ldc + row;
+                                    const float v = i ? y : x;
+                                    if (p.out_type == 0) fp8_store_one(static_cast<float *>(p.out) + at, v, p.accumulate);
+                                    else if (p.out_type == 1) fp8_store_one(static_cast<__half *>(p.out) + at, v, 0);
+                                    else fp8_store_one(static_cast<__nv_bfloat16 *>(p.out) + at, v, 0);
+                                }
+                            }
                         }
                     }
                 }
@@ -623,7 +688,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                 if (col >= t.q_end) break;
                 float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                 for (int32_t r = 0; r < p.split; ++r) {
-                    const float4 x = ld_shared_cluster_v4(mapa(smem_base + (static_cast<uint32_t>(c) * 128u + lane * 4u) * 4u, static_cast<uint32_t>(r)));
+                    const float4 x = ld_shared_cluster_v4(mapa(smem_base + (static_cast<uint32_t>(c) * kFp8PartPitch + lane * 4u) * 4u, static_cast<uint32_t>(r)));
                     v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
                 }
                 const int64_t at = t.group * p.c_group + static_cast<int64_t>(col) * p.ldc + row;

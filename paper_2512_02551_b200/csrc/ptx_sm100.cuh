@@ -512,15 +512,33 @@ __device__ __forceinline__ void umma_commit_both_elect(uint32_t bar)
         ::"r"(bar) : "memory");
 }
 
-// Whole warp: thread t reads 8 (16) consecutive fp32 columns of tensor-memory lane (base lane + t).
-__device__ __forceinline__ void tmem_ld_32x32b_x8(uint32_t taddr, uint32_t *r)
+// Whole warp: 16 tensor-memory lanes x 8 (16, 32) columns.  Thread t gets, for every 8 columns, four values: columns 2 (t % 4) and + 1 of
+// lane t / 4, then those of lane t / 4 + 8.
+__device__ __forceinline__ void tmem_ld_16x256b(uint32_t taddr, uint32_t (&r)[4])
 {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+
+__device__ __forceinline__ void tmem_ld_16x256b(uint32_t taddr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                  : "r"(taddr)
                  : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld_16x256b(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+
+// Whole warp: thread t reads 16 consecutive fp32 columns of tensor-memory lane (base lane + t).
 __device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t *r)
 {
     asm volatile(
@@ -533,6 +551,11 @@ __device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t *r)
 }
 
 // Waits for this thread's tensor-memory loads; the registers pass through, so that nothing that uses them moves ahead of the wait.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[4])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3])::"memory");
+}
+
 __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[8])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -602,10 +625,21 @@ __device__ __forceinline__ void st_shared_f32(uint32_t addr, float v)
     asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
-// Two 64-bit pairs of fp32 values at once.
-__device__ __forceinline__ void ld_shared_2x64(uint32_t addr, uint64_t &a, uint64_t &b)
+__device__ __forceinline__ uint64_t ld_shared_u64(uint32_t addr)
 {
-    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr) : "memory");
+    uint64_t v;
+    asm volatile("ld.shared.b64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void st_shared_u32(uint32_t addr, uint32_t v)
+{
+    asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+__device__ __forceinline__ void st_shared_u64(uint32_t addr, uint64_t v)
+{
+    asm volatile("st.shared.b64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
 
 // Moves registers between warpgroups (all warps of a warpgroup execute it): raises or lowers this warp's share.
