@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <new>
 
@@ -58,29 +59,60 @@ int64_t tiles_of(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups, 
     return (std::min<int64_t>(groups, M) + M / bt) * ceil_div(outs, bo);
 }
 
+// Estimated time of a configuration in microseconds: a start-up, then rounds of tiles over the SMs, each block of 128 of a tile's contraction
+// and each tile's end at their measured cost (B200, operands in L2).  One block of a pair's 256 x 256 tile takes 0.46 us (0.56
+// with a scale per column), of a single CTA's 128 x {16, 32, 64, 128} tile 0.16, 0.20, 0.27, 0.45 us
+// (0.62 with most SMs busy: operands from L2); sharing a contraction costs about 1 us
+// for two CTAs and 1.7 us for eight.  512 x 4096 x 4096: pairs 21.5 us, 128-row tiles 24.9 us; 256 x 4096 x 4096: 20.5 and 16.4 us
+// (two CTAs a tile); 64 x 4096 x 4096: one CTA a tile 13.8 us, four 9.9 us.
+double estimate_us(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups, int32_t num_sms, const hgemm_fp8_config_t &c)
+{
+    const bool wgrad = form == HGEMM_FP8_WEIGHT_GRAD, pair = c.cta_group == 2;
+    const int64_t outs = form == HGEMM_FP8_FORWARD ? N : K;
+    const double rows = groups > 0 ? double(M) / groups : double(M);           // rows of one group, on average
+    double tiles, blocks;
+    if (wgrad) {
+        tiles = double(tiles_of(form, M, N, K, groups, c));
+        blocks = std::ceil(rows / 128.0) + (groups > 0 && rows > 128.0 ? 0.5 : 0.0);
+    } else {
+        const int64_t bt = pair ? 256 : c.block_q, bo = pair ? 256 : 128;
+        // groups are uneven: each ends in a partly filled tile
+        const double of_rows = groups > 0 ? std::min<double>(groups, double(M)) * std::max(1.0, rows / double(bt) + 0.7) : double(ceil_div(M, bt));
+        tiles = of_rows * double(ceil_div(outs, bo));
+        blocks = double(ceil_div(form == HGEMM_FP8_FORWARD ? K : N, 128));
+    }
+    const double block_us = pair ? (wgrad ? 0.56 : 0.46) : c.block_q == 16 ? 0.16 : c.block_q == 32 ? 0.20 : c.block_q == 64 ? 0.27 : tiles * c.split_k > 0.6 * num_sms ? 0.62 : 0.45;
+    const int units = std::max(1, num_sms / (pair ? 2 : c.split_k));
+    const double rounds = std::ceil(tiles / units);
+    const double shared_us = c.split_k == 1 ? 0.0 : c.split_k == 2 ? 1.0 : c.split_k == 4 ? 1.2 : 1.7;
+    const double tile_us = (pair ? 1.6 : 1.0) + (c.split_k > 1 ? 2.0 : 0.0);   // CTAs that share a tile do not go on to another: each round starts anew
+    return 4.5 + rounds * (std::ceil(blocks / c.split_k) * block_us) + std::max(0.0, rounds - 1.0) * tile_us + (pair ? 1.6 : 0.5) + shared_us;
+}
+
 hgemm_fp8_config_t choose(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups, int32_t num_sms)
 {
-    hgemm_fp8_config_t c;
-    std::memset(&c, 0, sizeof(c));
-    c.cta_group = 2;
-    c.block_q = 256;
-    c.split_k = 1;
-    const int64_t outs = form == HGEMM_FP8_FORWARD ? N : K;
-    const int64_t rows = groups > 0 ? ceil_div(std::max<int64_t>(M, 1), groups) : M;       // rows that share a weight, on average
-    if (form == HGEMM_FP8_WEIGHT_GRAD) {
-        if (tiles_of(form, M, N, K, groups, c) >= num_sms / 2) return c;
-        c.cta_group = 1;
-        c.block_q = 128;
-    } else {
-        const int64_t pair_tiles = groups > 0 ? groups * ceil_div(rows, 256) * ceil_div(outs, 256) : ceil_div(rows, 256) * ceil_div(outs, 256);
-        if (rows > 128 && pair_tiles >= num_sms / 2) return c;
-        c.cta_group = 1;
-        c.block_q = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    hgemm_fp8_config_t best;
+    std::memset(&best, 0, sizeof(best));
+    best.cta_group = 2;
+    best.block_q = 256;
+    best.split_k = 1;
+    double least = estimate_us(form, M, N, K, groups, num_sms, best);
+    for (int32_t bq = form == HGEMM_FP8_WEIGHT_GRAD ? 128 : 16; bq <= 128; bq *= 2) {
+        for (int32_t split = 1; split <= 8; split *= 2) {
+            hgemm_fp8_config_t c = best;
+            c.cta_group = 1;
+            c.block_q = bq;
+            c.split_k = split;
+            // CTAs beyond the tiles that exist are launched where groups share contractions: only for problems that fit one round
+            if (split > 1 && tiles_of(form, M, N, K, groups, c) * split > (split == 8 ? num_sms / 2 : num_sms)) continue;     // (clusters of eight do not fill the GPU)
+            const double t = estimate_us(form, M, N, K, groups, num_sms, c);
+            if (t < least) {
+                least = t;
+                best = c;
+            }
+        }
     }
-    const int64_t contraction = form == HGEMM_FP8_FORWARD ? K : form == HGEMM_FP8_INPUT_GRAD ? N : rows;
-    const int64_t tiles = form == HGEMM_FP8_WEIGHT_GRAD || groups == 0 ? tiles_of(form, M, N, K, groups, c) : std::min<int64_t>(groups, M) * ceil_div(rows, c.block_q) * ceil_div(outs, 128);
-    while (c.split_k < 8 && tiles * c.split_k * 2 <= num_sms && ceil_div(contraction, 128) >= 4 * c.split_k) c.split_k *= 2;
-    return c;
+    return best;
 }
 
 int stages_of(int32_t form, const hgemm_fp8_config_t &c, int32_t groups, int *smem)

@@ -185,8 +185,8 @@ __host__ __device__ constexpr int fp8_frag_index(int f, int hi) { return (((f / 
 // One warp's 32 rows x 128 columns of running sums (64 columns from col0, 64 from col0 + 128) to C, by rows.  Each lane packs its
 // row into boxes of 32 rows x 128 bytes in shared memory (16-byte pieces swizzled as TMA reads them: conflict-free), which leave as
 // tensor stores while the warp goes on with the next tile; stores by the warp itself kept it for 3500 cycles a tile.  A warp whose
-// rows end inside its 32 (a group's end), rows of C that do not start at multiples of 16 bytes, and C += take ordinary
-// stores of 32 consecutive elements instead.
+// rows end inside its 32 (a group's end) stores 16 bytes a lane; rows of C that are not multiples of 16 bytes, and C +=, take
+// ordinary stores of 32 consecutive elements.
 // FRAG: the sums lie as the fragments of 16 x 8 that the column-scaled promotion reads (see there), else a lane holds its row.
 template <class T, bool FRAG>
 __device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32_t staging, const Fp8Params &p, const CUtensorMap *tmap_c, const Fp8Tile &t,
@@ -246,17 +246,30 @@ __device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32
                 const int at = c + r * kBox, col = col0 + at + (at & 64);
                 if (row0 < t.p_end && col < t.q_end) tma_store_3d_elect(tmap_c, col, row0, p.ragged == kRaggedK ? t.group : 0, staging + r * 4096u);
             }
+        } else if (p.vec_ok && !p.accumulate) {
+            // a group's end inside the 32 rows: 16 bytes a lane, two rows at a time
+            __syncwarp();
+            T *out = static_cast<T *>(p.out) + t.group * p.c_group;
+            const uint32_t k = lane & 7u, box = (lane >> 3) & 1u;
+            const int32_t at = c + static_cast<int32_t>(box) * kBox + static_cast<int32_t>(k) * (16 / kSize), col = col0 + at + (at & 64);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t r = 2u * i + (lane >> 4);
+                const float4 v = ld_shared_v4(staging + box * 4096u + r * 128u + ((k ^ (r & 7u)) * 16u));
+                if (row0 + static_cast<int32_t>(r) < t.p_end && col < t.q_end)         // rows of C are multiples of 16 bytes: a piece is inside or outside
+                    *reinterpret_cast<float4 *>(out + static_cast<int64_t>(row0 + static_cast<int32_t>(r)) * p.ldc + col) = v;
+            }
         } else {
             __syncwarp();
             T *out = static_cast<T *>(p.out) + t.group * p.c_group;
-#pragma unroll 1
-            for (int32_t i = 0; i < 32 && row0 + i < t.p_end; ++i) {
+#pragma unroll 4
+            for (int32_t i = 0; i < 32; ++i) {
                 T *dst = out + static_cast<int64_t>(row0 + i) * p.ldc;
 #pragma unroll
                 for (int x = 0; x < kPass; x += 32) {
                     const int32_t at = x + static_cast<int32_t>(lane), byte = at * kSize, col = col0 + c + at + ((c + at) & 64);
                     const uint32_t src = staging + (byte / 128) * 4096 + i * 128 + (((byte / 16) ^ i) & 7) * 16 + (byte & 15);
-                    if (col < t.q_end) {
+                    if (row0 + i < t.p_end && col < t.q_end) {
                         if constexpr (kSize == 4) {
                             const float v = ld_shared_f32(src);
                             dst[col] = p.accumulate ? dst[col] + v : v;

@@ -74,14 +74,16 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
     return mbar_wait_slow(bar, parity, ctl, code);
 }
 
+constexpr uint32_t kWaitSuspendNs = 20000;     // a suspended warp leaves its scheduler to the others; the budget is looked at this often
+
 // The same wait for a converged warp, without a call (for code that keeps most of its registers live across it); the result is
 // the same in every lane.
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, const WaitCtl &ctl, uint32_t code)
 {
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if (__all_sync(0xffffffffu, mbar_try_wait_for(bar, parity, kWaitSuspendNs))) return true;
     const long long t0 = clock64();
 #pragma unroll 1
-    while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
+    while (!__all_sync(0xffffffffu, mbar_try_wait_for(bar, parity, kWaitSuspendNs))) {
         const bool late = clock64() - t0 > ctl.budget;
         if (__any_sync(0xffffffffu, late || *ctl.abort_flag != 0u)) {
             if (late && *ctl.abort_flag == 0u) {
