@@ -479,3 +479,87 @@ def test_gradients_against_differences(ctx):
             up[t][i, j] += h
             down[t][i, j] -= h
             assert float(d[i, j]) == pytest.approx((loss(*up) - loss(*down)) / (2 * h), rel=1e-6)
+
+
+# ---- refusals --------------------------------------------------------------------------------------------------------
+
+def test_refusals(ctx):
+    """Wrong arguments raise, and nothing is launched: the result keeps its values."""
+    M, N, K = 20, 64, 256
+    g = rng("refusals")
+    a, w = bytes8(g, (M, K), E4M3), bytes8(g, (N, K), E4M3)
+    sa, sb = scales(g, M, 2), scales(g, 1, 2)
+    out = torch.full((M, N), 7.0, device="cuda")
+    offsets = torch.tensor([0, M], dtype=torch.int32, device="cuda")
+    plan = fp8.Plan(ctx, M, N, K, out_dtype=torch.float32)
+    bf = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    for args, kw in [
+        ((a[:, :255], sa, w, sb, out), {}), ((a.float(), sa, w, sb, out), {}), ((a, sa[:, :1], w, sb, out), {}), ((a, sa.double(), w, sb, out), {}),
+        ((a, sa, w[:10], sb, out), {}), ((a, sa, w, sb, bf), {}), ((a, sa, w, sb, out.t().contiguous().t()), {}), ((a.cpu(), sa, w, sb, out), {}),
+        ((a, sa, w, sb, out), {"offsets": offsets}), ((a.view(torch.uint8), sa, w, sb, out), {}),
+    ]:
+        with pytest.raises(ValueError):
+            plan.run(*args, **kw)
+    grouped = fp8.Plan(ctx, M, N, K, groups=1, out_dtype=torch.float32)
+    with pytest.raises(ValueError):
+        grouped.run(a, sa, w.unsqueeze(0), sb.unsqueeze(0), out)
+    with pytest.raises(ValueError):
+        grouped.run(a, sa, w.unsqueeze(0), sb.unsqueeze(0), out, offsets=offsets.long())
+    for bad in (dict(form="sideways"), dict(a_dtype=torch.uint8), dict(out_dtype=torch.float64)):
+        with pytest.raises(ValueError):
+            fp8.Plan(ctx, M, N, K, **bad)
+    for shape in ((-1, N, K), (M, 0, K), (M, N, 1 << 23)):
+        with pytest.raises(hgemm.HgemmError):
+            fp8.Plan(ctx, *shape)
+    with pytest.raises(hgemm.HgemmError):
+        fp8.Plan(ctx, M, N, K, groups=1025)
+    for config in ((2, 128, 1), (2, 256, 2), (1, 256, 1), (1, 8, 1), (1, 64, 3), (3, 64, 1), (1, 64, 16)):
+        with pytest.raises(hgemm.HgemmError):
+            plan.set_config(*config)
+    with pytest.raises(hgemm.HgemmError):
+        fp8.Plan(ctx, M, N, K, form="weight_grad").set_config(1, 64, 1)
+    # rows that are not 16 bytes apart, a base that is not aligned, C += into a 16-bit result: refused by the library itself
+    tight = torch.zeros(M, 250, dtype=torch.uint8, device="cuda").view(E4M3)
+    with pytest.raises(hgemm.HgemmError):
+        fp8.Plan(ctx, M, N, 250, out_dtype=torch.float32).run(tight, sa, bytes8(g, (N, 250), E4M3), sb, out)
+    shifted = torch.zeros(M * 272 + 16, dtype=torch.uint8, device="cuda")[8:8 + M * 272].view(E4M3).view(M, 272)[:, :K]
+    with pytest.raises(hgemm.HgemmError):
+        plan.run(shifted, sa, w, sb, out)
+    with pytest.raises(hgemm.HgemmError):
+        fp8.Plan(ctx, M, N, K).run(a, sa, w, sb, bf, accumulate=True)
+    x = torch.randn(M, K, device="cuda")
+    q, s = fp8.empty_rows(M, K)
+    for call in (lambda: fp8.quantize_rows(ctx, x.int(), q, s), lambda: fp8.quantize_rows(ctx, x, q[:3], s), lambda: fp8.quantize_rows(ctx, x, q, s[:, :1]),
+                 lambda: fp8.quantize_rows(ctx, x, x, s), lambda: fp8.quantize_rows(ctx, x, q, s, rows=offsets.long()), lambda: fp8.quantize_cols(ctx, x, q, s),
+                 lambda: fp8.quantize_cols(ctx, x, q, torch.empty(1, K, device="cuda"), offsets=offsets[:1]), lambda: fp8.quantize_tiles(ctx, x[0], q, s)):
+        with pytest.raises(ValueError):
+            call()
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
+
+
+# ---- the operators together ---------------------------------------------------------------------------------------------
+
+def test_layer_of_experts(ctx):
+    """A training step of a layer of experts against the same layer in 64 bits without quantisation, the choice taken as it was made.
+    An 8-bit value is within 2^-4 of its element, so a quantised operand is within 2^-4 of the operand's norm at most (about 2^-4 /
+    sqrt(3) for spread-out mantissas); at most four such operands, and bf16 results, stand between input and output."""
+    from paper_2512_02551_b200.run_experts import ExpertLayer
+    T, H, I, E, k = 300, 256, 192, 6, 2
+    layer = ExpertLayer(ctx, T, H, I, E, k, seed=5)
+    g = rng("layer")
+    x, dy = torch.randn(T, H, generator=g, device="cuda").half(), torch.randn(T, H, generator=g, device="cuda")
+    y = layer.forward(x)
+    dx, dw1, dw2, dlogits = layer.backward(dy)
+    assert ctx.last_device_status()[0] == hgemm.OK
+    xd, wr, w1, w2 = x.double().requires_grad_(), layer.wr.double().requires_grad_(), layer.w1.double().requires_grad_(), layer.w2.double().requires_grad_()
+    p = torch.softmax(xd @ wr.t(), -1).gather(1, layer.indices.long())
+    p = p / p.sum(-1, keepdim=True)
+    want = torch.zeros(T, H, dtype=torch.float64, device="cuda")
+    for e in range(E):
+        t, j = torch.nonzero(layer.indices == e, as_tuple=True)
+        want = want.index_add(0, t, p[t, j].unsqueeze(-1) * (torch.nn.functional.silu(xd[t] @ w1[e].t()) @ w2[e].t()))
+    want.backward(dy.double())
+    near = lambda a, b: float((a.double() - b).norm() / b.norm())  # noqa: E731
+    bound = 4 * 2.0 ** -4 / 3 ** 0.5
+    assert near(y, want) < bound and near(dx, xd.grad) < bound and near(dw1, w1.grad) < bound and near(dw2, w2.grad) < bound

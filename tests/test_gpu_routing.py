@@ -226,3 +226,28 @@ def test_no_tokens(ctx):
     router.forward(empty(0, 16), empty(0, 2), empty(0, 2, dtype=torch.int32))
     router.backward(empty(0, 16), empty(0, 2, dtype=torch.int32), empty(0, 2), empty(0, 16))
     torch.cuda.synchronize()
+
+
+def test_refusals(ctx):
+    Router = routing.Router
+    for kw in (dict(experts=0, top_k=1), dict(experts=513, top_k=1), dict(experts=8, top_k=9), dict(experts=64, top_k=33), dict(experts=8, top_k=0),
+               dict(experts=8, top_k=1, groups=3), dict(experts=8, top_k=1, groups=4, top_groups=5), dict(experts=8, top_k=3, groups=4, top_groups=1),
+               dict(experts=8, top_k=1, groups=8, top_groups=2, group_score="top2", score="sigmoid"), dict(experts=8, top_k=1, scale=float("nan"))):
+        with pytest.raises(hgemm.HgemmError):
+            Router(ctx, **kw)
+    with pytest.raises(ValueError):
+        Router(ctx, 8, 1, score="tanh")
+    r = Router(ctx, 8, 2)
+    l, w, i = torch.zeros(5, 8, device="cuda"), torch.full((5, 2), 3.0, device="cuda"), torch.zeros(5, 2, dtype=torch.int32, device="cuda")
+    for call in (lambda: r.forward(l[:, :7], w, i), lambda: r.forward(l.double(), w, i), lambda: r.forward(l, w[:4], i), lambda: r.forward(l, w, i.long()),
+                 lambda: r.forward(l, w, i, bias=torch.zeros(7, device="cuda")), lambda: r.forward(l.t().contiguous().t(), w, i),
+                 lambda: r.backward(l, i, w, l.half()), lambda: r.sort(i, torch.zeros(8, dtype=torch.int32, device="cuda"), i.flatten(), i.flatten())):
+        with pytest.raises(ValueError):
+            call()
+    # the two best softmax scores of a group need scores, not logits: only with a bias
+    two = Router(ctx, 8, 2, groups=2, top_groups=1, group_score="top2")
+    with pytest.raises(hgemm.HgemmError):
+        two.forward(l, w, i)
+    two.forward(l, w.clone(), i, bias=torch.zeros(8, device="cuda"))
+    torch.cuda.synchronize()
+    assert bool((w == 3.0).all())
