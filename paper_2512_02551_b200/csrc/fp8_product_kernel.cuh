@@ -186,7 +186,7 @@ __host__ __device__ constexpr int fp8_frag_index(int f, int hi) { return (((f / 
 // row into boxes of 32 rows x 128 bytes in shared memory (16-byte pieces swizzled as TMA reads them: conflict-free), which leave as
 // tensor stores while the warp goes on with the next tile; stores by the warp itself kept it for 3500 cycles a tile.  A warp whose
 // rows end inside its 32 (a group's end) stores 16 bytes a lane; rows of C that are not multiples of 16 bytes, and C +=, take
-// ordinary stores of 32 consecutive elements.
+// ordinary stores of 4 bytes a lane.
 // FRAG: the sums lie as the fragments of 16 x 8 that the column-scaled promotion reads (see there), else a lane holds its row.
 template <class T, bool FRAG>
 __device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32_t staging, const Fp8Params &p, const CUtensorMap *tmap_c, const Fp8Tile &t,
@@ -259,24 +259,62 @@ __device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32
                 if (row0 + static_cast<int32_t>(r) < t.p_end && col < t.q_end)         // rows of C are multiples of 16 bytes: a piece is inside or outside
                     *reinterpret_cast<float4 *>(out + static_cast<int64_t>(row0 + static_cast<int32_t>(r)) * p.ldc + col) = v;
             }
-        } else {
+        } else if constexpr (kSize == 2) {
+            // rows at any even address: two elements a lane where the pair starts at a multiple of 4 bytes.  In a run of 64 that does not,
+            // lane 0 takes its first and its last element.
             __syncwarp();
             T *out = static_cast<T *>(p.out) + t.group * p.c_group;
-#pragma unroll 4
-            for (int32_t i = 0; i < 32; ++i) {
-                T *dst = out + static_cast<int64_t>(row0 + i) * p.ldc;
+#pragma unroll 1
+            for (int32_t i0 = 0; i0 < 32; i0 += 8) {                     // the loads of eight rows before their stores
+                uint32_t h[8][2];
 #pragma unroll
-                for (int x = 0; x < kPass; x += 32) {
-                    const int32_t at = x + static_cast<int32_t>(lane), byte = at * kSize, col = col0 + c + at + ((c + at) & 64);
-                    const uint32_t src = staging + (byte / 128) * 4096 + i * 128 + (((byte / 16) ^ i) & 7) * 16 + (byte & 15);
-                    if (row0 + i < t.p_end && col < t.q_end) {
-                        if constexpr (kSize == 4) {
-                            const float v = ld_shared_f32(src);
-                            dst[col] = p.accumulate ? dst[col] + v : v;
+                for (int j = 0; j < 8; ++j) {
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const int32_t i = i0 + j;
+                        const int32_t e = 2 * static_cast<int32_t>(lane) - (static_cast<int32_t>(reinterpret_cast<uintptr_t>(out + static_cast<int64_t>(row0 + i) * p.ldc + col0) >> 1) & 1);
+                        const int32_t ea = e < 0 ? 0 : e, eb = e < 0 ? 63 : e + 1;
+                        const uint32_t from = staging + r * 4096u + i * 128u;
+                        h[j][r] = ld_shared_u16(from + (((ea >> 3) ^ j) * 16u) + (ea & 7) * 2u) | static_cast<uint32_t>(ld_shared_u16(from + (((eb >> 3) ^ j) * 16u) + (eb & 7) * 2u)) << 16;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (row0 + i0 + j >= t.p_end) break;
+                    T *row = out + static_cast<int64_t>(row0 + i0 + j) * p.ldc + col0;
+                    const int32_t e = 2 * static_cast<int32_t>(lane) - (static_cast<int32_t>(reinterpret_cast<uintptr_t>(row) >> 1) & 1);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const int32_t left = t.q_end - col0 - 128 * r;             // columns of the run
+                        unsigned short *d = reinterpret_cast<unsigned short *>(row + 128 * r);
+                        if (e >= 0 && e + 1 < left) {
+                            *reinterpret_cast<uint32_t *>(d + e) = h[j][r];
                         } else {
-                            const unsigned short h = ld_shared_u16(src);
-                            dst[col] = *reinterpret_cast<const T *>(&h);
+                            if (max(e, 0) < left) d[max(e, 0)] = static_cast<unsigned short>(h[j][r]);
+                            if (e < 0 && 63 < left) d[63] = static_cast<unsigned short>(h[j][r] >> 16);
                         }
+                    }
+                }
+            }
+        } else {
+            __syncwarp();
+            float *out = static_cast<float *>(p.out) + t.group * p.c_group;
+#pragma unroll 1
+            for (int32_t i0 = 0; i0 < 32; i0 += 8) {
+                float v[8][2];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) v[j][x] = ld_shared_f32(staging + x * 4096u + (i0 + j) * 128u + (((lane >> 2) ^ j) * 16u) + (lane & 3u) * 4u);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (row0 + i0 + j >= t.p_end) break;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int32_t at = c + x * 32 + static_cast<int32_t>(lane), col = col0 + at + (at & 64);
+                        float *dst = out + static_cast<int64_t>(row0 + i0 + j) * p.ldc + col;
+                        if (col < t.q_end) *dst = p.accumulate ? *dst + v[j][x] : v[j][x];
                     }
                 }
             }
