@@ -233,7 +233,7 @@ fp8_quantize_rows_kernel(const QuantParams p)
     for (int64_t b0 = static_cast<int64_t>(warp) * (4 * UNROLL); b0 < total; b0 += static_cast<int64_t>(warps) * (4 * UNROLL)) {
         Raw8<T> raw[UNROLL][2];
         int64_t q_at[UNROLL];                                             // where a lane's values go (-1: no block)
-        int32_t s_at[UNROLL], room[UNROLL];                               // where its block's scale goes; elements up to the row's end
+        int32_t room[UNROLL];                                             // elements up to the row's end
         const int32_t r0 = DENSE ? 0 : fast_div(static_cast<int32_t>(b0), p.fd_blocks), k0 = static_cast<int32_t>(b0) - r0 * blocks;
         if (DENSE || k0 + 4 * UNROLL <= blocks) {
             // the warp's blocks lie in one row
@@ -244,7 +244,6 @@ fp8_quantize_rows_kernel(const QuantParams p)
                 const bool mine = !DENSE || k < total;
                 const int64_t col = k * 128 + sub * 16;
                 q_at[u] = mine ? (DENSE ? col : r0 * p.ldq + col) : -1;
-                s_at[u] = static_cast<int32_t>(b0) + u * 4 + lane_block;
                 room[u] = DENSE ? 128 : static_cast<int32_t>(p.cols - col);
                 if (DENSE || (src != nullptr && p.vec_ok && room[u] >= 16)) {
                     raw[u][0] = load8_whole<T>(src + (mine ? col : 0));
@@ -263,30 +262,41 @@ fp8_quantize_rows_kernel(const QuantParams p)
                 const int64_t col = (static_cast<int32_t>(b) - r * blocks) * 128ll + sub * 16;
                 const T *src = mine ? source_row<T>(p, r) : nullptr;
                 q_at[u] = mine ? r * p.ldq + col : -1;
-                s_at[u] = static_cast<int32_t>(b);
                 room[u] = static_cast<int32_t>(p.cols - col);
                 raw[u][0] = load8<T>(src, col, p.cols, p.vec_ok);
                 raw[u][1] = load8<T>(src, col + 8, p.cols, p.vec_ok);
             }
         }
+        bool careful = false;
+        float m[UNROLL], top = 0.0f;
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            bool careful = false;
-            float m = fmaxf(amax8(raw[u][0]), amax8(raw[u][1]));
+            m[u] = fmaxf(amax8(raw[u][0]), amax8(raw[u][1]));
+            top = fmaxf(top, m[u]);
+        }
+        if (__any_sync(0xffffffffu, top == quant_inf())) {
+            careful = true;
 #pragma unroll
-            for (int d = 4; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-            if (__any_sync(0xffffffffu, m == quant_inf())) {
-                careful = true;
-                m = fmaxf(amax8_finite(raw[u][0]), amax8_finite(raw[u][1]));
+            for (int u = 0; u < UNROLL; ++u) m[u] = fmaxf(amax8_finite(raw[u][0]), amax8_finite(raw[u][1]));
+        }
+        float own = 0.0f;                                                 // lane u of a group of 8 makes the scale of its block u
 #pragma unroll
-                for (int d = 4; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-            }
-            const BlockScale s = block_scale(m, p.e5m2, p.pow2);
+        for (int u = 0; u < UNROLL; ++u) {
+#pragma unroll
+            for (int d = 4; d >= 1; d >>= 1) m[u] = fmaxf(m[u], __shfl_xor_sync(0xffffffffu, m[u], d));
+            if (sub == u) own = m[u];
+        }
+        const BlockScale s = block_scale(own, p.e5m2, p.pow2);
+        const int64_t own_block = b0 + sub * 4 + lane_block;
+        if (sub < UNROLL && own_block < total) p.scales[own_block] = s.scale;
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const float factor = __shfl_sync(0xffffffffu, s.factor, u, 8);
             if (q_at[u] >= 0) {
                 float f[8], g[8];
                 floats_of(raw[u][0], f, careful);
                 floats_of(raw[u][1], g, careful);
-                const uint2 lo = quantize8(f, s.factor, p.e5m2), hi = quantize8(g, s.factor, p.e5m2);
+                const uint2 lo = quantize8(f, factor, p.e5m2), hi = quantize8(g, factor, p.e5m2);
                 uint8_t *dst = p.q + q_at[u];
                 if (DENSE || room[u] >= 16) {
                     *reinterpret_cast<uint4 *>(dst) = make_uint4(lo.x, lo.y, hi.x, hi.y);
@@ -294,7 +304,6 @@ fp8_quantize_rows_kernel(const QuantParams p)
                     store8(dst, 0, room[u], lo);
                     store8(dst, 8, room[u], hi);
                 }
-                if (sub == 0) p.scales[s_at[u]] = s.scale;
             }
         }
     }
