@@ -149,6 +149,8 @@ hgemm_status_t hgemm_route_sort(hgemm_ctx_t *ctx, const int32_t *indices, int64_
     p.indices = indices;
     p.count = int32_t(count);
     p.experts = experts;
+    p.bits = 1;
+    while ((experts >> p.bits) != 0) ++p.bits;
     const int64_t warps = int64_t(ctas) * kSortWarps;
     p.run = int32_t(((count + warps - 1) / warps + 31) / 32 * 32);
     p.offsets = offsets;
