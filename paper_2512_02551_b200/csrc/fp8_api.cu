@@ -158,18 +158,24 @@ bool encode(hgemm_ctx_s *ctx, CUtensorMap *map, CUtensorMapDataType type, int by
     return true;
 }
 
-template <class T>
+template <class T, bool E5M2>
 const void *quantize_kernel(int32_t blocks, bool many, bool dense)
 {
     using namespace hgemm_dev;
     switch (blocks) {
     case HGEMM_FP8_ROWS:
-        if (dense) return many ? reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 4, true>) : reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 1, true>);
-        return many ? reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 4, false>) : reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 1, false>);
-    case HGEMM_FP8_COLS: return reinterpret_cast<const void *>(fp8_quantize_tile_kernel<T, 2>);
-    case HGEMM_FP8_ROWS | HGEMM_FP8_COLS: return reinterpret_cast<const void *>(fp8_quantize_tile_kernel<T, 3>);
-    default: return reinterpret_cast<const void *>(fp8_quantize_tile_kernel<T, 4>);
+        if (dense) return many ? reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 4, true, E5M2>) : reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 1, true, E5M2>);
+        return many ? reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 4, false, E5M2>) : reinterpret_cast<const void *>(fp8_quantize_rows_kernel<T, 1, false, E5M2>);
+    case HGEMM_FP8_COLS: return reinterpret_cast<const void *>(fp8_quantize_tile_kernel<T, 2, E5M2>);
+    case HGEMM_FP8_ROWS | HGEMM_FP8_COLS: return reinterpret_cast<const void *>(fp8_quantize_tile_kernel<T, 3, E5M2>);
+    default: return reinterpret_cast<const void *>(fp8_quantize_tile_kernel<T, 4, E5M2>);
     }
+}
+
+template <class T>
+const void *quantize_kernel(const hgemm_fp8_quantize_t &d, bool many, bool dense)
+{
+    return d.q_type == HGEMM_TYPE_E5M2 ? quantize_kernel<T, true>(d.blocks, many, dense) : quantize_kernel<T, false>(d.blocks, many, dense);
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -245,7 +251,6 @@ hgemm_status_t hgemm_fp8_quantize(hgemm_ctx_t *ctx, const hgemm_fp8_quantize_t *
     p.offsets = d->offsets;
     p.groups = d->groups;
     p.vec_ok = aligned16(d->x) && (d->ldx * es) % 16 == 0 ? 1 : 0;
-    p.e5m2 = d->q_type == HGEMM_TYPE_E5M2 ? 1 : 0;
     p.pow2 = d->pow2;
     p.q = static_cast<uint8_t *>(d->q);
     p.ldq = d->ldq;
@@ -269,8 +274,8 @@ hgemm_status_t hgemm_fp8_quantize(hgemm_ctx_t *ctx, const hgemm_fp8_quantize_t *
         grid.y = unsigned(std::min<int64_t>(row_blocks, 65535));
         grid.z = unsigned(tiles ? d->groups : 1);
     }
-    const void *fn = d->x_type == HGEMM_TYPE_F32 ? quantize_kernel<float>(d->blocks, many, dense) : d->x_type == HGEMM_TYPE_F16 ? quantize_kernel<__half>(d->blocks, many, dense)
-                                                                                                               : quantize_kernel<__nv_bfloat16>(d->blocks, many, dense);
+    const void *fn = d->x_type == HGEMM_TYPE_F32 ? quantize_kernel<float>(*d, many, dense) : d->x_type == HGEMM_TYPE_F16 ? quantize_kernel<__half>(*d, many, dense)
+                                                                                                               : quantize_kernel<__nv_bfloat16>(*d, many, dense);
     void *args[1] = {&p};
     return launch(ctx, fn, grid, hgemm_dev::kQuantThreads, 0, 1, args, stream);
 }

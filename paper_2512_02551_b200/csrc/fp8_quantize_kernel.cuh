@@ -32,7 +32,7 @@ struct QuantParams {
     const int32_t *offsets;
     int32_t groups;
     int32_t vec_ok;            // rows of x start at multiples of 16 bytes
-    int32_t e5m2, pow2;
+    int32_t pow2;
     FastDiv fd_blocks;         // blocks of a row
     uint8_t *q;
     int64_t ldq;
@@ -218,7 +218,7 @@ __device__ __forceinline__ const T *source_row(const QuantParams &p, int64_t r)
 
 // UNROLL: blocks in flight per group of 8 lanes.  DENSE: x and the copy are one run of whole blocks (no gather, rows of whole blocks
 // that follow one another), so that a block's place is its number.
-template <class T, int UNROLL, bool DENSE>
+template <class T, int UNROLL, bool DENSE, bool E5M2>
 __global__ void __launch_bounds__(kQuantThreads, UNROLL == 1 ? 4 : sizeof(T) == 4 ? 2 : 3)
 fp8_quantize_rows_kernel(const QuantParams p)
 {
@@ -286,7 +286,7 @@ fp8_quantize_rows_kernel(const QuantParams p)
             for (int d = 4; d >= 1; d >>= 1) m[u] = fmaxf(m[u], __shfl_xor_sync(0xffffffffu, m[u], d));
             if (sub == u) own = m[u];
         }
-        const BlockScale s = block_scale(own, p.e5m2, p.pow2);
+        const BlockScale s = block_scale(own, E5M2, p.pow2);
         const int64_t own_block = b0 + sub * 4 + lane_block;
         if (sub < UNROLL && own_block < total) p.scales[own_block] = s.scale;
 #pragma unroll
@@ -296,7 +296,7 @@ fp8_quantize_rows_kernel(const QuantParams p)
                 float f[8], g[8];
                 floats_of(raw[u][0], f, careful);
                 floats_of(raw[u][1], g, careful);
-                const uint2 lo = quantize8(f, factor, p.e5m2), hi = quantize8(g, factor, p.e5m2);
+                const uint2 lo = quantize8(f, factor, E5M2), hi = quantize8(g, factor, E5M2);
                 uint8_t *dst = p.q + q_at[u];
                 if (DENSE || room[u] >= 16) {
                     *reinterpret_cast<uint4 *>(dst) = make_uint4(lo.x, lo.y, hi.x, hi.y);
@@ -310,7 +310,7 @@ fp8_quantize_rows_kernel(const QuantParams p)
 }
 
 // MODE: HGEMM_FP8_COLS (2), ROWS | COLS (3) or TILES (4).  grid: x = column blocks of 128, y = row blocks (of the padded copy), z = matrices (TILES).
-template <class T, int MODE>
+template <class T, int MODE, bool E5M2>
 __global__ void __launch_bounds__(kQuantThreads, sizeof(T) == 4 ? 2 : 3)
 fp8_quantize_tile_kernel(const QuantParams p)
 {
@@ -445,7 +445,7 @@ fp8_quantize_tile_kernel(const QuantParams p)
             for (int i = 0; i < 2; ++i) m2[i] = fmaxf(h4 ? m4[i + 2] : m4[i], __shfl_xor_sync(0xffffffffu, h4 ? m4[i] : m4[i + 2], 4));
             m1 = fmaxf(h2 ? m2[1] : m2[0], __shfl_xor_sync(0xffffffffu, h2 ? m2[0] : m2[1], 2));
             m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1));
-            const BlockScale s = block_scale(m1, p.e5m2, p.pow2);
+            const BlockScale s = block_scale(m1, E5M2, p.pow2);
             const int64_t own = my_row + 16 * ((h8 ? 4 : 0) + (h4 ? 2 : 0) + (h2 ? 1 : 0));
             if ((lane & 1u) == 0u && own < row_end) p.scales[own * blocks + blockIdx.x] = s.scale;
 #pragma unroll
@@ -454,7 +454,7 @@ fp8_quantize_tile_kernel(const QuantParams p)
                 const int64_t r = my_row + 16 * i;
                 float f[8];
                 floats_of(raw[i], f, careful);
-                const uint2 v = quantize8(f, factor, p.e5m2);
+                const uint2 v = quantize8(f, factor, E5M2);
                 if (whole) *reinterpret_cast<uint2 *>(p.q + r * p.ldq + col) = v;
                 else if (r < row_end) store8(p.q + r * p.ldq, col, p.cols, v);
                 if constexpr (sizeof(T) == 2) forget_conversions(raw[i]);
@@ -470,13 +470,13 @@ fp8_quantize_tile_kernel(const QuantParams p)
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = fmaxf(m, s_max[0][i]);
-            const BlockScale s = block_scale(m, p.e5m2, p.pow2);
+            const BlockScale s = block_scale(m, E5M2, p.pow2);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int64_t r = my_row + 16 * i;
                 float f[8];
                 floats_of(raw[i], f, careful);
-                const uint2 v = quantize8(f, s.factor, p.e5m2);
+                const uint2 v = quantize8(f, s.factor, E5M2);
                 uint8_t *dst = p.q + (matrix * p.rows + r) * p.ldq;
                 if (whole) *reinterpret_cast<uint2 *>(dst + col) = v;
                 else if (r < row_end) store8(dst, col, p.cols, v);
@@ -495,7 +495,7 @@ fp8_quantize_tile_kernel(const QuantParams p)
                 float m = 0.0f;
 #pragma unroll
                 for (int w = 0; w < 8; ++w) m = fmaxf(m, s_max[w][threadIdx.x]);
-                const BlockScale s = block_scale(m, p.e5m2, p.pow2);
+                const BlockScale s = block_scale(m, E5M2, p.pow2);
                 s_factor[threadIdx.x] = s.factor;
                 const int64_t c = blockIdx.x * 128ll + threadIdx.x;
                 if (c < p.cols) p.scales_cols[rb * p.cols + c] = s.scale;
@@ -509,8 +509,8 @@ fp8_quantize_tile_kernel(const QuantParams p)
                 {
                     float f[8];
                     floats_of(raw[i], f, careful);
-                    const uint32_t h0 = to_fp8x2(f[0] * fa.x, f[1] * fa.y, p.e5m2), h1 = to_fp8x2(f[2] * fa.z, f[3] * fa.w, p.e5m2);
-                    const uint32_t h2 = to_fp8x2(f[4] * fb.x, f[5] * fb.y, p.e5m2), h3 = to_fp8x2(f[6] * fb.z, f[7] * fb.w, p.e5m2);
+                    const uint32_t h0 = to_fp8x2(f[0] * fa.x, f[1] * fa.y, E5M2), h1 = to_fp8x2(f[2] * fa.z, f[3] * fa.w, E5M2);
+                    const uint32_t h2 = to_fp8x2(f[4] * fb.x, f[5] * fb.y, E5M2), h3 = to_fp8x2(f[6] * fb.z, f[7] * fb.w, E5M2);
                     const uint2 v = make_uint2(h0 | (h1 << 16), h2 | (h3 << 16));
                     uint8_t *dst = p.q_cols + (out0 + k) * p.ldq_cols;
                     if (whole) *reinterpret_cast<uint2 *>(dst + col) = v;
