@@ -10,13 +10,15 @@
 //
 // Values are x * (m / a) with the quotient rounded once per block; a division per element would bound the kernel by arithmetic, and
 // so would every lane dividing for every row or column it holds: one lane per block does.  NaN passes through maximum (which skips
-// it) and product by itself; a block whose maximum is infinite is evaluated again with its infinities made NaN.
+// it) and product by itself; a block whose maximum is infinite has its infinities made NaN first.
 #pragma once
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "hgemm_device.cuh"
 
@@ -100,20 +102,16 @@ __device__ __forceinline__ Raw8<T> load8(const T *row, int64_t col, int64_t cols
     return r;
 }
 
-// careful: infinities become NaN.
-__device__ __forceinline__ void floats_of(const Raw8<float> &r, float (&f)[8], bool careful)
+__device__ __forceinline__ void floats_of(const Raw8<float> &r, float (&f)[8])
 {
     const uint32_t w[8] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        f[i] = __uint_as_float(w[i]);
-        if (careful && fabsf(f[i]) == quant_inf()) f[i] = __int_as_float(0x7fffffff);
-    }
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
 }
 __device__ __forceinline__ float2 pair_of(uint32_t w, __half) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
 __device__ __forceinline__ float2 pair_of(uint32_t w, __nv_bfloat16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 template <class T>
-__device__ __forceinline__ void floats_of(const Raw8<T> &r, float (&f)[8], bool careful)
+__device__ __forceinline__ void floats_of(const Raw8<T> &r, float (&f)[8])
 {
     const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
 #pragma unroll
@@ -122,11 +120,24 @@ __device__ __forceinline__ void floats_of(const Raw8<T> &r, float (&f)[8], bool 
         f[2 * i] = p.x;
         f[2 * i + 1] = p.y;
     }
-    if (careful) {
+}
+
+// Infinities become NaN.
+__device__ __forceinline__ uint32_t no_infinity(uint32_t w, float) { return (w & 0x7fffffffu) == 0x7f800000u ? 0x7fffffffu : w; }
+template <class T>
+__device__ __forceinline__ uint32_t no_infinity(uint32_t w, T)
+{
+    constexpr uint32_t inf = std::is_same<T, __half>::value ? 0x7c00u : 0x7f80u;
+    if ((w & 0x7fffu) == inf) w |= 0x7fffu;
+    if (((w >> 16) & 0x7fffu) == inf) w |= 0x7fff0000u;
+    return w;
+}
+template <class T>
+__device__ __forceinline__ void no_infinities(Raw8<T> &r)
+{
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (fabsf(f[i]) == quant_inf()) f[i] = __int_as_float(0x7fffffff);
-    }
+    for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i)
+        r.v[i] = make_uint4(no_infinity(r.v[i].x, T()), no_infinity(r.v[i].y, T()), no_infinity(r.v[i].z, T()), no_infinity(r.v[i].w, T()));
 }
 
 // Two magnitudes of a 16-bit type in one register, compared two at a time; NaN loses against a number.
@@ -151,7 +162,7 @@ __device__ __forceinline__ float larger_half(uint32_t m)
 __device__ __forceinline__ float amax8(const Raw8<float> &r)
 {
     float f[8], m = 0.0f;
-    floats_of(r, f, false);
+    floats_of(r, f);
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[i]));
     return m;
@@ -164,17 +175,6 @@ __device__ __forceinline__ float amax8(const Raw8<T> &r)
     m = abs_max2(m, r.v[0].z, T());
     return larger_half<T>(abs_max2(m, r.v[0].w, T()));
 }
-// The same without infinities.
-template <class T>
-__device__ __forceinline__ float amax8_finite(const Raw8<T> &r)
-{
-    float f[8], m = 0.0f;
-    floats_of(r, f, true);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(f[i]));
-    return m;
-}
-
 // Keeps the compiler from holding converted copies of `r` in registers from here on.
 template <class T>
 __device__ __forceinline__ void forget_conversions(Raw8<T> &r)
@@ -267,7 +267,6 @@ fp8_quantize_rows_kernel(const QuantParams p)
                 raw[u][1] = load8<T>(src, col + 8, p.cols, p.vec_ok);
             }
         }
-        bool careful = false;
         float m[UNROLL], top = 0.0f;
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
@@ -275,9 +274,12 @@ fp8_quantize_rows_kernel(const QuantParams p)
             top = fmaxf(top, m[u]);
         }
         if (__any_sync(0xffffffffu, top == quant_inf())) {
-            careful = true;
 #pragma unroll
-            for (int u = 0; u < UNROLL; ++u) m[u] = fmaxf(amax8_finite(raw[u][0]), amax8_finite(raw[u][1]));
+            for (int u = 0; u < UNROLL; ++u) {
+                no_infinities(raw[u][0]);
+                no_infinities(raw[u][1]);
+                m[u] = fmaxf(amax8(raw[u][0]), amax8(raw[u][1]));
+            }
         }
         float own = 0.0f;                                                 // lane u of a group of 8 makes the scale of its block u
 #pragma unroll
@@ -294,8 +296,8 @@ fp8_quantize_rows_kernel(const QuantParams p)
             const float factor = __shfl_sync(0xffffffffu, s.factor, u, 8);
             if (q_at[u] >= 0) {
                 float f[8], g[8];
-                floats_of(raw[u][0], f, careful);
-                floats_of(raw[u][1], g, careful);
+                floats_of(raw[u][0], f);
+                floats_of(raw[u][1], g);
                 const uint2 lo = quantize8(f, factor, E5M2), hi = quantize8(g, factor, E5M2);
                 uint8_t *dst = p.q + q_at[u];
                 if (DENSE || room[u] >= 16) {
@@ -377,18 +379,16 @@ fp8_quantize_tile_kernel(const QuantParams p)
                 raw[i] = load8<T>(src, col, p.cols, p.vec_ok);
             }
         }
-        // Maxima; once more, from floats and without the infinities, if the tile has any.
+        // Maxima; once more, with the infinities made NaN, if the tile has any.
         float row_max[8], col_max[8];
-        bool careful = false;
-        {
-            float top = 0.0f;
+        auto maxima = [&]() {
             if constexpr (sizeof(T) == 4) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) col_max[j] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     float f[8];
-                    floats_of(raw[i], f, false);
+                    floats_of(raw[i], f);
                     row_max[i] = amax8(raw[i]);
                     if (MODE != 4) {
 #pragma unroll
@@ -414,21 +414,15 @@ fp8_quantize_tile_kernel(const QuantParams p)
                     col_max[2 * j + 1] = f.y;
                 }
             }
+            float top = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = fmaxf(top, row_max[i]);
-            if (__syncthreads_or(top == quant_inf())) {                // (also: the previous turn's readers of s_max are done)
-                careful = true;
+            return top;
+        };
+        if (__syncthreads_or(maxima() == quant_inf())) {               // (also: the previous turn's readers of s_max are done)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) col_max[j] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float f[8];
-                    floats_of(raw[i], f, true);
-                    row_max[i] = amax8_finite(raw[i]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) col_max[j] = fmaxf(col_max[j], fabsf(f[j]));
-                }
-            }
+            for (int i = 0; i < 8; ++i) no_infinities(raw[i]);
+            (void)maxima();
         }
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -453,7 +447,7 @@ fp8_quantize_tile_kernel(const QuantParams p)
                 const float factor = __shfl_sync(0xffffffffu, s.factor, (i & 4) * 2 + (i & 2) * 2 + (i & 1) * 2, 16);
                 const int64_t r = my_row + 16 * i;
                 float f[8];
-                floats_of(raw[i], f, careful);
+                floats_of(raw[i], f);
                 const uint2 v = quantize8(f, factor, E5M2);
                 if (whole) *reinterpret_cast<uint2 *>(p.q + r * p.ldq + col) = v;
                 else if (r < row_end) store8(p.q + r * p.ldq, col, p.cols, v);
@@ -475,7 +469,7 @@ fp8_quantize_tile_kernel(const QuantParams p)
             for (int i = 0; i < 8; ++i) {
                 const int64_t r = my_row + 16 * i;
                 float f[8];
-                floats_of(raw[i], f, careful);
+                floats_of(raw[i], f);
                 const uint2 v = quantize8(f, s.factor, E5M2);
                 uint8_t *dst = p.q + (matrix * p.rows + r) * p.ldq;
                 if (whole) *reinterpret_cast<uint2 *>(dst + col) = v;
@@ -508,7 +502,7 @@ fp8_quantize_tile_kernel(const QuantParams p)
                 const int64_t k = (threadIdx.x >> 4) + 16 * i;
                 {
                     float f[8];
-                    floats_of(raw[i], f, careful);
+                    floats_of(raw[i], f);
                     const uint32_t h0 = to_fp8x2(f[0] * fa.x, f[1] * fa.y, E5M2), h1 = to_fp8x2(f[2] * fa.z, f[3] * fa.w, E5M2);
                     const uint32_t h2 = to_fp8x2(f[4] * fb.x, f[5] * fb.y, E5M2), h3 = to_fp8x2(f[6] * fb.z, f[7] * fb.w, E5M2);
                     const uint2 v = make_uint2(h0 | (h1 << 16), h2 | (h3 << 16));
