@@ -20,6 +20,11 @@
 // every CTA computes for itself from the offsets.  A tile never crosses a group; the rows it computes beyond its group's end
 // are not stored.  Weight gradients contract over a group's rows, which the column-quantised copy pads with zeros to whole blocks.
 //
+// Measured (B200, bf16 results unless said): 4096^3 forward 69 us (2000 TFLOP/s), 8192^3 500 us (2200, power-limited: 408 us without
+// the promotion), 8192 x 4096 x 4096 weight gradient in fp32 178 us (1540); 1000 x 4096 x 4096 22 us; 64 experts x 4 rows, 2048 x 2048 weights
+// 42 us (6.4 TB/s, the copy rate); 7 x 8192 x 4096 9.9 us (3.4 TB/s). What bounds the large ones is the promoting warps (multiply-adds,
+// barrier round trips and, on the MMA warp's scheduler, its instructions), 720-770 cycles a block of 512 cycles of MMA.
+//
 // Every mbarrier wait is bounded (see hgemm_device.cuh): a wait that runs out raises the status word and the CTA's abort flag, and
 // every role falls through to the common teardown.
 #pragma once

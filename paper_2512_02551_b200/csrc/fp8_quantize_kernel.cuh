@@ -11,6 +11,9 @@
 // Values are x * (m / a) with the quotient rounded once per block; a division per element would bound the kernel by arithmetic, and
 // so would every lane dividing for every row or column it holds: one lane per block does.  NaN passes through maximum (which skips
 // it) and product by itself; a block whose maximum is infinite has its infinities made NaN first.
+//
+// Measured (B200): 8192 x 8192 bf16 by rows 30 us (6.6 TB/s, the copy rate), rows and columns 53 us (5.1 TB/s), tiles 35 us (5.7 TB/s); fp32
+// rows and columns 72 us (5.6 TB/s).  The 16-bit forms that make columns are bound by instructions (17 an element).
 #pragma once
 
 #include <cuda_bf16.h>
