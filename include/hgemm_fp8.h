@@ -62,7 +62,7 @@ typedef struct {
     int64_t ldx;               /* elements between rows of x */
     const void *x;
     const int32_t *row_index;  /* NULL, or `rows` numbers: row r of the result is row row_index[r] of x, zeros if that is outside [0, x_rows) (not for _TILES) */
-    int64_t x_rows;            /* rows of x (row_index only) */
+    int64_t x_rows;            /* rows of x (row_index only); 0: x may be NULL */
     const int32_t *offsets;    /* NULL, or the groups + 1 offsets: the column-quantised copy is laid out per group (_COLS only) */
     int32_t groups;            /* with offsets: their groups; for _TILES: the number of matrices (x holds groups * rows rows); else 0 */
     int32_t reserved;

@@ -237,7 +237,8 @@ hgemm_status_t hgemm_fp8_quantize(hgemm_ctx_t *ctx, const hgemm_fp8_quantize_t *
     if (d->offsets && !aligned4(d->offsets)) return HGEMM_ERR_INVALID_ARG;
     if (d->rows == 0) return HGEMM_OK;
     const int es = type_bytes(d->x_type);
-    if (!d->x || (reinterpret_cast<uintptr_t>(d->x) % unsigned(es)) != 0) return HGEMM_ERR_INVALID_ARG;
+    const bool no_source = d->row_index && d->x_rows == 0;   // rows of zeros: x is never read
+    if ((!d->x && !no_source) || (reinterpret_cast<uintptr_t>(d->x) % unsigned(es)) != 0) return HGEMM_ERR_INVALID_ARG;
     if ((by_rows || tiles) && (!d->q || !d->scales || !aligned16(d->q) || !aligned4(d->scales) || d->ldq < d->cols || (d->ldq & 15) != 0)) return HGEMM_ERR_INVALID_ARG;
     if (by_cols && (!d->q_cols || !d->scales_cols || !aligned16(d->q_cols) || !aligned4(d->scales_cols) || d->ldq_cols < d->cols || (d->ldq_cols & 15) != 0)) return HGEMM_ERR_INVALID_ARG;
     hgemm_dev::QuantParams p;

@@ -402,6 +402,20 @@ def test_quantize_strides_and_guards(ctx):
             assert bool((wide[:, C:] == 0x55).all()) and bool((wide_c[:, C:] == 0x55).all())
 
 
+def test_quantize_gather_from_nothing(ctx):
+    """A source without rows: every row number lies outside it, the copies are zeros with scales of 1."""
+    x = torch.empty(0, 200, dtype=torch.bfloat16, device="cuda")
+    rows = torch.arange(-2, 3, dtype=torch.int32, device="cuda")
+    q, s = fp8.empty_rows(5, 200)
+    c, t = fp8.empty_cols(5, 200)
+    for v in (q, c):
+        v.view(torch.uint8).fill_(0x7F)
+    fp8.quantize_rows(ctx, x, q, s, rows)
+    fp8.quantize_both(ctx, x, q, s, c, t, rows)
+    for values, scale in ((q, s), (c, t)):
+        assert bool((values.view(torch.uint8) == 0).all()) and bool((scale == 1).all())
+
+
 def test_quantize_gather(ctx):
     g = rng("gather")
     x = torch.randn(50, 300, generator=g, device="cuda").to(torch.bfloat16)
