@@ -22,7 +22,7 @@
  *
  * Products over experts (groups >= 1): the M rows are sorted by group, rows offsets[g] .. offsets[g+1]-1 belong to
  * group g (int32, groups + 1 values on the DEVICE, non-decreasing, offsets[0] = 0, offsets[groups] <= M; values outside
- * [0, M] are clamped).  W and its scales are groups x N x K, dense matrices one after the other with `ld` between rows.  A
+ * [0, M] are clamped, and one that is smaller than one before it counts as that one, here and in the quantiser).  W and its scales are groups x N x K, dense matrices one after the other with `ld` between rows.  A
  * group without rows is legal; rows from offsets[groups] on are not written.  For the weight gradient (result groups x N x K, zeros for an
  * empty group) the operands are the column-quantised copies that hgemm_fp8_quantize makes when it is given the
  * offsets: group g's rows start at row 128 * sum_{h < g} ceil(count_h / 128) of the copy, the rows up to the next

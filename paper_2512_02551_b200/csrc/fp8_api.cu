@@ -272,7 +272,7 @@ hgemm_status_t hgemm_fp8_quantize(hgemm_ctx_t *ctx, const hgemm_fp8_quantize_t *
     } else {
         const int64_t row_blocks = d->offsets ? hgemm_fp8_padded_rows(d->rows, d->groups) / 128 : ceil_div(d->rows, 128);
         grid.x = unsigned(col_blocks);
-        grid.y = unsigned(std::min<int64_t>(row_blocks, 65535));
+        grid.y = unsigned(row_blocks);                         // at most 2^15 + 1025 with these sizes: within the limit of 65535
         grid.z = unsigned(tiles ? d->groups : 1);
     }
     const void *fn = d->x_type == HGEMM_TYPE_F32 ? quantize_kernel<float>(*d, many, dense) : d->x_type == HGEMM_TYPE_F16 ? quantize_kernel<__half>(*d, many, dense)

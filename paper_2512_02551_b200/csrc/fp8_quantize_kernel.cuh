@@ -314,7 +314,7 @@ fp8_quantize_rows_kernel(const QuantParams p)
     }
 }
 
-// MODE: HGEMM_FP8_COLS (2), ROWS | COLS (3) or TILES (4).  grid: x = column blocks of 128, y = row blocks (of the padded copy), z = matrices (TILES).
+// MODE: HGEMM_FP8_COLS (2), ROWS | COLS (3) or TILES (4).  grid: x = column blocks of 128, y = row blocks (as many as the padded copy has), z = matrices (TILES).
 template <class T, int MODE, bool E5M2>
 __global__ void __launch_bounds__(kQuantThreads, sizeof(T) == 4 ? 2 : 3)
 fp8_quantize_tile_kernel(const QuantParams p)
@@ -326,193 +326,200 @@ fp8_quantize_tile_kernel(const QuantParams p)
     grid_dependency_wait();
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const int64_t blocks = (p.cols + 127) / 128;
-    for (int64_t rb = blockIdx.y;; rb += gridDim.y) {
-        int64_t row0 = rb * 128, row_end = p.rows, out0 = row0;        // rows row0 .. row_end - 1 of the input, out0: first row of the copy
-        if (MODE != 4 && p.offsets != nullptr) {
-            // the group that holds block rb of the padded copy
-            __syncthreads();
-            if (warp == 0) {
-                int32_t carry = 0, found = 0, first = 0, end = 0;
-                const int32_t limit = static_cast<int32_t>(p.rows);
-                for (int32_t base = 0; base < p.groups && !found; base += 32) {
-                    const int32_t e = base + static_cast<int32_t>(lane);
-                    const int32_t a = min(max(p.offsets[min(e, p.groups)], 0), limit), z = min(max(p.offsets[min(e + 1, p.groups)], 0), limit);
-                    const int32_t n = e < p.groups && z > a ? (z - a + 127) / 128 : 0;
-                    int32_t sum = n;
+    const int64_t rb = blockIdx.y;
+    int64_t row0 = rb * 128, row_end = p.rows;                         // rows row0 .. row_end - 1 of the input
+    const int64_t out0 = row0;                                         // first row of the copy
+    if (MODE != 4 && p.offsets != nullptr) {
+        // The group that holds block rb of the padded copy.  The offsets are clamped as the products clamp them: to [0, rows], each at
+        // least as large as those before it.  Then the groups' blocks fit the copy, whatever the caller's values.
+        if (warp == 0) {
+            int32_t carry = 0, found = 0, first = 0, end = 0, last = 0;
+            const int32_t limit = static_cast<int32_t>(p.rows);
+            for (int32_t base = 0; base < p.groups && !found; base += 32) {
+                const int32_t e = base + static_cast<int32_t>(lane);
+                int32_t a = min(max(p.offsets[min(e, p.groups)], 0), limit);
 #pragma unroll
-                    for (int d = 1; d < 32; d <<= 1) {
-                        const int32_t x = __shfl_up_sync(0xffffffffu, sum, d);
-                        if (static_cast<int32_t>(lane) >= d) sum += x;
-                    }
-                    const uint32_t hit = __ballot_sync(0xffffffffu, n > 0 && carry + sum > rb);
-                    if (hit) {
-                        const int src = __ffs(hit) - 1;
-                        const int32_t before = carry + sum - n;
-                        first = __shfl_sync(0xffffffffu, a + (static_cast<int32_t>(rb) - before) * 128, src);
-                        end = __shfl_sync(0xffffffffu, z, src);
-                        found = 1;
-                    }
-                    carry += __shfl_sync(0xffffffffu, sum, 31);
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int32_t x = __shfl_up_sync(0xffffffffu, a, d);
+                    if (static_cast<int32_t>(lane) >= d) a = max(a, x);
                 }
-                if (lane == 0) { s_place[0] = found; s_place[1] = first; s_place[2] = end; }
-            }
-            __syncthreads();
-            if (!s_place[0]) return;                                   // beyond the last group's rows (block-uniform)
-            row0 = s_place[1];
-            row_end = s_place[2];
-        } else if (row0 >= p.rows) {
-            return;
-        }
-        const int64_t matrix = MODE == 4 ? blockIdx.z : 0;
-        const int64_t col = blockIdx.x * 128ll + (threadIdx.x & 15u) * 8;
-        const int64_t my_row = row0 + (threadIdx.x >> 4);              // and every 16th after it
-        Raw8<T> raw[8];
-        // a whole tile of a plain matrix takes its loads and stores without a test per row
-        const bool whole = p.vec_ok && p.row_index == nullptr && row0 + 128 <= row_end && blockIdx.x * 128ll + 128 <= p.cols;
-        if (whole) {
-            const T *src = static_cast<const T *>(p.x) + (matrix * p.rows + my_row) * p.ldx + col;
+                a = max(a, last);
+                int32_t z = __shfl_down_sync(0xffffffffu, a, 1);
+                if (lane == 31) z = max(a, min(max(p.offsets[min(e + 1, p.groups)], 0), limit));
+                last = __shfl_sync(0xffffffffu, z, 31);
+                const int32_t n = e < p.groups ? (z - a + 127) / 128 : 0;
+                int32_t sum = n;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) raw[i] = load8_whole<T>(src + 16 * i * p.ldx);
-        } else {
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int32_t x = __shfl_up_sync(0xffffffffu, sum, d);
+                    if (static_cast<int32_t>(lane) >= d) sum += x;
+                }
+                const uint32_t hit = __ballot_sync(0xffffffffu, n > 0 && carry + sum > rb);
+                if (hit) {
+                    const int src = __ffs(hit) - 1;
+                    const int32_t before = carry + sum - n;
+                    first = __shfl_sync(0xffffffffu, a + (static_cast<int32_t>(rb) - before) * 128, src);
+                    end = __shfl_sync(0xffffffffu, z, src);
+                    found = 1;
+                }
+                carry += __shfl_sync(0xffffffffu, sum, 31);
+            }
+            if (lane == 0) { s_place[0] = found; s_place[1] = first; s_place[2] = end; }
+        }
+        __syncthreads();
+        if (!s_place[0]) return;                                       // beyond the last group's rows (block-uniform)
+        row0 = s_place[1];
+        row_end = s_place[2];
+    }
+    const int64_t matrix = MODE == 4 ? blockIdx.z : 0;
+    const int64_t col = blockIdx.x * 128ll + (threadIdx.x & 15u) * 8;
+    const int64_t my_row = row0 + (threadIdx.x >> 4);              // and every 16th after it
+    Raw8<T> raw[8];
+    // a whole tile of a plain matrix takes its loads and stores without a test per row
+    const bool whole = p.vec_ok && p.row_index == nullptr && row0 + 128 <= row_end && blockIdx.x * 128ll + 128 <= p.cols;
+    if (whole) {
+        const T *src = static_cast<const T *>(p.x) + (matrix * p.rows + my_row) * p.ldx + col;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) raw[i] = load8_whole<T>(src + 16 * i * p.ldx);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t r = my_row + 16 * i;
+            const T *src = nullptr;
+            if (r < row_end) src = MODE == 4 ? static_cast<const T *>(p.x) + (matrix * p.rows + r) * p.ldx : source_row<T>(p, r);
+            raw[i] = load8<T>(src, col, p.cols, p.vec_ok);
+        }
+    }
+    // Maxima; once more, with the infinities made NaN, if the tile has any.
+    float row_max[8], col_max[8];
+    auto maxima = [&]() {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) col_max[j] = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int64_t r = my_row + 16 * i;
-                const T *src = nullptr;
-                if (r < row_end) src = MODE == 4 ? static_cast<const T *>(p.x) + (matrix * p.rows + r) * p.ldx : source_row<T>(p, r);
-                raw[i] = load8<T>(src, col, p.cols, p.vec_ok);
-            }
-        }
-        // Maxima; once more, with the infinities made NaN, if the tile has any.
-        float row_max[8], col_max[8];
-        auto maxima = [&]() {
-            if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) col_max[j] = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float f[8];
-                    floats_of(raw[i], f);
-                    row_max[i] = amax8(raw[i]);
-                    if (MODE != 4) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) col_max[j] = fmaxf(col_max[j], fabsf(f[j]));
-                    }
-                }
-            } else {
-                uint32_t c[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    row_max[i] = amax8(raw[i]);
-                    if (MODE != 4) {
-                        c[0] = abs_max2(c[0], raw[i].v[0].x, T());
-                        c[1] = abs_max2(c[1], raw[i].v[0].y, T());
-                        c[2] = abs_max2(c[2], raw[i].v[0].z, T());
-                        c[3] = abs_max2(c[3], raw[i].v[0].w, T());
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 f = pair_of(c[j], T());
-                    col_max[2 * j] = f.x;
-                    col_max[2 * j + 1] = f.y;
-                }
-            }
-            float top = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, row_max[i]);
-            return top;
-        };
-        if (__syncthreads_or(maxima() == quant_inf())) {               // (also: the previous turn's readers of s_max are done)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) no_infinities(raw[i]);
-            (void)maxima();
-        }
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) forget_conversions(raw[i]);
-        }
-        if (MODE == 3) {
-            // Rows: 16 lanes hold 8 rows.  Each exchange halves the rows a lane keeps, so that after three of them (and a last
-            // plain one) a lane has the maximum of one row, whose scale it makes; the factors go back by shuffles.
-            float m4[4], m2[2], m1;
-            const bool h8 = (lane & 8u) != 0u, h4 = (lane & 4u) != 0u, h2 = (lane & 2u) != 0u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) m4[i] = fmaxf(h8 ? row_max[i + 4] : row_max[i], __shfl_xor_sync(0xffffffffu, h8 ? row_max[i] : row_max[i + 4], 8));
-#pragma unroll
-            for (int i = 0; i < 2; ++i) m2[i] = fmaxf(h4 ? m4[i + 2] : m4[i], __shfl_xor_sync(0xffffffffu, h4 ? m4[i] : m4[i + 2], 4));
-            m1 = fmaxf(h2 ? m2[1] : m2[0], __shfl_xor_sync(0xffffffffu, h2 ? m2[0] : m2[1], 2));
-            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1));
-            const BlockScale s = block_scale(m1, E5M2, p.pow2);
-            const int64_t own = my_row + 16 * ((h8 ? 4 : 0) + (h4 ? 2 : 0) + (h2 ? 1 : 0));
-            if ((lane & 1u) == 0u && own < row_end) p.scales[own * blocks + blockIdx.x] = s.scale;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float factor = __shfl_sync(0xffffffffu, s.factor, (i & 4) * 2 + (i & 2) * 2 + (i & 1) * 2, 16);
-                const int64_t r = my_row + 16 * i;
                 float f[8];
                 floats_of(raw[i], f);
-                const uint2 v = quantize8(f, factor, E5M2);
-                if (whole) *reinterpret_cast<uint2 *>(p.q + r * p.ldq + col) = v;
-                else if (r < row_end) store8(p.q + r * p.ldq, col, p.cols, v);
-                if constexpr (sizeof(T) == 2) forget_conversions(raw[i]);
+                row_max[i] = amax8(raw[i]);
+                if (MODE != 4) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) col_max[j] = fmaxf(col_max[j], fabsf(f[j]));
+                }
+            }
+        } else {
+            uint32_t c[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                row_max[i] = amax8(raw[i]);
+                if (MODE != 4) {
+                    c[0] = abs_max2(c[0], raw[i].v[0].x, T());
+                    c[1] = abs_max2(c[1], raw[i].v[0].y, T());
+                    c[2] = abs_max2(c[2], raw[i].v[0].z, T());
+                    c[3] = abs_max2(c[3], raw[i].v[0].w, T());
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = pair_of(c[j], T());
+                col_max[2 * j] = f.x;
+                col_max[2 * j + 1] = f.y;
             }
         }
-        if (MODE == 4) {
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, row_max[i]);
+        return top;
+    };
+    if (__syncthreads_or(maxima() == quant_inf())) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) no_infinities(raw[i]);
+        (void)maxima();
+    }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) forget_conversions(raw[i]);
+    }
+    if (MODE == 3) {
+        // Rows: 16 lanes hold 8 rows.  Each exchange halves the rows a lane keeps, so that after three of them (and a last
+        // plain one) a lane has the maximum of one row, whose scale it makes; the factors go back by shuffles.
+        float m4[4], m2[2], m1;
+        const bool h8 = (lane & 8u) != 0u, h4 = (lane & 4u) != 0u, h2 = (lane & 2u) != 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m4[i] = fmaxf(h8 ? row_max[i + 4] : row_max[i], __shfl_xor_sync(0xffffffffu, h8 ? row_max[i] : row_max[i + 4], 8));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) m2[i] = fmaxf(h4 ? m4[i + 2] : m4[i], __shfl_xor_sync(0xffffffffu, h4 ? m4[i] : m4[i + 2], 4));
+        m1 = fmaxf(h2 ? m2[1] : m2[0], __shfl_xor_sync(0xffffffffu, h2 ? m2[0] : m2[1], 2));
+        m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1));
+        const BlockScale s = block_scale(m1, E5M2, p.pow2);
+        const int64_t own = my_row + 16 * ((h8 ? 4 : 0) + (h4 ? 2 : 0) + (h2 ? 1 : 0));
+        if ((lane & 1u) == 0u && own < row_end) p.scales[own * blocks + blockIdx.x] = s.scale;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float factor = __shfl_sync(0xffffffffu, s.factor, (i & 4) * 2 + (i & 2) * 2 + (i & 1) * 2, 16);
+            const int64_t r = my_row + 16 * i;
+            float f[8];
+            floats_of(raw[i], f);
+            const uint2 v = quantize8(f, factor, E5M2);
+            if (whole) *reinterpret_cast<uint2 *>(p.q + r * p.ldq + col) = v;
+            else if (r < row_end) store8(p.q + r * p.ldq, col, p.cols, v);
+            if constexpr (sizeof(T) == 2) forget_conversions(raw[i]);
+        }
+    }
+    if (MODE == 4) {
+        float m = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, row_max[i]);
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        if (lane == 0) s_max[0][warp] = m;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, s_max[0][i]);
+        const BlockScale s = block_scale(m, E5M2, p.pow2);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t r = my_row + 16 * i;
+            float f[8];
+            floats_of(raw[i], f);
+            const uint2 v = quantize8(f, s.factor, E5M2);
+            uint8_t *dst = p.q + (matrix * p.rows + r) * p.ldq;
+            if (whole) *reinterpret_cast<uint2 *>(dst + col) = v;
+            else if (r < row_end) store8(dst, col, p.cols, v);
+        }
+        if (threadIdx.x == 0) p.scales[(matrix * ((p.rows + 127) / 128) + rb) * blocks + blockIdx.x] = s.scale;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) col_max[j] = fmaxf(col_max[j], __shfl_xor_sync(0xffffffffu, col_max[j], 16));
+        if (lane < 16) {
+            float4 *dst = reinterpret_cast<float4 *>(&s_max[warp][lane * 8]);
+            dst[0] = make_float4(col_max[0], col_max[1], col_max[2], col_max[3]);
+            dst[1] = make_float4(col_max[4], col_max[5], col_max[6], col_max[7]);
+        }
+        __syncthreads();
+        if (threadIdx.x < 128) {                                    // thread c makes the scale of column c
             float m = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, row_max[i]);
-#pragma unroll
-            for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-            if (lane == 0) s_max[0][warp] = m;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, s_max[0][i]);
+            for (int w = 0; w < 8; ++w) m = fmaxf(m, s_max[w][threadIdx.x]);
             const BlockScale s = block_scale(m, E5M2, p.pow2);
+            s_factor[threadIdx.x] = s.factor;
+            const int64_t c = blockIdx.x * 128ll + threadIdx.x;
+            if (c < p.cols) p.scales_cols[rb * p.cols + c] = s.scale;
+        }
+        __syncthreads();
+        const float4 fa = *reinterpret_cast<const float4 *>(&s_factor[(threadIdx.x & 15u) * 8]), fb = *reinterpret_cast<const float4 *>(&s_factor[(threadIdx.x & 15u) * 8 + 4]);
+        const bool padded = p.offsets != nullptr;                   // rows up to the next multiple of 128 are written (zeros)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int64_t r = my_row + 16 * i;
+        for (int i = 0; i < 8; ++i) {
+            const int64_t k = (threadIdx.x >> 4) + 16 * i;
+            {
                 float f[8];
                 floats_of(raw[i], f);
-                const uint2 v = quantize8(f, s.factor, E5M2);
-                uint8_t *dst = p.q + (matrix * p.rows + r) * p.ldq;
+                const uint32_t h0 = to_fp8x2(f[0] * fa.x, f[1] * fa.y, E5M2), h1 = to_fp8x2(f[2] * fa.z, f[3] * fa.w, E5M2);
+                const uint32_t h2 = to_fp8x2(f[4] * fb.x, f[5] * fb.y, E5M2), h3 = to_fp8x2(f[6] * fb.z, f[7] * fb.w, E5M2);
+                const uint2 v = make_uint2(h0 | (h1 << 16), h2 | (h3 << 16));
+                uint8_t *dst = p.q_cols + (out0 + k) * p.ldq_cols;
                 if (whole) *reinterpret_cast<uint2 *>(dst + col) = v;
-                else if (r < row_end) store8(dst, col, p.cols, v);
-            }
-            if (threadIdx.x == 0) p.scales[(matrix * ((p.rows + 127) / 128) + rb) * blocks + blockIdx.x] = s.scale;
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) col_max[j] = fmaxf(col_max[j], __shfl_xor_sync(0xffffffffu, col_max[j], 16));
-            if (lane < 16) {
-                float4 *dst = reinterpret_cast<float4 *>(&s_max[warp][lane * 8]);
-                dst[0] = make_float4(col_max[0], col_max[1], col_max[2], col_max[3]);
-                dst[1] = make_float4(col_max[4], col_max[5], col_max[6], col_max[7]);
-            }
-            __syncthreads();
-            if (threadIdx.x < 128) {                                    // thread c makes the scale of column c
-                float m = 0.0f;
-#pragma unroll
-                for (int w = 0; w < 8; ++w) m = fmaxf(m, s_max[w][threadIdx.x]);
-                const BlockScale s = block_scale(m, E5M2, p.pow2);
-                s_factor[threadIdx.x] = s.factor;
-                const int64_t c = blockIdx.x * 128ll + threadIdx.x;
-                if (c < p.cols) p.scales_cols[rb * p.cols + c] = s.scale;
-            }
-            __syncthreads();
-            const float4 fa = *reinterpret_cast<const float4 *>(&s_factor[(threadIdx.x & 15u) * 8]), fb = *reinterpret_cast<const float4 *>(&s_factor[(threadIdx.x & 15u) * 8 + 4]);
-            const bool padded = p.offsets != nullptr;                   // rows up to the next multiple of 128 are written (zeros)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int64_t k = (threadIdx.x >> 4) + 16 * i;
-                {
-                    float f[8];
-                    floats_of(raw[i], f);
-                    const uint32_t h0 = to_fp8x2(f[0] * fa.x, f[1] * fa.y, E5M2), h1 = to_fp8x2(f[2] * fa.z, f[3] * fa.w, E5M2);
-                    const uint32_t h2 = to_fp8x2(f[4] * fb.x, f[5] * fb.y, E5M2), h3 = to_fp8x2(f[6] * fb.z, f[7] * fb.w, E5M2);
-                    const uint2 v = make_uint2(h0 | (h1 << 16), h2 | (h3 << 16));
-                    uint8_t *dst = p.q_cols + (out0 + k) * p.ldq_cols;
-                    if (whole) *reinterpret_cast<uint2 *>(dst + col) = v;
-                    else if (row0 + k < row_end || padded) store8(dst, col, p.cols, v);
-                }
+                else if (row0 + k < row_end || padded) store8(dst, col, p.cols, v);
             }
         }
     }

@@ -460,6 +460,46 @@ def test_quantize_per_group(ctx, counts):
     assert bool((c.view(torch.uint8)[at:] == 0x55).all()) and bool((sc[at // 128:] == -1.0).all())
 
 
+FALLING = {
+    "falls and overshoots": (40, [0, 10, 5, 2000000000, 50]),
+    "negative": (40, [-5, -1, 20, 10, 40]),
+    "starts late": (40, [7, 7, 7, 7, 1 << 30]),
+    "up and down": (1000, [0, 1000] * 4 + [0]),
+    "up and down, many": (300, [0, 300, -1, 150] * 25 + [299]),
+    "falls between chunks of 32": (500, list(range(0, 32)) + [400, 3] + list(range(4, 40)) + [450]),
+}
+
+
+@pytest.mark.parametrize("case", list(FALLING), ids=str)
+@pytest.mark.parametrize("both", [False, True], ids=["cols", "both"])
+def test_quantize_offsets_out_of_range_stay_inside(ctx, case, both):
+    """Offsets that are negative, fall or reach beyond the rows count as the products count them -- clamped to the rows, each at least
+    as large as those before it -- and nothing behind the padded copy or its scales is written."""
+    M, bad = FALLING[case]
+    C, E, spare = 200, len(bad) - 1, 100                      # spare: blocks behind the copy
+    x = torch.randn(M, C, generator=rng("falling", case), device="cuda")
+    capacity = fp8.padded_rows(M, E)
+    wide = torch.full((capacity + spare * 128, 208), 0x55, dtype=torch.uint8, device="cuda")
+    wide_s = torch.full((blocks(capacity) + spare, C), -1.0, device="cuda")
+    c, sc = wide[:capacity, :C].view(E4M3), wide_s[:blocks(capacity)]
+    offsets = torch.tensor(bad, dtype=torch.int32, device="cuda")
+    if both:
+        fp8.quantize_both(ctx, x, *fp8.empty_rows(M, C), c, sc, offsets=offsets)
+    else:
+        fp8.quantize_cols(ctx, x, c, sc, offsets=offsets)
+    torch.cuda.synchronize()
+    ends = np.maximum.accumulate(np.clip(bad, 0, M))
+    at = 0
+    for a, z in zip(ends[:-1], ends[1:]):
+        n, up = z - a, blocks(z - a) * 128
+        if n:
+            check_quantized(c[at:at + n], sc[at // 128:(at + up) // 128], ref.f64(x)[a:z], 128, 1, "e4m3", False, "a group's columns")
+            assert bool((c[at + n:at + up].float() == 0).all())
+        at += up
+    assert at <= capacity
+    assert bool((wide[at:] == 0x55).all()) and bool((wide[:, C:] == 0x55).all()) and bool((wide_s[at // 128:] == -1.0).all())
+
+
 # ---- the layer as a whole ---------------------------------------------------------------------------------------
 
 def test_gradients_against_differences(ctx):
