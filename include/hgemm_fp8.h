@@ -22,8 +22,8 @@
  *
  * Products over experts (groups >= 1): the M rows are sorted by group, rows offsets[g] .. offsets[g+1]-1 belong to
  * group g (int32, groups + 1 values on the DEVICE, non-decreasing, offsets[0] = 0, offsets[groups] <= M; values outside
- * [0, M] are clamped, and one that is smaller than one before it counts as that one, here and in the quantiser).  W and its scales are groups x N x K, dense matrices one after the other with `ld` between rows.  A
- * group without rows is legal; rows from offsets[groups] on are not written.  For the weight gradient (result groups x N x K, zeros for an
+ * [0, M] are clamped, and one that is smaller than one before it counts as that one, here and in the quantiser).  W and
+ * its scales are groups x N x K, dense matrices one after the other with `ld` between rows.  A group without rows is legal; rows from offsets[groups] on are not written.  For the weight gradient (result groups x N x K, zeros for an
  * empty group) the operands are the column-quantised copies that hgemm_fp8_quantize makes when it is given the
  * offsets: group g's rows start at row 128 * sum_{h < g} ceil(count_h / 128) of the copy, the rows up to the next
  * multiple of 128 are zero, and the copy has hgemm_fp8_padded_rows(M, groups) rows.
@@ -63,7 +63,8 @@ typedef struct {
     const void *x;
     const int32_t *row_index;  /* NULL, or `rows` numbers: row r of the result is row row_index[r] of x, zeros if that is outside [0, x_rows) (not for _TILES) */
     int64_t x_rows;            /* rows of x (row_index only); 0: x may be NULL */
-    const int32_t *offsets;    /* NULL, or the groups + 1 offsets: the column-quantised copy is laid out per group (_COLS only) */
+    const int32_t *offsets;    /* NULL, or the groups + 1 offsets: the column-quantised copy is laid out per group (_COLS; what lies behind its last
+                                  group is not written).  A row copy made in the same pass has every row, those of no group too */
     int32_t groups;            /* with offsets: their groups; for _TILES: the number of matrices (x holds groups * rows rows); else 0 */
     int32_t reserved;
     void *q;                   /* row- or tile-quantised values */

@@ -270,7 +270,8 @@ hgemm_status_t hgemm_fp8_quantize(hgemm_ctx_t *ctx, const hgemm_fp8_quantize_t *
     if (d->blocks == HGEMM_FP8_ROWS) {
         grid.x = unsigned(std::min<int64_t>(ceil_div(row_work, many ? 128 : 32), int64_t(ctx->num_sms) * 64));
     } else {
-        const int64_t row_blocks = d->offsets ? hgemm_fp8_padded_rows(d->rows, d->groups) / 128 : ceil_div(d->rows, 128);
+        // per group: as many as the copy has room for; the row copies of rows of no group lie in two more runs of rows
+        const int64_t row_blocks = d->offsets ? ceil_div(d->rows + 127 * int64_t(d->groups + (by_rows ? 2 : 0)), 128) : ceil_div(d->rows, 128);
         grid.x = unsigned(col_blocks);
         grid.y = unsigned(row_blocks);                         // at most 2^15 + 1025 with these sizes: within the limit of 65535
         grid.z = unsigned(tiles ? d->groups : 1);

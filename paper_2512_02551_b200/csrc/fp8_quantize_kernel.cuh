@@ -314,7 +314,7 @@ fp8_quantize_rows_kernel(const QuantParams p)
     }
 }
 
-// MODE: HGEMM_FP8_COLS (2), ROWS | COLS (3) or TILES (4).  grid: x = column blocks of 128, y = row blocks (as many as the padded copy has), z = matrices (TILES).
+// MODE: HGEMM_FP8_COLS (2), ROWS | COLS (3) or TILES (4).  grid: x = column blocks of 128, y = row blocks (as many as the padded copy has; ROWS | COLS: and those of rows of no group), z = matrices (TILES).
 template <class T, int MODE, bool E5M2>
 __global__ void __launch_bounds__(kQuantThreads, sizeof(T) == 4 ? 2 : 3)
 fp8_quantize_tile_kernel(const QuantParams p)
@@ -329,9 +329,11 @@ fp8_quantize_tile_kernel(const QuantParams p)
     const int64_t rb = blockIdx.y;
     int64_t row0 = rb * 128, row_end = p.rows;                         // rows row0 .. row_end - 1 of the input
     const int64_t out0 = row0;                                         // first row of the copy
+    bool rows_only = false;                                            // rows of no group: they have a row copy alone
     if (MODE != 4 && p.offsets != nullptr) {
         // The group that holds block rb of the padded copy.  The offsets are clamped as the products clamp them: to [0, rows], each at
-        // least as large as those before it.  Then the groups' blocks fit the copy, whatever the caller's values.
+        // least as large as those before it.  Then the groups' blocks fit the copy, whatever the caller's values.  Blocks behind those of the
+        // groups take the rows of no group, those ahead of the first group's and then those from the last offset on.
         if (warp == 0) {
             int32_t carry = 0, found = 0, first = 0, end = 0, last = 0;
             const int32_t limit = static_cast<int32_t>(p.rows);
@@ -364,10 +366,17 @@ fp8_quantize_tile_kernel(const QuantParams p)
                 }
                 carry += __shfl_sync(0xffffffffu, sum, 31);
             }
+            if (MODE == 3 && !found) {
+                const int32_t ahead = min(max(p.offsets[0], 0), limit), n = (ahead + 127) / 128, i = static_cast<int32_t>(rb) - carry;
+                first = i < n ? i * 128 : last + (i - n) * 128;
+                end = i < n ? ahead : limit;
+                found = first < end ? 2 : 0;
+            }
             if (lane == 0) { s_place[0] = found; s_place[1] = first; s_place[2] = end; }
         }
         __syncthreads();
-        if (!s_place[0]) return;                                       // beyond the last group's rows (block-uniform)
+        if (!s_place[0]) return;                                       // beyond the last rows (block-uniform)
+        rows_only = s_place[0] == 2;
         row0 = s_place[1];
         row_end = s_place[2];
     }
@@ -465,6 +474,7 @@ fp8_quantize_tile_kernel(const QuantParams p)
             if constexpr (sizeof(T) == 2) forget_conversions(raw[i]);
         }
     }
+    if (MODE == 3 && rows_only) return;
     if (MODE == 4) {
         float m = 0.0f;
 #pragma unroll

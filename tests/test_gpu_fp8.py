@@ -500,6 +500,31 @@ def test_quantize_offsets_out_of_range_stay_inside(ctx, case, both):
     assert bool((wide[at:] == 0x55).all()) and bool((wide[:, C:] == 0x55).all()) and bool((wide_s[at // 128:] == -1.0).all())
 
 
+@pytest.mark.parametrize("offsets", [[0, 30, 30, 170], [200, 330], [5, 5], [300, 300, 300], [0, 0], [129, 128, 131]], ids=str)
+@pytest.mark.parametrize("gathered", [False, True], ids=["plain", "gathered"])
+def test_quantize_both_makes_every_row(ctx, offsets, gathered):
+    """Rows of no group -- ahead of the first one's, from the last offset on -- have their row copy as quantize_rows makes it."""
+    M, C = 300, 200
+    g = rng("every row", offsets)
+    x = torch.randn(M, C, generator=g, device="cuda")
+    rows = torch.randint(-1, M + 1, (M,), generator=g, device="cuda", dtype=torch.int32) if gathered else None
+    off = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    E = len(offsets) - 1
+    q, s = fp8.empty_rows(M, C)
+    want_q, want_s = fp8.empty_rows(M, C)
+    c, sc = fp8.empty_cols(M, C, E)
+    want_c, want_sc = fp8.empty_cols(M, C, E)
+    for t in (q, c, want_c):
+        t.view(torch.uint8)[:] = 0x55
+    for t in (s, sc, want_sc):
+        t.fill_(-1.0)
+    fp8.quantize_both(ctx, x, q, s, c, sc, rows=rows, offsets=off)
+    fp8.quantize_rows(ctx, x, want_q, want_s, rows=rows)
+    fp8.quantize_cols(ctx, x, want_c, want_sc, rows=rows, offsets=off)
+    assert torch.equal(q.view(torch.uint8), want_q.view(torch.uint8)) and torch.equal(s, want_s)
+    assert torch.equal(c.view(torch.uint8), want_c.view(torch.uint8)) and torch.equal(sc, want_sc)
+
+
 # ---- the layer as a whole ---------------------------------------------------------------------------------------
 
 def test_gradients_against_differences(ctx):
