@@ -446,6 +446,12 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                 if (++s == p.stages) { s = 0; ph ^= 1u; }
             }
         }
+        // Every commit that signals this CTA's stage barriers (the pair's leader signals both CTAs') arrives before the CTA may leave:
+        // the promoting warps wait for the accumulators' barriers only.
+        for (int i = 0; ok && i < p.stages; ++i) {
+            ok = mbar_wait_warp(bar_empty + 8 * s, ph ^ 1u, ctl, status_code(kRoleFp8Load, 1, s));
+            if (++s == p.stages) { s = 0; ph ^= 1u; }
+        }
     } else if (warp == 1) {
         // ===== MMA issuer =====
         if constexpr (CG == 2) regs_lower<56>();

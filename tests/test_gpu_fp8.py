@@ -312,6 +312,29 @@ def test_streams_and_repeats_give_the_same_bits(ctx):
     plan.close()
 
 
+def test_short_launches_one_after_another(ctx):
+    """Tiles of one block, pairs and single CTAs in turn on the same SMs, with nothing between the launches: each CTA leaves while its last
+    commits are recent.  Exact integers."""
+    M, N, K = 1100, 1300, 128
+    g = rng("short")
+    fa, fb = (torch.randint(-2, 3, s, generator=g, device="cuda").float() for s in ((M, K), (N, K)))
+    a, b = fp8.empty_rows(M, K)[0], fp8.empty_rows(N, K)[0]
+    a.copy_(fa), b.copy_(fb)
+    sa, sb = torch.full((M, 1), 0.5, device="cuda"), torch.full((blocks(N), 1), 0.5, device="cuda")
+    want = fa @ fb.t() * 0.25
+    plans = []
+    for config in ((2, 256, 1), (1, 16, 1), (1, 128, 1)):
+        plans.append(fp8.Plan(ctx, M, N, K, out_dtype=torch.float32))
+        plans[-1].set_config(*config)
+    outs = [torch.full((M, N), float("nan"), device="cuda") for _ in range(60)]
+    for i, out in enumerate(outs):
+        plans[i % 3].run(a, sa, b, sb, out)
+    assert ctx.last_device_status()[0] == hgemm.OK
+    assert all(torch.equal(out, want) for out in outs)
+    for plan in plans:
+        plan.close()
+
+
 # ---- quantisation --------------------------------------------------------------------------------------------
 
 def check_quantized(q, s, x, rows, cols, name, pow2, what):
