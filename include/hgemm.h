@@ -358,9 +358,11 @@ int32_t hgemm_plan_launches_per_run(const hgemm_plan_t *plan);
  * plan is usable afterwards.
  *
  * hgemm_ctx_last_device_status(ctx, code): the same over the whole context -- its own word (written
- * by hgemm_debug_timeout_probe) and the word of every live plan; *code receives the first non-zero
- * one (the context's, then plans in creation order), all are cleared, and every plan whose word was
- * set has its counters restarted. */
+ * by hgemm_debug_timeout_probe) and the words of all plans, those destroyed since the last such call
+ * included; *code receives the first non-zero one (the context's, then live plans in creation order,
+ * then the others), all are cleared, and every plan whose word was set has its counters restarted.
+ * Words are used again: a new plan may find in its own the event of a destroyed one that nobody asked
+ * for. */
 hgemm_status_t hgemm_last_device_status(hgemm_plan_t *plan, uint32_t *code);
 hgemm_status_t hgemm_ctx_last_device_status(hgemm_ctx_t *ctx, uint32_t *code);
 

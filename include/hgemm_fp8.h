@@ -92,6 +92,12 @@ hgemm_status_t hgemm_fp8_plan_destroy(hgemm_fp8_plan_t *plan);
 hgemm_status_t hgemm_fp8_run(hgemm_fp8_plan_t *plan, const void *A, int64_t lda, const float *a_scales, const void *B, int64_t ldb,
                              const float *b_scales, void *C, int64_t ldc, const int32_t *offsets, int32_t accumulate, void *stream);
 
+/* As hgemm_last_device_status, for this plan: whether a bounded wait of its launches ran out.  A plan may be destroyed while its
+ * launches are under way; what they report then shows in hgemm_ctx_last_device_status. */
+hgemm_status_t hgemm_fp8_last_device_status(hgemm_fp8_plan_t *plan, uint32_t *code);
+/* Test hook: hgemm_debug_timeout_probe, reporting to this plan's status word. */
+hgemm_status_t hgemm_fp8_debug_timeout_probe(hgemm_fp8_plan_t *plan, void *stream);
+
 /* How a plan runs: tile (block_p x block_q: rows of the kernel's two operands), whether the operands are swapped, CTAs
  * that share one tile's contraction, and CTAs per tile.  hgemm_fp8_plan_set_config takes what hgemm_fp8_plan_get_config
  * gives, or another combination that the plan's product has kernels for (HGEMM_ERR_UNSUPPORTED otherwise). */

@@ -340,6 +340,20 @@ hgemm_status_t hgemm_fp8_plan_destroy(hgemm_fp8_plan_t *plan)
     return HGEMM_OK;
 }
 
+hgemm_status_t hgemm_fp8_last_device_status(hgemm_fp8_plan_t *plan, uint32_t *code)
+{
+    if (!plan || !code) return HGEMM_ERR_INVALID_ARG;
+    uint32_t v = 0;
+    const hgemm_status_t st = hgemm_host::take_status_word(plan->ctx, plan->status_slot, &v);
+    if (st != HGEMM_ERR_CUDA) *code = v;
+    return st;
+}
+
+hgemm_status_t hgemm_fp8_debug_timeout_probe(hgemm_fp8_plan_t *plan, void *stream)
+{
+    return plan ? hgemm_host::launch_timeout_probe(plan->ctx, plan->status_slot, stream) : HGEMM_ERR_INVALID_ARG;
+}
+
 hgemm_status_t hgemm_fp8_plan_get_config(const hgemm_fp8_plan_t *plan, hgemm_fp8_config_t *out)
 {
     if (!plan || !out) return HGEMM_ERR_INVALID_ARG;

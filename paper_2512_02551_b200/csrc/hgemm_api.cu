@@ -356,7 +356,33 @@ bool encode_3d_ksub(hgemm_ctx_s *ctx, CUtensorMap *map, const void *base, uint64
     return true;
 }
 
+hgemm_status_t status_of(uint32_t word)
+{
+    return word == 0 ? HGEMM_OK : (word >> 24) == hgemm_dev::kRoleCheck ? HGEMM_ERR_CHECK : HGEMM_ERR_TIMEOUT;
+}
+
 } // namespace
+
+namespace hgemm_host {
+
+hgemm_status_t take_status_word(hgemm_ctx_s *ctx, int slot, uint32_t *code)
+{
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e != cudaSuccess) return cuda_fail(ctx, e);
+    uint32_t *word = ctx->d_status + slot;
+    e = cudaMemcpy(code, word, 4, cudaMemcpyDeviceToHost);
+    if (e == cudaSuccess && *code != 0) e = cudaMemset(word, 0, 4);
+    return e == cudaSuccess ? status_of(*code) : cuda_fail(ctx, e);
+}
+
+hgemm_status_t launch_timeout_probe(hgemm_ctx_s *ctx, int slot, void *stream)
+{
+    hgemm_dev::hgemm_timeout_probe_kernel<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>(ctx->d_status + slot, ctx->wait_budget);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? HGEMM_OK : cuda_fail(ctx, e);
+}
+
+} // namespace hgemm_host
 
 extern "C" {
 
@@ -1006,21 +1032,15 @@ static hgemm_status_t reset_counters(hgemm_plan_s *pl)
 hgemm_status_t hgemm_last_device_status(hgemm_plan_t *plan, uint32_t *code)
 {
     if (!plan || !code) return HGEMM_ERR_INVALID_ARG;
-    hgemm_ctx_s *ctx = plan->ctx;
-    cudaError_t e = cudaDeviceSynchronize();
-    if (e != cudaSuccess) return cuda_fail(ctx, e);
     uint32_t v = 0;
-    uint32_t *word = ctx->d_status + plan->status_slot;
-    e = cudaMemcpy(&v, word, 4, cudaMemcpyDeviceToHost);
-    if (e != cudaSuccess) return cuda_fail(ctx, e);
+    const hgemm_status_t st = hgemm_host::take_status_word(plan->ctx, plan->status_slot, &v);
+    if (st == HGEMM_ERR_CUDA) return st;
     if (v != 0) {
-        e = cudaMemset(word, 0, 4);
-        if (e != cudaSuccess) return cuda_fail(ctx, e);
         const hgemm_status_t s = reset_counters(plan);
         if (s != HGEMM_OK) return s;
     }
     *code = v;
-    return v == 0 ? HGEMM_OK : (v >> 24) == hgemm_dev::kRoleCheck ? HGEMM_ERR_CHECK : HGEMM_ERR_TIMEOUT;
+    return st;
 }
 
 hgemm_status_t hgemm_ctx_last_device_status(hgemm_ctx_t *ctx, uint32_t *code)
@@ -1031,7 +1051,7 @@ hgemm_status_t hgemm_ctx_last_device_status(hgemm_ctx_t *ctx, uint32_t *code)
     std::vector<uint32_t> words(size_t(kStatusSlots), 0u);
     e = cudaMemcpy(words.data(), ctx->d_status, words.size() * sizeof(uint32_t), cudaMemcpyDeviceToHost);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
-    uint32_t v = words[0];                                   // the context's own word first, then the plans' in creation order
+    uint32_t v = words[0];                                   // the context's own word first, then the plans' in creation order, then closed plans'
     bool any = v != 0;
     for (hgemm_plan_s *pl : ctx->plans) {
         const uint32_t w = words[size_t(pl->status_slot)];
@@ -1046,12 +1066,16 @@ hgemm_status_t hgemm_ctx_last_device_status(hgemm_ctx_t *ctx, uint32_t *code)
         any = any || w != 0;
         if (v == 0) v = w;
     }
+    for (const uint32_t w : words) {                         // words whose plan was destroyed before anyone asked
+        any = any || w != 0;
+        if (v == 0) v = w;
+    }
     if (any) {
         e = cudaMemset(ctx->d_status, 0, words.size() * sizeof(uint32_t));
         if (e != cudaSuccess) return cuda_fail(ctx, e);
     }
     *code = v;
-    return v == 0 ? HGEMM_OK : (v >> 24) == hgemm_dev::kRoleCheck ? HGEMM_ERR_CHECK : HGEMM_ERR_TIMEOUT;
+    return status_of(v);
 }
 
 hgemm_status_t hgemm_debug_fail_allocs(hgemm_ctx_t *ctx, int32_t after, int32_t count)
@@ -1099,10 +1123,7 @@ hgemm_status_t hgemm_set_dependent_launch(hgemm_ctx_t *ctx, int32_t enabled)
 hgemm_status_t hgemm_debug_timeout_probe(hgemm_ctx_t *ctx, void *stream)
 {
     if (!ctx) return HGEMM_ERR_INVALID_ARG;
-    hgemm_dev::hgemm_timeout_probe_kernel<<<1, 32, 0, static_cast<cudaStream_t>(stream)>>>(ctx->d_status, ctx->wait_budget);   // slot 0
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_fail(ctx, e);
-    return HGEMM_OK;
+    return hgemm_host::launch_timeout_probe(ctx, 0, stream);
 }
 
 int32_t hgemm_build_is_checked(void)

@@ -39,6 +39,10 @@ struct hgemm_ctx_s {
 
 namespace hgemm_host {
 int status_slot_of(const hgemm_fp8_plan_s *plan);   // the plan's word in the context's status array
+// Synchronises the device, reads a status word and clears it: HGEMM_OK, or what the word stands for.
+hgemm_status_t take_status_word(hgemm_ctx_s *ctx, int slot, uint32_t *code);
+// One small kernel whose only wait is on a barrier that nothing signals; it reports to the slot.
+hgemm_status_t launch_timeout_probe(hgemm_ctx_s *ctx, int slot, void *stream);
 }
 
 inline hgemm_status_t cuda_fail(hgemm_ctx_s *ctx, cudaError_t e)

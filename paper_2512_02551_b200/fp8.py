@@ -26,7 +26,7 @@ _FP8 = (torch.float8_e4m3fn, torch.float8_e5m2)
 
 # every symbol include/hgemm_fp8.h declares
 EXPORTS = ["hgemm_fp8_quantize", "hgemm_fp8_padded_rows", "hgemm_fp8_plan", "hgemm_fp8_plan_destroy", "hgemm_fp8_run", "hgemm_fp8_plan_get_config",
-           "hgemm_fp8_plan_set_config", "hgemm_fp8_planned_config"]
+           "hgemm_fp8_plan_set_config", "hgemm_fp8_planned_config", "hgemm_fp8_last_device_status", "hgemm_fp8_debug_timeout_probe"]
 
 
 class Quantize(ctypes.Structure):
@@ -63,6 +63,8 @@ def lib() -> ctypes.CDLL:
             "hgemm_fp8_run": (i32, [p, p, i64, p, p, i64, p, p, i64, p, i32, p]),
             "hgemm_fp8_plan_get_config": (i32, [p, cfgp]),
             "hgemm_fp8_plan_set_config": (i32, [p, cfgp]),
+            "hgemm_fp8_last_device_status": (i32, [p, ctypes.POINTER(ctypes.c_uint32)]),
+            "hgemm_fp8_debug_timeout_probe": (i32, [p, p]),
             "hgemm_fp8_planned_config": (i32, [i32, i64, i64, i64, i32, i32, cfgp]),
         }
         for name, (res, args) in sig.items():
@@ -274,6 +276,15 @@ class Plan:
     def set_config(self, cta_group: int, block_q: int, split_k: int = 1) -> None:
         c = Config(cta_group, block_q, split_k, 0)
         _check(lib().hgemm_fp8_plan_set_config(self._h, ctypes.byref(c)), f"hgemm_fp8_plan_set_config({c.as_dict()})")
+
+    def last_device_status(self) -> tuple[int, int]:
+        """``hgemm_fp8_last_device_status``: (status, code) of this plan's own status word; synchronises the device."""
+        code = ctypes.c_uint32(0)
+        st = lib().hgemm_fp8_last_device_status(self._h, ctypes.byref(code))
+        return int(st), int(code.value)
+
+    def debug_timeout_probe(self, stream: int = 0) -> None:
+        _check(lib().hgemm_fp8_debug_timeout_probe(self._h, ctypes.c_void_p(stream)), "hgemm_fp8_debug_timeout_probe")
 
     def run(self, a, a_scales, b, b_scales, out, offsets=None, accumulate: bool = False, stream=None) -> None:
         ta, tb, tc = self._types

@@ -335,6 +335,29 @@ def test_short_launches_one_after_another(ctx):
         plan.close()
 
 
+def test_status_words(ctx):
+    """A wait that ran out is reported by the plan whose launch it was, by the context, and by the context too when the plan is gone
+    before anyone asks."""
+    one, two = fp8.Plan(ctx, 64, 64, 64), fp8.Plan(ctx, 64, 64, 64)
+    ctx.set_wait_budget(2_000_000)                      # about a millisecond
+    try:
+        one.debug_timeout_probe()
+        assert two.last_device_status() == (hgemm.OK, 0)
+        st, code = one.last_device_status()
+        assert st == hgemm.ERR_TIMEOUT and (code >> 24) == 4
+        assert one.last_device_status() == (hgemm.OK, 0) and ctx.last_device_status() == (hgemm.OK, 0)
+        two.debug_timeout_probe()
+        assert ctx.last_device_status()[0] == hgemm.ERR_TIMEOUT and two.last_device_status() == (hgemm.OK, 0)
+        two.debug_timeout_probe()
+        two.close()
+        st, code = ctx.last_device_status()
+        assert st == hgemm.ERR_TIMEOUT and (code >> 24) == 4
+        assert ctx.last_device_status() == (hgemm.OK, 0)
+    finally:
+        ctx.set_wait_budget(2_000_000_000)
+    one.close()
+
+
 # ---- quantisation --------------------------------------------------------------------------------------------
 
 def check_quantized(q, s, x, rows, cols, name, pow2, what):
