@@ -270,21 +270,25 @@ class Plan:
     @property
     def config(self) -> Config:
         c = Config()
-        _check(lib().hgemm_fp8_plan_get_config(self._h, ctypes.byref(c)), "hgemm_fp8_plan_get_config")
+        _check(lib().hgemm_fp8_plan_get_config(self._open(), ctypes.byref(c)), "hgemm_fp8_plan_get_config")
         return c
 
     def set_config(self, cta_group: int, block_q: int, split_k: int = 1) -> None:
         c = Config(cta_group, block_q, split_k, 0)
-        _check(lib().hgemm_fp8_plan_set_config(self._h, ctypes.byref(c)), f"hgemm_fp8_plan_set_config({c.as_dict()})")
+        _check(lib().hgemm_fp8_plan_set_config(self._open(), ctypes.byref(c)), f"hgemm_fp8_plan_set_config({c.as_dict()})")
+
+    def _open(self):
+        """The library's handle; none once the plan or its context is closed (the library then refuses the call)."""
+        return self._h if self.ctx._h else None
 
     def last_device_status(self) -> tuple[int, int]:
         """``hgemm_fp8_last_device_status``: (status, code) of this plan's own status word; synchronises the device."""
         code = ctypes.c_uint32(0)
-        st = lib().hgemm_fp8_last_device_status(self._h, ctypes.byref(code))
+        st = lib().hgemm_fp8_last_device_status(self._open(), ctypes.byref(code))
         return int(st), int(code.value)
 
     def debug_timeout_probe(self, stream: int = 0) -> None:
-        _check(lib().hgemm_fp8_debug_timeout_probe(self._h, ctypes.c_void_p(stream)), "hgemm_fp8_debug_timeout_probe")
+        _check(lib().hgemm_fp8_debug_timeout_probe(self._open(), ctypes.c_void_p(stream)), "hgemm_fp8_debug_timeout_probe")
 
     def run(self, a, a_scales, b, b_scales, out, offsets=None, accumulate: bool = False, stream=None) -> None:
         ta, tb, tc = self._types
@@ -297,7 +301,7 @@ class Plan:
             off = _dense(offsets, (self.groups + 1,), torch.int32, "offsets")
         elif offsets is not None:
             raise ValueError("offsets belong to a plan with groups")
-        st = self._run(self._h, a.data_ptr(), lda, sa, b.data_ptr(), ldb, sb, out.data_ptr(), ldc, off, 1 if accumulate else 0, _stream(self.ctx, stream))
+        st = self._run(self._open(), a.data_ptr(), lda, sa, b.data_ptr(), ldb, sb, out.data_ptr(), ldc, off, 1 if accumulate else 0, _stream(self.ctx, stream))
         if st != OK:
             raise HgemmError(st, f"hgemm_fp8_run({self.form}{self.shape}, groups={self.groups})")
 

@@ -663,6 +663,25 @@ def test_refusals(ctx):
     assert bool((out == 7.0).all())
 
 
+def test_closed_plans_and_contexts_are_refused():
+    """A plan that is closed, or whose context is, raises in every call."""
+    with hgemm.Context(0) as c:
+        plans = [fp8.Plan(c, 16, 64, 128), fp8.Plan(c, 16, 64, 128)]
+        plans[0].close()
+    a, sa = fp8.empty_rows(16, 128)
+    w, sw = fp8.empty_tiles(64, 128)
+    y = torch.full((16, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    for plan in plans:
+        for call in (lambda: plan.run(a, sa, w, sw, y), lambda: plan.config, lambda: plan.set_config(1, 16, 1), plan.debug_timeout_probe):
+            with pytest.raises(hgemm.HgemmError):
+                call()
+        assert plan.last_device_status()[0] == hgemm.ERR_INVALID_ARG
+        plan.close()
+    with pytest.raises(hgemm.HgemmError):
+        fp8.quantize_rows(c, torch.zeros(16, 128, device="cuda"), a, sa)
+    assert bool((y == 7.0).all())
+
+
 # ---- the operators together ---------------------------------------------------------------------------------------------
 
 def test_layer_of_experts(ctx):
