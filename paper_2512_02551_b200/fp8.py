@@ -241,7 +241,9 @@ class Plan:
     form "forward": run(x (M,K), row scales, w (N,K), tile scales, y (M,N)); "input_grad": run(dy (M,N), row scales, w, tile
     scales, dx (M,K)); "weight_grad": run(dy (M,N), column scales, x (M,K), column scales, dw (N,K)).  groups > 0: one
     weight per group -- w (groups,N,K), dw (groups,N,K), ``offsets`` with every run, the weight gradient's operands
-    laid out per group."""
+    laid out per group.
+
+    Each plan holds one of the context's 4095 status words until it is closed or dropped; a program keeps its plans."""
 
     def __init__(self, ctx, M: int, N: int, K: int, form: str = "forward", groups: int = 0, a_dtype=torch.float8_e4m3fn, b_dtype=torch.float8_e4m3fn,
                  out_dtype=torch.bfloat16):
@@ -253,6 +255,7 @@ class Plan:
         self.shape = (int(M), int(N), int(K))
         self.form, self.groups = form, int(groups)
         self._h = ctypes.c_void_p()
+        self._run, self._destroy = lib().hgemm_fp8_run, lib().hgemm_fp8_plan_destroy
         _check(lib().hgemm_fp8_plan(ctx._h, FORMS[form], *self.shape, self.groups, TYPES[a_dtype], TYPES[b_dtype], TYPES[out_dtype], ctypes.byref(self._h)),
                f"hgemm_fp8_plan({form},{M},{N},{K},groups={groups})")
         M, N, K = self.shape
@@ -265,7 +268,6 @@ class Plan:
             sa, b, sb = (M, _blocks(a[1])), (*g, N, K), (*g, _blocks(N), _blocks(K))
         self._a, self._sa, self._b, self._sb, self._c = (torch.Size(v) for v in (a, sa, b, sb, c))
         self._types = ((a_dtype,), (b_dtype,), (out_dtype,))
-        self._run = lib().hgemm_fp8_run
 
     @property
     def config(self) -> Config:
@@ -307,8 +309,12 @@ class Plan:
 
     def close(self) -> None:
         if self._h and self.ctx._h:
-            lib().hgemm_fp8_plan_destroy(self._h)
+            self._destroy(self._h)
         self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        if getattr(self, "_h", None):                  # a plan that was made
+            self.close()
 
     def __enter__(self):
         return self

@@ -17,7 +17,8 @@ from . import fp8, hgemm, routing
 
 
 class ExpertLayer:
-    """y[t] = sum over the chosen experts e of w[t,e] * silu(x[t] W1[e]^T) W2[e]^T, with buffers and plans for one number of tokens."""
+    """y[t] = sum over the chosen experts e of w[t,e] * silu(x[t] W1[e]^T) W2[e]^T, with buffers and plans for one number of tokens (``close``
+    gives the plans back)."""
 
     def __init__(self, ctx, tokens: int, hidden: int, inner: int, experts: int, top_k: int, seed: int = 0):
         g = torch.Generator(device="cuda").manual_seed(seed)
@@ -44,6 +45,17 @@ class ExpertLayer:
         # 8-bit copies by rows and, per expert, by columns
         self.x8, self.a8, self.dy8, self.dh8 = (fp8.empty_rows(R, n) for n in (H, I, H, I))
         self.x8c, self.a8c, self.dy8c, self.dh8c = (fp8.empty_cols(R, n, E) for n in (H, I, H, I))
+
+    def close(self) -> None:
+        """Gives the plans back to the context."""
+        for plan in (self.router_plan, self.up, self.down, self.up_dx, self.down_dx, self.up_dw, self.down_dw):
+            plan.close()
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
 
     def refresh_weights(self) -> None:
         """After a change of the weights: their 8-bit tiles."""
@@ -90,8 +102,7 @@ def main() -> None:
     for name, value in (("tokens", 4096), ("hidden", 2048), ("inner", 1024), ("experts", 32), ("top-k", 4), ("iters", 5)):
         ap.add_argument(f"--{name}", type=int, default=value)
     args = ap.parse_args()
-    with hgemm.Context(0) as ctx:
-        layer = ExpertLayer(ctx, args.tokens, args.hidden, args.inner, args.experts, args.top_k)
+    with hgemm.Context(0) as ctx, ExpertLayer(ctx, args.tokens, args.hidden, args.inner, args.experts, args.top_k) as layer:
         x = torch.randn(args.tokens, args.hidden, device="cuda").half()
         dy = torch.randn(args.tokens, args.hidden, device="cuda")
         for _ in range(2):

@@ -358,6 +358,23 @@ def test_status_words(ctx):
     one.close()
 
 
+def test_dropped_plans_give_their_place_back():
+    """A context has room for 4095 plans at once; plans and layers that are dropped or closed make room for others."""
+    from paper_2512_02551_b200.run_experts import ExpertLayer
+    with hgemm.Context(0) as c:
+        for i in range(5000):
+            fp8.Plan(c, 1 + i % 100, 64, 64)
+        held = [fp8.Plan(c, 1, 64, 64) for _ in range(4095 - 7)]
+        for _ in range(2):
+            with ExpertLayer(c, 8, 128, 128, 2, 1) as layer:              # seven plans
+                layer.forward(torch.zeros(8, 128, dtype=torch.float16, device="cuda"))
+                with pytest.raises(hgemm.HgemmError):
+                    fp8.Plan(c, 1, 64, 64)
+        assert c.last_device_status() == (hgemm.OK, 0)
+        del held
+        c.plan(256, 256, 256).close()
+
+
 # ---- quantisation --------------------------------------------------------------------------------------------
 
 def check_quantized(q, s, x, rows, cols, name, pow2, what):
