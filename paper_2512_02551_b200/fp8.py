@@ -143,6 +143,10 @@ def _ld(t, shape, dtypes, name):
         return st[0]
     if st[-1] != 1 and shape[-1] > 1:
         raise ValueError(f"{name}: the elements of a row must be consecutive")
+    if len(shape) == 3 and shape[1] == 1 and shape[0] > 1:      # matrices of one row: the next row is the next matrix's
+        if st[0] < shape[2]:
+            raise ValueError(f"{name}: strides {st} are not those of row-major matrices one after the other")
+        return st[0]
     # one row: its distance to a next one is free, any that the library accepts
     ld = max(st[-2], shape[-1]) if shape[-2] > 1 else -(-max(st[-2], shape[-1]) // 16) * 16
     if (shape[-2] > 1 and st[-2] < shape[-1]) or (len(shape) == 3 and shape[0] > 1 and st[0] != shape[1] * ld):

@@ -254,6 +254,14 @@ def test_experts_weight_gradient(ctx, counts, config):
     grouped_case(ctx, "weight_grad", COUNTS[counts], 144, 272, config, OUTS[len(counts) % 3])
 
 
+@pytest.mark.parametrize("form", ["forward", "input_grad", "weight_grad"])
+@pytest.mark.parametrize("K", [1, 65, 100, 256])
+def test_experts_of_one_output(ctx, form, K):
+    """Weights of one row: stacks whose matrices are rows, of any width."""
+    for out_dtype in OUTS:
+        grouped_case(ctx, form, [3, 0, 130, 1], 1, K, None, out_dtype)
+
+
 def test_experts_offsets_out_of_range_stay_inside(ctx):
     """Offsets beyond the rows, negative or falling are clamped: nothing outside the operands is touched."""
     M, N, K, E = 40, 64, 128, 4
@@ -521,6 +529,20 @@ def test_quantize_per_group(ctx, counts):
             assert torch.equal(c[at:at + up].contiguous().view(torch.uint8), c1[at:at + up].contiguous().view(torch.uint8))
         at, start = at + up, start + n
     assert bool((c.view(torch.uint8)[at:] == 0x55).all()) and bool((sc[at // 128:] == -1.0).all())
+
+
+def test_quantize_tiles_of_one_row(ctx):
+    """Stacks of one-row matrices, dense or taken out of a larger stack."""
+    g = rng("one row")
+    for C in (1, 65, 128, 300):
+        wide = torch.randn(4, 5, C, generator=g, device="cuda")
+        for x in (torch.randn(4, 1, C, generator=g, device="cuda"), wide[:, 2:3], wide[1:2, 2:3]):
+            q, s = fp8.empty_tiles(*x.shape)
+            fp8.quantize_tiles(ctx, x, q, s)
+            for e in range(x.shape[0]):
+                check_quantized(q[e], s[e], ref.f64(x[e]), 128, 128, "e4m3", False, f"matrix {e} of {tuple(x.shape)}")
+    with pytest.raises(ValueError):
+        fp8.quantize_tiles(ctx, wide[:1, :1].expand(4, 1, 300), *fp8.empty_tiles(4, 1, 300))
 
 
 FALLING = {
