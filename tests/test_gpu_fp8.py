@@ -545,6 +545,99 @@ def test_quantize_tiles_of_one_row(ctx):
         fp8.quantize_tiles(ctx, wide[:1, :1].expand(4, 1, 300), *fp8.empty_tiles(4, 1, 300))
 
 
+def definition32(x, name, pow2, rows, cols):
+    """Values and scales by the header's definition, every step one correctly rounded 32-bit operation (tensors divide tensors: a number as
+    the divisor or the dividend becomes a product with a reciprocal)."""
+    R, C = x.shape
+    x = x.float()
+    b = torch.nn.functional.pad(x, (0, -C % cols, 0, -R % rows)).view(blocks(R) if rows > 1 else R, rows, -(-C // cols), cols)
+    amax = torch.where(torch.isfinite(b), b.abs(), 0.0).amax((1, 3), keepdim=True)
+    some = amax >= 2.0 ** -100
+    a, top = torch.where(some, amax, 1.0), torch.full_like(amax, ref.FP8_MAX[name])
+    scale = a / top
+    factor = top / a
+    if pow2:
+        mantissa, exponent = torch.frexp(scale)
+        exponent = exponent - (mantissa == 0.5).int()
+        scale, factor = torch.ldexp(torch.ones_like(scale), exponent), torch.ldexp(torch.ones_like(scale), -exponent)
+    v = (b * torch.where(some, factor, 0.0)).clamp(-ref.FP8_MAX[name], ref.FP8_MAX[name])
+    v = torch.where(torch.isfinite(b), v, torch.nan).to(ref.FP8[name])
+    bits = v.view(torch.uint8).reshape(-(-R // rows) * rows, -(-C // cols) * cols)[:R, :C]
+    return bits, torch.where(some, scale, 1.0)[:, 0, :, 0]
+
+
+def same_as_definition(q, s, x, name, pow2, rows, cols, what):
+    bits, scale = definition32(x, name, pow2, rows, cols)
+    got = q.view(torch.uint8)
+    nan = torch.isnan(q.float())
+    assert torch.equal(nan, ~torch.isfinite(x.float())), what
+    off = (got != bits) & ~nan
+    assert not bool(off.any()), f"{what}: {int(off.sum())} of {off.numel()} values, first at {off.nonzero()[0].tolist()}"
+    assert torch.equal(s, scale), what
+
+
+@pytest.mark.parametrize("dtype", OUTS, ids=str)
+@pytest.mark.parametrize("name", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("pow2", [False, True])
+def test_quantize_bit_for_bit(ctx, dtype, name, pow2):
+    """All forms against the definition in 32 bits: the same bits."""
+    for R, C in ((24, 4096), (700, 520)):
+        x = awkward(rng("bits", R, C), R, C, dtype)
+        q, s = fp8.empty_rows(R, C, ref.FP8[name])
+        c, sc = fp8.empty_cols(R, C, dtype=ref.FP8[name])
+        fp8.quantize_both(ctx, x, q, s, c, sc, pow2=pow2)
+        same_as_definition(q, s, x, name, pow2, 1, 128, "rows with columns")
+        same_as_definition(c, sc, x, name, pow2, 128, 1, "columns")
+        fp8.quantize_rows(ctx, x, q, s, pow2=pow2)
+        same_as_definition(q, s, x, name, pow2, 1, 128, "rows")
+        t, st = fp8.empty_tiles(R, C, dtype=ref.FP8[name])
+        fp8.quantize_tiles(ctx, x, t, st, pow2=pow2)
+        same_as_definition(t, st, x, name, pow2, 128, 128, "tiles")
+
+
+# rows, columns, extra elements between rows, shift of the base, gathered: each with more blocks than the threshold from which a lane
+# has four of them in flight (1024 a multiprocessor: 151552)
+MANY = {
+    "dense, last group partly filled": (50523, 384, 0, 0, False),
+    "dense, long rows": (1187, 16384, 0, 0, False),
+    "groups straddle rows": (19001, 1000, 0, 0, False),
+    "more than a group a row, ragged": (7601, 2469, 3, 0, False),
+    "unaligned": (7601, 2469, 0, 1, False),
+    "whole rows apart": (8000, 2432, 8, 8, False),
+    "one block a row": (151777, 100, 4, 0, False),
+    "gathered": (7601, 2469, 3, 0, True),
+    "gathered whole blocks": (9500, 2048, 0, 0, True),
+}
+
+
+@pytest.mark.parametrize("case", list(MANY), ids=str)
+@pytest.mark.parametrize("dtype", OUTS, ids=str)
+@pytest.mark.parametrize("name", ["e4m3", "e5m2"])
+def test_quantize_many_rows(ctx, case, dtype, name):
+    """The row kernels for large inputs, with NaN and infinities in first and last blocks of a warp's sixteen, bit for bit."""
+    R, C, extra, shift, gathered = MANY[case]
+    g = rng("many", case)
+    source = R // 2 if gathered else R
+    base = (torch.randn(source * (C + extra) + shift, generator=g, device="cuda") * 3.0).to(dtype)
+    x = base[shift:].view(source, C + extra)[:, :C]
+    per_row = blocks(C)
+    for b, at, value in ((0, 0, float("inf")), (15, 5, float("nan")), (16, 99, -float("inf")), (31, 64, float("inf")), (source * per_row // 2, 1, float("nan")),
+                         (source * per_row - 1, 7, float("inf")), (source * per_row - 17, 3, -float("inf"))):
+        r, k = divmod(b, per_row)
+        x[r, min(k * 128 + at, C - 1)] = value
+    x[source // 3] = 0.0
+    rows, want = None, x
+    if gathered:
+        rows = torch.randint(0, source, (R,), generator=g, device="cuda", dtype=torch.int32)
+        rows[:3], rows[-1], rows[100::977] = torch.tensor([0, -1, source]), source - 1, source + 5
+        inside = (rows >= 0) & (rows < source)
+        want = torch.where(inside.unsqueeze(1), x[rows.clamp(0, source - 1).long()], torch.zeros((), dtype=dtype, device="cuda"))
+    q, s = fp8.empty_rows(R, C, ref.FP8[name])
+    assert R * per_row >= 1024 * torch.cuda.get_device_properties(0).multi_processor_count
+    fp8.quantize_rows(ctx, x, q, s, rows=rows)
+    same_as_definition(q, s, want, name, False, 1, 128, case)
+
+
 FALLING = {
     "falls and overshoots": (40, [0, 10, 5, 2000000000, 50]),
     "negative": (40, [-5, -1, 20, 10, 40]),
