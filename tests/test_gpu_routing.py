@@ -156,6 +156,29 @@ def test_sort(ctx, count, experts):
     assert np.array_equal(position.cpu().numpy(), pos)
 
 
+@pytest.mark.parametrize("count", [1000, 100003])
+def test_sort_as_many_experts_as_the_library_takes(ctx, count):
+    """1024 experts (a router has 512 at most), one cluster's shared memory nearly full."""
+    experts = 1024
+    g = torch.Generator(device="cuda").manual_seed(count)
+    idx = torch.randint(-1, experts + 1, (count,), generator=g, device="cuda", dtype=torch.int32)
+    offsets = torch.full((experts + 1,), -9, dtype=torch.int32, device="cuda")
+    order, position = (torch.full((count,), -9, dtype=torch.int32, device="cuda") for _ in range(2))
+    L = routing.lib()
+    stream = torch.cuda.current_stream().cuda_stream
+    assert L.hgemm_route_sort(ctx._h, idx.data_ptr(), count, experts, offsets.data_ptr(), order.data_ptr(), position.data_ptr(), stream) == hgemm.OK
+    i = idx.cpu().numpy().astype(np.int64)
+    valid = np.flatnonzero((i >= 0) & (i < experts))
+    want = valid[np.argsort(i[valid], kind="stable")]
+    assert offsets.tolist() == np.concatenate([[0], np.cumsum(np.bincount(i[valid], minlength=experts))]).tolist()
+    got = order.cpu().numpy()
+    assert np.array_equal(got[:len(want)], want) and (got[len(want):] == -1).all()
+    pos = np.full(count, -1)
+    pos[want] = np.arange(len(want))
+    assert np.array_equal(position.cpu().numpy(), pos)
+    assert L.hgemm_route_sort(ctx._h, idx.data_ptr(), count, experts + 1, offsets.data_ptr(), order.data_ptr(), position.data_ptr(), stream) == hgemm.ERR_INVALID_ARG
+
+
 def loss64(l, idx, dw, r):
     s = scores64(l, r["score"])
     w = np.take_along_axis(s, idx, -1)
