@@ -1,7 +1,7 @@
 #!/usr/bin/env python
 """HGEMM benchmark: prints ONE JSON line.
 
-    python bench.py [--gpus N] [--steps K] [--warmup W] [--impl ours|reference] [--no-grid] [--grid-csv PATH]
+    python bench.py [--gpus N] [--steps K] [--warmup W] [--impl ours|reference] [--no-grid] [--grid-csv PATH] [--detail PATH]
 
 A "step" is one pass of the hot path over the square HGEMM sweep (M = N = K in
 {1024, 2048, 4096, 8192}: one plan/launch per shape, fp16 operands uniform in [-1, 1]
@@ -15,8 +15,8 @@ rotate), single calls after idle gaps, and the GPU-side duration of one call of 
 profiler records it, which leaves the host path out --; the memory-bound projection shapes against
 the HBM roofline; one line each for the row-major-B layout, the alpha/beta form and fp16
 accumulators; the roofline of the dominant kernel; the CPU oracle timed on the machine's cores; SM clocks
-sampled during the timed region.  The long per-shape arrays come first in the JSON line and the
-scalars last.
+sampled during the timed region.  The long per-shape arrays (50 KB: every shape of the grid and of the
+projections) are not part of the line; --detail PATH writes them.
 
 Timing follows the paper's listing (section 2.4): synchronise, record an event, launch, record
 an event, synchronise; no side streams.  With N > 1 every rank runs the same sweep on its own
@@ -167,6 +167,14 @@ def run_reference(args) -> None:
 
 # --------------------------------------------------------------------------------------------------
 # our arm
+
+def emit(line: dict, detail: dict, path: str | None) -> None:
+    """The JSON line to stdout; the long arrays, which would make it too long for some readers, to a file if one is named."""
+    if path:
+        with open(path, "w") as f:
+            json.dump(detail, f)
+    print(json.dumps(line), flush=True)
+
 
 def run_ours(args) -> None:
     import torch
@@ -411,11 +419,9 @@ def run_ours(args) -> None:
                "sample": f"first {rows} rows of C for 8192^3 ({rows * 8192 * 8192 / 1e9:.1f} GMAC, {dt:.2f} s wall)"}
 
     if rank == 0:
-        # long arrays first, scalars last: a reader that keeps only the end of the line keeps the figures
         grid_detail = grid.pop("detail") if grid else None
         skinny_shapes = skinny.pop("shapes") if skinny else None
         line = {
-            "skinny_shapes": skinny_shapes, "grid_detail": grid_detail, "per_shape": per_shape,
             "metric": METRIC, "value": value, "unit": "TFLOP/s", "n_gpus": world, "steps": args.steps, "warmup": args.warmup,
             "ms_per_step": ms_per_step, "higher_is_better": True, "scaling": "weak", "vs_baseline": None, "dtype": "f16",
             "data": "synthetic",
@@ -425,12 +431,12 @@ def run_ours(args) -> None:
                                  "durations in per_shape come from a separate pass after it; torch.matmul is timed the same way",
                        "parallelism": "replicas" if world > 1 else "single GPU"},
             "pct_of_spec_peak": 100.0 * value / world / SPEC_TFLOPS,
-            "variants": variants, "skinny": skinny, "grid": grid, "torch_matmul": torch_cmp, "sustained": sustained,
+            "per_shape": per_shape, "variants": variants, "skinny": skinny, "grid": grid, "torch_matmul": torch_cmp, "sustained": sustained,
             "roofline": roofline, "cpu_baseline": cpu, "clocks": clocks,
             "e2e": {"value": e2e_value, "unit": "TFLOP/s", "h2d_bytes_per_step": h2d, "d2h_bytes_per_step": d2h, "steps": e2e_steps},
             "gpu_launches": args.steps * len(SWEEP),
         }
-        print(json.dumps(line), flush=True)
+        emit(line, {"skinny_shapes": skinny_shapes, "grid_detail": grid_detail}, args.detail)
     ctx.close()
     if dist is not None:
         dist.destroy_process_group()
@@ -840,6 +846,7 @@ def main():
     ap.add_argument("--impl", choices=["ours", "reference"], default="ours")
     ap.add_argument("--no-grid", action="store_true", help="skip everything but the timed sweep, torch.matmul beside it and the end-to-end leg")
     ap.add_argument("--grid-csv", metavar="PATH", help="also write the grid's per-shape times to this CSV file")
+    ap.add_argument("--detail", metavar="PATH", help="write the long per-shape arrays of the grid and the projections to this JSON file")
     args = ap.parse_args()
     if args.warmup < 3 and args.impl == "ours":
         args.warmup = 3
