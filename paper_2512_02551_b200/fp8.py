@@ -317,8 +317,9 @@ class Plan:
         self._h = ctypes.c_void_p()
 
     def __del__(self):
-        if getattr(self, "_h", None):                  # a plan that was made
-            self.close()
+        h = getattr(self, "_h", None)                  # none: the plan was never made.  No module's names: at exit they may be gone
+        if h and self.ctx._h:
+            self._destroy(h)
 
     def __enter__(self):
         return self

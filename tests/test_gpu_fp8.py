@@ -383,6 +383,17 @@ def test_dropped_plans_give_their_place_back():
         c.plan(256, 256, 256).close()
 
 
+def test_plans_open_at_exit():
+    """A program that ends with open plans ends without a word on stderr."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = "from paper_2512_02551_b200 import fp8, hgemm\nctx = hgemm.Context(0)\nplan = fp8.Plan(ctx, 16, 64, 128)\nkept = [fp8.Plan(ctx, 16, 64, 128)]\nprint('made')\n"
+    out = subprocess.run([sys.executable, "-c", code], env=dict(os.environ, PYTHONPATH=root), capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and out.stdout == "made\n" and "Exception" not in out.stderr and "Error" not in out.stderr, out.stderr
+
+
 # ---- quantisation --------------------------------------------------------------------------------------------
 
 def check_quantized(q, s, x, rows, cols, name, pow2, what):
