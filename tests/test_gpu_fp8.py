@@ -714,6 +714,86 @@ def test_quantize_both_makes_every_row(ctx, offsets, gathered):
     assert torch.equal(c.view(torch.uint8), want_c.view(torch.uint8)) and torch.equal(sc, want_sc)
 
 
+# ---- more elements than 32 bits count ------------------------------------------------------------------------------
+
+def test_quantize_beyond_32_bits(ctx):
+    """The ends of matrices of more than 2^31 elements: by rows, with columns, gathered from, and as a stack of weights."""
+    R, C = 530048, 4096
+    x = torch.zeros(R, C, dtype=torch.bfloat16, device="cuda")
+    x[-256:] = torch.randn(256, C, generator=rng("large"), device="cuda") * 3.0
+    q, s = fp8.empty_rows(R, C)
+    c, sc = fp8.empty_cols(R, C)
+    fp8.quantize_rows(ctx, x, q, s)
+    same_as_definition(q[-256:], s[-256:], x[-256:], "e4m3", False, 1, 128, "rows")
+    q.view(torch.uint8)[-256:] = 0
+    fp8.quantize_both(ctx, x, q, s, c, sc)
+    same_as_definition(q[-256:], s[-256:], x[-256:], "e4m3", False, 1, 128, "rows with columns")
+    same_as_definition(c[-256:], sc[-2:], x[-256:], "e4m3", False, 128, 1, "columns")
+    rows = torch.arange(R - 256, R, dtype=torch.int32, device="cuda")
+    few = fp8.empty_rows(256, C)
+    fp8.quantize_rows(ctx, x, *few, rows=rows)
+    same_as_definition(*few, x[-256:], "e4m3", False, 1, 128, "gathered")
+    del q, s, c, sc
+    stack = x[:128 * 4096].view(128, 4096, C)
+    stack[-1, -200:] = x[-200:]
+    t, st = fp8.empty_tiles(*stack.shape)
+    fp8.quantize_tiles(ctx, stack, t, st)
+    same_as_definition(t[-1], st[-1], stack[-1], "e4m3", False, 128, 128, "tiles")
+
+
+@pytest.mark.parametrize("config,extra", [((2, 256, 1), 0), ((2, 256, 1), 1), ((1, 128, 1), 0), ((1, 64, 2), 0)], ids=str)
+def test_results_beyond_32_bits(ctx, config, extra):
+    """The last rows of a result of more than 2^31 elements; its other rows keep out of them."""
+    M, N, K = 262500, 8192, 200
+    g = rng("large result")
+    a, b, sa, sb = bytes8(g, (M, K), E4M3), bytes8(g, (N, K), E4M3), scales(g, M, 2), scales(g, blocks(N), 2)
+    out = torch.empty(M, N + extra, dtype=torch.bfloat16, device="cuda")[:, :N]
+    with fp8.Plan(ctx, M, N, K) as plan:
+        plan.set_config(*config)
+        plan.run(a, sa, b, sb, out)
+        assert plan.last_device_status()[0] == hgemm.OK
+    w = ref.values(b, sb, 128, 128)
+    for at in (slice(0, 100), slice(M - 300, M)):
+        ref.check_product(out[at], ref.values(a[at], sa[at], 1, 128), w, 2, f"{config} {at}")
+
+
+def test_experts_beyond_32_bits(ctx):
+    """The last of 40 experts, whose weight and whose weight gradient begin behind 2^31 elements."""
+    E, N, K, M = 40, 8192, 8192, 130
+    g = rng("large experts")
+    w = torch.full((E, N, K), 0x7F, dtype=torch.uint8, device="cuda").view(E4M3)       # NaN: only the last one may be read
+    sb = scales(g, E, blocks(N), blocks(K))
+    a, sa = bytes8(g, (M, K), E4M3), scales(g, M, blocks(K))
+    last, slast = bytes8(g, (N, K), E4M3, 0.1), sb[-1]
+    w[-1].copy_(last)
+    offsets = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    offsets[-1] = M
+    picked = slice(N - 150, N)
+    want_w = ref.values(last, slast, 128, 128)
+    for config in ((2, 256, 1), (1, 128, 1)):
+        out = torch.full((M, N), float("nan"), device="cuda")
+        with fp8.Plan(ctx, M, N, K, groups=E, out_dtype=torch.float32) as plan:
+            plan.set_config(*config)
+            plan.run(a, sa, w, sb, out, offsets=offsets)
+            assert plan.last_device_status()[0] == hgemm.OK
+        ref.check_product(out[:, picked], ref.values(a, sa, 1, 128), want_w[picked], blocks(K), f"forward {config}")
+    del w
+    R = fp8.padded_rows(M, E)
+    dy, x = bytes8(g, (R, N), E4M3), bytes8(g, (R, K), E4M3)
+    for t in (dy, x):
+        t.view(torch.uint8)[M:] = 0
+    sy, sx = scales(g, blocks(R), N), scales(g, blocks(R), K)
+    p, q = ref.values(dy[:M], sy[:2], 128, 1).T, ref.values(x[:M], sx[:2], 128, 1).T
+    for config in ((2, 256, 1), (1, 128, 1)):
+        dw = torch.full((E, N, K), float("nan"), dtype=torch.bfloat16, device="cuda")
+        with fp8.Plan(ctx, M, N, K, form="weight_grad", groups=E) as plan:
+            plan.set_config(*config)
+            plan.run(dy, sy, x, sx, dw, offsets=offsets)
+            assert plan.last_device_status()[0] == hgemm.OK
+        ref.check_product(dw[-1, picked], p[picked], q, 2, f"weight gradient {config}")
+        assert not bool(dw[:-1].any())                          # (NaN counts as true)
+
+
 # ---- the layer as a whole ---------------------------------------------------------------------------------------
 
 def test_gradients_against_differences(ctx):
