@@ -98,9 +98,10 @@ hgemm_status_t hgemm_fp8_last_device_status(hgemm_fp8_plan_t *plan, uint32_t *co
 /* Test hook: hgemm_debug_timeout_probe, reporting to this plan's status word. */
 hgemm_status_t hgemm_fp8_debug_timeout_probe(hgemm_fp8_plan_t *plan, void *stream);
 
-/* How a plan runs: tile (block_p x block_q: rows of the kernel's two operands), whether the operands are swapped, CTAs
- * that share one tile's contraction, and CTAs per tile.  hgemm_fp8_plan_set_config takes what hgemm_fp8_plan_get_config
- * gives, or another combination that the plan's product has kernels for (HGEMM_ERR_UNSUPPORTED otherwise). */
+/* How a plan runs: CTAs per tile (which also says whether the kernel's operands are swapped), the tile's extent along the
+ * kernel's second operand, and the CTAs that share one tile's contraction.  hgemm_fp8_plan_set_config takes what
+ * hgemm_fp8_plan_get_config gives, or another combination that the plan's product has kernels for (HGEMM_ERR_UNSUPPORTED
+ * otherwise). */
 typedef struct {
     int32_t cta_group;         /* 2: CTA pairs, tiles of 256 x 256; 1: one CTA, tiles of 128 x block_q with the operands swapped */
     int32_t block_q;           /* 256 (pairs); 16, 32, 64 or 128 (one CTA; 128 only for the weight gradient) */
