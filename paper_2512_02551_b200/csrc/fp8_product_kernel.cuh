@@ -4,8 +4,9 @@
 // block of 128 is a product of its own: four tcgen05.mma (kind::f8f6f4, K = 32) into a fresh tensor-memory accumulator, which
 // eight warps then read, multiply by the block's scales and add to running sums in REGISTERS ("promotion").  One accumulator is
 // read while the next is computed, so the tensor pipe and the promotion overlap; the budget per block and SM of a 256 x 256
-// pair tile is 512 cycles of MMA against 256 cycles of tensor-memory reads and 128 (one scale per row and 128-column block) or
-// 256 (a scale per column) cycles of packed fp32 multiply-adds per scheduler.
+// pair tile is 512 cycles of MMA against 256 cycles of tensor-memory reads and 256 (one scale per row and 128-column block: a
+// multiply-add per element) or 512 (a scale per column: a product besides) cycles of fp32 arithmetic per scheduler.  The packed
+// form of two elements an instruction issues at half rate: it saves instructions, not pipe time.
 //
 // Roles (384 threads): warp 0 fills a ring of shared-memory stages by TMA (one stage = one block of 128: 128 bytes of every
 // row, or 128 rows of 128 columns where an operand is stored along its own dimension); warp 1 issues the MMAs; warp 2 fetches
@@ -20,10 +21,12 @@
 // every CTA computes for itself from the offsets.  A tile never crosses a group; the rows it computes beyond its group's end
 // are not stored.  Weight gradients contract over a group's rows, which the column-quantised copy pads with zeros to whole blocks.
 //
-// Measured (B200, bf16 results unless said): 4096^3 forward 69 us (2000 TFLOP/s), 8192^3 500 us (2200, power-limited: 408 us without
-// the promotion), 8192 x 4096 x 4096 weight gradient in fp32 178 us (1540); 1000 x 4096 x 4096 22 us; 64 experts x 4 rows, 2048 x 2048 weights
-// 42 us (6.4 TB/s, the copy rate); 7 x 8192 x 4096 9.9 us (3.4 TB/s). What bounds the large ones is the promoting warps (multiply-adds,
-// barrier round trips and, on the MMA warp's scheduler, its instructions), 720-770 cycles a block of 512 cycles of MMA.
+// Measured (B200, bf16 results unless said), launches back to back on the same operands: 4096^3 forward 69 us (2000 TFLOP/s), 8192^3
+// 501 us (2190; 408 us without the promotion), 8192 x 4096 x 4096 weight gradient in fp32 178 us (1540); 1000 x 4096 x 4096 21.5 us;
+// 7 x 8192 x 4096 9.9 us (3.4 TB/s).  As passes whose operands change from one to the next: 8192^3 555 us (1980), the weight gradient
+// 201 us (1370), 1000 x 4096 x 4096 22.8 us, 7 x 8192 x 4096 11.6 us, 64 experts x 4 rows with 2048 x 2048 weights 43 us (6.3 TB/s).
+// What bounds the large ones is the promoting warps (multiply-adds, barrier round trips and, on the MMA warp's scheduler, its
+// instructions), 720-770 cycles a block of 512 cycles of MMA.
 //
 // Every mbarrier wait is bounded (see hgemm_device.cuh): a wait that runs out raises the status word and the CTA's abort flag, and
 // every role falls through to the common teardown.

@@ -13,7 +13,9 @@
 // it) and product by itself; a block whose maximum is infinite has its infinities made NaN first.
 //
 // Measured (B200): 8192 x 8192 bf16 by rows 30 us (6.6 TB/s, the copy rate), rows and columns 53 us (5.1 TB/s), tiles 35 us (5.7 TB/s); fp32
-// rows and columns 72 us (5.6 TB/s).  The 16-bit forms that make columns are bound by instructions (17 an element).
+// rows and columns 72 us (5.6 TB/s).  The 16-bit forms that make columns are bound by instructions (17 an element).  Laid out per group, a
+// warp of every CTA walks the offsets first, 32 groups a step: 32768 x 2048 bf16, rows and columns, 51 us without groups, 62 us with 32 of
+// them, 124 us with 256, 528 us with 1024; gathered from 8192 rows on the way 89 us with 32.
 #pragma once
 
 #include <cuda_bf16.h>

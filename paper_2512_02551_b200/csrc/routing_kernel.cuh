@@ -3,11 +3,12 @@
 // hgemm_route: one warp per token, its experts in registers, consecutive ones in one lane.  A value becomes an unsigned key in the same
 // order, so that a maximum over the warp is one redux instruction; the lowest lane that has it holds the lowest index.  Groups that
 // are whole lanes, a power of two of them, find their best values all at once by shuffles among those lanes.  Bound by
-// instruction issue (top_k rounds of redux, ballot and a scan of the lane's slots), not by the logits' bytes.
+// instruction issue (top_k rounds of redux, ballot and a scan of the lane's slots; an instruction in 76 % of the active cycles at
+// 16384 x 128), not by the logits' bytes.  The gradient issues in 66 % of them and waits for its 2-byte loads.
 //
 // hgemm_route_sort: a stable counting sort in one launch.  The CTAs of one cluster divide the choices into consecutive runs, one per
 // warp; per-warp histograms, prefix sums over warps, CTAs (through distributed shared memory) and experts give every run its
-// first place for every expert, and each warp then places its run in order.
+// first place for every expert, and each warp then places its run in order.  It has 16 SMs, which issue in 52 % of the active cycles.
 //
 // Measured (B200): 16384 tokens, 8 of 128 experts: choice 11.8 us, order 11.1 us, gradient 7.8 us; 256 experts in 8 groups, sigmoid: choice
 // 23 us; 33 tokens: 4.2 and 3.8 us.
