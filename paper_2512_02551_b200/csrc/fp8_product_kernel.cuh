@@ -25,8 +25,8 @@
 // 501 us (2190; 408 us without the promotion), 8192 x 4096 x 4096 weight gradient in fp32 178 us (1540); 1000 x 4096 x 4096 21.5 us;
 // 7 x 8192 x 4096 9.9 us (3.4 TB/s).  As passes whose operands change from one to the next: 8192^3 555 us (1980), the weight gradient
 // 201 us (1370), 1000 x 4096 x 4096 22.8 us, 7 x 8192 x 4096 11.6 us, 64 experts x 4 rows with 2048 x 2048 weights 43 us (6.3 TB/s).
-// In loops of seconds the power cap adds to that (8192^3 584 us at 1.36 GHz).  What bounds the large ones is the promoting warps (multiply-adds, barrier round trips and, on the MMA warp's scheduler, its
-// instructions), 720-770 cycles a block of 512 cycles of MMA.
+// In loops of seconds the power cap adds to that (8192^3 584 us at 1.36 GHz).  What bounds the large ones is the promoting warps
+// (multiply-adds, barrier round trips and, on the MMA warp's scheduler, its instructions), 720-770 cycles a block of 512 cycles of MMA.
 //
 // Every mbarrier wait is bounded (see hgemm_device.cuh): a wait that runs out raises the status word and the CTA's abort flag, and
 // every role falls through to the common teardown.
