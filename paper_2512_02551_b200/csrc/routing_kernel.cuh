@@ -246,8 +246,9 @@ route_backward_kernel(const RouteParams p)
         const float s = has ? route_score(route_load(row + e), sigmoid, m, sum) : 0.0f;
         float d = has ? dw : 0.0f;
         if (p.renormalize) {
-            const float total = warp_sum(s) + 1e-20f;
-            const float mean = warp_sum(d * s) / total;
+            // by the weights themselves: a weight of exactly 1 (one choice) then leaves exactly 0, not the rounding of dw s / s, which
+            // the division by a small sum would blow up
+            const float total = warp_sum(s) + 1e-20f, mean = warp_sum(d * (s / total));
             d = has ? (d - mean) / total : 0.0f;
         }
         if (sigmoid) {

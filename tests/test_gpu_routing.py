@@ -229,6 +229,23 @@ def test_gradient(ctx, t, dtype):
             np.testing.assert_allclose(got[:, e], slope, atol=float((bound[:, e] + 1e-8 * size[:, 0]).max()), rtol=0)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_gradient_of_one_renormalised_choice_is_zero(ctx, score, dtype):
+    """s / (s + 1e-20) is 1 in 32 bits for every s above 2^24 * 1e-20 (the logits here keep s above 1e-12), so the weight does not
+    depend on the logits: its gradient is exactly zero."""
+    T, E = 1000, 60
+    g = torch.Generator(device="cuda").manual_seed(11)
+    logits = torch.randn(T, E, generator=g, device="cuda").mul(3.0).clamp(-9, 9).to(dtype)
+    router = routing.Router(ctx, E, 1, score=score, renormalize=True, scale=2.5)
+    w, i = run(router, logits)
+    assert bool((w == 2.5).all())
+    for idx in (i, torch.randint(0, E, (T, 1), generator=g, device="cuda", dtype=torch.int32)):
+        dl = torch.full_like(logits, float("nan"))
+        router.backward(logits, idx, torch.randn(T, 1, generator=g, device="cuda") * 100.0, dl)
+        assert bool((dl == 0).all())
+
+
 def test_same_bits_every_time(ctx):
     g = torch.Generator(device="cuda").manual_seed(3)
     logits = torch.randn(5000, 256, generator=g, device="cuda")
