@@ -246,10 +246,12 @@ route_backward_kernel(const RouteParams p)
         const float s = has ? route_score(route_load(row + e), sigmoid, m, sum) : 0.0f;
         float d = has ? dw : 0.0f;
         if (p.renormalize) {
-            // by the weights themselves: a weight of exactly 1 (one choice) then leaves exactly 0, not the rounding of dw s / s, which
-            // the division by a small sum would blow up
-            const float total = warp_sum(s) + 1e-20f, mean = warp_sum(d * (s / total));
-            d = has ? (d - mean) / total : 0.0f;
+            // dw_j - sum_i dw_i w_i, taken from the first choice's dw: with r = dw_0 it is  (dw_j - r) - (sum_i s_i (dw_i - r) - r (S - sum s)) / S.
+            // Equal dw (one choice above all) then leave exactly 0 where S = sum s in 32 bits, not the rounding of dw s / s, which the
+            // division by S would blow up; and the two sums do not wait for one another.
+            const float r = __shfl_sync(0xffffffffu, d, 0);
+            const float sum_s = warp_sum(s), moved = warp_sum(s * (d - r)), total = sum_s + 1e-20f;
+            d = has ? ((d - r) - (moved - r * (total - sum_s)) / total) / total : 0.0f;
         }
         if (sigmoid) {
 #pragma unroll
