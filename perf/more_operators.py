@@ -280,7 +280,7 @@ def _codes(x, fmt, factor):
     v = torch.where(step > 0, b / step, 0.0)
     m = v.abs()
     code = (m > 0.25).to(torch.uint8) + (m >= 0.75) + (m > 1.25) + (m >= 1.75) + (m > 2.5) + (m >= 3.5) + (m > 5.0)
-    code = code + 8 * (v < 0)
+    code = code + 8 * (v < 0).to(torch.uint8)
     return code.reshape(*x.shape[:-1], -1)[..., :C], scale
 
 
