@@ -1,0 +1,560 @@
+// 4-bit quantisation with one scale per block of 16 (e4m3, and a factor for the tensor) or 32 (a power of two) along rows, along columns, or both
+// in one pass; the tensor's factor; and the way back.
+//
+// Bound by memory: 2 or 4 bytes read and a half (both copies: one) written per element.  256 threads own a tile of 128 x 128 elements.  As it is
+// loaded, 8 lanes hold a row's 128 elements, 16 each: a block, or half of one, whose maximum needs at most one shuffle.  For the column copy
+// the tile goes to shared memory as it came; there a thread takes 32 rows of two columns (16-bit types) or of one (fp32, twice), so that
+// blocks lie in registers again, and the packed columns and their scale tiles leave through shared memory in runs of 64 and 1024 bytes.
+//
+// A value is the nearest 4-bit value of the correctly rounded quotient x / step (step = scale * factor): q = x * r, then one residual step with two
+// multiply-adds (r = 1 / step is correctly rounded, which makes that quotient so).  A plain product with the reciprocal would be off by an ulp where x lies
+// halfway between two values, which inputs of few bits often do.  Maxima are taken on the bit patterns: a NaN or an infinity is larger than every number.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp4.h>
+#include <cuda_fp8.h>
+#include <stdint.h>
+
+#include "hgemm_device.cuh"
+#include "product_tiles.cuh"
+
+namespace hgemm_dev {
+
+constexpr int kFp4QuantThreads = 256;
+constexpr int kFp4OutPitch = 80;                  // bytes between packed columns in shared memory
+__host__ __device__ constexpr int fp4_raw_pitch(int size) { return 128 * size + 16; }      // bytes between a tile's rows in shared memory
+__host__ __device__ constexpr int fp4_quant_smem(int size, bool nv, bool columns) { return columns ? 128 * (fp4_raw_pitch(size) + kFp4OutPitch) + (nv ? 1024 : 512) : 0; }
+
+struct Fp4QuantParams {
+    const void *x;
+    int64_t ldx, rows, cols, x_rows;
+    const int32_t *row_index;
+    const int32_t *offsets;
+    int32_t groups;
+    int32_t vec_ok;            // rows of x start at multiples of 16 bytes
+    const float *factor;
+    uint8_t *q;
+    int64_t ldq;
+    uint8_t *scales;
+    uint8_t *q_cols;
+    int64_t ldq_cols;
+    uint8_t *scales_cols;
+    int64_t col_rows;          // contracted elements of the column copy
+    int64_t row_tiles;         // scale tiles along the rows of one matrix
+};
+
+// 16 consecutive elements as they came.
+template <class T>
+struct Raw16 {
+    uint32_t w[4 * sizeof(T)];
+};
+
+template <class T>
+__device__ __forceinline__ Raw16<T> load16(const T *row, int64_t col, int64_t cols, int32_t vec_ok)
+{
+    Raw16<T> r;
+    constexpr int kVec = static_cast<int>(sizeof(T));            // 16-byte pieces
+    if (row != nullptr && vec_ok && col + 16 <= cols) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const uint4 v = reinterpret_cast<const uint4 *>(row + col)[i];
+            r.w[4 * i] = v.x, r.w[4 * i + 1] = v.y, r.w[4 * i + 2] = v.z, r.w[4 * i + 3] = v.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4 * kVec; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                r.w[i] = row != nullptr && col + i < cols ? __float_as_uint(row[col + i]) : 0u;
+            } else {
+                const unsigned short *s = reinterpret_cast<const unsigned short *>(row);
+                const uint32_t a = row != nullptr && col + 2 * i < cols ? s[col + 2 * i] : 0u, b = row != nullptr && col + 2 * i + 1 < cols ? s[col + 2 * i + 1] : 0u;
+                r.w[i] = a | (b << 16);
+            }
+        }
+    }
+    return r;
+}
+
+// Bit patterns of magnitudes; for the 16-bit types two at a time.
+template <class T>
+__device__ __forceinline__ uint32_t magnitude_max(uint32_t m, uint32_t w)
+{
+    if constexpr (sizeof(T) == 4) return max(m, w & 0x7fffffffu);
+    else return __vmaxu2(m, w & 0x7fff7fffu);
+}
+// The larger of a register's two 16-bit magnitudes, as the type's bit pattern.
+__device__ __forceinline__ uint32_t larger16(uint32_t m) { return max(m & 0xffffu, m >> 16); }
+
+// A magnitude's bit pattern as fp32; NaN for a NaN or an infinity.
+__device__ __forceinline__ float magnitude_of(uint32_t m, float) { return m >= 0x7f800000u ? __int_as_float(0x7fffffff) : __uint_as_float(m); }
+__device__ __forceinline__ float magnitude_of(uint32_t m, __half) { return m >= 0x7c00u ? __int_as_float(0x7fffffff) : __half2float(__ushort_as_half(static_cast<unsigned short>(m))); }
+__device__ __forceinline__ float magnitude_of(uint32_t m, __nv_bfloat16) { return m >= 0x7f80u ? __int_as_float(0x7fffffff) : __uint_as_float(m << 16); }
+
+__device__ __forceinline__ void two_floats(uint32_t w, float &a, float &b, __half)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    a = f.x, b = f.y;
+}
+__device__ __forceinline__ void two_floats(uint32_t w, float &a, float &b, __nv_bfloat16) { a = __uint_as_float(w << 16), b = __uint_as_float(w & 0xffff0000u); }
+
+// The exponent byte of the smallest power of two s with a <= top * s; top = (1 + top_mantissa / 2^23) * 2^top_exponent.
+__device__ __forceinline__ int32_t power_above(float a, int32_t top_exponent, uint32_t top_mantissa)
+{
+    const uint32_t b = __float_as_uint(a);
+    return static_cast<int32_t>(b >> 23) - top_exponent + ((b & 0x7fffffu) > top_mantissa ? 1 : 0);
+}
+constexpr uint32_t kMantissa6 = 0x400000u, kMantissa2688 = 0x280000u;        // 6 = 1.5 * 2^2, 2688 = 1.3125 * 2^11
+
+struct BlockStep {
+    uint32_t byte;             // the scale
+    float step, inverse;       // what values are divided by, and its reciprocal (0 where values are 0)
+};
+
+// amax: NaN for a block with a NaN or an infinity.  g = 1 / factor (NV).
+template <bool NV>
+__device__ __forceinline__ BlockStep block_step(float amax, float factor, float g)
+{
+    BlockStep s;
+    if constexpr (NV) {
+        const float u = amax * g * (1.0f / 6.0f);
+        s.byte = __nv_cvt_float_to_fp8(u, __NV_SATFINITE, __NV_E4M3);
+        const float step = __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(s.byte), __NV_E4M3))) * factor;
+        s.step = step > 0.0f ? step : 0.0f;                      // (a NaN: the block's zeros stay zeros)
+        s.inverse = step > 0.0f ? __frcp_rn(step) : 0.0f;
+    } else {
+        const int32_t e = min(max(power_above(amax, 2, kMantissa6), 0), 254);
+        s.byte = amax != amax ? 255u : static_cast<uint32_t>(e);
+        s.step = 0.0f;
+        s.inverse = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);   // 2^(127 - e), exactly (e = 254: below the smallest normal number; no finite block has it)
+    }
+    return s;
+}
+
+// Two quotients as 4-bit values in one byte.
+template <bool NV>
+__device__ __forceinline__ uint32_t quantize_pair(float a, float b, const BlockStep &s)
+{
+    float x = a * s.inverse, y = b * s.inverse;
+    if constexpr (NV) {
+        x = fmaf(fmaf(-x, s.step, a), s.inverse, x);
+        y = fmaf(fmaf(-y, s.step, b), s.inverse, y);
+    }
+    return __nv_cvt_float2_to_fp4x2(make_float2(x, y), __NV_E2M1, cudaRoundNearest);
+}
+
+// Eight values in a word.
+template <bool NV>
+__device__ __forceinline__ uint32_t quantize8(const float *f, const BlockStep &s)
+{
+    return quantize_pair<NV>(f[0], f[1], s) | (quantize_pair<NV>(f[2], f[3], s) << 8) | (quantize_pair<NV>(f[4], f[5], s) << 16) | (quantize_pair<NV>(f[6], f[7], s) << 24);
+}
+
+// The group that holds block rb (of 128 rows) of the copy laid out per group, and the block's rows: first .. end - 1 of the input (end: the group's).  The offsets are
+// clamped as the products clamp them.  One whole warp; false beyond the last group's.
+__device__ __forceinline__ bool block_of_group(const int32_t *offsets, int32_t groups, int32_t limit, int32_t rb, uint32_t lane, int32_t &first, int32_t &end)
+{
+    int32_t carry = 0, last = 0;
+    for (int32_t base = 0; base < groups; base += 32) {
+        const int32_t e = base + static_cast<int32_t>(lane);
+        int32_t a = min(max(offsets[min(e, groups)], 0), limit);
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int32_t x = __shfl_up_sync(0xffffffffu, a, d);
+            if (static_cast<int32_t>(lane) >= d) a = max(a, x);
+        }
+        a = max(a, last);
+        int32_t z = __shfl_down_sync(0xffffffffu, a, 1);
+        if (lane == 31) z = max(a, min(max(offsets[min(e + 1, groups)], 0), limit));
+        last = __shfl_sync(0xffffffffu, z, 31);
+        const int32_t n = e < groups ? (z - a + 127) / 128 : 0;
+        int32_t sum = n;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int32_t x = __shfl_up_sync(0xffffffffu, sum, d);
+            if (static_cast<int32_t>(lane) >= d) sum += x;
+        }
+        const uint32_t hit = __ballot_sync(0xffffffffu, n > 0 && carry + sum > rb);
+        if (hit) {
+            const int src = __ffs(hit) - 1;
+            first = __shfl_sync(0xffffffffu, a + (rb - (carry + sum - n)) * 128, src);
+            end = __shfl_sync(0xffffffffu, z, src);
+            return true;
+        }
+        carry += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    return false;
+}
+
+// MODE: HGEMM_FP4_ROWS (1), COLS (2) or both (3).  grid: x = column tiles (each CTA walks on by gridDim.x), y = row tiles (as many as the padded copy has), z = matrices.
+template <class T, int MODE, bool NV>
+__global__ void __launch_bounds__(kFp4QuantThreads, sizeof(T) == 4 || MODE == 1 ? 3 : 4)
+fp4_quantize_kernel(const Fp4QuantParams p)
+{
+    constexpr int kBlock = NV ? 16 : 32, kAtom = 4 * kBlock;     // elements of a block; of a scale tile's four
+    constexpr int kPitch = fp4_raw_pitch(sizeof(T)), kOutPitch = kFp4OutPitch;
+    extern __shared__ __align__(16) uint8_t s_raw[];              // the tile as it came, packed columns, their scales (not with MODE 1)
+    uint8_t *s_out = s_raw + 128 * kPitch, *s_scale = s_out + 128 * kOutPitch;
+    __shared__ int32_t s_place[3];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int32_t rb = static_cast<int32_t>(blockIdx.y);
+    int64_t row0 = rb * 128ll, row_end = p.rows;                  // rows row0 .. row_end - 1 of the input
+    if (p.offsets != nullptr) {
+        if (threadIdx.x < 32) {
+            int32_t first = 0, end = 0;
+            const bool found = block_of_group(p.offsets, p.groups, static_cast<int32_t>(p.rows), rb, threadIdx.x, first, end);
+            if (threadIdx.x == 0) { s_place[0] = found; s_place[1] = first; s_place[2] = end; }
+        }
+        __syncthreads();
+        if (!s_place[0]) return;                                  // beyond the last group (block-uniform)
+        row0 = s_place[1];
+        row_end = s_place[2];
+    }
+    const int64_t matrix = blockIdx.z;
+    const float factor = NV ? p.factor[matrix] : 0.0f, g = factor >= 7.888609052210118e-31f ? __frcp_rn(factor) : 0.0f;        // 2^-100
+    const T *x = static_cast<const T *>(p.x) + matrix * p.rows * p.ldx;
+    uint8_t *q = p.q + matrix * p.rows * p.ldq, *q_cols = p.q_cols + matrix * p.cols * p.ldq_cols;
+    const int64_t atoms = (p.cols + kAtom - 1) / kAtom, col_atoms = (p.col_rows + kAtom - 1) / kAtom, col_tiles = (p.cols + 127) / 128;
+    uint8_t *scales = p.scales + (matrix * p.row_tiles + rb) * atoms * 512, *scales_cols = p.scales_cols + matrix * col_tiles * col_atoms * 512;
+    const uint32_t sub = threadIdx.x & 7u;
+    for (int64_t ct = blockIdx.x; ct < col_tiles; ct += gridDim.x) {
+        const int64_t col = ct * 128 + sub * 16;
+        Raw16<T> raw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t r = row0 + (threadIdx.x >> 3) + 32 * i;
+            const T *src = nullptr;
+            if (r < row_end) {
+                if (p.row_index == nullptr) {
+                    src = x + r * p.ldx;
+                } else {
+                    const int64_t k = p.row_index[r];
+                    if (k >= 0 && k < p.x_rows) src = x + k * p.ldx;
+                }
+            }
+            raw[i] = load16<T>(src, col, p.cols, p.vec_ok);
+        }
+        if constexpr (MODE != 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint8_t *dst = s_raw + ((threadIdx.x >> 3) + 32 * i) * kPitch + sub * 16 * sizeof(T);
+                constexpr int kVec = static_cast<int>(sizeof(T));
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) {
+                    // lanes 4 to 7 start at another piece: the eight lanes of a row then reach all banks
+                    const uint32_t k = sizeof(T) == 2 ? (static_cast<uint32_t>(j) ^ (sub >> 2)) : (static_cast<uint32_t>(j) + (sub >> 1)) & 3u;
+                    uint4 v;
+                    if constexpr (kVec == 2) {
+                        v = k ? make_uint4(raw[i].w[4], raw[i].w[5], raw[i].w[6], raw[i].w[7]) : make_uint4(raw[i].w[0], raw[i].w[1], raw[i].w[2], raw[i].w[3]);
+                    } else {
+                        const uint4 a = k & 1u ? make_uint4(raw[i].w[4], raw[i].w[5], raw[i].w[6], raw[i].w[7]) : make_uint4(raw[i].w[0], raw[i].w[1], raw[i].w[2], raw[i].w[3]);
+                        const uint4 b = k & 1u ? make_uint4(raw[i].w[12], raw[i].w[13], raw[i].w[14], raw[i].w[15]) : make_uint4(raw[i].w[8], raw[i].w[9], raw[i].w[10], raw[i].w[11]);
+                        v = k & 2u ? b : a;
+                    }
+                    reinterpret_cast<uint4 *>(dst)[k] = v;
+                }
+            }
+        }
+        if constexpr (MODE != 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t m = 0u;
+#pragma unroll
+                for (int j = 0; j < static_cast<int>(4 * sizeof(T)); ++j) m = magnitude_max<T>(m, raw[i].w[j]);
+                if constexpr (sizeof(T) == 2) m = larger16(m);
+                if constexpr (!NV) m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+                const BlockStep s = block_step<NV>(magnitude_of(m, T()), factor, g);
+                // the scales of four blocks make a word
+                uint32_t word = NV ? s.byte << (8u * (sub & 3u)) : s.byte << (8u * (sub >> 1));
+                word |= __shfl_xor_sync(0xffffffffu, word, NV ? 1 : 2);
+                word |= __shfl_xor_sync(0xffffffffu, word, NV ? 2 : 4);
+                const uint32_t k = (threadIdx.x >> 3) + 32u * i;
+                const int64_t atom = ct * (128 / kAtom) + (NV ? sub >> 2 : 0u);
+                if ((NV ? sub & 3u : sub) == 0u && atom < atoms) *reinterpret_cast<uint32_t *>(scales + atom * 512 + (k & 31u) * 16u + (k >> 5) * 4u) = word;
+                float f[16];
+                if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) f[j] = __uint_as_float(raw[i].w[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) two_floats(raw[i].w[j], f[2 * j], f[2 * j + 1], T());
+                }
+                const uint2 v = make_uint2(quantize8<NV>(f, s), quantize8<NV>(f + 8, s));
+                const int64_t r = row0 + k;
+                if (r < row_end) {
+                    uint8_t *dst = q + r * p.ldq + col / 2;
+                    if (col + 16 <= p.cols) {
+                        *reinterpret_cast<uint2 *>(dst) = v;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (col + 2 * j < p.cols) dst[j] = static_cast<uint8_t>((j < 4 ? v.x >> (8 * j) : v.y >> (8 * (j - 4))) & 0xffu);
+                    }
+                }
+            }
+        }
+        if constexpr (MODE != 1) {
+            __syncthreads();
+            // 32 rows (part of the tile's four) of a column, or of two: blocks, values, scales
+            auto column = [&](const float (&f)[32], const uint32_t (&m)[2], uint32_t c, uint32_t part) {
+                uint4 v;
+                if constexpr (NV) {
+                    const BlockStep s0 = block_step<NV>(magnitude_of(m[0], T()), factor, g), s1 = block_step<NV>(magnitude_of(m[1], T()), factor, g);
+                    v = make_uint4(quantize8<NV>(f, s0), quantize8<NV>(f + 8, s0), quantize8<NV>(f + 16, s1), quantize8<NV>(f + 24, s1));
+                    *reinterpret_cast<unsigned short *>(s_scale + (part >> 1) * 512u + (c & 31u) * 16u + (c >> 5) * 4u + (part & 1u) * 2u) = static_cast<unsigned short>(s0.byte | (s1.byte << 8));
+                } else {
+                    const BlockStep s = block_step<NV>(magnitude_of(max(m[0], m[1]), T()), factor, g);
+                    v = make_uint4(quantize8<NV>(f, s), quantize8<NV>(f + 8, s), quantize8<NV>(f + 16, s), quantize8<NV>(f + 24, s));
+                    s_scale[(c & 31u) * 16u + (c >> 5) * 4u + part] = static_cast<uint8_t>(s.byte);
+                }
+                *reinterpret_cast<uint4 *>(s_out + c * kOutPitch + part * 16u) = v;
+            };
+            if constexpr (sizeof(T) == 2) {
+                const uint32_t pair = threadIdx.x & 63u, part = threadIdx.x >> 6;
+                uint32_t w[32], m[2] = {0u, 0u};
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    w[j] = *reinterpret_cast<const uint32_t *>(s_raw + (part * 32u + j) * kPitch + pair * 4u);
+                    m[j / 16] = magnitude_max<T>(m[j / 16], w[j]);
+                }
+                float f[32], h[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) two_floats(w[j], f[j], h[j], T());
+                const uint32_t lo[2] = {m[0] & 0xffffu, m[1] & 0xffffu}, hi[2] = {m[0] >> 16, m[1] >> 16};
+                column(f, lo, 2u * pair, part);
+                column(h, hi, 2u * pair + 1u, part);
+            } else {
+#pragma unroll 1
+                for (uint32_t i = 0; i < 2; ++i) {
+                    const uint32_t c = threadIdx.x & 127u, part = (threadIdx.x >> 7) + 2u * i;
+                    float f[32];
+                    uint32_t m[2] = {0u, 0u};
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const uint32_t w = *reinterpret_cast<const uint32_t *>(s_raw + (part * 32u + j) * kPitch + c * 4u);
+                        m[j / 16] = magnitude_max<T>(m[j / 16], w);
+                        f[j] = __uint_as_float(w);
+                    }
+                    column(f, m, c, part);
+                }
+            }
+            __syncthreads();
+            const int64_t at = rb * 64ll, width = (p.col_rows + 1) / 2;           // the tile's bytes of a column; the column's
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i) {
+                const uint32_t c = (threadIdx.x >> 2) + 64u * i, k = threadIdx.x & 3u;
+                if (ct * 128 + c < p.cols) {
+                    uint8_t *dst = q_cols + (ct * 128 + c) * p.ldq_cols + at + k * 16u;
+                    const uint4 v = *reinterpret_cast<const uint4 *>(s_out + c * kOutPitch + k * 16u);
+                    const int64_t room = width - at - k * 16;
+                    if (room >= 16) {
+                        *reinterpret_cast<uint4 *>(dst) = v;
+                    } else {
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (j < room) dst[j] = static_cast<uint8_t>((w[j / 4] >> (8 * (j & 3))) & 0xffu);
+                    }
+                }
+            }
+            if (threadIdx.x < (128 / kAtom) * 32u) {
+                const int64_t atom = rb * (128 / kAtom) + (threadIdx.x >> 5);
+                if (atom < col_atoms)
+                    *reinterpret_cast<uint4 *>(scales_cols + (ct * col_atoms + atom) * 512 + (threadIdx.x & 31u) * 16u) = *reinterpret_cast<const uint4 *>(s_scale + threadIdx.x * 16u);
+            }
+            if (ct + gridDim.x < col_tiles) __syncthreads();      // the next tile's staging
+        }
+    }
+}
+
+// ---- the tensor's factor -------------------------------------------------------------------------------------------
+
+constexpr int kFp4FactorThreads = 512;
+constexpr int kFp4FactorCluster = 8;
+
+// max |x| over the finite elements of a matrix, as the factor's bit pattern (monotone in the maximum, so that factors meet by their maximum).  CLUSTER: the CTAs of one
+// cluster have the whole matrix (grid.y: matrices) and write the factor; else every CTA raises it by an atomic maximum (whose order does not matter).
+template <class T, bool CLUSTER>
+__global__ void __launch_bounds__(kFp4FactorThreads)
+fp4_factor_kernel(const T *x0, int64_t ldx, int64_t rows, int64_t cols, int32_t vec_ok, float *factor)
+{
+    __shared__ uint32_t s_max[kFp4FactorThreads / 32];
+    __shared__ uint32_t s_all;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const T *x = x0 + blockIdx.y * rows * ldx;
+    constexpr uint32_t kInf = sizeof(T) == 4 ? 0x7f800000u : 0u;
+    uint32_t m = 0u;
+    const int64_t chunks = (cols + 15) / 16, all = rows * chunks;
+    const bool flat = ldx == cols && cols % 16 == 0;               // one run of elements
+    auto take = [&](const Raw16<T> &r) {
+        uint32_t k = 0u;
+#pragma unroll
+        for (int j = 0; j < static_cast<int>(4 * sizeof(T)); ++j) k = magnitude_max<T>(k, r.w[j]);
+        bool odd;                                                  // a NaN or an infinity among them: element by element
+        if constexpr (sizeof(T) == 4) odd = k >= kInf;
+        else odd = magnitude_of(larger16(k), T()) != magnitude_of(larger16(k), T());
+        if (odd) {
+            k = 0u;
+#pragma unroll
+            for (int j = 0; j < static_cast<int>(4 * sizeof(T)); ++j) {
+                if constexpr (sizeof(T) == 4) {
+                    const uint32_t a = r.w[j] & 0x7fffffffu;
+                    if (a < kInf) k = max(k, a);
+                } else {
+                    const uint32_t a = r.w[j] & 0x7fffu, b = (r.w[j] >> 16) & 0x7fffu;
+                    if (magnitude_of(a, T()) == magnitude_of(a, T())) k = max(k, a);
+                    if (magnitude_of(b, T()) == magnitude_of(b, T())) k = max(k, b);
+                }
+            }
+        } else if constexpr (sizeof(T) == 2) {
+            k = larger16(k);
+        }
+        m = max(m, k);
+    };
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kFp4FactorThreads;
+    int64_t i = static_cast<int64_t>(blockIdx.x) * kFp4FactorThreads + threadIdx.x;
+    if (flat && vec_ok) {
+        for (; i + 3 * step < all; i += 4 * step) {
+            Raw16<T> r[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) r[u] = load16<T>(x, (i + u * step) * 16, INT64_MAX, 1);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) take(r[u]);
+        }
+        for (; i < all; i += step) take(load16<T>(x, i * 16, INT64_MAX, 1));
+    } else {
+        for (; i < all; i += step) {
+            const int64_t r = i / chunks;
+            take(load16<T>(x + r * ldx, (i - r * chunks) * 16, cols, vec_ok));
+        }
+    }
+    m = __reduce_max_sync(0xffffffffu, m);
+    if ((threadIdx.x & 31u) == 0u) s_max[threadIdx.x >> 5] = m;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        m = threadIdx.x < kFp4FactorThreads / 32 ? s_max[threadIdx.x] : 0u;
+        m = __reduce_max_sync(0xffffffffu, m);
+        if (threadIdx.x == 0) s_all = m;
+    }
+    if constexpr (CLUSTER) {
+        __syncthreads();
+        cluster_arrive();
+        cluster_wait();
+        if (cluster_ctarank() == 0 && threadIdx.x < 32) {
+            m = 0u;
+            if (threadIdx.x < kFp4FactorCluster) {
+                const uint32_t from = mapa(smem_addr(&s_all), threadIdx.x);
+                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(m) : "r"(from) : "memory");
+            }
+            m = __reduce_max_sync(0xffffffffu, m);
+        }
+        cluster_arrive();
+        cluster_wait();                                            // no CTA leaves while its maximum is read
+    }
+    if (threadIdx.x == 0 && (!CLUSTER || cluster_ctarank() == 0)) {
+        const float a = magnitude_of(m, T());
+        // exponents stay inside fp32's: 2^-127 and below become 0, which the quantiser takes for a tensor of zeros
+        const int32_t e = a > 0.0f ? max(power_above(a, 11, kMantissa2688), 0) : 0;
+        const uint32_t bits = static_cast<uint32_t>(e) << 23;
+        if constexpr (CLUSTER) factor[blockIdx.y] = __uint_as_float(bits);
+        else atomicMax(reinterpret_cast<uint32_t *>(factor) + blockIdx.y, bits);
+    }
+}
+
+// ---- back to wide values -------------------------------------------------------------------------------------------
+
+struct Fp4DequantParams {
+    const uint8_t *q;
+    int64_t ldq;
+    const uint8_t *scales;
+    const float *factor;
+    int64_t rows, cols, matrices;
+    FastDiv fd_chunks;         // runs of 16 elements in a row
+    int32_t vec_ok;            // rows of out start at multiples of 16 bytes
+    void *out;
+    int64_t ldo;
+    // scan_groups:
+    const int32_t *offsets;
+    int32_t groups, ragged, rows_ragged, k_capacity;
+};
+
+// A thread per 16 elements: 8 bytes of values, one scale.  Dynamic shared memory: 2 (groups + 1) words.
+template <class T, bool NV>
+__global__ void __launch_bounds__(256)
+fp4_dequantize_kernel(const Fp4DequantParams p)
+{
+    extern __shared__ int32_t s_groups[];
+    int32_t *pre = s_groups, *off = pre + p.groups + 1;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    if (p.groups > 0) {
+        if (threadIdx.x < 32) scan_groups(p, pre, off, 128, threadIdx.x);
+        __syncthreads();
+    }
+    constexpr int kBlock = NV ? 16 : 32, kAtom = 4 * kBlock;
+    const int64_t atoms = (p.cols + kAtom - 1) / kAtom, row_tiles = (p.rows + 127) / 128;
+    const int64_t all = p.rows * p.fd_chunks.d, step = static_cast<int64_t>(gridDim.x) * blockDim.x;     // one matrix: below 2^31, checked by the host
+    const int64_t matrix = blockIdx.y;
+    const uint8_t *q = p.q + matrix * p.rows * p.ldq, *scales = p.scales + matrix * row_tiles * atoms * 512;
+    T *out = static_cast<T *>(p.out) + matrix * p.rows * p.ldo;
+    const float factor = NV ? p.factor[matrix] : 1.0f;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += step) {
+        const int64_t r = fast_div(static_cast<int32_t>(i), p.fd_chunks), col = (i - r * p.fd_chunks.d) * 16;
+        int64_t place = r;
+        if (p.groups > 0) {
+            if (r < off[0] || r >= off[p.groups]) continue;        // a row of no group
+            int32_t lo = 0, hi = p.groups;                         // the last group that starts at or before r
+            while (hi - lo > 1) {
+                const int32_t mid = (lo + hi) / 2;
+                if (off[mid] <= r) lo = mid;
+                else hi = mid;
+            }
+            place = 128ll * pre[lo] + r - off[lo];
+        }
+        const uint8_t *src = q + r * p.ldq + col / 2;
+        uint2 v;
+        if (col + 16 <= p.cols) {
+            v = *reinterpret_cast<const uint2 *>(src);             // rows start at multiples of 16 bytes, col / 2 is a multiple of 8
+        } else {
+            v = make_uint2(0u, 0u);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (col + 2 * j < p.cols) (j < 4 ? v.x : v.y) |= static_cast<uint32_t>(src[j]) << (8 * (j & 3));
+        }
+        const int64_t b = col / kBlock;
+        const uint32_t byte = scales[((place >> 7) * atoms + (b >> 2)) * 512 + (place & 31) * 16 + ((place >> 5) & 3) * 4 + (b & 3)];
+        float s;
+        if constexpr (NV) s = __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(byte), __NV_E4M3))) * factor;
+        else s = byte == 0u ? 5.877471754111438e-39f : byte == 255u ? __int_as_float(0x7fffffff) : __uint_as_float(byte << 23);
+        float f[16];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(((j < 4 ? v.x : v.y) >> (8 * (j & 3))) & 0xffu), __NV_E2M1);
+            const float2 e = __half22float2(__half2(h));
+            f[2 * j] = e.x * s;
+            f[2 * j + 1] = e.y * s;
+        }
+        T *dst = out + r * p.ldo + col;
+        if (p.vec_ok && col + 16 <= p.cols) {
+            if constexpr (sizeof(T) == 4) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) reinterpret_cast<float4 *>(dst)[j] = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+            } else {
+                uint32_t h[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[j] = pack_pair(f[2 * j], f[2 * j + 1], T());
+                reinterpret_cast<uint4 *>(dst)[0] = make_uint4(h[0], h[1], h[2], h[3]);
+                reinterpret_cast<uint4 *>(dst)[1] = make_uint4(h[4], h[5], h[6], h[7]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (col + j < p.cols) dst[j] = narrow_to<T>(f[j]);
+        }
+    }
+}
+
+} // namespace hgemm_dev

@@ -40,6 +40,7 @@
 #include <type_traits>
 
 #include "hgemm_device.cuh"
+#include "product_tiles.cuh"
 
 namespace hgemm_dev {
 
@@ -56,16 +57,13 @@ constexpr int kFp8Batch = 4;                      // scales travel in batches of
 __host__ __device__ constexpr int fp8_ring(int cta_group) { return cta_group == 2 ? 2 : 4; }     // batches in flight: single CTAs go through theirs faster than two arrive
 __host__ __device__ constexpr int fp8_slot_bytes(int bn, bool q_col) { return (128 + (q_col ? bn : 4)) * 4; }     // one block's scales
 
-// which side of the tile grid follows the groups' offsets
-enum : int32_t { kRaggedNone = 0, kRaggedP = 1, kRaggedQ = 2, kRaggedK = 3 };
-
 struct Fp8Params {
     int32_t rows_p, rows_q;        // rows of P and Q (per group, or all of them on the side that follows the offsets)
     int32_t kblocks;               // blocks of the contraction (not with kRaggedK)
     int32_t tiles_p, tiles_q;      // tiles per group (unused for the side that follows the offsets)
     int32_t total;                 // tiles, where the host knows them (kRaggedNone, kRaggedK)
     int32_t raster;                // tiles of P visited together
-    FastDiv fd_other, fd_group, fd_sweep, fd_raster, fd_last;   // divisors of the tile numbering: see fp8_tile
+    FastDiv fd_other, fd_group, fd_sweep, fd_raster, fd_last;   // divisors of the tile numbering: see product_tile
     int32_t groups, ragged, rows_ragged, k_capacity;   // rows_ragged: clamp of the offsets; k_capacity: blocks the padded copy has
     const int32_t *offsets;
     const float *sp, *sq;          // scale of row r (or of block r / 128), block b: s[r * _row + b * _kb + group * _group]
@@ -80,111 +78,6 @@ struct Fp8Params {
     long long wait_budget;
 };
 
-struct Fp8Tile {
-    int32_t group, p0, p_end, q0, q_end, kb0, kbn;
-};
-
-// The tile with number w; whole (converged) warp.  pre: prefix sums over the groups (tiles, or blocks for kRaggedK); off: clamped offsets.
-template <int TP, int TQ>
-__device__ __forceinline__ Fp8Tile fp8_tile(int32_t w, const Fp8Params &p, const int32_t *pre, const int32_t *off, uint32_t lane)
-{
-    Fp8Tile t;
-    t.group = 0;
-    t.kb0 = 0;
-    t.kbn = p.kblocks;
-    t.p_end = p.rows_p;
-    t.q_end = p.rows_q;
-    if (p.ragged == kRaggedP || p.ragged == kRaggedQ) {
-        const int32_t other = p.ragged == kRaggedP ? p.tiles_q : p.tiles_p;
-        const int32_t r = fast_div(w, p.fd_other), o = w - r * other;
-        int32_t g = 0;                                   // groups whose tiles all come before r
-        for (int32_t base = 0; base < p.groups; base += 32) {
-            const int32_t e = base + static_cast<int32_t>(lane);
-            const uint32_t before = __ballot_sync(0xffffffffu, e < p.groups && pre[e + 1] <= r);
-            g += __popc(before);
-            if (before != 0xffffffffu) break;
-        }
-        t.group = g;
-        const int32_t i = r - pre[g];
-        if (p.ragged == kRaggedP) {
-            t.p0 = off[g] + i * TP;
-            t.p_end = off[g + 1];
-            t.q0 = o * TQ;
-        } else {
-            t.q0 = off[g] + i * TQ;
-            t.q_end = off[g + 1];
-            t.p0 = o * TP;
-        }
-        return t;
-    }
-    if (p.ragged == kRaggedK) {
-        const int32_t per = p.tiles_p * p.tiles_q;
-        t.group = fast_div(w, p.fd_group);
-        w -= t.group * per;
-        t.kb0 = pre[t.group];
-        t.kbn = pre[t.group + 1] - t.kb0;
-    }
-    const int32_t sweep = p.raster * p.tiles_q;          // tiles of `raster` rows of tiles
-    const int32_t rg = fast_div(w, p.fd_sweep), first = rg * p.raster, size = min(p.raster, p.tiles_p - first), rem = w - rg * sweep;
-    const int32_t tq = fast_div(rem, size == p.raster ? p.fd_raster : p.fd_last);
-    t.p0 = (first + rem - tq * size) * TP;
-    t.q0 = tq * TQ;
-    return t;
-}
-
-// Clamped offsets and the prefix sums fp8_tile reads; one whole warp.
-__device__ __forceinline__ void fp8_scan_groups(const Fp8Params &p, int32_t *pre, int32_t *off, int32_t unit, uint32_t lane)
-{
-    int32_t carry = 0, last = 0;
-    for (int32_t base = 0; base < p.groups; base += 32) {
-        const int32_t e = base + static_cast<int32_t>(lane);
-        int32_t o = p.offsets[min(e, p.groups)];
-        o = min(max(o, 0), p.rows_ragged);
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {               // non-decreasing whatever the caller's values
-            const int32_t x = __shfl_up_sync(0xffffffffu, o, d);
-            if (static_cast<int32_t>(lane) >= d) o = max(o, x);
-        }
-        o = max(o, last);
-        int32_t nxt = __shfl_down_sync(0xffffffffu, o, 1);
-        if (lane == 31) nxt = max(o, min(max(p.offsets[min(e + 1, p.groups)], 0), p.rows_ragged));
-        last = __shfl_sync(0xffffffffu, nxt, 31);
-        int32_t n = e < p.groups ? (nxt - o + unit - 1) / unit : 0;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int32_t x = __shfl_up_sync(0xffffffffu, n, d);
-            if (static_cast<int32_t>(lane) >= d) n += x;
-        }
-        if (e < p.groups) {
-            off[e] = o;
-            off[e + 1] = nxt;
-            pre[e + 1] = p.ragged == kRaggedK ? min(carry + n, p.k_capacity) : carry + n;
-        }
-        carry += __shfl_sync(0xffffffffu, n, 31);
-    }
-    if (lane == 0) pre[0] = 0;
-}
-
-template <class T>
-__device__ __forceinline__ T fp8_to(float v);
-template <>
-__device__ __forceinline__ float fp8_to<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ __half fp8_to<__half>(float v) { return __float2half_rn(v); }
-template <>
-__device__ __forceinline__ __nv_bfloat16 fp8_to<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-
-__device__ __forceinline__ uint32_t fp8_pack2(float a, float b, __half)
-{
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-__device__ __forceinline__ uint32_t fp8_pack2(float a, float b, __nv_bfloat16)
-{
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
-
 // Where the column-scaled promotion keeps its sums: chunks of 16 rows x 32 columns, rows 0..15 before 16..31, each chunk by eights of
 // columns, each of those as the lane's column pair of row t / 4, then of row t / 4 + 8.  f: eight of columns, hi: eight of rows (0..3).
 template <int REPS = 4>
@@ -197,7 +90,7 @@ __host__ __device__ constexpr int fp8_frag_index(int f, int hi) { return (((f / 
 // ordinary stores of 4 bytes a lane.
 // FRAG: the sums lie as the fragments of 16 x 8 that the column-scaled promotion reads (see there), else a lane holds its row.
 template <class T, bool FRAG>
-__device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32_t staging, const Fp8Params &p, const CUtensorMap *tmap_c, const Fp8Tile &t,
+__device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32_t staging, const Fp8Params &p, const CUtensorMap *tmap_c, const ProductTile &t,
                                                int32_t row0, int32_t col0, uint32_t lane)
 {
     constexpr int kSize = static_cast<int>(sizeof(T));
@@ -223,7 +116,7 @@ __device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32
                     } else {
                         float x, y;
                         unpack_f32x2(v, x, y);
-                        st_shared_u32(at + ((static_cast<uint32_t>(n) & 7u) ^ fr) * 16u + fc * 4u, fp8_pack2(x, y, T()));
+                        st_shared_u32(at + ((static_cast<uint32_t>(n) & 7u) ^ fr) * 16u + fc * 4u, pack_pair(x, y, T()));
                     }
                 }
             }
@@ -240,7 +133,7 @@ __device__ __forceinline__ void fp8_store_rows(const uint64_t (&acc)[64], uint32
                         v[i] = __float_as_uint((i & 1) ? hi : lo);
                     } else {
                         unpack_f32x2(acc[j * 4 + i], lo, hi);
-                        v[i] = fp8_pack2(lo, hi, T());
+                        v[i] = pack_pair(lo, hi, T());
                     }
                 }
                 st_shared_v4(mine + (j / 8) * 4096u + (((j & 7u) ^ swz) * 16u), v[0], v[1], v[2], v[3]);
@@ -334,7 +227,7 @@ template <class T>
 __device__ __forceinline__ void fp8_store_one(T *dst, float v, int32_t accumulate)
 {
     if constexpr (sizeof(T) == 4) *dst = accumulate ? *dst + v : v;
-    else *dst = fp8_to<T>(v);
+    else *dst = narrow_to<T>(v);
 }
 
 // CG: CTAs per tile.  BN: rows of Q per tile.  P_ROW: P has a scale per row (else one per 128 rows).  Q_COL: Q has a scale per row
@@ -398,7 +291,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
     if (warp == 1) tmem_alloc<CG>(smem_addr(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
     // No thread reads or writes global memory before the kernels ahead in the stream are complete.
     grid_dependency_wait();
-    if (warp == 2 && p.groups > 0) fp8_scan_groups(p, pre, off, p.ragged == kRaggedK ? kFp8Block : p.ragged == kRaggedP ? TP : TQ, lane);
+    if (warp == 2 && p.groups > 0) scan_groups(p, pre, off, p.ragged == kRaggedK ? kFp8Block : p.ragged == kRaggedP ? TP : TQ, lane);
     tc_fence_before_sync();
     __syncthreads();
     if (in_cluster) {
@@ -410,7 +303,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
     const int32_t total = p.ragged == kRaggedP ? pre[p.groups] * p.tiles_q : p.ragged == kRaggedQ ? pre[p.groups] * p.tiles_p : p.total;
 
     auto tile_of = [&](int32_t w) {
-        Fp8Tile t = fp8_tile<TP, TQ>(w, p, pre, off, lane);
+        ProductTile t = product_tile<TP, TQ>(w, p, pre, off, lane);
         if (CG == 1 && p.split > 1) {                              // this CTA's share of the contraction
             const int32_t b = t.kbn * static_cast<int32_t>(rank) / p.split, e = t.kbn * (static_cast<int32_t>(rank) + 1) / p.split;
             t.kb0 += b;
@@ -427,7 +320,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         const uint32_t full_leader = CG == 2 ? mapa(bar_full, 0) : bar_full;
         bool ok = true;
         for (int32_t w = unit; ok && w < total; w += units) {
-            const Fp8Tile t = tile_of(w);
+            const ProductTile t = tile_of(w);
             const int32_t prow = t.p0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * 128, qrow = t.q0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * (BN / CG);
             const int32_t pz = p.ragged == kRaggedQ ? t.group : 0, qz = p.ragged == kRaggedP ? t.group : 0;      // the operand with one matrix per group
             for (int32_t kb = 0; kb < t.kbn; ++kb) {
@@ -520,7 +413,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         uint32_t it = 0;
         bool ok = true;
         for (int32_t w = unit; ok && w < total; w += units) {
-            const Fp8Tile t = tile_of(w);
+            const ProductTile t = tile_of(w);
             const int32_t prow = t.p0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * 128;
             const float *sp = p.sp + t.group * p.sp_group + t.kb0 * p.sp_kb, *sq = p.sq + t.group * p.sq_group + t.kb0 * p.sq_kb;
             for (int32_t kb = 0; kb < t.kbn; ++kb, ++it, sp += p.sp_kb, sq += p.sq_kb) {
@@ -688,7 +581,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                     if (ok && kb + 3 < kbn) block(std::integral_constant<uint32_t, 3>(), kb + 4 == kbn);
                 }
             }
-            const Fp8Tile t = tile_of(w);
+            const ProductTile t = tile_of(w);
             if (!ok) break;
             if constexpr (CG == 2) {
                 const int32_t row0 = t.p0 + static_cast<int32_t>(rank * 128u + quarter * 32u), col0 = t.q0 + static_cast<int32_t>(half) * 64;
@@ -746,7 +639,7 @@ fp8_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         cluster_arrive();
         cluster_wait();
         if (unit < total && !*abort_flag) {
-            const Fp8Tile t = fp8_tile<TP, TQ>(unit, p, pre, off, lane);
+            const ProductTile t = product_tile<TP, TQ>(unit, p, pre, off, lane);
             const int32_t share = BN / p.split, row = t.p0 + static_cast<int32_t>(lane) * 4;
             for (int32_t c = static_cast<int32_t>(rank) * share + static_cast<int32_t>(warp); c < (static_cast<int32_t>(rank) + 1) * share; c += kFp8Threads / 32) {
                 const int32_t col = t.q0 + c;

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "../../include/hgemm.h"
+#include "../../include/hgemm_fp4.h"
 #include "../../include/hgemm_fp8.h"
 #include "hgemm_context.h"
 #include "hgemm_kernel.cuh"
@@ -514,6 +515,7 @@ hgemm_status_t hgemm_destroy(hgemm_ctx_t *ctx)
     if (!ctx) return HGEMM_ERR_INVALID_ARG;
     while (!ctx->plans.empty()) hgemm_plan_destroy(ctx->plans.back());
     while (!ctx->fp8_plans.empty()) hgemm_fp8_plan_destroy(ctx->fp8_plans.back());
+    while (!ctx->fp4_plans.empty()) hgemm_fp4_plan_destroy(ctx->fp4_plans.back());
     if (ctx->d_status) cudaFree(ctx->d_status);
     if (ctx->copy_in) cudaStreamDestroy(ctx->copy_in);
     if (ctx->copy_out) cudaStreamDestroy(ctx->copy_out);
@@ -1062,6 +1064,11 @@ hgemm_status_t hgemm_ctx_last_device_status(hgemm_ctx_t *ctx, uint32_t *code)
         if (s != HGEMM_OK) return s;
     }
     for (const hgemm_fp8_plan_s *pl : ctx->fp8_plans) {
+        const uint32_t w = words[size_t(hgemm_host::status_slot_of(pl))];
+        any = any || w != 0;
+        if (v == 0) v = w;
+    }
+    for (const hgemm_fp4_plan_s *pl : ctx->fp4_plans) {
         const uint32_t w = words[size_t(hgemm_host::status_slot_of(pl))];
         any = any || w != 0;
         if (v == 0) v = w;

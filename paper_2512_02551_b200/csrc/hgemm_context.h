@@ -10,6 +10,7 @@
 #include "../../include/hgemm.h"
 
 struct hgemm_fp8_plan_s;
+struct hgemm_fp4_plan_s;
 
 typedef CUresult (*encode_tiled_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                     const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
@@ -32,6 +33,7 @@ struct hgemm_ctx_s {
     bool tma_3d = true;
     std::vector<hgemm_plan_s *> plans;
     std::vector<hgemm_fp8_plan_s *> fp8_plans;
+    std::vector<hgemm_fp4_plan_s *> fp4_plans;
     // hgemm_run_host: the operand copies and the result copy run on streams of their own (created by its first call), so that
     // one call's copies overlap the compute and the opposite-direction copy of the calls around it
     cudaStream_t copy_in = nullptr, copy_out = nullptr;
@@ -39,6 +41,7 @@ struct hgemm_ctx_s {
 
 namespace hgemm_host {
 int status_slot_of(const hgemm_fp8_plan_s *plan);   // the plan's word in the context's status array
+int status_slot_of(const hgemm_fp4_plan_s *plan);
 // Synchronises the device, reads a status word and clears it: HGEMM_OK, or what the word stands for.
 hgemm_status_t take_status_word(hgemm_ctx_s *ctx, int slot, uint32_t *code);
 // One small kernel whose only wait is on a barrier that nothing signals; it reports to the slot.

@@ -133,4 +133,15 @@ __device__ __forceinline__ uint64_t make_smem_desc_sw128_mn_major(uint32_t smem_
     return d;
 }
 
+// Shared-memory matrix descriptor of 32 rows of 16 bytes that follow one another (no swizzle): groups of 8 rows are 128 bytes apart.
+__device__ __forceinline__ uint64_t make_smem_desc_rows16(uint32_t smem_byte_addr)
+{
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((smem_byte_addr & 0x3ffffu) >> 4);
+    d |= static_cast<uint64_t>(128 >> 4) << 16;
+    d |= static_cast<uint64_t>(128 >> 4) << 32;
+    d |= static_cast<uint64_t>(1) << 46;
+    return d;
+}
+
 } // namespace hgemm_dev

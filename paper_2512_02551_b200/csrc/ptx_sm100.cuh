@@ -669,6 +669,38 @@ __device__ __forceinline__ void regs_lower()
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS));
 }
 
+// ---- 4-bit operands with block scales -----------------------------------------------------
+
+// D[tmem] (+)= (A scaled) * (B scaled), e2m1 operands packed two to a byte, K = 64 per instruction, fp32 accumulation.  The scales lie in tensor memory, one
+// 32-bit word per row: four e4m3 scales of 16 elements each (NV), or four powers of two of 32 elements each, of which the instruction descriptor
+// picks a pair.
+template <int CTA_GROUP, bool NV>
+__device__ __forceinline__ void umma_f4_elect(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t a_scales, uint32_t b_scales, uint32_t accumulate)
+{
+#define HGEMM_UMMA_F4(KIND) \
+    asm volatile( \
+        "{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.b32 p, %6, 0;\n\t" \
+        "@e tcgen05.mma." KIND " [%0], %1, %2, %3, [%4], [%5], p;\n\t}" \
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(a_scales), "r"(b_scales), "r"(accumulate) \
+        : "memory")
+    if constexpr (CTA_GROUP == 1 && NV) HGEMM_UMMA_F4("cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X");
+    else if constexpr (CTA_GROUP == 1) HGEMM_UMMA_F4("cta_group::1.kind::mxf4.block_scale.scale_vec::2X");
+    else if constexpr (NV) HGEMM_UMMA_F4("cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X");
+    else HGEMM_UMMA_F4("cta_group::2.kind::mxf4.block_scale.scale_vec::2X");
+#undef HGEMM_UMMA_F4
+}
+
+// 32 rows of 16 bytes from shared memory to four 32-bit columns of tensor memory, the same in each quarter of the lanes (of both CTAs of a pair, from the
+// shared memory of each).  Ordered with the MMAs that the same thread issues.
+template <int CTA_GROUP>
+__device__ __forceinline__ void tmem_copy_scales_elect(uint32_t taddr, uint64_t desc)
+{
+    if constexpr (CTA_GROUP == 1)
+        asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t@e tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc) : "memory");
+}
+
 // ---- small helpers ------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t pack_half2_rn(uint32_t a_f32_bits, uint32_t b_f32_bits)
