@@ -1,0 +1,296 @@
+"""The layer of experts for a few tokens on the GPU, against the formula in 64 bits.
+
+Results sit inside guard bands, x's and the weights' rows inside NaN; the tolerance follows from the arithmetic (see ``check``)."""
+import ctypes
+import zlib
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import fp4_reference as ref  # noqa: E402
+from paper_2512_02551_b200 import few_tokens, fp4, hgemm, routing  # noqa: E402
+
+DTYPE = {"bf16": torch.bfloat16, "f16": torch.float16}
+KINDS = [("bf16", "bf16"), ("f16", "f16"), ("nvfp4", "bf16"), ("nvfp4", "f16"), ("mxfp4", "bf16"), ("mxfp4", "f16")]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    assert torch.cuda.is_available(), "these tests need a B200"
+    with hgemm.Context(0) as c:
+        yield c
+
+
+def rng(*key):
+    return np.random.default_rng(zlib.crc32(repr(key).encode()))
+
+
+def wide(t, extra, offset=0):
+    """A copy of a matrix or a stack whose rows are `extra` elements further apart than they need be, NaN between them, `offset` elements into its buffer."""
+    shape = (*t.shape[:-1], t.shape[-1] + extra)
+    buf = torch.full((offset + int(np.prod(shape)) + 8,), float("nan"), dtype=t.dtype, device="cuda")
+    v = buf[offset:offset + int(np.prod(shape))].view(shape)[..., :t.shape[-1]]
+    v.copy_(t)
+    return v
+
+
+def weights_of(r, shape, kind, extra=0, offset=0):
+    """(what the call takes, values in 64 bits)."""
+    E, N, K = shape
+    if kind in DTYPE:
+        w = torch.from_numpy(r.standard_normal(shape) * K ** -0.5).to(DTYPE[kind])
+        return wide(w, extra, offset), ref.f64(w)
+    code = r.integers(0, 16, shape).astype(np.uint8)
+    lo, hi = ((0x28, 0x48) if kind == "nvfp4" else (122, 130))
+    s = r.integers(lo, hi, (E, N, ref.blocks(K, kind))).astype(np.uint8)
+    factor = (np.exp2(r.integers(-2, 3, E)) * 1.25 / 8 * K ** -0.5).astype(np.float32) if kind == "nvfp4" else np.ones(E, np.float32)
+    if kind == "mxfp4":
+        s -= np.uint8(np.log2(K) // 2 + 2)
+    packed = ref.pack(code)
+    pitch = -(-packed.shape[-1] // 16) * 16 + 16 * (extra > 0)
+    buf = np.full((E, N, pitch), 0x77, np.uint8)
+    buf[..., :packed.shape[-1]] = packed
+    q = torch.from_numpy(buf).cuda()[..., :packed.shape[-1]]
+    tiles = torch.from_numpy(ref.tiles_from(s, kind)).cuda()
+    values = ref.decode(code) * ref.spread(ref.scale_values(s, kind), kind, K) * factor.astype(np.float64)[:, None, None]
+    return (q, tiles, torch.from_numpy(factor).cuda()) if kind == "nvfp4" else (q, tiles), values
+
+
+def silu(u):
+    with np.errstate(over="ignore"):
+        return u / (1 + np.exp(-u))
+
+
+def formula(x, w1, w2, indices, weights, gated):
+    """(y, bound of the error before y's rounding) in 64 bits.
+
+    The contraction over `hidden` adds H numbers in 32 bits (2^-23 of their magnitudes each covers truncation); silu changes by at most 1.1 times its
+    argument's error, and its exponential is off by 2^-21 (2 + |u|) of itself; h keeps 16 bits (2^-17 with the product's rounding); an fp16 weight
+    against h loses the product of two second parts, 2^-17; then I, and k, numbers are added."""
+    T, H = x.shape
+    E, I = w1.shape[0], w2.shape[-1]
+    y, err = np.zeros((T, H)), np.zeros((T, H))
+    for t in range(T):
+        for j in range(indices.shape[1]):
+            e = indices[t, j]
+            if not 0 <= e < E:
+                continue
+            u = w1[e] @ x[t]
+            du = (H + 8) * 2.0 ** -23 * (np.abs(w1[e]) @ np.abs(x[t]))
+            g = silu(u[:I])
+            dg = 1.1 * du[:I] + np.abs(g) * (2 + np.abs(u[:I])) * 2.0 ** -21
+            h, dh = (g * u[I:], np.abs(u[I:]) * dg + (np.abs(g) + dg) * du[I:]) if gated else (g, dg)
+            dh = dh + np.abs(h) * 2.0 ** -17 + 2.0 ** -130
+            z = w2[e] @ h
+            mag = np.abs(w2[e]) @ np.abs(h)
+            w = weights[t, j]
+            y[t] += w * z
+            err[t] += np.abs(w) * (np.abs(w2[e]) @ dh + ((I + indices.shape[1] + 8) * 2.0 ** -23 + 2.0 ** -17) * mag)
+    return y, err
+
+
+def check(got, y, err, what=""):
+    bound = err + ref.UNIT[got.dtype] * (np.abs(y) + err) + ref.SMALLEST[got.dtype]
+    off = np.abs(ref.f64(got) - y)
+    bad = ~(off <= bound)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.size} off, first at {np.argwhere(bad)[0]}: off {off[bad][0]:.3g}, bound {bound[bad][0]:.3g}"
+
+
+def case(ctx, kind, dtype, T, H, I, E, k, gated, extra=0, offset=0, indices=None):
+    r = rng(kind, dtype, T, H, I, E, k, gated)
+    dt = DTYPE[dtype]
+    x = torch.from_numpy(r.standard_normal((T, H))).to(dt)
+    w1, v1 = weights_of(r, (E, I * (2 if gated else 1), H), kind, extra, offset)
+    w2, v2 = weights_of(r, (E, H, I), kind, extra, offset)
+    if indices is None:
+        indices = np.stack([r.permutation(E)[:k] for _ in range(T)]) if k <= E else r.integers(0, E, (T, k))
+    weights = r.random((T, k)).astype(np.float32)
+    layer = few_tokens.Layer(ctx, H, I, E, k, weights=kind, activation="swiglu" if gated else "silu", dtype=dt)
+    buf = torch.full((offset + T * (H + extra) + 64,), float("nan"), dtype=dt, device="cuda")
+    y = buf[offset:offset + T * (H + extra)].view(T, H + extra)[:, :H]
+    scratch = layer.empty_scratch(T)
+    scratch.fill_(0xFF)                                            # NaN
+    xs = wide(x, extra, offset)
+    layer.run(xs, w1, w2, torch.tensor(indices, dtype=torch.int32, device="cuda"), torch.from_numpy(weights).cuda(), y, scratch)
+    torch.cuda.synchronize()
+    keep = torch.ones_like(buf, dtype=torch.bool)
+    keep.as_strided(y.shape, y.stride(), y.storage_offset()).fill_(False)
+    assert bool(torch.isnan(buf[keep]).all()), "something outside the result was written"
+    check(y, *formula(ref.f64(x), v1, v2, indices, weights.astype(np.float64), gated), f"{kind} {dtype} {T}x{H}x{I}, {k} of {E}")
+    return y
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("T,k,E", [(1, 1, 1), (1, 8, 16), (2, 2, 5), (8, 2, 3), (9, 1, 1), (17, 2, 2), (33, 4, 7), (64, 2, 3)])
+def test_tokens_and_experts(ctx, kind, dtype, T, k, E):
+    case(ctx, kind, dtype, T, 256, 192, E, k, True)
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("H,I", [(1, 1), (7, 9), (16, 8), (64, 100), (129, 77), (256, 33), (333, 520), (1000, 40), (2048, 24), (40, 2050)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_extents(ctx, kind, dtype, H, I, gated):
+    case(ctx, kind, dtype, 3, H, I, 4, 2, gated)
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("extra,offset", [(1, 0), (2, 0), (8, 0), (0, 1), (0, 2), (3, 5)])
+def test_strides_and_alignment(ctx, kind, dtype, extra, offset):
+    for H, I in ((96, 130), (131, 65)):
+        case(ctx, kind, dtype, 5, H, I, 3, 2, True, extra, offset)
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS[::2])
+def test_choices_outside_twice_and_none(ctx, kind, dtype):
+    """Numbers outside the experts count as zero; an expert chosen twice counts twice; a token, or all of them, may have no expert."""
+    E = 3
+    indices = np.array([[0, 0, 2], [-1, 5, 1], [E, -7, 1 << 30], [2, 2, 2], [1, 0, -(1 << 31)]], dtype=np.int64)
+    case(ctx, kind, dtype, 5, 128, 64, E, 3, True, indices=indices)
+    y = case(ctx, kind, dtype, 2, 128, 64, E, 3, False, indices=np.full((2, 3), -1))
+    assert bool((y == 0).all())
+
+
+@pytest.mark.parametrize("kind,dtype", [("nvfp4", "bf16"), ("bf16", "bf16")])
+def test_most_choices(ctx, kind, dtype):
+    case(ctx, kind, dtype, 64, 64, 48, 40, 32, True)
+    case(ctx, kind, dtype, 64, 48, 40, 1, 32, False, indices=np.zeros((64, 32), np.int64))
+
+
+def test_many_experts_and_rounds(ctx):
+    """More tiles than warps: every warp walks on to further experts."""
+    case(ctx, "nvfp4", "bf16", 24, 512, 1024, 96, 8, True)
+    case(ctx, "f16", "f16", 24, 512, 1024, 64, 4, False)
+
+
+def test_infinite_and_nan_inputs_stay_in_their_token(ctx):
+    for kind, dtype in KINDS:
+        r = rng(kind, dtype)
+        dt = DTYPE[dtype]
+        w1, _ = weights_of(r, (4, 64, 128), kind)
+        w2, _ = weights_of(r, (4, 128, 32), kind)
+        x = torch.randn(6, 128, device="cuda").to(dt)
+        layer = few_tokens.Layer(ctx, 128, 32, 4, 2, weights=kind, dtype=dt)
+        idx, w = torch.tensor([[0, 1]] * 6, dtype=torch.int32, device="cuda"), torch.full((6, 2), 0.5, device="cuda")
+        clean, y, s = torch.empty_like(x), torch.empty_like(x), layer.empty_scratch(6)
+        layer.run(x, w1, w2, idx, w, clean, s)
+        x[1, 5], x[4, 100] = float("nan"), float("inf")
+        layer.run(x, w1, w2, idx, w, y, s)
+        rest = [0, 2, 3, 5]
+        assert torch.equal(y[rest], clean[rest])
+        assert not torch.isfinite(y[1].float()).any() and not torch.isfinite(y[4].float()).all()
+
+
+def test_large_h_and_small_x(ctx):
+    """h beyond fp16's range, and x among its smallest numbers: no range is lost on the way."""
+    for kind, dtype, scale in (("f16", "f16", 2.0 ** 7), ("nvfp4", "f16", 2.0 ** 7), ("mxfp4", "f16", 2.0 ** -14), ("f16", "f16", 2.0 ** -14), ("bf16", "bf16", 2.0 ** -60), ("nvfp4", "bf16", 2.0 ** -60)):
+        r = rng(kind, dtype, 3)
+        dt = DTYPE[dtype]
+        w1, v1 = weights_of(r, (2, 128, 64), kind)
+        w2, v2 = weights_of(r, (2, 64, 64), kind)
+        x = torch.from_numpy(r.standard_normal((4, 64)) * scale * 8).to(dt)
+        layer = few_tokens.Layer(ctx, 64, 64, 2, 1, weights=kind, dtype=dt)
+        idx, w = np.array([[0], [1], [0], [1]]), np.full((4, 1), 2.0 ** -12 if scale > 1 else 1.0, np.float32)
+        y = torch.empty(4, 64, dtype=dt, device="cuda")
+        layer.run(x.cuda(), w1, w2, torch.tensor(idx, dtype=torch.int32, device="cuda"), torch.from_numpy(w).cuda(), y, layer.empty_scratch(4))
+        check(y, *formula(ref.f64(x), v1, v2, idx, w.astype(np.float64), True), f"{kind} {dtype} {scale}")
+
+
+def test_with_the_quantiser_and_the_router(ctx):
+    """As a decoding step uses it: routed by the library, weights made by its quantiser."""
+    T, H, I, E, k = 11, 320, 136, 12, 3
+    g = torch.Generator(device="cuda").manual_seed(2)
+    for fmt in ("nvfp4", "mxfp4"):
+        ops = []
+        for shape in ((E, 2 * I, H), (E, H, I)):
+            w = torch.randn(*shape, generator=g, device="cuda") * shape[-1] ** -0.5
+            f = None
+            if fmt == "nvfp4":
+                f = torch.empty(E, device="cuda")
+                fp4.tensor_factor(ctx, w, f)
+            q, s = fp4.empty_rows(*shape, format=fmt)
+            fp4.quantize_rows(ctx, w, q, s, factor=f, format=fmt)
+            back = torch.empty_like(w)
+            fp4.dequantize(ctx, q, s, back, factor=f, format=fmt)
+            ops.append(((q, s) if f is None else (q, s, f), ref.f64(back)))
+        router = routing.Router(ctx, E, k, score="softmax", renormalize=True)
+        logits = torch.randn(T, E, generator=g, device="cuda")
+        weights, indices = torch.empty(T, k, device="cuda"), torch.empty(T, k, dtype=torch.int32, device="cuda")
+        x = torch.randn(T, H, generator=g, device="cuda").bfloat16()
+        y = torch.empty_like(x)
+        layer = few_tokens.Layer(ctx, H, I, E, k, weights=fmt)
+        router.forward(logits, weights, indices)
+        layer.run(x, ops[0][0], ops[1][0], indices, weights, y, layer.empty_scratch(T))
+        check(y, *formula(ref.f64(x), ops[0][1], ops[1][1], indices.cpu().numpy(), ref.f64(weights), True), fmt)
+
+
+def test_captured_replayed_and_at_once(ctx):
+    """Two captured layers with scratch memory of their own, replayed on two streams at once and over and over, on new inputs: the bits of single calls."""
+    r = rng(8)
+    E, H, I, k, T = 8, 512, 256, 2, 7
+    w1, _ = weights_of(r, (E, 2 * I, H), "nvfp4")
+    w2, _ = weights_of(r, (E, H, I), "nvfp4")
+    layer = few_tokens.Layer(ctx, H, I, E, k)
+    x = torch.randn(T, H, device="cuda").bfloat16()
+    idx, w = torch.zeros(T, k, dtype=torch.int32, device="cuda"), torch.rand(T, k, device="cuda")
+    ys, scratches, graphs = [torch.empty_like(x) for _ in range(2)], [layer.empty_scratch(T) for _ in range(2)], []
+    run = lambda i: layer.run(x, w1, w2, idx, w, ys[i], scratches[i])  # noqa: E731
+    run(0)
+    torch.cuda.synchronize()
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            run(i)
+            run(i)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for n in range(4):
+        x.copy_(torch.randn(T, H, device="cuda"))
+        idx.copy_(torch.from_numpy(r.integers(-1, E, (T, k))))
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for i in range(2):
+                with torch.cuda.stream(streams[i]):
+                    graphs[i].replay()
+        torch.cuda.synchronize()
+        got = [y.clone() for y in ys]
+        run(0)
+        assert torch.equal(got[0], ys[0]) and torch.equal(got[1], ys[0])
+
+
+def test_no_tokens(ctx):
+    layer = few_tokens.Layer(ctx, 64, 64, 2, 1, weights="bf16", dtype=torch.bfloat16, activation="silu")
+    w = torch.zeros(2, 64, 64, dtype=torch.bfloat16, device="cuda")
+    x = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
+    layer.run(x, w, w, torch.empty(0, 1, dtype=torch.int32, device="cuda"), torch.empty(0, 1, device="cuda"), x.clone(), layer.empty_scratch(0))
+
+
+def test_refusals(ctx):
+    with pytest.raises(ValueError):
+        few_tokens.Layer(ctx, 64, 64, 2, 1, weights="int4")
+    with pytest.raises(ValueError):
+        few_tokens.Layer(ctx, 64, 64, 2, 1, weights="f16", dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        few_tokens.Layer(ctx, 64, 64, 2, 33)
+    layer = few_tokens.Layer(ctx, 64, 64, 2, 1, weights="bf16", activation="silu")
+    with pytest.raises(ValueError):
+        layer.empty_scratch(65)
+    new = lambda *s, dtype=torch.bfloat16: torch.zeros(*s, dtype=dtype, device="cuda")  # noqa: E731
+    x, w, idx, wt, s = new(3, 64), new(2, 64, 64), new(3, 1, dtype=torch.int32), new(3, 1, dtype=torch.float32), layer.empty_scratch(3)
+    layer.run(x, w, w, idx, wt, x.clone(), s)
+    for bad in (dict(x=new(3, 63)), dict(x=x.half()), dict(w1=w.half()), dict(w2=new(2, 64, 65)), dict(indices=idx.long()), dict(weights=wt.half()), dict(y=new(2, 64)), dict(w1=(w, w))):
+        with pytest.raises((ValueError, AttributeError)):
+            layer.run(**{**dict(x=x, w1=w, w2=w, indices=idx, weights=wt, y=x.clone(), scratch=s), **bad})
+    with pytest.raises(hgemm.HgemmError):
+        layer.run(x, w, w, idx, wt, x.clone(), layer.empty_scratch(2))                    # too little scratch memory
+    with pytest.raises(hgemm.HgemmError):
+        layer.run(new(65, 64), w, w, new(65, 1, dtype=torch.int32), new(65, 1, dtype=torch.float32), new(65, 64), layer.empty_scratch(64))
+    L, d = few_tokens.lib(), layer._desc
+    m = few_tokens.Weights(w.data_ptr(), 64, None, None)
+    args = [ctypes.byref(d), 3, x.data_ptr(), 64, ctypes.byref(m), ctypes.byref(m), idx.data_ptr(), wt.data_ptr(), x.data_ptr(), 64, s.data_ptr(), s.numel(), None]
+    for i, v in ((0, None), (1, -1), (1, 65), (2, None), (2, x.data_ptr() + 1), (3, 63), (4, None), (4, ctypes.byref(few_tokens.Weights(None, 64, None, None))),
+                 (4, ctypes.byref(few_tokens.Weights(w.data_ptr(), 63, None, None))), (4, ctypes.byref(few_tokens.Weights(w.data_ptr() + 1, 64, None, None))),
+                 (5, ctypes.byref(few_tokens.Weights(w.data_ptr(), 64, w.data_ptr(), None))), (5, ctypes.byref(few_tokens.Weights(w.data_ptr(), 64, None, wt.data_ptr()))),
+                 (6, None), (6, idx.data_ptr() + 2), (7, None), (8, None), (8, x.data_ptr() + 1), (9, 63), (10, None), (10, s.data_ptr() + 8), (11, 16)):
+        assert L.hgemm_few_tokens(ctx._h, *[v if j == i else a for j, a in enumerate(args)]) == hgemm.ERR_INVALID_ARG, (i, v)
