@@ -1,15 +1,18 @@
 /*
- * hgemm_few_tokens.h -- a layer of experts for the few tokens of a decoding step, in two launches.
+ * hgemm_few_tokens.h -- a layer of experts for the few tokens of a decoding step.
  *
  *     h[t,j] = act(W1[e] x[t])            e = indices[t,j]:  the experts that token t's router chose (hgemm_route)
  *     y[t]   = sum over j of  weights[t,j] * (W2[e] h[t,j])
  *
  * with act(u) = u / (1 + exp(-u)) (SILU; W1[e] has `inner` rows), or act(g, u) = g / (1 + exp(-g)) * u (SWIGLU; W1[e] has 2 * inner rows, those of g first).
- * W1 is experts x (inner or 2 * inner) x hidden, W2 is experts x hidden x inner.  Only the chosen experts' weights are read, each once for up to 16 of its
+ * W1 is experts x (inner or 2 * inner) x hidden, W2 is experts x hidden x inner.  Only the chosen experts' weights are read, each once for up to 8 of its
  * choices.  Weights are fp16 or bf16, of x's type, or 4-bit row copies with block scales (hgemm_fp4.h) with x of either type.
  *
- * All sums are in fp32.  x and the weights enter the products as they are (4-bit values times their scale exactly); h is held to 16 bits of mantissa; the result is
- * rounded once.  Results do not depend on scheduling: a token's choices are added up in their order.
+ * All sums are in fp32, and the result is rounded once; a token's choices are added up in their order, so that results do not depend on scheduling.
+ *     16-bit weights    two launches; x and the weights enter the products as they are, h to 16 bits of mantissa (bf16), or to 11 bits, scaled by a power of two for
+ *                       each choice (fp16: what is below 2^-39 of its largest magnitude is lost)
+ *     4-bit weights     five launches; the weights enter the products as they are, x and h as sums of 4-bit digits: off by at most 2^-19 of the token's (the
+ *                       choice's) largest magnitude.  A NaN or an infinity in x makes its token's results NaN
  *
  * Choices with an index outside [0, experts) count as zero.  A token may choose an expert twice.
  *

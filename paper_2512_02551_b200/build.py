@@ -16,7 +16,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhgemm.so")
 LIB_CHECKED = os.path.join(HERE, "libhgemm_checked.so")      # the same sources with -DHGEMM_CHECKED=1 (see include/hgemm.h)
 SOURCES = ["hgemm_api.cu", "hgemm_static_scratch.cu", "hgemm_planner.cpp", "hgemm_table.cpp", "fp8_api.cu", "fp4_api.cu", "few_tokens_api.cu", "routing_api.cu"]
-DEPS = SOURCES + ["hgemm_context.h", "hgemm_device.cuh", "product_tiles.cuh", "fp8_product_kernel.cuh", "fp8_quantize_kernel.cuh", "fp4_product_kernel.cuh", "fp4_quantize_kernel.cuh", "few_tokens_kernel.cuh", "routing_kernel.cuh", "hgemm_kernel.cuh", "hgemm_light_kernel.cuh", "hgemm_small_kernel.cuh", "ptx_sm100.cuh", "hgemm_planner.h", "hgemm_table.inc",
+DEPS = SOURCES + ["hgemm_context.h", "hgemm_device.cuh", "product_tiles.cuh", "fp8_product_kernel.cuh", "fp8_quantize_kernel.cuh", "fp4_product_kernel.cuh", "fp4_quantize_kernel.cuh", "few_tokens_kernel.cuh", "few_digits_kernel.cuh", "routing_kernel.cuh", "hgemm_kernel.cuh", "hgemm_light_kernel.cuh", "hgemm_small_kernel.cuh", "ptx_sm100.cuh", "hgemm_planner.h", "hgemm_table.inc",
                   os.path.join("..", "..", "include", "hgemm.h"), os.path.join("..", "..", "include", "hgemm_fp8.h"),
                   os.path.join("..", "..", "include", "hgemm_fp4.h"), os.path.join("..", "..", "include", "hgemm_few_tokens.h"),
                   os.path.join("..", "..", "include", "hgemm_routing.h")]

@@ -5,6 +5,7 @@
 #include <cstring>
 
 #include "../../include/hgemm_few_tokens.h"
+#include "few_digits_kernel.cuh"
 #include "few_tokens_kernel.cuh"
 #include "hgemm_context.h"
 
@@ -14,12 +15,17 @@ using hgemm_dev::FewWeights;
 namespace {
 
 constexpr int32_t kMaxWidth = 1 << 20;
+constexpr int kSmemOptIn = 232448;
+constexpr int kMaxX = 64 * 1024;                 // shared memory of the 16-bit kernels' first launch for x: two CTAs share an SM
+constexpr int kDigits = hgemm_dev::kDigits;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t up_to(int64_t a, int64_t unit) { return ceil_div(a, unit) * unit; }
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 bool is4(const hgemm_few_tokens_t &d) { return d.weights == HGEMM_WEIGHTS_NVFP4 || d.weights == HGEMM_WEIGHTS_MXFP4; }
-int32_t chunk_of(const hgemm_few_tokens_t &d) { return is4(d) ? 128 : 32; }
+int32_t format_of(const hgemm_few_tokens_t &d) { return d.weights == HGEMM_WEIGHTS_NVFP4 ? HGEMM_FP4_NV : HGEMM_FP4_MX; }
+int32_t up_rows(const hgemm_few_tokens_t &d) { return d.activation == HGEMM_ACT_SWIGLU ? 2 * d.inner : d.inner; }
 
 bool legal(const hgemm_few_tokens_t &d)
 {
@@ -31,51 +37,38 @@ bool legal(const hgemm_few_tokens_t &d)
     return is4(d);
 }
 
-int64_t h_stride(const hgemm_few_tokens_t &d) { return ceil_div(d.inner, chunk_of(d)) * chunk_of(d); }
+// ---- 16-bit weights ------------------------------------------------------------------------------------------------
 
-bool fill(FewWeights *w, const hgemm_few_tokens_t &d, const hgemm_expert_weights_t &m, int32_t rows, int32_t depth)
+// h of a choice in scratch memory: whole chunks; behind all of them the largest magnitude of each eight
+int64_t h_stride(const hgemm_few_tokens_t &d) { return up_to(d.inner, hgemm_dev::kFewChunk); }
+
+FewWeights weights16(const hgemm_expert_weights_t &m, int32_t rows, int32_t depth)
 {
-    const bool four = is4(d);
-    if (!m.values || (d.weights == HGEMM_WEIGHTS_NVFP4) != (m.factor != nullptr) || four != (m.scales != nullptr) || !aligned4(m.factor)) return false;
-    if (four ? m.ld < ceil_div(depth, 2) || (m.ld & 15) != 0 || !aligned16(m.values) || !aligned16(m.scales) : m.ld < depth || (reinterpret_cast<uintptr_t>(m.values) & 1u) != 0) return false;
-    w->values = static_cast<const uint8_t *>(m.values);
-    w->ld = four ? m.ld : m.ld * 2;
-    w->matrix = w->ld * rows;
-    w->scales = static_cast<const uint8_t *>(m.scales);
-    w->atoms = int32_t(ceil_div(depth, d.weights == HGEMM_WEIGHTS_NVFP4 ? 64 : 128));
-    w->scale_matrix = ceil_div(rows, 128) * w->atoms * 512;
-    w->factor = m.factor;
-    w->rows = rows;
-    w->depth = depth;
-    w->align = aligned16(m.values) && w->ld % 16 == 0 ? 16 : aligned4(m.values) && w->ld % 4 == 0 ? 4 : 2;
-    return true;
+    FewWeights w;
+    w.values = static_cast<const uint8_t *>(m.values);
+    w.ld = m.ld * 2;
+    w.matrix = w.ld * rows;
+    w.rows = rows;
+    w.depth = depth;
+    w.align = aligned16(m.values) && w.ld % 16 == 0 ? 16 : aligned4(m.values) && w.ld % 4 == 0 ? 4 : 2;
+    return w;
 }
 
-const void *up_kernel(const hgemm_few_tokens_t &d)
+template <class T>
+const void *up_kernel(int align)
 {
     using namespace hgemm_dev;
-    const bool x16 = d.type == HGEMM_TYPE_F16;
-    switch (d.weights) {
-    case HGEMM_WEIGHTS_F16: return reinterpret_cast<const void *>(few_up_kernel<kFewF16, true>);
-    case HGEMM_WEIGHTS_BF16: return reinterpret_cast<const void *>(few_up_kernel<kFewBf16, false>);
-    case HGEMM_WEIGHTS_NVFP4: return x16 ? reinterpret_cast<const void *>(few_up_kernel<kFewNv, true>) : reinterpret_cast<const void *>(few_up_kernel<kFewNv, false>);
-    default: return x16 ? reinterpret_cast<const void *>(few_up_kernel<kFewMx, true>) : reinterpret_cast<const void *>(few_up_kernel<kFewMx, false>);
-    }
+    return align == 16 ? reinterpret_cast<const void *>(few_up_kernel<T, 16>) : align == 4 ? reinterpret_cast<const void *>(few_up_kernel<T, 4>) : reinterpret_cast<const void *>(few_up_kernel<T, 2>);
 }
 
-const void *down_kernel(const hgemm_few_tokens_t &d)
+template <class T>
+const void *down_kernel(int align)
 {
     using namespace hgemm_dev;
-    const bool y16 = d.type == HGEMM_TYPE_F16;
-    switch (d.weights) {
-    case HGEMM_WEIGHTS_F16: return reinterpret_cast<const void *>(few_down_kernel<kFewF16, __half>);
-    case HGEMM_WEIGHTS_BF16: return reinterpret_cast<const void *>(few_down_kernel<kFewBf16, __nv_bfloat16>);
-    case HGEMM_WEIGHTS_NVFP4: return y16 ? reinterpret_cast<const void *>(few_down_kernel<kFewNv, __half>) : reinterpret_cast<const void *>(few_down_kernel<kFewNv, __nv_bfloat16>);
-    default: return y16 ? reinterpret_cast<const void *>(few_down_kernel<kFewMx, __half>) : reinterpret_cast<const void *>(few_down_kernel<kFewMx, __nv_bfloat16>);
-    }
+    return align == 16 ? reinterpret_cast<const void *>(few_down_kernel<T, 16>) : align == 4 ? reinterpret_cast<const void *>(few_down_kernel<T, 4>) : reinterpret_cast<const void *>(few_down_kernel<T, 2>);
 }
 
-hgemm_status_t launch(hgemm_ctx_s *ctx, const void *fn, unsigned grid, int threads, int smem, FewParams *p, void *stream)
+hgemm_status_t launch(hgemm_ctx_s *ctx, const void *fn, dim3 grid, int threads, int smem, void *params, void *stream)
 {
     if (smem > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -83,7 +76,7 @@ hgemm_status_t launch(hgemm_ctx_s *ctx, const void *fn, unsigned grid, int threa
     }
     cudaLaunchConfig_t lc;
     std::memset(&lc, 0, sizeof(lc));
-    lc.gridDim = dim3(grid, 1, 1);
+    lc.gridDim = grid;
     lc.blockDim = dim3(unsigned(threads), 1, 1);
     lc.dynamicSmemBytes = size_t(smem);
     lc.stream = static_cast<cudaStream_t>(stream);
@@ -92,17 +85,184 @@ hgemm_status_t launch(hgemm_ctx_s *ctx, const void *fn, unsigned grid, int threa
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = attr;
     lc.numAttrs = ctx->dependent_launch ? 1 : 0;
-    void *args[1] = {p};
+    void *args[1] = {params};
     const cudaError_t e = cudaLaunchKernelExC(&lc, fn, args);
     return e == cudaSuccess ? HGEMM_OK : cuda_fail(ctx, e);
 }
 
-// Warps that share a contraction of `chunks` chunks: as many as leave each the four chunks that it fetches together, so that rounds of work are short and the last one too.
-int32_t slices_of(int64_t chunks, int64_t most)
+struct Call {
+    int64_t tokens;
+    const void *x;
+    int64_t ldx;
+    const int32_t *indices;
+    const float *weights;
+    void *y;
+    int64_t ldy;
+    uint8_t *scratch;
+    void *stream;
+};
+
+hgemm_status_t run16(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c, const hgemm_expert_weights_t &w1, const hgemm_expert_weights_t &w2)
 {
-    int32_t s = 1;
-    while (s < 8 && s * 2 <= most && chunks >= int64_t(s) * 2 * 4) s *= 2;
-    return s;
+    const bool half = d.type == HGEMM_TYPE_F16;
+    FewParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.gated = d.activation == HGEMM_ACT_SWIGLU ? 1 : 0;
+    p.x = c.x;
+    p.ldx = c.ldx;
+    p.x_vec = aligned16(c.x) && c.ldx % 8 == 0 ? 1 : 0;
+    p.y = c.y;
+    p.ldy = c.ldy;
+    p.indices = c.indices;
+    p.weights = c.weights;
+    p.h_stride = int32_t(h_stride(d));
+    p.inner = d.inner;
+    p.experts = d.experts;
+    p.top_k = d.top_k;
+    p.tokens = int32_t(c.tokens);
+    p.choices = int32_t(c.tokens * d.top_k);
+    p.h = reinterpret_cast<float *>(c.scratch);
+    p.top = p.h + int64_t(p.choices) * p.h_stride;
+    // launch 1 writes whole chunks of h (zeros beyond inner), eight tiles of 8 (SWIGLU) or 16 rows together
+    p.groups = int32_t(ceil_div(p.h_stride, p.gated ? 64 : 128));
+    p.fd_groups = hgemm_dev::make_fast_div(uint32_t(p.groups));
+    const int lists = hgemm_dev::few_list_bytes(p.experts, p.choices);
+    const int64_t entries = hgemm_dev::few_max_entries(p.experts, p.choices);
+
+    // x of 8 choices at once, or as many chunks of it as fit
+    p.w = weights16(w1, up_rows(d), d.hidden);
+    p.piece = int32_t(std::min<int64_t>(up_to(d.hidden, 4 * hgemm_dev::kFewChunk) * 16, kMaxX));
+    p.most_slices = 8;
+    const unsigned grid = unsigned(std::min<int64_t>(entries * p.groups * 8, int64_t(ctx->num_sms) * 2));
+    const hgemm_status_t st = launch(ctx, half ? up_kernel<__half>(p.w.align) : up_kernel<__nv_bfloat16>(p.w.align), dim3(grid), hgemm_dev::kFewUpThreads, lists + p.piece, &p, c.stream);
+    if (st != HGEMM_OK) return st;
+
+    p.w = weights16(w2, d.hidden, d.inner);
+    p.most_slices = 1;
+    while (p.most_slices < 8 && p.most_slices * 2 * p.choices <= hgemm_dev::kFewMaxChoices) p.most_slices *= 2;
+    // each warp's part of h: as much as an entry of eight choices could use, or what is left of the shared memory (at the most choices and experts 4 KB, three chunks of eight)
+    const int fixed = lists + 4 * ((p.choices + 3) & ~3) + p.most_slices * p.choices * 64;
+    const int64_t h_bytes = hgemm_dev::kFewEntry * (p.h_stride * (half ? 2ll : 4ll) + 64);
+    p.piece = int32_t(std::min<int64_t>(h_bytes, (kSmemOptIn - fixed) / (hgemm_dev::kFewDownThreads / 32) & ~15));
+    return launch(ctx, half ? down_kernel<__half>(p.w.align) : down_kernel<__nv_bfloat16>(p.w.align), dim3(unsigned(ceil_div(d.hidden, 16))), hgemm_dev::kFewDownThreads,
+                  fixed + p.piece * (hgemm_dev::kFewDownThreads / 32), &p, c.stream);
+}
+
+// ---- 4-bit weights -------------------------------------------------------------------------------------------------
+
+// Scratch memory: where its parts begin (multiples of 256 bytes).  Both products' digits share a place, and so do both products' results: each is used up before
+// the second's is written.
+struct Layout {
+    int64_t offsets, position, place, one, x_factor, h_factor, digits, scales, results, bytes;
+    int64_t ld_x, ld_h;        // bytes between digit rows
+    int64_t ld_u, ld_z;        // results' rows, in numbers
+};
+
+Layout layout_of(const hgemm_few_tokens_t &d, int64_t choices)
+{
+    Layout l;
+    int64_t at = 0;
+    auto part = [&](int64_t bytes) {
+        const int64_t here = at;
+        at = up_to(at + bytes, 256);
+        return here;
+    };
+    l.ld_x = up_to(ceil_div(d.hidden, 2), 16);
+    l.ld_h = up_to(ceil_div(d.inner, 2), 16);
+    l.ld_u = up_to(up_rows(d), 4);
+    l.ld_z = up_to(d.hidden, 4);
+    const int64_t rows = hgemm_fp8_padded_rows(choices * kDigits, d.experts);
+    l.offsets = part(4 * (d.experts + 1));
+    l.position = part(4 * choices);
+    l.place = part(4 * choices);
+    l.one = part(4);
+    l.x_factor = part(4 * choices);
+    l.h_factor = part(4 * choices);
+    l.digits = part(choices * kDigits * std::max(l.ld_x, l.ld_h));
+    l.scales = part(std::max(hgemm_fp4_scale_bytes(rows, d.hidden, format_of(d)), hgemm_fp4_scale_bytes(rows, d.inner, format_of(d))));
+    l.results = part(choices * 4 * std::max(l.ld_u, l.ld_z));
+    l.bytes = at;
+    return l;
+}
+
+hgemm_status_t run4(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c, const hgemm_expert_weights_t &w1, const hgemm_expert_weights_t &w2)
+{
+    using namespace hgemm_dev;
+    const int64_t choices = c.tokens * d.top_k;
+    const Layout l = layout_of(d, choices);
+    const bool nv = d.weights == HGEMM_WEIGHTS_NVFP4;
+    const int32_t format = format_of(d), gated = d.activation == HGEMM_ACT_SWIGLU ? 1 : 0;
+    float *one = reinterpret_cast<float *>(c.scratch + l.one), *results = reinterpret_cast<float *>(c.scratch + l.results);
+    int32_t *offsets = reinterpret_cast<int32_t *>(c.scratch + l.offsets);
+
+    // x as digits
+    DigitParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.x = c.x;
+    p.ldx = c.ldx;
+    p.x_half = d.type == HGEMM_TYPE_F16 ? 1 : 0;
+    p.x_vec = aligned16(c.x) && c.ldx % 8 == 0 ? 1 : 0;
+    p.depth = d.hidden;
+    p.top_k = d.top_k;
+    p.experts = d.experts;
+    p.choices = int32_t(choices);
+    p.indices = c.indices;
+    p.offsets = offsets;
+    p.position = reinterpret_cast<int32_t *>(c.scratch + l.position);
+    p.place = reinterpret_cast<int32_t *>(c.scratch + l.place);
+    p.one = one;
+    p.q = c.scratch + l.digits;
+    p.ldq = l.ld_x;
+    p.scales = c.scratch + l.scales;
+    p.atoms = int32_t(ceil_div(d.hidden, nv ? 64 : 128));
+    p.factor = reinterpret_cast<float *>(c.scratch + l.x_factor);
+    hgemm_status_t st = launch(ctx, nv ? reinterpret_cast<const void *>(few_digits_kernel<true, true>) : reinterpret_cast<const void *>(few_digits_kernel<false, true>), dim3(unsigned(choices + 1)),
+                               kDigitThreads, 4 * d.experts, &p, c.stream);
+    if (st != HGEMM_OK) return st;
+    st = hgemm_host::fp4_digits_product(ctx, format, choices, up_rows(d), d.hidden, d.experts, p.q, l.ld_x, p.scales, w1.values, w1.ld, w1.scales, nv ? one : nullptr, w1.factor, results, l.ld_u,
+                                        offsets, c.stream);
+    if (st != HGEMM_OK) return st;
+
+    // h as digits
+    p.x = nullptr;
+    p.u = results;
+    p.ldu = l.ld_u;
+    p.gated = gated;
+    p.u_vec = !gated || d.inner % 4 == 0 ? 1 : 0;
+    p.u_factor = p.factor;
+    p.depth = d.inner;
+    p.ldq = l.ld_h;
+    p.atoms = int32_t(ceil_div(d.inner, nv ? 64 : 128));
+    p.factor = reinterpret_cast<float *>(c.scratch + l.h_factor);
+    st = launch(ctx, nv ? reinterpret_cast<const void *>(few_digits_kernel<true, false>) : reinterpret_cast<const void *>(few_digits_kernel<false, false>), dim3(unsigned(choices)), kDigitThreads, 0, &p,
+                c.stream);
+    if (st != HGEMM_OK) return st;
+    st = hgemm_host::fp4_digits_product(ctx, format, choices, d.hidden, d.inner, d.experts, p.q, l.ld_h, p.scales, w2.values, w2.ld, w2.scales, nv ? one : nullptr, w2.factor, results, l.ld_z, offsets,
+                                        c.stream);
+    if (st != HGEMM_OK) return st;
+
+    CombineParams q;
+    std::memset(&q, 0, sizeof(q));
+    q.z = results;
+    q.ldz = l.ld_z;
+    q.factor = p.factor;
+    q.position = p.position;
+    q.weights = c.weights;
+    q.top_k = d.top_k;
+    q.hidden = d.hidden;
+    q.y = c.y;
+    q.ldy = c.ldy;
+    q.y_vec = (reinterpret_cast<uintptr_t>(c.y) & 7u) == 0 && c.ldy % 4 == 0 ? 1 : 0;
+    return launch(ctx, d.type == HGEMM_TYPE_F16 ? reinterpret_cast<const void *>(few_combine_kernel<__half>) : reinterpret_cast<const void *>(few_combine_kernel<__nv_bfloat16>),
+                  dim3(unsigned(ceil_div(d.hidden, 4 * kDigitThreads)), unsigned(c.tokens)), kDigitThreads, 0, &q, c.stream);
+}
+
+bool legal_weights(const hgemm_few_tokens_t &d, const hgemm_expert_weights_t &m, int32_t depth)
+{
+    const bool four = is4(d);
+    if (!m.values || (d.weights == HGEMM_WEIGHTS_NVFP4) != (m.factor != nullptr) || four != (m.scales != nullptr) || !aligned4(m.factor)) return false;
+    if (four) return m.ld >= ceil_div(depth, 2) && (m.ld & 15) == 0 && aligned16(m.values) && aligned16(m.scales);
+    return m.ld >= depth && (reinterpret_cast<uintptr_t>(m.values) & 1u) == 0;
 }
 
 } // namespace
@@ -112,7 +272,9 @@ extern "C" {
 int64_t hgemm_few_tokens_scratch(const hgemm_few_tokens_t *d, int64_t tokens)
 {
     if (!d || !legal(*d) || tokens < 0 || tokens > HGEMM_FEW_TOKENS_MAX) return -1;
-    return tokens * d->top_k * h_stride(*d) * 4;
+    const int64_t choices = tokens * d->top_k;
+    if (choices == 0) return 0;
+    return is4(*d) ? layout_of(*d, choices).bytes : choices * (h_stride(*d) + h_stride(*d) / 8) * 4;
 }
 
 hgemm_status_t hgemm_few_tokens(hgemm_ctx_t *ctx, const hgemm_few_tokens_t *d, int64_t tokens, const void *x, int64_t ldx, const hgemm_expert_weights_t *w1,
@@ -122,45 +284,9 @@ hgemm_status_t hgemm_few_tokens(hgemm_ctx_t *ctx, const hgemm_few_tokens_t *d, i
     if (tokens == 0) return HGEMM_OK;
     if (!x || !y || !indices || !weights || !scratch || (reinterpret_cast<uintptr_t>(x) & 1u) != 0 || (reinterpret_cast<uintptr_t>(y) & 1u) != 0) return HGEMM_ERR_INVALID_ARG;
     if (!aligned4(indices) || !aligned4(weights) || !aligned16(scratch) || scratch_bytes < hgemm_few_tokens_scratch(d, tokens)) return HGEMM_ERR_INVALID_ARG;
-    FewParams p;
-    std::memset(&p, 0, sizeof(p));
-    p.gated = d->activation == HGEMM_ACT_SWIGLU ? 1 : 0;
-    FewWeights up, down;
-    std::memset(&up, 0, sizeof(up));
-    std::memset(&down, 0, sizeof(down));
-    if (!fill(&up, *d, *w1, d->inner * (p.gated ? 2 : 1), d->hidden) || !fill(&down, *d, *w2, d->hidden, d->inner)) return HGEMM_ERR_INVALID_ARG;
-    p.x = x;
-    p.ldx = ldx;
-    p.x_vec = aligned16(x) && ldx % 8 == 0 ? 1 : 0;
-    p.y = y;
-    p.ldy = ldy;
-    p.indices = indices;
-    p.weights = weights;
-    p.h = static_cast<__nv_bfloat16 *>(scratch);
-    p.h_stride = h_stride(*d);
-    p.inner = d->inner;
-    p.experts = d->experts;
-    p.top_k = d->top_k;
-    p.tokens = int32_t(tokens);
-    p.choices = int32_t(tokens * d->top_k);
-    p.tiles = int32_t(ceil_div(d->inner, p.gated ? 8 : 16));
-    const int lists = (hgemm_dev::few_list_bytes(p.experts, p.choices) + 15) & ~15;
-    const int64_t entries = hgemm_dev::few_max_entries(p.experts, p.choices);
-
-    p.w = up;
-    const int64_t up_chunks = ceil_div(d->hidden, chunk_of(*d));
-    p.slices = slices_of(up_chunks, 8);
-    p.slice_chunks = int32_t(ceil_div(up_chunks, p.slices));
-    const int64_t per_cta = hgemm_dev::kFewUpThreads / 32 / p.slices;
-    const unsigned grid = unsigned(std::min<int64_t>(ceil_div(entries * p.tiles, per_cta), int64_t(ctx->num_sms) * 2));
-    hgemm_status_t st = launch(ctx, up_kernel(*d), grid, hgemm_dev::kFewUpThreads, lists, &p, stream);
-    if (st != HGEMM_OK) return st;
-
-    p.w = down;
-    const int64_t down_chunks = ceil_div(d->inner, chunk_of(*d));
-    p.slices = slices_of(down_chunks, hgemm_dev::kFewMaxChoices / p.choices);
-    p.slice_chunks = int32_t(ceil_div(down_chunks, p.slices));
-    return launch(ctx, down_kernel(*d), unsigned(ceil_div(d->hidden, 16)), hgemm_dev::kFewDownThreads, lists + p.slices * p.choices * 64, &p, stream);
+    if (!legal_weights(*d, *w1, d->hidden) || !legal_weights(*d, *w2, d->inner)) return HGEMM_ERR_INVALID_ARG;
+    const Call c{tokens, x, ldx, indices, weights, y, ldy, static_cast<uint8_t *>(scratch), stream};
+    return is4(*d) ? run4(ctx, *d, c, *w1, *w2) : run16(ctx, *d, c, *w1, *w2);
 }
 
 } // extern "C"

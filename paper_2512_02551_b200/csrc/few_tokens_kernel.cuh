@@ -1,50 +1,45 @@
-// A layer of experts for a few tokens: W1 and the activation in one launch, W2 and the weighted sum over a token's choices in another.
+// A layer of experts with 16-bit weights for a few tokens: W1 and the activation in one launch, W2 and the weighted sum over a token's choices in another.
+// (4-bit weights: few_digits_kernel.cuh.)
 //
-// Bound by the chosen experts' weights, read once from memory: 0.5 to 2 bytes a weight for a handful of multiply-adds.  The weights go from memory to
-// registers (16 bytes a lane, eight or sixteen of them in flight) and from there to mma.sync: a warp's 16 rows of a weight matrix are the operand that
-// fills the instruction's rows, up to 16 choices of the expert are its columns.  (Tensor memory and a ring of shared-memory stages would only lengthen the
-// way: the tensor pipe is idle nearly all the time, and 4-bit weights have to become 16-bit ones on the way, which tcgen05 cannot do.)
+// Bound by the chosen experts' weights, read once from memory for a handful of multiply-adds.  They go from memory to registers (16 bytes a lane, four
+// chunks of two rows in flight at any time) and from there to mma.sync: a warp's 16 rows of a weight matrix are the operand that fills the instruction's
+// rows, up to 8 choices of the expert are its columns.  A lane takes 16 consecutive bytes of its row, four lanes 64 (a chunk): which k a lane holds is free as
+// long as both operands agree.  (Tensor memory and a ring of shared-memory stages would lengthen the way of rows that start anywhere: tensor copies
+// need rows at multiples of 16 bytes.)
 //
-// Which k a lane holds is free as long as both operands agree.  A lane takes 16 consecutive bytes of its row, four lanes 64: 32 weights of 16 bits,
-// or 128 of 4 bits.  4-bit weights: the four bits s e e m become a bf16 by moving s and eem to their places, which is the value times 2^-126;
-// one packed product with the block's scale (times 2^118) makes it the weight times 2^-8, exactly.  Moved this way, a word's codes come out as pairs 4 apart, so
-// the other operand is permuted alike.  Instructions bound the 4-bit kernels (24 a warp for 256 weights) as much as memory does.
+// bf16 weights have bf16 products, with h as the sum of two bf16 (16 bits of mantissa); fp16 weights fp16 ones, with h scaled by a power of two for each choice, so that
+// its largest magnitude is just below 2^15 (what is below 2^-39 of it is lost), and rounded to 11 bits.
 //
-// The products are bf16 with fp32 sums wherever an operand's range asks for it: 4-bit weights with powers of two, and h, which is held as the sum of
-// two bf16 (16 bits of mantissa).  fp16 weights and x meet as fp16; against h an fp16 weight is the sum of two bf16 too, and of the four products that of both
-// second parts, 2^-16 of the whole, is left out.  fp16 x against powers of two is the sum of two bf16 (exactly).
-//
-// Work: launch 1 has a tile of 16 rows (SWIGLU: 8 rows of each half, whose products meet in one lane) of one expert per warp, its contraction shared by up to eight
-// warps of the CTA; launch 2 has one CTA for 16 outputs of all tokens, whose warps take the chosen experts in turn, so that every sum over a token's
-// choices stays in a CTA and has a fixed order.  Every CTA makes the list of the experts' choices for itself; launch 2 does so, and fetches its
-// first weights, before launch 1 ends (both are inputs of the call, which launch 1 has waited for).
+// Work.  Launch 1: a warp has a tile of 16 rows (SWIGLU: 8 rows of each half, whose products meet in one lane), a CTA eight tiles of one expert, whose
+// tokens it lays out in shared memory as the instruction wants them.  As many rounds as give every CTA the same; the groups of tiles that are left over are
+// shared by up to eight CTAs each, whose warps split the contraction.  Launch 2: one CTA for 16 outputs of all tokens; its warps take the chosen
+// experts in turn (those left over by several warps each), so that every sum over a token's choices stays in a CTA and has a fixed order.  Every CTA makes
+// the list of the experts' choices for itself; launch 2 does so, and fetches its first weights, before launch 1 ends (both are inputs of the call,
+// which launch 1 has waited for).  A column of the instruction that has no choice computes with whatever is there; its sums are not used.
 #pragma once
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
-#include <cuda_fp8.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "hgemm_device.cuh"
 #include "product_tiles.cuh"
 
 namespace hgemm_dev {
 
-enum : int { kFewBf16 = 0, kFewF16 = 1, kFewNv = 2, kFewMx = 3 };
 constexpr int kFewUpThreads = 256, kFewDownThreads = 512;
 constexpr int kFewMaxChoices = 2048;              // 64 tokens of 32
-constexpr int kFewEntry = 16;                     // choices of an expert that share a pass over its weights
+constexpr int kFewEntry = 8;                      // choices of an expert that share a pass over its weights
+constexpr int kFewAhead = 4;                      // chunks in flight
 constexpr uint32_t kFewNone = 0xffffu;
 
 struct FewWeights {
     const uint8_t *values;
     int64_t ld, matrix;        // bytes between rows, between experts
-    const uint8_t *scales;
-    int64_t scale_matrix;
-    const float *factor;
     int32_t rows, depth;       // of one expert
-    int32_t atoms;             // scale tiles across
-    int32_t align;             // 16-bit weights: what rows' addresses are multiples of: 16, 4 or 2
+    int32_t align;             // what rows' addresses are multiples of: 16, 4 or 2
 };
 
 struct FewParams {
@@ -56,29 +51,33 @@ struct FewParams {
     int64_t ldy;
     const int32_t *indices;
     const float *weights;
-    __nv_bfloat16 *h;          // [2 parts][choices][h_stride]
-    int64_t h_stride;
+    float *h;                  // choices x h_stride (whole chunks)
+    float *top;                // choices x h_stride / 8: the largest magnitude of each 8 of them
+    int32_t h_stride;
     int32_t inner, experts, top_k, tokens, choices, gated;
-    int32_t tiles;             // launch 1: tiles of an expert
-    int32_t slices;            // warps that share a contraction
-    int32_t slice_chunks;      // chunks of a slice
+    int32_t groups;            // launch 1: groups of eight tiles of an expert
+    FastDiv fd_groups;
+    int32_t piece;             // launch 1: bytes of shared memory for x
+    int32_t most_slices;       // warps that may share a contraction
 };
 
-__host__ __device__ constexpr int few_chunk(int w) { return w >= kFewNv ? 128 : 32; }          // k of a chunk: 64 bytes of a row
-__host__ __device__ constexpr bool few_is4(int w) { return w >= kFewNv; }
+constexpr int kFewChunk = 32;                     // k of a chunk: 64 bytes of a row
 
-// Shared memory of the lists: words for the experts' counts, the entries (expert | first << 16), 16-bit places and lists of the choices.
+// ---- lists --------------------------------------------------------------------------------------------------------
+
+// Shared memory of the lists: words for the experts' counts and the entries, 16-bit experts, places and lists of the choices.
 __host__ __device__ constexpr int few_max_entries(int experts, int choices) { return (experts < choices ? experts : choices) + choices / kFewEntry; }
 __host__ __device__ constexpr int few_list_bytes(int experts, int choices)
 {
-    return 16 + 4 * experts + 8 * few_max_entries(experts, choices) + 2 * 2 * ((choices + 7) & ~7);
+    return ((16 + 4 * experts + 8 * few_max_entries(experts, choices) + 15) & ~15) + ((3 * 2 * ((choices + 7) & ~7) + 15) & ~15);
 }
 
 struct FewLists {
     int32_t *total;            // entries
     uint32_t *count;           // of an expert, later where its list begins
     uint32_t *entry;           // [2 i]: expert; [2 i + 1]: first | number << 16
-    uint16_t *rank, *list;     // place of a choice among its expert's (kFewNone: of no expert); choices by expert
+    uint16_t *expert;          // of a choice (kFewNone: none)
+    uint16_t *rank, *list;     // place of a choice among its expert's; choices by expert
 };
 
 __device__ __forceinline__ FewLists few_lists(uint8_t *smem, const FewParams &p)
@@ -87,7 +86,8 @@ __device__ __forceinline__ FewLists few_lists(uint8_t *smem, const FewParams &p)
     l.total = reinterpret_cast<int32_t *>(smem);
     l.count = reinterpret_cast<uint32_t *>(smem + 16);
     l.entry = l.count + p.experts;
-    l.rank = reinterpret_cast<uint16_t *>(l.entry + 2 * few_max_entries(p.experts, p.choices));
+    l.expert = reinterpret_cast<uint16_t *>(smem + ((16 + 4 * p.experts + 8 * few_max_entries(p.experts, p.choices) + 15) & ~15));
+    l.rank = l.expert + ((p.choices + 7) & ~7);
     l.list = l.rank + ((p.choices + 7) & ~7);
     return l;
 }
@@ -95,30 +95,53 @@ __device__ __forceinline__ FewLists few_lists(uint8_t *smem, const FewParams &p)
 // The whole CTA.  An expert's choices keep their order.
 __device__ __forceinline__ void few_make_lists(const FewParams &p, const FewLists &l)
 {
-    for (int32_t e = static_cast<int32_t>(threadIdx.x); e < p.experts; e += static_cast<int32_t>(blockDim.x)) l.count[e] = 0u;
+    const int32_t threads = static_cast<int32_t>(blockDim.x), me = static_cast<int32_t>(threadIdx.x);
+    for (int32_t e = me; e < p.experts; e += threads) l.count[e] = 0u;
+    for (int32_t c = me; c < ((p.choices + 7) & ~7); c += threads) {
+        const int32_t e = c < p.choices ? p.indices[c] : -1;
+        l.expert[c] = static_cast<uint16_t>(e >= 0 && e < p.experts ? e : kFewNone);
+    }
     __syncthreads();
-    if (threadIdx.x < 32) {
-        const uint32_t lane = threadIdx.x;
-        for (int32_t base = 0; base < p.choices; base += 32) {
-            const int32_t c = base + static_cast<int32_t>(lane);
-            int32_t e = c < p.choices ? p.indices[c] : -1;
-            if (e < 0 || e >= p.experts) e = -1;
-            const uint32_t peers = __match_any_sync(0xffffffffu, e);
-            const uint32_t before = __popc(peers & ((1u << lane) - 1u)), start = e >= 0 ? l.count[e] : 0u;
-            __syncwarp();
-            if (e >= 0 && before == 0u) l.count[e] = start + __popc(peers);
-            __syncwarp();
-            if (c < p.choices) l.rank[c] = static_cast<uint16_t>(e >= 0 ? start + before : kFewNone);
+    if (p.choices <= 128) {
+        // a choice's place is the number of choices of its expert ahead of it: all of them compared at once
+        if (me < p.choices) {
+            const uint32_t e = l.expert[me], ee = e | (e << 16);
+            uint32_t before = 0u;
+            for (int32_t c = 0; c < me; c += 8) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(l.expert + c);
+                const uint32_t w[4] = {v.x ^ ee, v.y ^ ee, v.z ^ ee, v.w ^ ee};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    before += (w[i] & 0xffffu) == 0u && c + 2 * i < me;
+                    before += (w[i] >> 16) == 0u && c + 2 * i + 1 < me;
+                }
+            }
+            l.rank[me] = static_cast<uint16_t>(before);
+            if (e != kFewNone) atomicAdd(&l.count[e], 1u);
         }
+    } else if (me < 32) {
+        for (int32_t base = 0; base < p.choices; base += 32) {
+            const int32_t c = base + me;
+            const uint32_t e = c < p.choices ? l.expert[c] : kFewNone;
+            const uint32_t peers = __match_any_sync(0xffffffffu, e);
+            const uint32_t before = __popc(peers & ((1u << me) - 1u)), start = e != kFewNone ? l.count[e] : 0u;
+            __syncwarp();
+            if (e != kFewNone && before == 0u) l.count[e] = start + __popc(peers);
+            __syncwarp();
+            if (c < p.choices) l.rank[c] = static_cast<uint16_t>(start + before);
+        }
+    }
+    __syncthreads();
+    if (me < 32) {
         uint32_t places = 0u, entries = 0u;
         for (int32_t base = 0; base < p.experts; base += 32) {
-            const int32_t e = base + static_cast<int32_t>(lane);
+            const int32_t e = base + me;
             const uint32_t n = e < p.experts ? l.count[e] : 0u, m = (n + kFewEntry - 1) / kFewEntry;
             uint32_t sum = n | (m << 16);                      // both sums at once: below 2^12 each
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const uint32_t v = __shfl_up_sync(0xffffffffu, sum, d);
-                if (static_cast<int32_t>(lane) >= d) sum += v;
+                if (me >= d) sum += v;
             }
             const uint32_t first = places + (sum & 0xffffu) - n, at = entries + (sum >> 16) - m;
             if (e < p.experts) l.count[e] = first;
@@ -130,174 +153,332 @@ __device__ __forceinline__ void few_make_lists(const FewParams &p, const FewList
             places += all & 0xffffu;
             entries += all >> 16;
         }
-        if (lane == 0) *l.total = static_cast<int32_t>(entries);
+        if (me == 0) *l.total = static_cast<int32_t>(entries);
     }
     __syncthreads();
-    for (int32_t c = static_cast<int32_t>(threadIdx.x); c < p.choices; c += static_cast<int32_t>(blockDim.x))
-        if (l.rank[c] != kFewNone) l.list[l.count[p.indices[c]] + l.rank[c]] = static_cast<uint16_t>(c);
+    for (int32_t c = me; c < p.choices; c += threads)
+        if (l.expert[c] != kFewNone) l.list[l.count[l.expert[c]] + l.rank[c]] = static_cast<uint16_t>(c);
     __syncthreads();
+}
+
+// ---- weights ------------------------------------------------------------------------------------------------------
+
+// Two rows' 16 bytes of a chunk.
+struct FewRaw {
+    uint4 v[2];
+};
+
+// Part of a contraction: chunks of a lane's two rows.  Rows that are not there (a matrix's last tile) stand for the expert's first: they are loaded like the
+// others, and their sums are not used.
+struct FewSpan {
+    const uint8_t *row[2];     // at the lane's bytes of the first chunk
+    int32_t first, n;          // chunks; those of them that rows have whole
+    bool tail;                 // a last chunk follows, of which rows have a part
+};
+
+__device__ __forceinline__ FewSpan few_span(const FewWeights &w, int32_t expert, int32_t r0, int32_t r1, int32_t first, int32_t n, uint32_t q)
+{
+    FewSpan f;
+    f.row[0] = w.values + expert * w.matrix + r0 * w.ld + first * 64 + q * 16;
+    f.row[1] = w.values + expert * w.matrix + r1 * w.ld + first * 64 + q * 16;
+    f.first = first;
+    f.n = max(0, min(first + n, w.depth / kFewChunk) - first);
+    f.tail = f.n < n;
+    return f;
+}
+
+// 16 bytes at a multiple of ALIGN.
+template <int ALIGN>
+__device__ __forceinline__ uint4 few_load16(const uint8_t *p)
+{
+    uint4 v;
+    if constexpr (ALIGN == 16) {
+        asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    } else if constexpr (ALIGN == 4) {
+        asm volatile("ld.global.u32 %0, [%4];\n\tld.global.u32 %1, [%4 + 4];\n\tld.global.u32 %2, [%4 + 8];\n\tld.global.u32 %3, [%4 + 12];"
+                     : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p));
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            asm volatile("{\n\t.reg .b16 a, b;\n\tld.global.u16 a, [%1];\n\tld.global.u16 b, [%1 + 2];\n\tmov.b32 %0, {a, b};\n\t}" : "=r"(w[i]) : "l"(p + 4 * i));
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return v;
+}
+
+// Chunk i behind a span's pointers (loads without a condition around them: they stay in flight).
+template <int ALIGN>
+__device__ __forceinline__ void few_fetch(FewRaw &raw, const uint8_t *const (&row)[2], int i)
+{
+#pragma unroll
+    for (int j = 0; j < 2; ++j) raw.v[j] = few_load16<ALIGN>(row[j] + i * 64);
+}
+
+// The chunk behind the whole ones; zeros beyond the rows' ends.
+__device__ __forceinline__ void few_fetch_tail(FewRaw &raw, const FewWeights &w, const FewSpan &f, uint32_t q)
+{
+    const int32_t room = w.depth * 2 - (f.first + f.n) * 64 - static_cast<int32_t>(q) * 16;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint8_t *p = f.row[j] + static_cast<int64_t>(f.n) * 64;
+        uint32_t v[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (2 * i < room) v[i / 2] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(p + 2 * i)) << (16 * (i & 1));
+        raw.v[j] = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+}
+
+// The chunks of a span, one after the other: chunk(raw, i).  The first four are on their way on entry (few_begin), those of `next` when it returns, if
+// there are as many.  The last four of a number that is no multiple of four overlap those before them; fewer than four, and a chunk that is there in
+// part, are fetched on their own.
+template <int ALIGN, class Chunk>
+__device__ __forceinline__ void few_walk(FewRaw (&raw)[kFewAhead], const FewWeights &w, const FewSpan &f, const FewSpan &next, uint32_t q, Chunk &&chunk)
+{
+    const int32_t n = f.n;
+    if (n >= kFewAhead) {
+        const uint8_t *row[2] = {f.row[0], f.row[1]};
+#pragma unroll 1
+        for (int32_t j = 0; j < n; j += kFewAhead) {
+            const int32_t from = min(j, n - kFewAhead), step = min(j + kFewAhead, n - kFewAhead) - from;
+            const bool other = j + kFewAhead >= n && next.n >= kFewAhead;       // (with none to come, the last ones again, to no use)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) row[i] = other ? next.row[i] : row[i] + step * 64;
+#pragma unroll
+            for (int u = 0; u < kFewAhead; ++u) {
+                if (from + u >= j) chunk(raw[u], from + u);
+                few_fetch<ALIGN>(raw[u], row, u);
+            }
+        }
+    }
+#pragma unroll 1
+    for (int32_t i = n >= kFewAhead ? n : 0; i < n + (f.tail ? 1 : 0); ++i) {
+        FewRaw r;
+        if (i < n) {
+            few_fetch<ALIGN>(r, f.row, i);
+        } else {
+            few_fetch_tail(r, w, f, q);
+        }
+        chunk(r, i);
+    }
+}
+template <int ALIGN>
+__device__ __forceinline__ void few_begin(FewRaw (&raw)[kFewAhead], const FewSpan &f)
+{
+    if (f.n >= kFewAhead) {
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u) few_fetch<ALIGN>(raw[u], f.row, u);
+    }
 }
 
 // ---- operands -----------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ void few_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, __nv_bfloat16)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void few_mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, __half)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// 16 bytes of a row of 4-bit weights, or of 16-bit ones (whose addresses are multiples of `align`); zeros beyond the row's `bytes`.
-template <int W>
-__device__ __forceinline__ uint4 few_load(const uint8_t *row, int32_t at, int32_t bytes, int32_t align)
+// Two rows' eight k of each lane against those of eight choices.
+template <class T>
+__device__ __forceinline__ void few_products(float (&acc)[4], const FewRaw &r, const uint4 &v)
 {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (row == nullptr || at >= bytes) return v;
-    if ((few_is4(W) || align == 16) && at + 16 <= bytes) {
-        asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(row + at));
-        return v;
-    }
+    few_mma(acc, r.v[0].x, r.v[1].x, r.v[0].y, r.v[1].y, v.x, v.y, T());
+    few_mma(acc, r.v[0].z, r.v[1].z, r.v[0].w, r.v[1].w, v.z, v.w, T());
+}
+
+// The power of two that brings a largest magnitude (bits of an fp32 number) to 2^14 or more, below 2^15, and its inverse; 1 for zero.
+struct FewScale {
+    float scale, inverse;
+};
+__device__ __forceinline__ FewScale few_range(uint32_t bits)
+{
+    const int32_t e = static_cast<int32_t>(bits >> 23), up = bits == 0u || e == 255 ? 127 : min(268 - e, 254);
+    FewScale s;
+    s.scale = __uint_as_float(static_cast<uint32_t>(up) << 23);
+    s.inverse = up == 254 ? 0x1p-127f : __uint_as_float(static_cast<uint32_t>(254 - up) << 23);
+    return s;
+}
+
+// The chunks of slice s of S: whole runs of four but for the last slice's.
+__device__ __forceinline__ void few_slice(int32_t chunks, int32_t s, int32_t slices, int32_t &first, int32_t &n)
+{
+    const int32_t runs = (chunks + kFewAhead - 1) / kFewAhead;
+    first = min(chunks, runs * s / slices * kFewAhead);
+    n = min(chunks, runs * (s + 1) / slices * kFewAhead) - first;
+}
+
+// ---- launch 1: h = act(W1 x) ------------------------------------------------------------------------------------------
+
+// 8 consecutive elements of x, zeros beyond its end.
+__device__ __forceinline__ uint4 few_load_x(const uint16_t *row, int32_t k, int32_t depth, int32_t vec)
+{
+    if (k >= depth) return make_uint4(0u, 0u, 0u, 0u);
+    if (vec && k + 8 <= depth) return *reinterpret_cast<const uint4 *>(row + k);
     uint32_t w[4] = {0u, 0u, 0u, 0u};
-    if constexpr (few_is4(W)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (at + i < bytes) w[i / 4] |= static_cast<uint32_t>(row[at + i]) << (8 * (i & 3));
-    } else if (align >= 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (at + 4 * i + 4 <= bytes) w[i] = *reinterpret_cast<const uint32_t *>(row + at + 4 * i);
-            else if (at + 4 * i < bytes) w[i] = *reinterpret_cast<const uint16_t *>(row + at + 4 * i);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (at + 2 * i < bytes) w[i / 2] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(row + at + 2 * i)) << (16 * (i & 1));
-    }
+    for (int i = 0; i < 8; ++i)
+        if (k + i < depth) w[i / 2] |= static_cast<uint32_t>(row[k + i]) << (16 * (i & 1));
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Two rows' 16 bytes of a chunk, and the scale bytes of a lane's blocks.
-struct FewRaw {
-    uint4 v[2];
-    uint32_t s[2];
-};
+__device__ __forceinline__ float few_silu(float u) { return u / (1.0f + __expf(-u)); }
+__device__ __forceinline__ float few_finite(float v) { return fabsf(v) < __int_as_float(0x7f800000) ? fabsf(v) : 0.0f; }
 
-// What a lane needs to know about its two rows.
-struct FewRows {
-    const uint8_t *row[2];     // nullptr: no such row
-    const uint8_t *scale[2];   // scale tiles of the row's 128, at the row's place
-};
-
-template <int W>
-__device__ __forceinline__ FewRows few_rows(const FewWeights &w, int32_t expert, int32_t r0, int32_t r1, bool has0, bool has1)
+// T: the type of x and of the weights.  Dynamic shared memory: the lists, then x.
+template <class T, int ALIGN>
+__global__ void __launch_bounds__(kFewUpThreads, 2)
+few_up_kernel(const FewParams p)
 {
-    FewRows f;
-    const int32_t r[2] = {r0, r1};
-    const bool has[2] = {has0, has1};
+    constexpr int kWarps = kFewUpThreads / 32;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ float4 s_part[kWarps][32];
+    __shared__ const uint16_t *s_row[kFewEntry];                  // the entry's tokens
+    const FewLists l = few_lists(smem, p);
+    uint4 *s_x = reinterpret_cast<uint4 *>(smem + few_list_bytes(p.experts, p.choices));      // [chunk][8 choices][4 lanes]
+    grid_dependency_wait();
+    grid_launch_dependents();                                     // launch 2 may read the call's inputs from here on
+    few_make_lists(p, l);
+    const int32_t warp = static_cast<int32_t>(threadIdx.x >> 5);
+    const uint32_t lane = threadIdx.x & 31u, q = lane & 3u, m = lane >> 2;
+    const int32_t chunks = (p.w.depth + kFewChunk - 1) / kFewChunk;
+
+    // Every CTA has as many whole groups, one after the other; those left over are shared by `rest_slices` CTAs each.
+    const int32_t units = *l.total * p.groups, ctas = static_cast<int32_t>(gridDim.x), cta = static_cast<int32_t>(blockIdx.x);
+    const int32_t rounds = units / ctas, rest = units - rounds * ctas;
+    int32_t rest_slices = 1;
+    while (rest_slices * 2 <= p.most_slices && rest * rest_slices * 2 <= ctas) rest_slices *= 2;
+    const int32_t my_rounds = rounds + (cta < rest * rest_slices ? 1 : 0);
+
+    struct Work {
+        int32_t entry, expert, first, count, row0, row1, slices, slice;
+        bool has0, has1;
+    };
+    auto work_of = [&](int32_t round) {
+        Work t;
+        const bool whole = round < rounds;
+        t.slices = whole ? 1 : rest_slices;
+        const int32_t unit = whole ? cta * rounds + round : rounds * ctas + cta / rest_slices;
+        t.entry = fast_div(unit, p.fd_groups);
+        const int32_t group = unit - t.entry * p.groups;
+        // a CTA's share of the group's eight tiles, and of each tile's contraction
+        const int32_t tile = group * kWarps + (whole ? warp : (cta % rest_slices) * (kWarps / rest_slices) + warp / rest_slices);
+        t.slice = whole ? 0 : warp % rest_slices;
+        t.expert = static_cast<int32_t>(l.entry[2 * t.entry]);
+        t.first = static_cast<int32_t>(l.entry[2 * t.entry + 1] & 0xffffu);
+        t.count = static_cast<int32_t>(l.entry[2 * t.entry + 1] >> 16);
+        const int32_t r0 = tile * (p.gated ? 8 : 16) + static_cast<int32_t>(m), r1 = p.gated ? r0 : r0 + 8;
+        t.has0 = r0 < p.inner;
+        t.has1 = r1 < p.inner;
+        t.row0 = t.has0 ? r0 : 0;
+        t.row1 = !t.has1 ? 0 : p.gated ? r1 + p.inner : r1;
+        return t;
+    };
+    // x in pieces: the chunks (whole runs of four) whose tokens fit the shared memory
+    const int32_t piece = min(chunks, p.piece / 512 & ~(kFewAhead - 1));
+    auto span_of = [&](const Work &t, int32_t begin) {
+        int32_t first, n;
+        few_slice(min(piece, chunks - begin), t.slice, t.slices, first, n);
+        return few_span(p.w, t.expert, t.row0, t.row1, begin + first, __any_sync(0xffffffffu, t.has0) ? n : 0, q);
+    };
+
+    FewRaw raw[kFewAhead];
+    FewSpan span{};
+    if (my_rounds > 0) {
+        span = span_of(work_of(0), 0);
+        few_begin<ALIGN>(raw, span);
+    }
+    int32_t staged_entry = -1, staged_begin = -1;
+    for (int32_t round = 0; round < my_rounds; ++round) {
+        const Work now = work_of(round);
+        float acc[4] = {};
+        for (int32_t begin = 0; begin < chunks; begin += piece) {
+            if (now.entry != staged_entry || begin != staged_begin) {
+                // the entry's tokens, as the products read them
+                __syncthreads();
+                if (now.entry != staged_entry) {
+                    if (threadIdx.x < now.count)
+                        s_row[threadIdx.x] = static_cast<const uint16_t *>(p.x) + static_cast<int64_t>(l.list[now.first + threadIdx.x] / p.top_k) * p.ldx;
+                    __syncthreads();
+                }
+                // 16-byte pieces in their places: chunk, eight choices, four lanes.  Four on their way at a time.
+                const int32_t pieces = min(piece, chunks - begin) * 4;      // of a choice
+                for (int32_t n = 0; n < now.count; ++n) {
+                    const uint16_t *row = s_row[n];
+                    for (int32_t u0 = static_cast<int32_t>(threadIdx.x); u0 < pieces; u0 += 4 * kFewUpThreads) {
+                        uint4 v[4];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        f.row[i] = has[i] ? w.values + expert * w.matrix + r[i] * w.ld : nullptr;
-        f.scale[i] = nullptr;
-        if constexpr (few_is4(W)) {
-            if (has[i]) f.scale[i] = w.scales + expert * w.scale_matrix + static_cast<int64_t>(r[i] >> 7) * w.atoms * 512 + (r[i] & 31) * 16 + ((r[i] >> 5) & 3) * 4;
+                        for (int i = 0; i < 4; ++i) {
+                            const int32_t u = u0 + i * kFewUpThreads;
+                            v[i] = u < pieces ? few_load_x(row, begin * kFewChunk + u * 8, p.w.depth, p.x_vec) : make_uint4(0u, 0u, 0u, 0u);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int32_t u = u0 + i * kFewUpThreads;
+                            if (u < pieces) s_x[(u >> 2) * 32 + n * 4 + (u & 3)] = v[i];
+                        }
+                    }
+                }
+                __syncthreads();
+                staged_entry = now.entry;
+                staged_begin = begin;
+            }
+            const FewSpan here = span;
+            span.n = 0;
+            if (begin + piece < chunks) span = span_of(now, begin + piece);
+            else if (round + 1 < my_rounds) span = span_of(work_of(round + 1), 0);
+            const uint4 *x = s_x + (here.first - begin) * 32 + lane;
+            few_walk<ALIGN>(raw, p.w, here, span, q, [&](const FewRaw &r, int32_t i) { few_products<T>(acc, r, x[i * 32]); });
+            if (here.n < kFewAhead) few_begin<ALIGN>(raw, span);      // nothing was fetched on the way
+        }
+        if (now.slices > 1) {
+            if (now.slice > 0) s_part[warp][lane] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            __syncthreads();
+            if (now.slice == 0) {
+                for (int32_t s = 1; s < now.slices; ++s) {
+                    const float4 v = s_part[warp + s][lane];
+                    acc[0] += v.x, acc[1] += v.y, acc[2] += v.z, acc[3] += v.w;
+                }
+            }
+        }
+        if (now.slice == 0) {
+            // this lane's row of h (without a gate: its two rows); whole chunks are written, zeros beyond inner
+            const int32_t unit = round < rounds ? cta * rounds + round : rounds * ctas + cta / rest_slices;
+            const int32_t tile = (unit - now.entry * p.groups) * kWarps + (round < rounds ? warp : (cta % rest_slices) * (kWarps / rest_slices) + warp / rest_slices);
+            const int32_t k0 = tile * (p.gated ? 8 : 16) + static_cast<int32_t>(m);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int32_t at = static_cast<int32_t>(q) * 2 + j;
+                const bool used = at < now.count;
+                const int64_t c = used ? l.list[now.first + at] : 0;
+                const float u0 = acc[j], u1 = acc[2 + j];
+                const float v[2] = {now.has0 ? (p.gated ? few_silu(u0) * u1 : few_silu(u0)) : 0.0f, now.has1 && !p.gated ? few_silu(u1) : 0.0f};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (i == 1 && p.gated) break;
+                    const int32_t k = k0 + 8 * i;
+                    float top = few_finite(v[i]);
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    if (used && k < p.h_stride) {
+                        p.h[c * p.h_stride + k] = v[i];
+                        if (!std::is_same<T, __nv_bfloat16>::value && m == 0) p.top[(c * p.h_stride + k) >> 3] = top;
+                    }
+                }
+            }
         }
     }
-    return f;
 }
 
-template <int W>
-__device__ __forceinline__ void few_fetch(FewRaw &raw, const FewWeights &w, const FewRows &f, int32_t chunk, int32_t end, uint32_t q)
-{
-    const int32_t bytes = few_is4(W) ? (w.depth + 1) / 2 : w.depth * 2;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        raw.v[i] = few_load<W>(chunk < end ? f.row[i] : nullptr, chunk * 64 + static_cast<int32_t>(q) * 16, bytes, w.align);
-        raw.s[i] = 0u;
-        if constexpr (W == kFewNv) {
-            const int32_t atom = chunk * 2 + static_cast<int32_t>(q >> 1);
-            if (f.row[i] != nullptr && chunk < end && atom < w.atoms) raw.s[i] = *reinterpret_cast<const uint16_t *>(f.scale[i] + static_cast<int64_t>(atom) * 512 + (q & 1u) * 2u);
-        } else if constexpr (W == kFewMx) {
-            if (f.row[i] != nullptr && chunk < end) raw.s[i] = f.scale[i][static_cast<int64_t>(chunk) * 512 + q];
-        }
-    }
-}
-
-__device__ __forceinline__ uint32_t few_mul2(uint32_t a, uint32_t b, __nv_bfloat16)
-{
-    uint32_t d;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-__device__ __forceinline__ uint32_t few_mul2(uint32_t a, uint32_t b, __half)
-{
-    uint32_t d;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-
-// Eight codes as four pairs (0, 4), (1, 5), (2, 6), (3, 7): bf16 times 2^-126, or fp16 times 2^-14.
-template <class T>
-__device__ __forceinline__ void few_spread(uint32_t w, uint32_t (&d)[4])
-{
-    constexpr bool kHalf = sizeof(T) == 2 && std::is_same<T, __half>::value;
-    constexpr int kUp = kHalf ? 9 : 6;
-    constexpr uint32_t kMag = kHalf ? 0x0e000e00u : 0x01c001c0u, kSign = 0x80008000u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = kUp - 4 * i, s = 12 - 4 * i;
-        const uint32_t mag = m >= 0 ? w << m : w >> -m, sign = s >= 0 ? w << s : w >> -s;
-        d[i] = (mag & kMag) | (sign & kSign);
-    }
-}
-
-// The scales of a lane's run of 32 weights as pairs to multiply by (one for 16 of them each), and what the sums are then too small by.
-template <int W, class T>
-__device__ __forceinline__ void few_scales(uint32_t s, uint32_t (&d)[2])
-{
-    constexpr bool kHalf = std::is_same<T, __half>::value;
-    if constexpr (W == kFewNv) {
-        const __half2 h = __half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(s), __NV_E4M3));
-        if constexpr (kHalf) {
-            const __half2 v = __hmul2(h, __floats2half2_rn(128.0f, 128.0f));             // at most 57344
-            const uint32_t b = *reinterpret_cast<const uint32_t *>(&v);
-            d[0] = __byte_perm(b, 0u, 0x1010);
-            d[1] = __byte_perm(b, 0u, 0x3232);
-        } else {
-            const float2 f = __half22float2(h);
-            d[0] = __byte_perm(__float_as_uint(f.x * 0x1p118f), 0u, 0x3232);
-            d[1] = __byte_perm(__float_as_uint(f.y * 0x1p118f), 0u, 0x3232);
-        }
-    } else {
-        // 2^(s - 127), a bf16 (the smallest is subnormal; 255: NaN)
-        const uint32_t b = s == 0u ? 0x40u : s == 255u ? 0x7fffu : s << 7;
-        d[0] = d[1] = b | (b << 16);
-    }
-}
-template <int W, class T>
-__device__ __forceinline__ float few_missing(const FewWeights &w, int32_t expert)
-{
-    if constexpr (W == kFewNv) return w.factor[expert] * (std::is_same<T, __half>::value ? 128.0f : 256.0f);
-    else if constexpr (W == kFewMx) return 64.0f;
-    else return 1.0f;
-}
-
-// Word i of a run of 4-bit weights as the instruction's operand.
-template <int W, class T>
-__device__ __forceinline__ void few_weights4(uint32_t word, const uint32_t (&s)[2], int i, uint32_t (&d)[4])
-{
-    few_spread<T>(word, d);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if constexpr (W == kFewMx) d[j] = few_mul2(d[j], 0x7b807b80u, T());              // 2^120 first: 2^-126 times 2^(120 + ...) may not have a scale of its own
-        d[j] = few_mul2(d[j], s[i / 2], T());
-    }
-}
+// ---- launch 2: y = sum of weight * (W2 h) ------------------------------------------------------------------------------
 
 // The sum of two bf16 that a number is, or is nearest to; pairs of numbers.
 __device__ __forceinline__ void few_two_parts(float a, float b, uint32_t &hi, uint32_t &lo)
@@ -308,339 +489,135 @@ __device__ __forceinline__ void few_two_parts(float a, float b, uint32_t &hi, ui
     // infinities and NaN are their first part alone
     lo = pack_pair(fabsf(ah) < __int_as_float(0x7f800000) ? a - ah : 0.0f, fabsf(bh) < __int_as_float(0x7f800000) ? b - bh : 0.0f, __nv_bfloat16());
 }
-__device__ __forceinline__ void few_two_parts(uint32_t f16x2, uint32_t &hi, uint32_t &lo)
-{
-    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&f16x2));
-    few_two_parts(f.x, f.y, hi, lo);
-}
 
-// The order in which a run of 8 consecutive k meets 8 codes.
-__device__ __forceinline__ uint4 few_like_codes(uint4 v)
-{
-    return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-}
-
-// Where element k of h lies in its choice's row.
-template <int W>
-__device__ __forceinline__ int64_t few_h_place(int32_t k)
-{
-    if constexpr (few_is4(W)) {
-        const int32_t run = k >> 3, e = k & 7;                   // run (c * 4 + q) * 4 + i lies at (c * 4 + i) * 4 + q
-        return ((run & ~15) + (run & 3) * 4 + ((run >> 2) & 3)) * 8 + (e & 3) * 2 + (e >> 2);
-    } else {
-        return k;
-    }
-}
-
-// ---- launch 1: h = act(W1 x) ------------------------------------------------------------------------------------------
-
-// 8 consecutive elements of x, zeros beyond its end.
-__device__ __forceinline__ uint4 few_load_x(const uint16_t *row, int32_t k, int32_t depth, int32_t vec)
-{
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (row == nullptr || k >= depth) return v;
-    if (vec && k + 8 <= depth) return *reinterpret_cast<const uint4 *>(row + k);
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (k + i < depth) w[i / 2] |= static_cast<uint32_t>(row[k + i]) << (16 * (i & 1));
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// One chunk of a tile's contraction for NT runs of 8 choices.  T: the products' type; X16: x is fp16.
-template <int W, class T, bool X16, int NT>
-__device__ __forceinline__ void few_up_chunk(float (&acc)[2][4], const FewRaw &raw, const uint16_t *const (&x)[2], int32_t chunk, int32_t depth, int32_t vec, uint32_t q)
-{
-    constexpr bool kTwo = X16 && !std::is_same<T, __half>::value;      // x in two parts
-    auto products = [&](int n, const uint32_t (&a)[4], const uint32_t (&b)[4], const uint4 &v) {
-        few_mma(acc[n], a[0], b[0], a[1], b[1], v.x, v.y, T());
-        few_mma(acc[n], a[2], b[2], a[3], b[3], v.z, v.w, T());
-    };
-    auto with_x = [&](const uint32_t (&a)[4], const uint32_t (&b)[4], int32_t k) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            uint4 v = few_load_x(x[n], k, depth, vec);
-            if constexpr (few_is4(W)) v = few_like_codes(v);
-            if constexpr (kTwo) {
-                uint4 hi, lo;
-                few_two_parts(v.x, hi.x, lo.x);
-                few_two_parts(v.y, hi.y, lo.y);
-                few_two_parts(v.z, hi.z, lo.z);
-                few_two_parts(v.w, hi.w, lo.w);
-                products(n, a, b, hi);
-                products(n, a, b, lo);
-            } else {
-                products(n, a, b, v);
-            }
-        }
-    };
-    if constexpr (few_is4(W)) {
-        uint32_t s0[2], s1[2];
-        few_scales<W, T>(raw.s[0], s0);
-        few_scales<W, T>(raw.s[1], s1);
-        const uint32_t w0[4] = {raw.v[0].x, raw.v[0].y, raw.v[0].z, raw.v[0].w}, w1[4] = {raw.v[1].x, raw.v[1].y, raw.v[1].z, raw.v[1].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t a[4], b[4];
-            few_weights4<W, T>(w0[i], s0, i, a);
-            few_weights4<W, T>(w1[i], s1, i, b);
-            with_x(a, b, chunk * 128 + static_cast<int32_t>(q) * 32 + i * 8);
-        }
-    } else {
-        const uint32_t a[4] = {raw.v[0].x, raw.v[0].y, raw.v[0].z, raw.v[0].w}, b[4] = {raw.v[1].x, raw.v[1].y, raw.v[1].z, raw.v[1].w};
-        with_x(a, b, chunk * 32 + static_cast<int32_t>(q) * 8);
-    }
-}
-
-__device__ __forceinline__ float few_silu(float u) { return u / (1.0f + __expf(-u)); }
-
-template <int W, bool X16>
-__global__ void __launch_bounds__(kFewUpThreads, 2)
-few_up_kernel(const FewParams p)
-{
-    using T = std::conditional_t<X16 && W != kFewMx, __half, __nv_bfloat16>;
-    constexpr int kWarps = kFewUpThreads / 32, kAhead = 4;        // chunks fetched together
-    extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ float s_part[kWarps][32][8];
-    const FewLists l = few_lists(smem, p);
-    grid_dependency_wait();
-    grid_launch_dependents();                                     // launch 2 may read the call's inputs from here on
-    few_make_lists(p, l);
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, q = lane & 3u, m = lane >> 2;
-    const int32_t slice = static_cast<int32_t>(warp) % p.slices, per_cta = kWarps / p.slices;
-    const int64_t items = static_cast<int64_t>(*l.total) * p.tiles;
-    const int32_t begin = slice * p.slice_chunks, depth_chunks = (p.w.depth + few_chunk(W) - 1) / few_chunk(W), end = min(begin + p.slice_chunks, depth_chunks);
-    const int32_t groups = max(0, (end - begin + kAhead - 1) / kAhead);
-
-    struct Item {
-        int32_t expert, first, count, row0, row1;
-        bool has0, has1;
-    };
-    auto item_of = [&](int64_t i) {
-        Item t;
-        const int32_t e = static_cast<int32_t>(i / p.tiles), tile = static_cast<int32_t>(i - static_cast<int64_t>(e) * p.tiles);
-        t.expert = static_cast<int32_t>(l.entry[2 * e]);
-        t.first = static_cast<int32_t>(l.entry[2 * e + 1] & 0xffffu);
-        t.count = static_cast<int32_t>(l.entry[2 * e + 1] >> 16);
-        t.row0 = tile * (p.gated ? 8 : 16) + static_cast<int32_t>(m);
-        t.row1 = p.gated ? t.row0 + p.inner : t.row0 + 8;
-        t.has0 = t.row0 < p.inner;
-        t.has1 = p.gated ? t.has0 : t.row1 < p.inner;
-        return t;
-    };
-    FewRaw next[kAhead];
-    auto fetch = [&](const FewRows &f, int32_t chunk) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) few_fetch<W>(next[u], p.w, f, chunk + u, end, q);
-    };
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * per_cta;
-    int64_t i = static_cast<int64_t>(blockIdx.x) * per_cta + warp / p.slices;
-    if (i < items && groups > 0) {
-        const Item t = item_of(i);
-        fetch(few_rows<W>(p.w, t.expert, t.row0, t.row1, t.has0, t.has1), begin);
-    }
-    // CTA-uniform rounds: a round's slices meet in shared memory
-    for (int64_t round = static_cast<int64_t>(blockIdx.x) * per_cta; round < items; round += stride, i += stride) {
-        const bool mine = i < items;
-        Item t{};
-        float acc[2][4] = {};
-        if (mine) {
-            t = item_of(i);
-            const FewRows f = few_rows<W>(p.w, t.expert, t.row0, t.row1, t.has0, t.has1);
-            const uint16_t *x[2];
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const int32_t at = n * 8 + static_cast<int32_t>(m);
-                x[n] = at < t.count ? static_cast<const uint16_t *>(p.x) + static_cast<int64_t>(l.list[t.first + at] / p.top_k) * p.ldx : nullptr;
-            }
-            for (int32_t g = 0; g < groups; ++g) {
-                FewRaw now[kAhead];
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u) now[u] = next[u];
-                if (g + 1 < groups) {
-                    fetch(f, begin + (g + 1) * kAhead);
-                } else if (i + stride < items) {
-                    const Item o = item_of(i + stride);
-                    fetch(few_rows<W>(p.w, o.expert, o.row0, o.row1, o.has0, o.has1), begin);
-                }
-#pragma unroll
-                for (int u = 0; u < kAhead; ++u) {
-                    const int32_t chunk = begin + g * kAhead + u;
-                    if (chunk < end) {
-                        if (t.count <= 8) few_up_chunk<W, T, X16, 1>(acc, now[u], x, chunk, p.w.depth, p.x_vec, q);
-                        else few_up_chunk<W, T, X16, 2>(acc, now[u], x, chunk, p.w.depth, p.x_vec, q);
-                    }
-                }
-            }
-        }
-        if (p.slices > 1) {
-            if (slice > 0) {
-                *reinterpret_cast<float4 *>(&s_part[warp][lane][0]) = make_float4(acc[0][0], acc[0][1], acc[0][2], acc[0][3]);
-                *reinterpret_cast<float4 *>(&s_part[warp][lane][4]) = make_float4(acc[1][0], acc[1][1], acc[1][2], acc[1][3]);
-            }
-            __syncthreads();
-            if (slice == 0) {
-                for (int32_t s = 1; s < p.slices; ++s) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[j / 4][j & 3] += s_part[warp + s][lane][j];
-                }
-            }
-            __syncthreads();
-        }
-        if (mine && slice == 0) {
-            const float missing = few_missing<W, T>(p.w, t.expert);
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int32_t at = n * 8 + static_cast<int32_t>(q) * 2 + j;
-                    if (at >= t.count) continue;
-                    const int64_t c = l.list[t.first + at];
-                    const float u0 = acc[n][j] * missing, u1 = acc[n][2 + j] * missing;
-                    // runs of 8 are written whole: zeros beyond inner
-                    const int32_t room = (p.inner + 7) & ~7;
-                    auto put = [&](int32_t k, float v) {
-                        if (k >= room) return;
-                        uint32_t hi, lo;
-                        few_two_parts(v, 0.0f, hi, lo);
-                        __nv_bfloat16 *dst = p.h + c * p.h_stride + few_h_place<W>(k);
-                        *reinterpret_cast<uint16_t *>(dst) = static_cast<uint16_t>(hi);
-                        *reinterpret_cast<uint16_t *>(dst + p.choices * p.h_stride) = static_cast<uint16_t>(lo);
-                    };
-                    if (p.gated) {
-                        put(t.row0, t.has0 ? few_silu(u0) * u1 : 0.0f);
-                    } else {
-                        put(t.row0, t.has0 ? few_silu(u0) : 0.0f);
-                        put(t.row1, t.has1 ? few_silu(u1) : 0.0f);
-                    }
-                }
-            }
-        }
-    }
-}
-
-// ---- launch 2: y = sum of weight * (W2 h) ------------------------------------------------------------------------------
-
-template <int W, int NT>
-__device__ __forceinline__ void few_down_chunk(float (&acc)[2][4], const FewRaw &raw, const uint8_t *const (&h)[2], int64_t part, int32_t chunk, int32_t runs, uint32_t q)
-{
-    using B = __nv_bfloat16;
-    auto with_h = [&](const uint32_t (&a)[4], const uint32_t (&b)[4], const uint32_t (&a2)[4], const uint32_t (&b2)[4], int32_t run, int32_t at) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            uint4 hi = make_uint4(0u, 0u, 0u, 0u), lo = hi;
-            if (h[n] != nullptr && run < runs) {
-                hi = *reinterpret_cast<const uint4 *>(h[n] + at * 16);
-                lo = *reinterpret_cast<const uint4 *>(h[n] + part + at * 16);
-            }
-            few_mma(acc[n], a[0], b[0], a[1], b[1], hi.x, hi.y, B());
-            few_mma(acc[n], a[2], b[2], a[3], b[3], hi.z, hi.w, B());
-            few_mma(acc[n], a[0], b[0], a[1], b[1], lo.x, lo.y, B());
-            few_mma(acc[n], a[2], b[2], a[3], b[3], lo.z, lo.w, B());
-            if constexpr (W == kFewF16) {
-                few_mma(acc[n], a2[0], b2[0], a2[1], b2[1], hi.x, hi.y, B());
-                few_mma(acc[n], a2[2], b2[2], a2[3], b2[3], hi.z, hi.w, B());
-            }
-        }
-    };
-    if constexpr (few_is4(W)) {
-        uint32_t s0[2], s1[2];
-        few_scales<W, B>(raw.s[0], s0);
-        few_scales<W, B>(raw.s[1], s1);
-        const uint32_t w0[4] = {raw.v[0].x, raw.v[0].y, raw.v[0].z, raw.v[0].w}, w1[4] = {raw.v[1].x, raw.v[1].y, raw.v[1].z, raw.v[1].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t a[4], b[4];
-            few_weights4<W, B>(w0[i], s0, i, a);
-            few_weights4<W, B>(w1[i], s1, i, b);
-            with_h(a, b, a, b, (chunk * 4 + static_cast<int32_t>(q)) * 4 + i, (chunk * 4 + i) * 4 + static_cast<int32_t>(q));
-        }
-    } else {
-        uint32_t a[4] = {raw.v[0].x, raw.v[0].y, raw.v[0].z, raw.v[0].w}, b[4] = {raw.v[1].x, raw.v[1].y, raw.v[1].z, raw.v[1].w}, a2[4], b2[4];
-        if constexpr (W == kFewF16) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t wa = j == 0 ? raw.v[0].x : j == 1 ? raw.v[0].y : j == 2 ? raw.v[0].z : raw.v[0].w;
-                const uint32_t wb = j == 0 ? raw.v[1].x : j == 1 ? raw.v[1].y : j == 2 ? raw.v[1].z : raw.v[1].w;
-                few_two_parts(wa, a[j], a2[j]);
-                few_two_parts(wb, b[j], b2[j]);
-            }
-        }
-        const int32_t run = chunk * 4 + static_cast<int32_t>(q);
-        with_h(a, b, a2, b2, run, run);
-    }
-}
-
-// grid: 16 rows of W2 (outputs) a CTA.  Dynamic shared memory: the lists, then slices x choices x 16 sums.
-template <int W, class Y>
+// grid: 16 rows of W2 (outputs) a CTA.  Dynamic shared memory: the lists, the choices' weights, most_slices x choices x 16 sums, then each warp's part of h
+// (p.piece bytes) as the products read it: [choice][chunk][part][4 lanes], choices 64 bytes further apart than they need be.
+template <class T, int ALIGN>
 __global__ void __launch_bounds__(kFewDownThreads, 1)
 few_down_kernel(const FewParams p)
 {
-    constexpr int kWarps = kFewDownThreads / 32, kAhead = 4;
+    constexpr bool kHalf = std::is_same<T, __half>::value;
+    constexpr int kWarps = kFewDownThreads / 32, kParts = kHalf ? 1 : 2;
     extern __shared__ __align__(16) uint8_t smem[];
     const FewLists l = few_lists(smem, p);
-    float *part = reinterpret_cast<float *>(smem + ((few_list_bytes(p.experts, p.choices) + 15) & ~15));
+    float *s_weight = reinterpret_cast<float *>(smem + few_list_bytes(p.experts, p.choices)), *part = s_weight + ((p.choices + 3) & ~3);
+    const int32_t warp = static_cast<int32_t>(threadIdx.x >> 5);
+    uint4 *s_h = reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(part + p.most_slices * p.choices * 16) + warp * p.piece);
     grid_launch_dependents();
-    few_make_lists(p, l);                                         // an input of the call: launch 1 has waited for it
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, q = lane & 3u, m = lane >> 2;
-    const int32_t items = *l.total * p.slices, row0 = static_cast<int32_t>(blockIdx.x) * 16 + static_cast<int32_t>(m);
-    const int32_t depth_chunks = (p.w.depth + few_chunk(W) - 1) / few_chunk(W), runs = (p.w.depth + 7) / 8;
-    const bool has0 = row0 < p.w.rows, has1 = row0 + 8 < p.w.rows;
-    FewRaw next[kAhead];
-    struct Span {
-        int32_t begin, end;
+    for (int32_t c = static_cast<int32_t>(threadIdx.x); c < p.choices; c += kFewDownThreads) s_weight[c] = p.weights[c];      // inputs of the call: launch 1 has waited for them
+    few_make_lists(p, l);
+    const uint32_t lane = threadIdx.x & 31u, q = lane & 3u, m = lane >> 2;
+    const int32_t r0 = static_cast<int32_t>(blockIdx.x) * 16 + static_cast<int32_t>(m), chunks = (p.w.depth + kFewChunk - 1) / kFewChunk;
+    const int32_t row0 = r0 < p.w.rows ? r0 : 0, row1 = r0 + 8 < p.w.rows ? r0 + 8 : 0;
+    // rounds of an entry per warp; those left over are shared by several warps
+    const int32_t entries = *l.total, rounds = entries / kWarps, rest = entries - rounds * kWarps;
+    int32_t rest_slices = 1;
+    while (rest_slices * 2 <= p.most_slices && rest * rest_slices * 2 <= kWarps) rest_slices *= 2;
+    const int32_t my_rounds = rounds + (warp < rest * rest_slices ? 1 : 0);
+    struct Work {
+        int32_t expert, first, count, chunk0, n, slice;
     };
-    auto span_of = [&](int32_t i) {
-        const int32_t b = (i % p.slices) * p.slice_chunks;
-        return Span{b, min(b + p.slice_chunks, depth_chunks)};
+    auto work_of = [&](int32_t round) {
+        Work t;
+        const bool whole = round < rounds;
+        const int32_t entry = whole ? round * kWarps + warp : rounds * kWarps + warp / rest_slices;
+        t.slice = whole ? 0 : warp % rest_slices;
+        t.expert = static_cast<int32_t>(l.entry[2 * entry]);
+        t.first = static_cast<int32_t>(l.entry[2 * entry + 1] & 0xffffu);
+        t.count = static_cast<int32_t>(l.entry[2 * entry + 1] >> 16);
+        few_slice(chunks, t.slice, whole ? 1 : rest_slices, t.chunk0, t.n);
+        return t;
     };
-    auto fetch = [&](int32_t i, int32_t g) {
-        const Span s = span_of(i);
-        const FewRows f = few_rows<W>(p.w, static_cast<int32_t>(l.entry[2 * (i / p.slices)]), row0, row0 + 8, has0, has1);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) few_fetch<W>(next[u], p.w, f, s.begin + g * kAhead + u, s.end, q);
+    // the chunks of h that fit a warp's shared memory (whole runs of four, if it has room for four)
+    auto piece_of = [&](int32_t count) {
+        const int32_t fit = (p.piece / count - 64) / (64 * kParts);
+        return fit >= kFewAhead ? fit & ~(kFewAhead - 1) : fit;
     };
-    int32_t i = static_cast<int32_t>(warp);
-    if (i < items) fetch(i, 0);
+    auto span_of = [&](const Work &t, int32_t begin) { return few_span(p.w, t.expert, row0, row1, t.chunk0 + begin, min(piece_of(t.count), t.n - begin), q); };
+    FewRaw raw[kFewAhead];
+    FewSpan span{};
+    if (my_rounds > 0) {
+        span = span_of(work_of(0), 0);
+        few_begin<ALIGN>(raw, span);
+    }
     grid_dependency_wait();                                       // h
-    const int32_t groups = (p.slice_chunks + kAhead - 1) / kAhead;
-    for (; i < items; i += kWarps) {
-        const uint32_t expert = l.entry[2 * (i / p.slices)], where = l.entry[2 * (i / p.slices) + 1];
-        const int32_t first = static_cast<int32_t>(where & 0xffffu), count = static_cast<int32_t>(where >> 16);
-        const Span s = span_of(i);
-        const uint8_t *h[2];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int32_t at = n * 8 + static_cast<int32_t>(m);
-            h[n] = at < count ? reinterpret_cast<const uint8_t *>(p.h + l.list[first + at] * p.h_stride) : nullptr;
+    for (int32_t round = 0; round < my_rounds; ++round) {
+        const Work now = work_of(round);
+        const int32_t piece = piece_of(now.count), pitch = (min(piece, now.n) * kParts + 1) * 4;      // 16-byte pieces from a choice to the next
+        FewScale range{1.0f, 1.0f};                               // of choice m, in its four lanes
+        if constexpr (kHalf) {
+            const int64_t c = l.list[now.first + min(static_cast<int32_t>(m), now.count - 1)];
+            const float4 *tops = reinterpret_cast<const float4 *>(p.top + (c * p.h_stride >> 3));      // h_stride / 8 is a multiple of 4
+            float top = 0.0f;
+#pragma unroll 4
+            for (int32_t i = static_cast<int32_t>(q); i < p.h_stride >> 5; i += 4) {
+                const float4 v = tops[i];
+                top = fmaxf(fmaxf(top, v.x), fmaxf(fmaxf(v.y, v.z), v.w));
+            }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            range = few_range(__float_as_uint(fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2))));
         }
-        const int64_t second = p.choices * p.h_stride * 2;
-        float acc[2][4] = {};
-        for (int32_t g = 0; g < groups; ++g) {
-            FewRaw now[kAhead];
+        float acc[4] = {};
+        for (int32_t begin = 0; begin < now.n; begin += piece) {
+            const FewSpan here = span;
+            // h of the entry's choices: 16-byte pieces, four on their way at a time
+            __syncwarp();
+            const int32_t pieces = min(piece, now.n - begin) * 4;
+            for (int32_t n = 0; n < now.count; ++n) {
+                const float *src = p.h + static_cast<int64_t>(l.list[now.first + n]) * p.h_stride + here.first * kFewChunk;
+                const float s = __shfl_sync(0xffffffffu, range.scale, n * 4);
+                for (int32_t u0 = static_cast<int32_t>(lane); u0 < pieces; u0 += 128) {
+                    float4 v[4][2];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) now[u] = next[u];
-            if (g + 1 < groups) fetch(i, g + 1);
-            else if (i + kWarps < items) fetch(i + kWarps, 0);
+                    for (int i = 0; i < 4; ++i) {
+                        const float4 *at = reinterpret_cast<const float4 *>(src + min(u0 + i * 32, pieces - 1) * 8);
+                        v[i][0] = at[0];
+                        v[i][1] = at[1];
+                    }
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const int32_t chunk = s.begin + g * kAhead + u;
-                if (chunk < s.end) {
-                    if (count <= 8) few_down_chunk<W, 1>(acc, now[u], h, second, chunk, runs, q);
-                    else few_down_chunk<W, 2>(acc, now[u], h, second, chunk, runs, q);
+                    for (int i = 0; i < 4; ++i) {
+                        const int32_t u = u0 + i * 32;
+                        if (u >= pieces) break;
+                        const float4 a = v[i][0], b = v[i][1];
+                        if constexpr (kHalf) {
+                            s_h[n * pitch + u] = make_uint4(pack_pair(a.x * s, a.y * s, __half()), pack_pair(a.z * s, a.w * s, __half()), pack_pair(b.x * s, b.y * s, __half()),
+                                                            pack_pair(b.z * s, b.w * s, __half()));
+                        } else {
+                            uint4 hi, lo;
+                            few_two_parts(a.x, a.y, hi.x, lo.x);
+                            few_two_parts(a.z, a.w, hi.y, lo.y);
+                            few_two_parts(b.x, b.y, hi.z, lo.z);
+                            few_two_parts(b.z, b.w, hi.w, lo.w);
+                            s_h[n * pitch + (u >> 2) * 8 + (u & 3)] = hi;
+                            s_h[n * pitch + (u >> 2) * 8 + 4 + (u & 3)] = lo;
+                        }
+                    }
                 }
             }
+            __syncwarp();
+            span.n = 0;
+            if (begin + piece < now.n) span = span_of(now, begin + piece);
+            else if (round + 1 < my_rounds) span = span_of(work_of(round + 1), 0);
+            const uint4 *h = s_h + min(static_cast<int32_t>(m), now.count - 1) * pitch + q;
+            few_walk<ALIGN>(raw, p.w, here, span, q, [&](const FewRaw &r, int32_t i) {
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) few_products<T>(acc, r, h[(i * kParts + k) * 4]);
+            });
+            if (here.n < kFewAhead) few_begin<ALIGN>(raw, span);          // nothing was fetched on the way
         }
-        const float missing = few_missing<W, __nv_bfloat16>(p.w, static_cast<int32_t>(expert));
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int32_t at = n * 8 + static_cast<int32_t>(q) * 2 + j;
-                if (at >= count) continue;
-                float *dst = part + (static_cast<int64_t>(i % p.slices) * p.choices + l.list[first + at]) * 16;
-                dst[m] = acc[n][j] * missing;
-                dst[m + 8] = acc[n][2 + j] * missing;
+        for (int j = 0; j < 2; ++j) {
+            const int32_t at = static_cast<int32_t>(q) * 2 + j;
+            const float s = __shfl_sync(0xffffffffu, range.inverse, at * 4);
+            if (at >= now.count) continue;
+            float *dst = part + (now.slice * p.choices + l.list[now.first + at]) * 16;
+            dst[m] = acc[j] * s;
+            dst[m + 8] = acc[2 + j] * s;
+        }
+        // an entry that one warp had alone has one sum for each choice: the other slices' are zeros
+        if (round < rounds) {
+            for (int32_t s = 1; s < rest_slices; ++s) {
+                for (int32_t i = static_cast<int32_t>(lane); i < now.count * 16; i += 32) part[(s * p.choices + l.list[now.first + (i >> 4)]) * 16 + (i & 15)] = 0.0f;
             }
         }
     }
@@ -651,12 +628,12 @@ few_down_kernel(const FewParams p)
         float sum = 0.0f;
         for (int32_t j = 0; j < p.top_k; ++j) {
             const int32_t c = t * p.top_k + j;
-            if (l.rank[c] == kFewNone) continue;
+            if (l.expert[c] == kFewNone) continue;
             float v = 0.0f;
-            for (int32_t s = 0; s < p.slices; ++s) v += part[(static_cast<int64_t>(s) * p.choices + c) * 16 + r];
-            sum = fmaf(p.weights[c], v, sum);
+            for (int32_t s = 0; s < rest_slices; ++s) v += part[(s * p.choices + c) * 16 + r];
+            sum = fmaf(s_weight[c], v, sum);
         }
-        static_cast<Y *>(p.y)[t * p.ldy + row] = narrow_to<Y>(sum);
+        static_cast<T *>(p.y)[t * p.ldy + row] = narrow_to<T>(sum);
     }
 }
 

@@ -202,11 +202,151 @@ hgemm_status_t launch(hgemm_ctx_s *ctx, const void *fn, dim3 grid, int threads, 
     return e == cudaSuccess ? HGEMM_OK : cuda_fail(ctx, e);
 }
 
+constexpr int kDigits = hgemm_dev::kFp4Digits;
+
+const void *digits_kernel_of(const hgemm_fp4_config_t &c, int32_t format)
+{
+    using namespace hgemm_dev;
+    if (format == HGEMM_FP4_NV) return c.block_q == 128 ? reinterpret_cast<const void *>(fp4_product_kernel<1, 128, true, true>) : reinterpret_cast<const void *>(fp4_product_kernel<1, 64, true, true>);
+    return c.block_q == 128 ? reinterpret_cast<const void *>(fp4_product_kernel<1, 128, false, true>) : reinterpret_cast<const void *>(fp4_product_kernel<1, 64, false, true>);
+}
+
+// At most as many tiles as `choices` rows of eight digits, over `groups` groups, can have.
+int64_t digits_tiles(int64_t choices, int64_t N, int32_t groups, const hgemm_fp4_config_t &c)
+{
+    return (std::min<int64_t>(groups, choices) + choices * kDigits / c.block_q) * ceil_div(N, 128);
+}
+
+// The forward product of rows that are written as sums of eight 4-bit rows each (DIGITS: M counts those), or any product of a plan.
+template <bool DIGITS>
+hgemm_status_t run_product(const hgemm_fp4_plan_s &plan, const void *A, int64_t lda, const void *a_scales, const float *a_factor, const void *B, int64_t ldb, const void *b_scales,
+                           const float *b_factor, void *C, int64_t ldc, const int32_t *offsets, int32_t accumulate, void *stream)
+{
+    hgemm_ctx_s *ctx = plan.ctx;
+    const int32_t form = plan.form, groups = plan.groups;
+    const int64_t M = plan.M, N = plan.N, K = plan.K;
+    const bool wgrad = form == HGEMM_FP8_WEIGHT_GRAD, nv = plan.format == HGEMM_FP4_NV;
+    const int64_t out_cols = form == HGEMM_FP8_FORWARD ? N : K;
+    const int64_t depth = wgrad ? (groups > 0 ? hgemm_fp8_padded_rows(M, groups) : M) : form == HGEMM_FP8_FORWARD ? K : N;       // contracted elements of the copies
+    if ((groups > 0) != (offsets != nullptr) || accumulate < 0 || accumulate > 1 || (accumulate && plan.out_type != HGEMM_TYPE_F32)) return HGEMM_ERR_INVALID_ARG;
+    if (lda < ceil_div(depth, 2) || ldb < ceil_div(depth, 2) || ldc < out_cols || (lda & 15) != 0 || (ldb & 15) != 0) return HGEMM_ERR_INVALID_ARG;
+    const int es = type_bytes(plan.out_type);
+    if (M == 0 && !wgrad) return HGEMM_OK;
+    if (!C || (reinterpret_cast<uintptr_t>(C) % unsigned(es)) != 0) return HGEMM_ERR_INVALID_ARG;
+    if (M == 0) {
+        if (accumulate) return HGEMM_OK;
+        const cudaError_t e = cudaMemset2DAsync(C, size_t(ldc) * size_t(es), 0, size_t(K) * size_t(es), size_t(N) * size_t(std::max(groups, 1)), static_cast<cudaStream_t>(stream));
+        return e == cudaSuccess ? HGEMM_OK : cuda_fail(ctx, e);
+    }
+    if (!A || !B || !a_scales || !b_scales || !aligned16(A) || !aligned16(B) || !aligned16(a_scales) || !aligned16(b_scales) || !aligned4(offsets)) return HGEMM_ERR_INVALID_ARG;
+    if (nv != (a_factor != nullptr) || nv != (b_factor != nullptr) || !aligned4(a_factor) || !aligned4(b_factor)) return HGEMM_ERR_INVALID_ARG;
+
+    const hgemm_fp4_config_t &c = plan.cfg;
+    const bool swap = c.cta_group == 1;                      // the kernel's P operand is the caller's B
+    Fp4Params p;
+    std::memset(&p, 0, sizeof(p));
+    p.stages = stages_of(c, nv, groups);
+    if (p.stages < 2) return HGEMM_ERR_UNSUPPORTED;
+    p.split = c.split_k;
+    p.groups = groups;
+    p.offsets = offsets;
+    p.rows_ragged = int32_t(M);
+    p.kblocks = int32_t(ceil_div(depth, 128));
+    p.k_capacity = int32_t(ceil_div(depth, 128));
+    const int64_t matrices = std::max(groups, 1);
+
+    // one side of the product: values (rows x depth, `count` matrices), their scale tiles, their factors
+    struct Side {
+        const void *base;
+        int64_t rows, count, ld;
+        const void *scales;
+        int64_t scale_tiles;
+        const float *factor;
+    } a, b;
+    const int64_t a_rows = wgrad ? N : M, b_rows = form == HGEMM_FP8_FORWARD ? N : K;
+    a = {A, a_rows, 1, lda, a_scales, !wgrad && groups > 0 ? hgemm_fp8_padded_rows(M, groups) / 128 : ceil_div(a_rows, 128), a_factor};
+    b = {B, b_rows, wgrad ? 1 : matrices, ldb, b_scales, ceil_div(b_rows, 128) * (wgrad ? 1 : matrices), b_factor};
+    const Side &P = swap ? b : a, &Q = swap ? a : b;
+    const int tp = 128 * c.cta_group, tq = c.block_q;
+    p.rows_p = int32_t(P.rows);
+    p.rows_q = int32_t(Q.rows);
+    p.tiles_p = int32_t(ceil_div(P.rows, tp));
+    p.tiles_q = int32_t(ceil_div(Q.rows, tq));
+    p.ragged = groups == 0 ? hgemm_dev::kRaggedNone : wgrad ? hgemm_dev::kRaggedK : swap ? hgemm_dev::kRaggedQ : hgemm_dev::kRaggedP;
+    const int64_t tiles = DIGITS ? digits_tiles(M / kDigits, N, groups, c) : tiles_of(form, M, N, K, groups, c);
+    if (tiles > (int64_t(1) << 30)) return HGEMM_ERR_UNSUPPORTED;
+    p.total = int32_t(tiles);
+    p.raster = std::min(8, p.tiles_p);
+    {
+        using hgemm_dev::make_fast_div;
+        const int32_t last = p.tiles_p - (p.tiles_p - 1) / p.raster * p.raster;         // rows of tiles of the last sweep
+        p.fd_other = make_fast_div(uint32_t(p.ragged == hgemm_dev::kRaggedP ? p.tiles_q : p.tiles_p));
+        p.fd_group = make_fast_div(uint32_t(p.tiles_p) * uint32_t(p.tiles_q));
+        p.fd_sweep = make_fast_div(uint32_t(p.raster) * uint32_t(p.tiles_q));
+        p.fd_raster = make_fast_div(uint32_t(p.raster));
+        p.fd_last = make_fast_div(uint32_t(last));
+    }
+    p.sp_group = int32_t(ceil_div(P.rows, 128));
+    p.sq_group = int32_t(ceil_div(Q.rows, 128));
+    p.fp = P.factor;
+    p.fq = Q.factor;
+    p.fp_group = P.count > 1 ? 1 : 0;
+    p.fq_group = Q.count > 1 ? 1 : 0;
+    p.out = C;
+    p.ldc = ldc;
+    p.c_group = wgrad ? N * ldc : 0;
+    p.out_type = plan.out_type;
+    p.accumulate = accumulate;
+    p.vec_ok = aligned16(C) && (ldc * es) % 16 == 0 && (out_cols * es) % 16 == 0 ? 1 : 0;      // a tensor store clips at multiples of 16 bytes only
+    // instruction descriptor of the block-scaled kinds: e2m1 operands (1) along the contraction; bit 23: scales are powers of two; bits 4 and 29: the
+    // scales' place in their word, set by the kernel
+    p.idesc = (1u << 7) | (1u << 10) | (uint32_t(tq >> 3) << 17) | (nv ? 0u : 1u << 23) | (uint32_t(tp >> 4) << 24);
+    p.status = ctx->d_status + plan.status_slot;
+    p.wait_budget = ctx->wait_budget;
+
+    CUtensorMap map_p, map_q, map_sp, map_sq, map_c;
+    const int64_t bytes = ceil_div(depth, 2), atoms = atoms_of(depth, plan.format);
+    if (!encode_values(ctx, &map_p, P.base, bytes, P.rows, P.count, P.ld, 128)) return HGEMM_ERR_CUDA;
+    if (!encode_values(ctx, &map_q, Q.base, bytes, Q.rows, Q.count, Q.ld, uint32_t(tq / c.cta_group))) return HGEMM_ERR_CUDA;
+    if (!encode_scales(ctx, &map_sp, P.scales, atoms, P.scale_tiles, nv, 1)) return HGEMM_ERR_CUDA;
+    if (!encode_scales(ctx, &map_sq, Q.scales, atoms, Q.scale_tiles, nv, uint32_t(hgemm_dev::fp4_scale_tiles(tq)))) return HGEMM_ERR_CUDA;
+    map_c = map_p;                                           // not used by the kernels that store through pointers
+    if (c.cta_group == 2 && p.vec_ok && !accumulate) {
+        if (!encode_results(ctx, &map_c, plan.out_type, C, out_cols, wgrad ? N : M, wgrad ? matrices : 1, ldc)) return HGEMM_ERR_CUDA;
+    }
+    const int per_unit = c.cta_group == 2 ? 2 : c.split_k;
+    // CTAs that share a tile through a cluster's shared memory take one tile each; the others walk the tiles
+    const int64_t units = c.split_k > 1 ? tiles : std::min<int64_t>(tiles, std::max(1, ctx->num_sms / per_unit));
+    if (units * per_unit > 0x7fffffff) return HGEMM_ERR_UNSUPPORTED;
+    void *args[6] = {&map_p, &map_q, &map_sp, &map_sq, &map_c, &p};
+    return launch(ctx, DIGITS ? digits_kernel_of(c, plan.format) : kernel_of(c, plan.format), dim3(unsigned(units * per_unit), 1, 1), hgemm_dev::kFp4Threads, kSmemOptIn, per_unit, args, stream);
+}
+
 } // namespace
 
 namespace hgemm_host {
 
 int status_slot_of(const hgemm_fp4_plan_s *plan) { return plan->status_slot; }
+
+hgemm_status_t fp4_digits_product(hgemm_ctx_s *ctx, int32_t format, int64_t choices, int64_t N, int64_t K, int32_t groups, const void *digits, int64_t ld, const void *digit_scales, const void *B,
+                                  int64_t ldb, const void *b_scales, const float *one, const float *b_factor, float *C, int64_t ldc, const int32_t *offsets, void *stream)
+{
+    hgemm_fp4_plan_s plan;
+    plan.ctx = ctx;
+    plan.form = HGEMM_FP8_FORWARD;
+    plan.M = choices * kDigits;
+    plan.N = N;
+    plan.K = K;
+    plan.groups = groups;
+    plan.format = format;
+    plan.out_type = HGEMM_TYPE_F32;
+    // 8 or 16 rows a tile, by what an expert has on average; CTAs that share a contraction where tiles leave SMs without work
+    plan.cfg = {1, choices > 8 * std::min<int64_t>(groups, choices) ? 128 : 64, 1, 0};
+    while (plan.cfg.split_k < 8 && digits_tiles(choices, N, groups, plan.cfg) * plan.cfg.split_k * 2 <= ctx->num_sms && ceil_div(K, 256) >= 2 * plan.cfg.split_k * 2) plan.cfg.split_k *= 2;
+    const cudaError_t e = cudaFuncSetAttribute(digits_kernel_of(plan.cfg, format), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemOptIn);
+    if (e != cudaSuccess) return cuda_fail(ctx, e);
+    return run_product<true>(plan, digits, ld, digit_scales, one, B, ldb, b_scales, b_factor, C, ldc, offsets, 0, stream);
+}
 
 } // namespace hgemm_host
 
@@ -416,105 +556,7 @@ hgemm_status_t hgemm_fp4_plan_set_config(hgemm_fp4_plan_t *plan, const hgemm_fp4
 hgemm_status_t hgemm_fp4_run(hgemm_fp4_plan_t *plan, const void *A, int64_t lda, const void *a_scales, const float *a_factor, const void *B, int64_t ldb, const void *b_scales,
                              const float *b_factor, void *C, int64_t ldc, const int32_t *offsets, int32_t accumulate, void *stream)
 {
-    if (!plan) return HGEMM_ERR_INVALID_ARG;
-    hgemm_ctx_s *ctx = plan->ctx;
-    const int32_t form = plan->form, groups = plan->groups;
-    const int64_t M = plan->M, N = plan->N, K = plan->K;
-    const bool wgrad = form == HGEMM_FP8_WEIGHT_GRAD, nv = plan->format == HGEMM_FP4_NV;
-    const int64_t out_cols = form == HGEMM_FP8_FORWARD ? N : K;
-    const int64_t depth = wgrad ? (groups > 0 ? hgemm_fp8_padded_rows(M, groups) : M) : form == HGEMM_FP8_FORWARD ? K : N;       // contracted elements of the copies
-    if ((groups > 0) != (offsets != nullptr) || accumulate < 0 || accumulate > 1 || (accumulate && plan->out_type != HGEMM_TYPE_F32)) return HGEMM_ERR_INVALID_ARG;
-    if (lda < ceil_div(depth, 2) || ldb < ceil_div(depth, 2) || ldc < out_cols || (lda & 15) != 0 || (ldb & 15) != 0) return HGEMM_ERR_INVALID_ARG;
-    const int es = type_bytes(plan->out_type);
-    if (M == 0 && !wgrad) return HGEMM_OK;
-    if (!C || (reinterpret_cast<uintptr_t>(C) % unsigned(es)) != 0) return HGEMM_ERR_INVALID_ARG;
-    if (M == 0) {
-        if (accumulate) return HGEMM_OK;
-        const cudaError_t e = cudaMemset2DAsync(C, size_t(ldc) * size_t(es), 0, size_t(K) * size_t(es), size_t(N) * size_t(std::max(groups, 1)), static_cast<cudaStream_t>(stream));
-        return e == cudaSuccess ? HGEMM_OK : cuda_fail(ctx, e);
-    }
-    if (!A || !B || !a_scales || !b_scales || !aligned16(A) || !aligned16(B) || !aligned16(a_scales) || !aligned16(b_scales) || !aligned4(offsets)) return HGEMM_ERR_INVALID_ARG;
-    if (nv != (a_factor != nullptr) || nv != (b_factor != nullptr) || !aligned4(a_factor) || !aligned4(b_factor)) return HGEMM_ERR_INVALID_ARG;
-
-    const hgemm_fp4_config_t &c = plan->cfg;
-    const bool swap = c.cta_group == 1;                      // the kernel's P operand is the caller's B
-    Fp4Params p;
-    std::memset(&p, 0, sizeof(p));
-    p.stages = stages_of(c, nv, groups);
-    if (p.stages < 2) return HGEMM_ERR_UNSUPPORTED;
-    p.split = c.split_k;
-    p.groups = groups;
-    p.offsets = offsets;
-    p.rows_ragged = int32_t(M);
-    p.kblocks = int32_t(ceil_div(depth, 128));
-    p.k_capacity = int32_t(ceil_div(depth, 128));
-    const int64_t matrices = std::max(groups, 1);
-
-    // one side of the product: values (rows x depth, `count` matrices), their scale tiles, their factors
-    struct Side {
-        const void *base;
-        int64_t rows, count, ld;
-        const void *scales;
-        int64_t scale_tiles;
-        const float *factor;
-    } a, b;
-    const int64_t a_rows = wgrad ? N : M, b_rows = form == HGEMM_FP8_FORWARD ? N : K;
-    a = {A, a_rows, 1, lda, a_scales, !wgrad && groups > 0 ? hgemm_fp8_padded_rows(M, groups) / 128 : ceil_div(a_rows, 128), a_factor};
-    b = {B, b_rows, wgrad ? 1 : matrices, ldb, b_scales, ceil_div(b_rows, 128) * (wgrad ? 1 : matrices), b_factor};
-    const Side &P = swap ? b : a, &Q = swap ? a : b;
-    const int tp = 128 * c.cta_group, tq = c.block_q;
-    p.rows_p = int32_t(P.rows);
-    p.rows_q = int32_t(Q.rows);
-    p.tiles_p = int32_t(ceil_div(P.rows, tp));
-    p.tiles_q = int32_t(ceil_div(Q.rows, tq));
-    p.ragged = groups == 0 ? hgemm_dev::kRaggedNone : wgrad ? hgemm_dev::kRaggedK : swap ? hgemm_dev::kRaggedQ : hgemm_dev::kRaggedP;
-    const int64_t tiles = tiles_of(form, M, N, K, groups, c);
-    if (tiles > (int64_t(1) << 30)) return HGEMM_ERR_UNSUPPORTED;
-    p.total = int32_t(tiles);
-    p.raster = std::min(8, p.tiles_p);
-    {
-        using hgemm_dev::make_fast_div;
-        const int32_t last = p.tiles_p - (p.tiles_p - 1) / p.raster * p.raster;         // rows of tiles of the last sweep
-        p.fd_other = make_fast_div(uint32_t(p.ragged == hgemm_dev::kRaggedP ? p.tiles_q : p.tiles_p));
-        p.fd_group = make_fast_div(uint32_t(p.tiles_p) * uint32_t(p.tiles_q));
-        p.fd_sweep = make_fast_div(uint32_t(p.raster) * uint32_t(p.tiles_q));
-        p.fd_raster = make_fast_div(uint32_t(p.raster));
-        p.fd_last = make_fast_div(uint32_t(last));
-    }
-    p.sp_group = int32_t(ceil_div(P.rows, 128));
-    p.sq_group = int32_t(ceil_div(Q.rows, 128));
-    p.fp = P.factor;
-    p.fq = Q.factor;
-    p.fp_group = P.count > 1 ? 1 : 0;
-    p.fq_group = Q.count > 1 ? 1 : 0;
-    p.out = C;
-    p.ldc = ldc;
-    p.c_group = wgrad ? N * ldc : 0;
-    p.out_type = plan->out_type;
-    p.accumulate = accumulate;
-    p.vec_ok = aligned16(C) && (ldc * es) % 16 == 0 && (out_cols * es) % 16 == 0 ? 1 : 0;      // a tensor store clips at multiples of 16 bytes only
-    // instruction descriptor of the block-scaled kinds: e2m1 operands (1) along the contraction; bit 23: scales are powers of two; bits 4 and 29: the
-    // scales' place in their word, set by the kernel
-    p.idesc = (1u << 7) | (1u << 10) | (uint32_t(tq >> 3) << 17) | (nv ? 0u : 1u << 23) | (uint32_t(tp >> 4) << 24);
-    p.status = ctx->d_status + plan->status_slot;
-    p.wait_budget = ctx->wait_budget;
-
-    CUtensorMap map_p, map_q, map_sp, map_sq, map_c;
-    const int64_t bytes = ceil_div(depth, 2), atoms = atoms_of(depth, plan->format);
-    if (!encode_values(ctx, &map_p, P.base, bytes, P.rows, P.count, P.ld, 128)) return HGEMM_ERR_CUDA;
-    if (!encode_values(ctx, &map_q, Q.base, bytes, Q.rows, Q.count, Q.ld, uint32_t(tq / c.cta_group))) return HGEMM_ERR_CUDA;
-    if (!encode_scales(ctx, &map_sp, P.scales, atoms, P.scale_tiles, nv, 1)) return HGEMM_ERR_CUDA;
-    if (!encode_scales(ctx, &map_sq, Q.scales, atoms, Q.scale_tiles, nv, uint32_t(hgemm_dev::fp4_scale_tiles(tq)))) return HGEMM_ERR_CUDA;
-    map_c = map_p;                                           // not used by the kernels that store through pointers
-    if (c.cta_group == 2 && p.vec_ok && !accumulate) {
-        if (!encode_results(ctx, &map_c, plan->out_type, C, out_cols, wgrad ? N : M, wgrad ? matrices : 1, ldc)) return HGEMM_ERR_CUDA;
-    }
-    const int per_unit = c.cta_group == 2 ? 2 : c.split_k;
-    // CTAs that share a tile through a cluster's shared memory take one tile each; the others walk the tiles
-    const int64_t units = c.split_k > 1 ? tiles : std::min<int64_t>(tiles, std::max(1, ctx->num_sms / per_unit));
-    if (units * per_unit > 0x7fffffff) return HGEMM_ERR_UNSUPPORTED;
-    void *args[6] = {&map_p, &map_q, &map_sp, &map_sq, &map_c, &p};
-    return launch(ctx, kernel_of(c, plan->format), dim3(unsigned(units * per_unit), 1, 1), hgemm_dev::kFp4Threads, kSmemOptIn, per_unit, args, stream);
+    return plan ? run_product<false>(*plan, A, lda, a_scales, a_factor, B, ldb, b_scales, b_factor, C, ldc, offsets, accumulate, stream) : HGEMM_ERR_INVALID_ARG;
 }
 
 } // extern "C"

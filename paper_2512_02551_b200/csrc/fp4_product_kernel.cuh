@@ -39,6 +39,7 @@ constexpr int kFp4Unit = 128;                     // the contraction is counted 
 constexpr int kFp4MaxStages = 10;
 constexpr int kFp4MaxGroups = 1024;
 constexpr int kFp4CtrlBytes = 512;
+constexpr int kFp4Digits = 8;                     // rows of Q that stand for one (DIGITS)
 constexpr int kFp4StagingPerWarp = 4096;          // results on their way out: a box of 32 rows x 128 bytes
 constexpr uint32_t kRoleFp4Load = 12, kRoleFp4Mma = 13, kRoleFp4Store = 14;
 constexpr uint32_t kFp4PartPitch = 132;           // words between the columns of a slice's part
@@ -171,12 +172,14 @@ __device__ __forceinline__ void fp4_store_one(const Fp4Params &p, int64_t at, fl
 }
 
 // CG: CTAs per tile.  BN: rows of Q per tile.  NV: e4m3 scales of 16 elements, else powers of two of 32.  CG == 2 stores by rows, CG == 1 transposed.
-template <int CG, int BN, bool NV>
+// DIGITS (CG == 1): each eight rows of Q are one row of the caller's, written as a sum of eight; the result has their sums.
+template <int CG, int BN, bool NV, bool DIGITS = false>
 __global__ void __launch_bounds__(kFp4Threads, 1)
 fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_sp,
                    const __grid_constant__ CUtensorMap tmap_sq, const __grid_constant__ CUtensorMap tmap_c, const Fp4Params p)
 {
     constexpr int TP = 128 * CG, TQ = BN;
+    constexpr int kDigits = DIGITS ? kFp4Digits : 1;
     constexpr bool kShared = 2 * BN > 384;                        // the accumulators share columns
     constexpr uint32_t kAccStep = kShared ? BN - kFp4Overlap : BN;
     constexpr uint32_t kScaleCol = 384;                           // tensor memory of the scales: two stages' worth
@@ -398,7 +401,7 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                     }
                 }
             } else {
-                constexpr int kCols = BN / 2;
+                constexpr int kCols = BN / 2, kOut = kCols / kDigits;
                 uint32_t v[kCols];
                 if (kbn > 0) {
 #pragma unroll
@@ -411,19 +414,26 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
 #pragma unroll
                     for (int j = 0; j < kCols; ++j) v[j] = 0u;
                 }
+                float o[kOut];
+#pragma unroll
+                for (int j = 0; j < kOut; ++j) {
+                    o[j] = __uint_as_float(v[j * kDigits]);
+#pragma unroll
+                    for (int i = 1; i < kDigits; ++i) o[j] += __uint_as_float(v[j * kDigits + i]);
+                    o[j] *= alpha;
+                }
                 if (p.split > 1) {
                     // this slice's part where the operand stages were (every MMA that read them is complete): columns of 128 rows, 132 words apart
 #pragma unroll
-                    for (int j = 0; j < kCols; ++j)
-                        st_shared_f32(smem_base + ((half * kCols + j) * kFp4PartPitch + quarter * 32u + lane) * 4u, __uint_as_float(v[j]) * alpha);
+                    for (int j = 0; j < kOut; ++j) st_shared_f32(smem_base + ((half * kOut + j) * kFp4PartPitch + quarter * 32u + lane) * 4u, o[j]);
                 } else {
                     const int32_t row = t.p0 + static_cast<int32_t>(quarter * 32u + lane);
                     const int64_t base = t.group * p.c_group + row;
                     if (row < t.p_end) {
 #pragma unroll
-                        for (int j = 0; j < kCols; ++j) {
-                            const int32_t col = t.q0 + static_cast<int32_t>(half * kCols) + j;
-                            if (col < t.q_end) fp4_store_one(p, base + static_cast<int64_t>(col) * p.ldc, __uint_as_float(v[j]) * alpha);
+                        for (int j = 0; j < kOut; ++j) {
+                            const int32_t col = t.q0 / kDigits + static_cast<int32_t>(half * kOut) + j;
+                            if (col < t.q_end / kDigits) fp4_store_one(p, base + static_cast<int64_t>(col) * p.ldc, o[j]);
                         }
                     }
                 }
@@ -439,10 +449,10 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         cluster_wait();
         if (unit < total && !*abort_flag) {
             const ProductTile t = product_tile<TP, TQ>(unit, p, pre, off, lane);
-            const int32_t share = BN / p.split, row = t.p0 + static_cast<int32_t>(lane) * 4;
+            const int32_t share = BN / kDigits / p.split, row = t.p0 + static_cast<int32_t>(lane) * 4;
             for (int32_t c = static_cast<int32_t>(rank) * share + static_cast<int32_t>(warp); c < (static_cast<int32_t>(rank) + 1) * share; c += kFp4Threads / 32) {
-                const int32_t col = t.q0 + c;
-                if (col >= t.q_end) break;
+                const int32_t col = t.q0 / kDigits + c;
+                if (col >= t.q_end / kDigits) break;
                 float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                 for (int32_t r = 0; r < p.split; ++r) {
                     const float4 x = ld_shared_cluster_v4(mapa(smem_base + (static_cast<uint32_t>(c) * kFp4PartPitch + lane * 4u) * 4u, static_cast<uint32_t>(r)));

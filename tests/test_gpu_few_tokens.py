@@ -14,6 +14,8 @@ import fp4_reference as ref  # noqa: E402
 from paper_2512_02551_b200 import few_tokens, fp4, hgemm, routing  # noqa: E402
 
 DTYPE = {"bf16": torch.bfloat16, "f16": torch.float16}
+#: Bits of h against each kind of weights (None: digits).
+BITS = {"bf16": 16, "f16": 11, "nvfp4": None, "mxfp4": None}
 KINDS = [("bf16", "bf16"), ("f16", "f16"), ("nvfp4", "bf16"), ("nvfp4", "f16"), ("mxfp4", "bf16"), ("mxfp4", "f16")]
 
 
@@ -64,12 +66,15 @@ def silu(u):
         return u / (1 + np.exp(-u))
 
 
-def formula(x, w1, w2, indices, weights, gated):
+def formula(x, w1, w2, indices, weights, gated, bits=11):
     """(y, bound of the error before y's rounding) in 64 bits.
 
-    The contraction over `hidden` adds H numbers in 32 bits (2^-23 of their magnitudes each covers truncation); silu changes by at most 1.1 times its
-    argument's error, and its exponential is off by 2^-21 (2 + |u|) of itself; h keeps 16 bits (2^-17 with the product's rounding); an fp16 weight
-    against h loses the product of two second parts, 2^-17; then I, and k, numbers are added."""
+    `bits`: what h is rounded to (2^-bits: a half step, and the factors' products); None: x and h are sums of digits, off by at most 2^-19 of their largest
+    magnitude.  h of an fp16 product is scaled so that its largest magnitude is 2^14 or more: half a step among fp16's smallest numbers, 2^-25, is at most
+    2^-39 of it.  The contraction over `hidden` adds H numbers in 32 bits (2^-23 of their magnitudes each covers truncation; with digits, eight times as many, and
+    8 more); silu changes by at most 1.1 times its argument's error, and its exponential is off by 2^-21 (2 + |u|) of itself; then I, and k, numbers are added."""
+    digits = bits is None
+    many, lost = (8, 2.0 ** -19) if digits else (1, 0.0)
     T, H = x.shape
     E, I = w1.shape[0], w2.shape[-1]
     y, err = np.zeros((T, H)), np.zeros((T, H))
@@ -79,16 +84,16 @@ def formula(x, w1, w2, indices, weights, gated):
             if not 0 <= e < E:
                 continue
             u = w1[e] @ x[t]
-            du = (H + 8) * 2.0 ** -23 * (np.abs(w1[e]) @ np.abs(x[t]))
+            du = (many * H + 8) * 2.0 ** -23 * (np.abs(w1[e]) @ np.abs(x[t])) + lost * np.abs(x[t]).max() * np.abs(w1[e]).sum(1)
             g = silu(u[:I])
             dg = 1.1 * du[:I] + np.abs(g) * (2 + np.abs(u[:I])) * 2.0 ** -21
             h, dh = (g * u[I:], np.abs(u[I:]) * dg + (np.abs(g) + dg) * du[I:]) if gated else (g, dg)
-            dh = dh + np.abs(h) * 2.0 ** -17 + 2.0 ** -130
+            dh = dh + (lost * np.abs(h).max() if digits else np.abs(h) * 2.0 ** -bits + 2.0 ** -39 * np.abs(h).max()) + 2.0 ** -130
             z = w2[e] @ h
             mag = np.abs(w2[e]) @ np.abs(h)
             w = weights[t, j]
             y[t] += w * z
-            err[t] += np.abs(w) * (np.abs(w2[e]) @ dh + ((I + indices.shape[1] + 8) * 2.0 ** -23 + 2.0 ** -17) * mag)
+            err[t] += np.abs(w) * (np.abs(w2[e]) @ dh + (many * I + indices.shape[1] + 8) * 2.0 ** -23 * mag)
     return y, err
 
 
@@ -119,7 +124,7 @@ def case(ctx, kind, dtype, T, H, I, E, k, gated, extra=0, offset=0, indices=None
     keep = torch.ones_like(buf, dtype=torch.bool)
     keep.as_strided(y.shape, y.stride(), y.storage_offset()).fill_(False)
     assert bool(torch.isnan(buf[keep]).all()), "something outside the result was written"
-    check(y, *formula(ref.f64(x), v1, v2, indices, weights.astype(np.float64), gated), f"{kind} {dtype} {T}x{H}x{I}, {k} of {E}")
+    check(y, *formula(ref.f64(x), v1, v2, indices, weights.astype(np.float64), gated, BITS[kind]), f"{kind} {dtype} {T}x{H}x{I}, {k} of {E}")
     return y
 
 
@@ -195,7 +200,7 @@ def test_large_h_and_small_x(ctx):
         idx, w = np.array([[0], [1], [0], [1]]), np.full((4, 1), 2.0 ** -12 if scale > 1 else 1.0, np.float32)
         y = torch.empty(4, 64, dtype=dt, device="cuda")
         layer.run(x.cuda(), w1, w2, torch.tensor(idx, dtype=torch.int32, device="cuda"), torch.from_numpy(w).cuda(), y, layer.empty_scratch(4))
-        check(y, *formula(ref.f64(x), v1, v2, idx, w.astype(np.float64), True), f"{kind} {dtype} {scale}")
+        check(y, *formula(ref.f64(x), v1, v2, idx, w.astype(np.float64), True, BITS[kind]), f"{kind} {dtype} {scale}")
 
 
 def test_with_the_quantiser_and_the_router(ctx):
@@ -223,7 +228,7 @@ def test_with_the_quantiser_and_the_router(ctx):
         layer = few_tokens.Layer(ctx, H, I, E, k, weights=fmt)
         router.forward(logits, weights, indices)
         layer.run(x, ops[0][0], ops[1][0], indices, weights, y, layer.empty_scratch(T))
-        check(y, *formula(ref.f64(x), ops[0][1], ops[1][1], indices.cpu().numpy(), ref.f64(weights), True), fmt)
+        check(y, *formula(ref.f64(x), ops[0][1], ops[1][1], indices.cpu().numpy(), ref.f64(weights), True, None), fmt)
 
 
 def test_captured_replayed_and_at_once(ctx):
