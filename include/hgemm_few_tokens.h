@@ -9,8 +9,7 @@
  * choices.  Weights are fp16 or bf16, of x's type, or 4-bit row copies with block scales (hgemm_fp4.h) with x of either type.
  *
  * All sums are in fp32, and the result is rounded once; a token's choices are added up in their order, so that results do not depend on scheduling.
- *     16-bit weights    two launches; x and the weights enter the products as they are, h to 16 bits of mantissa (bf16), or to 11 bits, scaled by a power of two for
- *                       each choice (fp16: what is below 2^-39 of its largest magnitude is lost)
+ *     16-bit weights    two launches; x and the weights enter the products as they are, h to 16 bits of mantissa
  *     4-bit weights     five launches; the weights enter the products as they are, x and h as sums of 4-bit digits: off by at most 2^-19 of the token's (the
  *                       choice's) largest magnitude.  A NaN or an infinity in x makes its token's results NaN
  *

@@ -26,13 +26,14 @@
 
 namespace hgemm_dev {
 
-constexpr int kDigitThreads = 256;
+constexpr int kDigitThreads = 512, kDigitKeep = 4;      // runs of four elements that a thread keeps between its two looks at them
+constexpr int kCombineThreads = 128;
 constexpr int kDigits = 8;
 
 struct DigitParams {
     const void *x;             // tokens x depth (fp16 or bf16), or nullptr: u
     int64_t ldx;
-    int32_t x_half, x_vec;     // fp16; rows start at multiples of 16 bytes
+    int32_t x_half, x_vec;     // fp16; rows start at multiples of 8 bytes
     const float *u;            // the first product: [position][gated ? 2 * depth : depth], ldu apart
     int64_t ldu;
     int32_t u_vec, gated;      // rows (and their second halves) start at multiples of 16 bytes
@@ -52,84 +53,154 @@ struct DigitParams {
     float *factor;             // of a position: digits count times this (MX: 1)
 };
 
-// The sum of two numbers over the CTA, in every thread; scratch: 2 words, zero on entry.
-__device__ __forceinline__ void digit_sums(int32_t &a, int32_t &b, int32_t *scratch)
+// The sums of three numbers over the CTA, in every thread; scratch: 3 words, zero on entry.
+__device__ __forceinline__ void digit_sums(int32_t &a, int32_t &b, int32_t &c, int32_t *scratch)
 {
     a = __reduce_add_sync(0xffffffffu, a);
     b = __reduce_add_sync(0xffffffffu, b);
+    c = __reduce_add_sync(0xffffffffu, c);
     if ((threadIdx.x & 31u) == 0u) {
         atomicAdd(&scratch[0], a);
         atomicAdd(&scratch[1], b);
+        atomicAdd(&scratch[2], c);
     }
     __syncthreads();
     a = scratch[0];
     b = scratch[1];
+    c = scratch[2];
 }
 
 __device__ __forceinline__ float digit_silu(float u) { return u / (1.0f + __expf(-u)); }
 
-// Elements k .. k + 15 (zeros beyond the depth).
-__device__ __forceinline__ void digit_load(const DigitParams &p, const uint16_t *x, const float *u, float factor, int32_t k, float (&f)[16])
+// Elements k .. k + 3 (zeros beyond the depth).
+__device__ __forceinline__ void digit_load(const DigitParams &p, const uint16_t *x, const float *u, float factor, int32_t k, float (&f)[4])
 {
     if (x != nullptr) {
-        if (p.x_vec && k + 16 <= p.depth) {
-            const uint4 a = reinterpret_cast<const uint4 *>(x + k)[0], b = reinterpret_cast<const uint4 *>(x + k)[1];
-            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (p.x_half) two_floats(w[i], f[2 * i], f[2 * i + 1], __half());
-                else two_floats(w[i], f[2 * i], f[2 * i + 1], __nv_bfloat16());
-            }
+        uint32_t w[2];
+        if (p.x_vec && k + 4 <= p.depth) {
+            const uint2 a = *reinterpret_cast<const uint2 *>(x + k);
+            w[0] = a.x, w[1] = a.y;
         } else {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t w = k + i < p.depth ? x[k + i] : 0u;
-                f[i] = p.x_half ? __half2float(__ushort_as_half(static_cast<unsigned short>(w))) : __uint_as_float(w << 16);
-            }
+            for (int i = 0; i < 2; ++i) w[i] = (k + 2 * i < p.depth ? x[k + 2 * i] : 0u) | (k + 2 * i + 1 < p.depth ? static_cast<uint32_t>(x[k + 2 * i + 1]) << 16 : 0u);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (p.x_half) two_floats(w[i], f[2 * i], f[2 * i + 1], __half());
+            else two_floats(w[i], f[2 * i], f[2 * i + 1], __nv_bfloat16());
         }
         return;
     }
-    float g[16], v[16];
-    if (p.u_vec && k + 16 <= p.depth) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 a = reinterpret_cast<const float4 *>(u + k)[i];
-            g[4 * i] = a.x, g[4 * i + 1] = a.y, g[4 * i + 2] = a.z, g[4 * i + 3] = a.w;
-            if (p.gated) {
-                const float4 b = reinterpret_cast<const float4 *>(u + p.depth + k)[i];
-                v[4 * i] = b.x, v[4 * i + 1] = b.y, v[4 * i + 2] = b.z, v[4 * i + 3] = b.w;
-            }
+    float g[4] = {0.0f, 0.0f, 0.0f, 0.0f}, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (p.u_vec && k + 4 <= p.depth) {
+        const float4 a = *reinterpret_cast<const float4 *>(u + k);
+        g[0] = a.x, g[1] = a.y, g[2] = a.z, g[3] = a.w;
+        if (p.gated) {
+            const float4 b = *reinterpret_cast<const float4 *>(u + p.depth + k);
+            v[0] = b.x, v[1] = b.y, v[2] = b.z, v[3] = b.w;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            g[i] = k + i < p.depth ? u[k + i] : 0.0f;
-            v[i] = k + i < p.depth && p.gated ? u[p.depth + k + i] : 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            if (k + i < p.depth) {
+                g[i] = u[k + i];
+                if (p.gated) v[i] = u[p.depth + k + i];
+            }
         }
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 4; ++i) {
         const float h = digit_silu(g[i] * factor);
         f[i] = p.gated ? h * (v[i] * factor) : h;
     }
 }
 
+// The digits of a warp's runs of four elements (run r of this lane; beyond `runs`: nothing is written).  Whole warps.
+template <bool NV>
+__device__ __forceinline__ void digit_write(const DigitParams &p, float (&f)[4], float inverse, int32_t r, int32_t runs, uint8_t *q, uint8_t *scales)
+{
+    constexpr int32_t kLeast = NV ? 127 - 9 : 1;                  // the smallest scale's exponent, biased
+    const int32_t bytes = (p.depth + 1) / 2;
+    float amax = 0.0f;
+    bool odd = false;                                             // a NaN or an infinity in the block
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        odd = odd || (__float_as_uint(f[i]) & 0x7fffffffu) >= 0x7f800000u;
+        f[i] *= inverse;
+        amax = fmaxf(amax, fabsf(f[i]));
+    }
+    // the block's four (NV) or eight lanes
+    uint32_t top = odd ? 0x7f800000u : __float_as_uint(amax);
+#pragma unroll
+    for (int d = 1; d < (NV ? 4 : 8); d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+    odd = top >= 0x7f800000u;
+    int32_t e = top != 0u && !odd ? max(power_above(__uint_as_float(top), 2, kMantissa6), kLeast) : 0;      // s_1's exponent; 0: no digit
+    // the scales: lane d of an atom's lanes (16, or 32) makes digit d's, of four blocks a word
+    constexpr int kAtomLanes = NV ? 16 : 32;
+    {
+        const int32_t lane = static_cast<int32_t>(lane_id()), d = lane & 7;
+        uint32_t word = 0u;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int32_t first = __shfl_sync(0xffffffffu, odd ? -1 : e, (lane & ~(kAtomLanes - 1)) + b * (kAtomLanes / 4));
+            // digit d's exponent: first, less 2 and then 3 a digit, down to the least, which is the last
+            const int32_t ahead = d == 0 ? first : first - (d == 1 ? 0 : 3 * d - 4), here = d == 0 ? first : max(first - (3 * d - 1), kLeast);      // the digit before, this one
+            const bool there = first > 0 && (d == 0 || ahead > kLeast);
+            uint32_t byte = there ? static_cast<uint32_t>(min(here, 253)) : 0u;
+            if constexpr (NV) {
+                const int32_t n = here - 127;                     // 2^8 .. 2^-9 as e4m3
+                byte = !there ? 0u : n >= -6 ? static_cast<uint32_t>(n + 7) << 3 : 1u << (n + 9);
+            }
+            if (first < 0 && d == 0) byte = NV ? 0x7fu : 0xffu;
+            word |= byte << (8 * b);
+        }
+        if ((lane & (kAtomLanes - 1)) < kDigits && (r & ~(kAtomLanes - 1)) < runs) *reinterpret_cast<uint32_t *>(scales + static_cast<int64_t>(r / kAtomLanes) * 512 + d * 16) = word;
+    }
+    uint8_t *dst = q + r * 2;
+#pragma unroll
+    for (int32_t d = 0; d < kDigits; ++d, dst += p.ldq) {
+        const bool some = e > 0;
+        const float step = some ? __uint_as_float(static_cast<uint32_t>(min(e, 253)) << 23) : 0.0f, back = some ? __uint_as_float(static_cast<uint32_t>(254 - min(e, 253)) << 23) : 0.0f;
+        uint32_t w = 0u;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t b = __nv_cvt_float2_to_fp4x2(make_float2(f[2 * i] * back, f[2 * i + 1] * back), __NV_E2M1, cudaRoundNearest);
+            w |= b << (8 * i);
+            const float2 v = __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(b), __NV_E2M1)));
+            f[2 * i] = fmaf(-v.x, step, f[2 * i]);
+            f[2 * i + 1] = fmaf(-v.y, step, f[2 * i + 1]);
+        }
+        if (odd) w = 0u;                                          // the scale says it
+        if (r * 2 + 2 <= bytes) *reinterpret_cast<uint16_t *>(dst) = static_cast<uint16_t>(w);
+        else if (r * 2 < bytes) *dst = static_cast<uint8_t>(w);
+        e = e <= kLeast ? 0 : max(e - (d == 0 ? 2 : 3), kLeast);  // after the smallest scale, no more digits
+    }
+}
+
 // One CTA per choice.  FIRST: the kernel that reads x; it finds the choices' places (dynamic shared memory: a word for each expert), and its last CTA
-// writes the experts' offsets.
+// writes the experts' offsets.  (Fetching the next product's weights to L2 meanwhile was tried: the launch then ends with the last of them, 1 token 25 -> 31 us.)
 template <bool NV, bool FIRST>
 __global__ void __launch_bounds__(kDigitThreads)
 few_digits_kernel(const DigitParams p)
 {
     constexpr int kBlock = NV ? 16 : 32, kAtom = 4 * kBlock;
     extern __shared__ int32_t s_count[];
-    __shared__ int32_t s_sums[2];
+    __shared__ int32_t s_sums[3];
     __shared__ uint32_t s_top;
     grid_launch_dependents();
-    grid_dependency_wait();
     const int32_t c = static_cast<int32_t>(blockIdx.x), me = static_cast<int32_t>(threadIdx.x);
+    grid_dependency_wait();
+    const int32_t runs = p.atoms * (kAtom / 4);                   // of four elements, those that fill the last scale tile among them
+    const uint16_t *x = FIRST ? static_cast<const uint16_t *>(p.x) + static_cast<int64_t>(min(c, p.choices - 1) / p.top_k) * p.ldx : nullptr;
+    float f[kDigitKeep][4];
+    if constexpr (FIRST) {
+#pragma unroll
+        for (int i = 0; i < kDigitKeep; ++i)
+            if ((me & ~31) + i * kDigitThreads < runs) digit_load(p, x, nullptr, 1.0f, min(me + i * kDigitThreads, runs) * 4, f[i]);      // (run number `runs`: beyond the depth)
+    }
     int32_t position, place;
     if (me == 0) {
-        s_sums[0] = s_sums[1] = 0;
+        s_sums[0] = s_sums[1] = s_sums[2] = 0;
         s_top = 0u;
     }
     if constexpr (FIRST) {
@@ -170,45 +241,48 @@ few_digits_kernel(const DigitParams p)
             if (me == 0) p.position[c] = -1;
             return;
         }
-        int32_t before = ahead, tiles = 0;                        // positions ahead; scale tiles of the experts ahead
+        int32_t before = 0, tiles = 0;                            // positions and scale tiles of the experts ahead
         for (int32_t e = me; e < mine; e += kDigitThreads) {
             before += s_count[e];
             tiles += (s_count[e] * kDigits + 127) / 128;
         }
-        // `ahead` counts towards both this expert's place and all positions
-        int32_t own = ahead, none = 0;
-        digit_sums(before, tiles, s_sums);
-        __syncthreads();
-        if (me == 0) s_sums[0] = s_sums[1] = 0;
-        __syncthreads();
-        digit_sums(own, none, s_sums);
-        position = before;
-        place = tiles * 128 + own * kDigits;
+        digit_sums(before, tiles, ahead, s_sums);
+        position = before + ahead;
+        place = tiles * 128 + ahead * kDigits;
         if (me == 0) {
             p.position[c] = position;
             p.place[c] = place;
         }
     } else {
         position = p.position[c];
-        if (position < 0) return;
         place = p.place[c];
+        if (position < 0) return;
         __syncthreads();
     }
-    const uint16_t *x = FIRST ? static_cast<const uint16_t *>(p.x) + static_cast<int64_t>(c / p.top_k) * p.ldx : nullptr;
     const float *u = FIRST ? nullptr : p.u + position * p.ldu;
     const float u_factor = FIRST ? 1.0f : p.u_factor[position];
-    const int32_t runs = p.atoms * (kAtom / 16);                  // of 16 elements, those that fill the last scale tile among them
-    float f[16];
+    if constexpr (!FIRST) {
+#pragma unroll
+        for (int i = 0; i < kDigitKeep; ++i)
+            if ((me & ~31) + i * kDigitThreads < runs) digit_load(p, nullptr, u, u_factor, min(me + i * kDigitThreads, runs) * 4, f[i]);
+    }
     float inverse = 1.0f;
     if constexpr (NV) {
         uint32_t top = 0u;
-        for (int32_t r = me; r < runs; r += kDigitThreads) {
-            digit_load(p, x, u, u_factor, r * 16, f);
+        auto look = [&](const float (&v)[4]) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const uint32_t b = __float_as_uint(f[i]) & 0x7fffffffu;
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
                 if (b < 0x7f800000u) top = max(top, b);
             }
+        };
+#pragma unroll
+        for (int i = 0; i < kDigitKeep; ++i)
+            if ((me & ~31) + i * kDigitThreads < runs) look(f[i]);
+        for (int32_t r = me + kDigitKeep * kDigitThreads; r < runs; r += kDigitThreads) {
+            float v[4];
+            digit_load(p, x, u, u_factor, r * 4, v);
+            look(v);
         }
         top = __reduce_max_sync(0xffffffffu, top);
         if ((me & 31) == 0) atomicMax(&s_top, top);
@@ -222,66 +296,13 @@ few_digits_kernel(const DigitParams p)
     }
     uint8_t *q = p.q + static_cast<int64_t>(position) * kDigits * p.ldq;
     uint8_t *scales = p.scales + static_cast<int64_t>(place >> 7) * p.atoms * 512 + (place & 31) * 16 + ((place >> 5) & 3) * 4;      // a choice's rows never cross 32
-    const int32_t bytes = (p.depth + 1) / 2;
-    for (int32_t r0 = me & ~31; r0 < runs; r0 += kDigitThreads) {   // whole warps; runs is a multiple of 4
-        const int32_t r = r0 + (me & 31);
-        float amax = 0.0f;
-        bool odd = false;
-        if (r < runs) {
-            digit_load(p, x, u, u_factor, r * 16, f);
+    const int32_t base = me & ~31, lane = me & 31;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                odd = odd || (__float_as_uint(f[i]) & 0x7fffffffu) >= 0x7f800000u;
-                f[i] *= inverse;
-                amax = fmaxf(amax, fabsf(f[i]));
-            }
-        }
-        if constexpr (!NV) {
-            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-            odd = odd || __shfl_xor_sync(0xffffffffu, static_cast<int>(odd), 1) != 0;
-        }
-        constexpr int32_t kLeast = NV ? 127 - 9 : 1;              // the smallest scale's exponent, biased
-        int32_t e = power_above(amax, 2, kMantissa6);             // s_1's
-        e = amax > 0.0f && !odd ? max(e, kLeast) : 0;             // (0: no digit)
-#pragma unroll 1
-        for (int32_t d = 0; d < kDigits; ++d) {
-            const bool some = e > 0;
-            const float step = some ? __uint_as_float(static_cast<uint32_t>(min(e, 253)) << 23) : 0.0f, back = some ? __uint_as_float(static_cast<uint32_t>(254 - min(e, 253)) << 23) : 0.0f;
-            uint32_t w[2] = {0u, 0u};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t b = __nv_cvt_float2_to_fp4x2(make_float2(f[2 * i] * back, f[2 * i + 1] * back), __NV_E2M1, cudaRoundNearest);
-                w[i / 4] |= b << (8 * (i & 3));
-                const float2 v = __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(b), __NV_E2M1)));
-                f[2 * i] = fmaf(-v.x, step, f[2 * i]);
-                f[2 * i + 1] = fmaf(-v.y, step, f[2 * i + 1]);
-            }
-            if (odd) w[0] = w[1] = 0u;                            // the scale says it
-            uint32_t byte;
-            if constexpr (NV) {
-                const int32_t n = e - 127;                        // 2^8 .. 2^-9 as e4m3
-                byte = odd ? (d == 0 ? 0x7fu : 0u) : !some ? 0u : n >= -6 ? static_cast<uint32_t>(n + 7) << 3 : 1u << (n + 9);
-                byte <<= 8 * (r & 3);
-            } else {
-                byte = odd ? (d == 0 ? 0xffu : 0u) : static_cast<uint32_t>(min(e, 253));
-                byte <<= 8 * ((r >> 1) & 3);
-            }
-            // the scales of four blocks make a word
-            byte |= __shfl_xor_sync(0xffffffffu, byte, NV ? 1 : 2);
-            byte |= __shfl_xor_sync(0xffffffffu, byte, NV ? 2 : 4);
-            if (r < runs) {
-                if ((r & (NV ? 3 : 7)) == 0) *reinterpret_cast<uint32_t *>(scales + static_cast<int64_t>(r / (NV ? 4 : 8)) * 512 + d * 16) = byte;
-                uint8_t *dst = q + d * p.ldq + r * 8;
-                if (r * 8 + 8 <= bytes) {
-                    *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (r * 8 + j < bytes) dst[j] = static_cast<uint8_t>(w[j / 4] >> (8 * (j & 3)));
-                }
-            }
-            e = e <= kLeast ? 0 : max(e - (d == 0 ? 2 : 3), kLeast);      // after the smallest scale, no more digits
-        }
+    for (int i = 0; i < kDigitKeep; ++i)
+        if (base + i * kDigitThreads < runs) digit_write<NV>(p, f[i], inverse, base + i * kDigitThreads + lane, runs, q, scales);
+    for (int32_t r0 = base + kDigitKeep * kDigitThreads; r0 < runs; r0 += kDigitThreads) {
+        digit_load(p, x, u, u_factor, min(r0 + lane, runs) * 4, f[0]);
+        digit_write<NV>(p, f[0], inverse, r0 + lane, runs, q, scales);
     }
 }
 
@@ -297,27 +318,44 @@ struct CombineParams {
     int32_t y_vec;             // rows of y start at multiples of 8 bytes
 };
 
-// y = sum over a token's choices, in their order.  grid: x = runs of 1024 outputs, y = tokens.
+// y = sum over a token's choices, in their order.  grid: x = runs of 512 outputs, y = tokens.
 template <class Y>
-__global__ void __launch_bounds__(kDigitThreads)
+__global__ void __launch_bounds__(kCombineThreads)
 few_combine_kernel(const CombineParams p)
 {
     grid_launch_dependents();
+    const int32_t n = (static_cast<int32_t>(blockIdx.x) * kCombineThreads + static_cast<int32_t>(threadIdx.x)) * 4, t = static_cast<int32_t>(blockIdx.y);
     grid_dependency_wait();
-    const int32_t n = (static_cast<int32_t>(blockIdx.x) * kDigitThreads + static_cast<int32_t>(threadIdx.x)) * 4, t = static_cast<int32_t>(blockIdx.y);
-    if (n >= p.hidden) return;
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 8
-    for (int32_t j = 0; j < p.top_k; ++j) {
-        const int32_t at = p.position[t * p.top_k + j];
-        if (at < 0) continue;
-        const float w = p.weights[t * p.top_k + j], s = p.factor[at];
-        const float4 z = *reinterpret_cast<const float4 *>(p.z + at * p.ldz + n);      // (beyond hidden: the row's padding, not stored)
-        sum[0] = fmaf(w, z.x * s, sum[0]);
-        sum[1] = fmaf(w, z.y * s, sum[1]);
-        sum[2] = fmaf(w, z.z * s, sum[2]);
-        sum[3] = fmaf(w, z.w * s, sum[3]);
+    // lane j has choice j's row and factor
+    const int32_t lane = static_cast<int32_t>(threadIdx.x & 31u);
+    int32_t mine = -1;
+    float w = 0.0f;
+    if (lane < p.top_k) {
+        mine = p.position[t * p.top_k + lane];
+        w = p.weights[t * p.top_k + lane];
     }
+    const float s = mine >= 0 ? p.factor[mine] : 0.0f;
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int32_t j0 = 0; j0 < p.top_k; j0 += 8) {
+        float4 z[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int32_t at = __shfl_sync(0xffffffffu, mine, (j0 + j) & 31);
+            z[j] = j0 + j < p.top_k && at >= 0 && n < p.hidden ? *reinterpret_cast<const float4 *>(p.z + at * p.ldz + n) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);      // (beyond hidden: the row's padding, not stored)
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool there = j0 + j < p.top_k && __shfl_sync(0xffffffffu, mine, (j0 + j) & 31) >= 0;
+            const float wj = __shfl_sync(0xffffffffu, w, (j0 + j) & 31), sj = __shfl_sync(0xffffffffu, s, (j0 + j) & 31);
+            if (there) {
+                sum[0] = fmaf(wj, z[j].x * sj, sum[0]);
+                sum[1] = fmaf(wj, z[j].y * sj, sum[1]);
+                sum[2] = fmaf(wj, z[j].z * sj, sum[2]);
+                sum[3] = fmaf(wj, z[j].w * sj, sum[3]);
+            }
+        }
+    }
+    if (n >= p.hidden) return;
     Y *y = static_cast<Y *>(p.y) + t * p.ldy + n;
     if (p.y_vec && n + 4 <= p.hidden) {
         *reinterpret_cast<uint2 *>(y) = make_uint2(pack_pair(sum[0], sum[1], Y()), pack_pair(sum[2], sum[3], Y()));

@@ -15,7 +15,6 @@ using hgemm_dev::FewWeights;
 namespace {
 
 constexpr int32_t kMaxWidth = 1 << 20;
-constexpr int kSmemOptIn = 232448;
 constexpr int kMaxX = 64 * 1024;                 // shared memory of the 16-bit kernels' first launch for x: two CTAs share an SM
 constexpr int kDigits = hgemm_dev::kDigits;
 
@@ -39,7 +38,7 @@ bool legal(const hgemm_few_tokens_t &d)
 
 // ---- 16-bit weights ------------------------------------------------------------------------------------------------
 
-// h of a choice in scratch memory: whole chunks; behind all of them the largest magnitude of each eight
+// h of a choice in scratch memory: whole chunks, in two parts
 int64_t h_stride(const hgemm_few_tokens_t &d) { return up_to(d.inner, hgemm_dev::kFewChunk); }
 
 FewWeights weights16(const hgemm_expert_weights_t &m, int32_t rows, int32_t depth)
@@ -121,8 +120,7 @@ hgemm_status_t run16(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &
     p.top_k = d.top_k;
     p.tokens = int32_t(c.tokens);
     p.choices = int32_t(c.tokens * d.top_k);
-    p.h = reinterpret_cast<float *>(c.scratch);
-    p.top = p.h + int64_t(p.choices) * p.h_stride;
+    p.h = reinterpret_cast<__nv_bfloat16 *>(c.scratch);
     // launch 1 writes whole chunks of h (zeros beyond inner), eight tiles of 8 (SWIGLU) or 16 rows together
     p.groups = int32_t(ceil_div(p.h_stride, p.gated ? 64 : 128));
     p.fd_groups = hgemm_dev::make_fast_div(uint32_t(p.groups));
@@ -131,7 +129,7 @@ hgemm_status_t run16(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &
 
     // x of 8 choices at once, or as many chunks of it as fit
     p.w = weights16(w1, up_rows(d), d.hidden);
-    p.piece = int32_t(std::min<int64_t>(up_to(d.hidden, 4 * hgemm_dev::kFewChunk) * 16, kMaxX));
+    p.piece = int32_t(std::min<int64_t>(up_to(d.hidden, hgemm_dev::kFewAhead * hgemm_dev::kFewChunk) * 16, kMaxX));
     p.most_slices = 8;
     const unsigned grid = unsigned(std::min<int64_t>(entries * p.groups * 8, int64_t(ctx->num_sms) * 2));
     const hgemm_status_t st = launch(ctx, half ? up_kernel<__half>(p.w.align) : up_kernel<__nv_bfloat16>(p.w.align), dim3(grid), hgemm_dev::kFewUpThreads, lists + p.piece, &p, c.stream);
@@ -140,12 +138,8 @@ hgemm_status_t run16(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &
     p.w = weights16(w2, d.hidden, d.inner);
     p.most_slices = 1;
     while (p.most_slices < 8 && p.most_slices * 2 * p.choices <= hgemm_dev::kFewMaxChoices) p.most_slices *= 2;
-    // each warp's part of h: as much as an entry of eight choices could use, or what is left of the shared memory (at the most choices and experts 4 KB, three chunks of eight)
-    const int fixed = lists + 4 * ((p.choices + 3) & ~3) + p.most_slices * p.choices * 64;
-    const int64_t h_bytes = hgemm_dev::kFewEntry * (p.h_stride * (half ? 2ll : 4ll) + 64);
-    p.piece = int32_t(std::min<int64_t>(h_bytes, (kSmemOptIn - fixed) / (hgemm_dev::kFewDownThreads / 32) & ~15));
     return launch(ctx, half ? down_kernel<__half>(p.w.align) : down_kernel<__nv_bfloat16>(p.w.align), dim3(unsigned(ceil_div(d.hidden, 16))), hgemm_dev::kFewDownThreads,
-                  fixed + p.piece * (hgemm_dev::kFewDownThreads / 32), &p, c.stream);
+                  lists + 4 * ((p.choices + 3) & ~3) + p.most_slices * p.choices * 64, &p, c.stream);
 }
 
 // ---- 4-bit weights -------------------------------------------------------------------------------------------------
@@ -201,7 +195,7 @@ hgemm_status_t run4(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c
     p.x = c.x;
     p.ldx = c.ldx;
     p.x_half = d.type == HGEMM_TYPE_F16 ? 1 : 0;
-    p.x_vec = aligned16(c.x) && c.ldx % 8 == 0 ? 1 : 0;
+    p.x_vec = (reinterpret_cast<uintptr_t>(c.x) & 7u) == 0 && c.ldx % 4 == 0 ? 1 : 0;
     p.depth = d.hidden;
     p.top_k = d.top_k;
     p.experts = d.experts;
@@ -234,8 +228,8 @@ hgemm_status_t run4(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c
     p.ldq = l.ld_h;
     p.atoms = int32_t(ceil_div(d.inner, nv ? 64 : 128));
     p.factor = reinterpret_cast<float *>(c.scratch + l.h_factor);
-    st = launch(ctx, nv ? reinterpret_cast<const void *>(few_digits_kernel<true, false>) : reinterpret_cast<const void *>(few_digits_kernel<false, false>), dim3(unsigned(choices)), kDigitThreads, 0, &p,
-                c.stream);
+    st = launch(ctx, nv ? reinterpret_cast<const void *>(few_digits_kernel<true, false>) : reinterpret_cast<const void *>(few_digits_kernel<false, false>), dim3(unsigned(choices)),
+                kDigitThreads, 0, &p, c.stream);
     if (st != HGEMM_OK) return st;
     st = hgemm_host::fp4_digits_product(ctx, format, choices, d.hidden, d.inner, d.experts, p.q, l.ld_h, p.scales, w2.values, w2.ld, w2.scales, nv ? one : nullptr, w2.factor, results, l.ld_z, offsets,
                                         c.stream);
@@ -254,7 +248,7 @@ hgemm_status_t run4(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c
     q.ldy = c.ldy;
     q.y_vec = (reinterpret_cast<uintptr_t>(c.y) & 7u) == 0 && c.ldy % 4 == 0 ? 1 : 0;
     return launch(ctx, d.type == HGEMM_TYPE_F16 ? reinterpret_cast<const void *>(few_combine_kernel<__half>) : reinterpret_cast<const void *>(few_combine_kernel<__nv_bfloat16>),
-                  dim3(unsigned(ceil_div(d.hidden, 4 * kDigitThreads)), unsigned(c.tokens)), kDigitThreads, 0, &q, c.stream);
+                  dim3(unsigned(ceil_div(d.hidden, 4 * kCombineThreads)), unsigned(c.tokens)), kCombineThreads, 0, &q, c.stream);
 }
 
 bool legal_weights(const hgemm_few_tokens_t &d, const hgemm_expert_weights_t &m, int32_t depth)
@@ -274,7 +268,7 @@ int64_t hgemm_few_tokens_scratch(const hgemm_few_tokens_t *d, int64_t tokens)
     if (!d || !legal(*d) || tokens < 0 || tokens > HGEMM_FEW_TOKENS_MAX) return -1;
     const int64_t choices = tokens * d->top_k;
     if (choices == 0) return 0;
-    return is4(*d) ? layout_of(*d, choices).bytes : choices * (h_stride(*d) + h_stride(*d) / 8) * 4;
+    return is4(*d) ? layout_of(*d, choices).bytes : choices * h_stride(*d) * 4;
 }
 
 hgemm_status_t hgemm_few_tokens(hgemm_ctx_t *ctx, const hgemm_few_tokens_t *d, int64_t tokens, const void *x, int64_t ldx, const hgemm_expert_weights_t *w1,

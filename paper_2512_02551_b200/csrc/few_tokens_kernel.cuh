@@ -7,8 +7,8 @@
 // long as both operands agree.  (Tensor memory and a ring of shared-memory stages would lengthen the way of rows that start anywhere: tensor copies
 // need rows at multiples of 16 bytes.)
 //
-// bf16 weights have bf16 products, with h as the sum of two bf16 (16 bits of mantissa); fp16 weights fp16 ones, with h scaled by a power of two for each choice, so that
-// its largest magnitude is just below 2^15 (what is below 2^-39 of it is lost), and rounded to 11 bits.
+// h is the sum of two bf16 (16 bits of mantissa, in bf16's range).  Against it an fp16 weight is the sum of two bf16 too, and of the four products that of both
+// second parts, 2^-16 of the whole, is left out.
 //
 // Work.  Launch 1: a warp has a tile of 16 rows (SWIGLU: 8 rows of each half, whose products meet in one lane), a CTA eight tiles of one expert, whose
 // tokens it lays out in shared memory as the instruction wants them.  As many rounds as give every CTA the same; the groups of tiles that are left over are
@@ -51,8 +51,7 @@ struct FewParams {
     int64_t ldy;
     const int32_t *indices;
     const float *weights;
-    float *h;                  // choices x h_stride (whole chunks)
-    float *top;                // choices x h_stride / 8: the largest magnitude of each 8 of them
+    __nv_bfloat16 *h;          // two parts of choices x h_stride (whole chunks)
     int32_t h_stride;
     int32_t inner, experts, top_k, tokens, choices, gated;
     int32_t groups;            // launch 1: groups of eight tiles of an expert
@@ -163,22 +162,25 @@ __device__ __forceinline__ void few_make_lists(const FewParams &p, const FewList
 
 // ---- weights ------------------------------------------------------------------------------------------------------
 
-// Two rows' 16 bytes of a chunk.
+// Two rows' 16 bytes of a chunk (N = 2), and the other operand's two parts (N = 4: launch 2, where they come from memory too).
+template <int N>
 struct FewRaw {
-    uint4 v[2];
+    uint4 v[N];
 };
 
 // Part of a contraction: chunks of a lane's two rows.  Rows that are not there (a matrix's last tile) stand for the expert's first: they are loaded like the
 // others, and their sums are not used.
+template <int N>
 struct FewSpan {
-    const uint8_t *row[2];     // at the lane's bytes of the first chunk
+    const uint8_t *row[N];     // at the lane's bytes of the first chunk
     int32_t first, n;          // chunks; those of them that rows have whole
     bool tail;                 // a last chunk follows, of which rows have a part
 };
 
-__device__ __forceinline__ FewSpan few_span(const FewWeights &w, int32_t expert, int32_t r0, int32_t r1, int32_t first, int32_t n, uint32_t q)
+template <int N>
+__device__ __forceinline__ FewSpan<N> few_span(const FewWeights &w, int32_t expert, int32_t r0, int32_t r1, int32_t first, int32_t n, uint32_t q)
 {
-    FewSpan f;
+    FewSpan<N> f;
     f.row[0] = w.values + expert * w.matrix + r0 * w.ld + first * 64 + q * 16;
     f.row[1] = w.values + expert * w.matrix + r1 * w.ld + first * 64 + q * 16;
     f.first = first;
@@ -208,15 +210,16 @@ __device__ __forceinline__ uint4 few_load16(const uint8_t *p)
 }
 
 // Chunk i behind a span's pointers (loads without a condition around them: they stay in flight).
-template <int ALIGN>
-__device__ __forceinline__ void few_fetch(FewRaw &raw, const uint8_t *const (&row)[2], int i)
+template <int ALIGN, int N>
+__device__ __forceinline__ void few_fetch(FewRaw<N> &raw, const uint8_t *const (&row)[N], int i)
 {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) raw.v[j] = few_load16<ALIGN>(row[j] + i * 64);
+    for (int j = 0; j < N; ++j) raw.v[j] = j < 2 ? few_load16<ALIGN>(row[j] + i * 64) : few_load16<16>(row[j] + i * 64);
 }
 
 // The chunk behind the whole ones; zeros beyond the rows' ends.
-__device__ __forceinline__ void few_fetch_tail(FewRaw &raw, const FewWeights &w, const FewSpan &f, uint32_t q)
+template <int N>
+__device__ __forceinline__ void few_fetch_tail(FewRaw<N> &raw, const FewWeights &w, const FewSpan<N> &f, uint32_t q)
 {
     const int32_t room = w.depth * 2 - (f.first + f.n) * 64 - static_cast<int32_t>(q) * 16;
 #pragma unroll
@@ -228,47 +231,51 @@ __device__ __forceinline__ void few_fetch_tail(FewRaw &raw, const FewWeights &w,
             if (2 * i < room) v[i / 2] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(p + 2 * i)) << (16 * (i & 1));
         raw.v[j] = make_uint4(v[0], v[1], v[2], v[3]);
     }
+#pragma unroll
+    for (int j = 2; j < N; ++j) raw.v[j] = few_load16<16>(f.row[j] + static_cast<int64_t>(f.n) * 64);      // (h has whole chunks)
 }
 
-// The chunks of a span, one after the other: chunk(raw, i).  The first four are on their way on entry (few_begin), those of `next` when it returns, if
-// there are as many.  The last four of a number that is no multiple of four overlap those before them; fewer than four, and a chunk that is there in
+// The chunks of a span, one after the other: chunk(raw, i).  The first four are on their way on entry (few_begin), those of `next` when it returns,
+// if there are as many.  The last four of a number that is no multiple of four overlap those before them; fewer than four, and a chunk that is there in
 // part, are fetched on their own.
-template <int ALIGN, class Chunk>
-__device__ __forceinline__ void few_walk(FewRaw (&raw)[kFewAhead], const FewWeights &w, const FewSpan &f, const FewSpan &next, uint32_t q, Chunk &&chunk)
+template <int ALIGN, int N, class Chunk>
+__device__ __forceinline__ void few_walk(FewRaw<N> (&raw)[kFewAhead], const FewWeights &w, const FewSpan<N> &f, const FewSpan<N> &next, uint32_t q, Chunk &&chunk)
 {
     const int32_t n = f.n;
     if (n >= kFewAhead) {
-        const uint8_t *row[2] = {f.row[0], f.row[1]};
+        const uint8_t *row[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) row[i] = f.row[i];
 #pragma unroll 1
         for (int32_t j = 0; j < n; j += kFewAhead) {
             const int32_t from = min(j, n - kFewAhead), step = min(j + kFewAhead, n - kFewAhead) - from;
             const bool other = j + kFewAhead >= n && next.n >= kFewAhead;       // (with none to come, the last ones again, to no use)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) row[i] = other ? next.row[i] : row[i] + step * 64;
+            for (int i = 0; i < N; ++i) row[i] = other ? next.row[i] : row[i] + step * 64;
 #pragma unroll
             for (int u = 0; u < kFewAhead; ++u) {
                 if (from + u >= j) chunk(raw[u], from + u);
-                few_fetch<ALIGN>(raw[u], row, u);
+                few_fetch<ALIGN, N>(raw[u], row, u);
             }
         }
     }
 #pragma unroll 1
     for (int32_t i = n >= kFewAhead ? n : 0; i < n + (f.tail ? 1 : 0); ++i) {
-        FewRaw r;
+        FewRaw<N> r;
         if (i < n) {
-            few_fetch<ALIGN>(r, f.row, i);
+            few_fetch<ALIGN, N>(r, f.row, i);
         } else {
             few_fetch_tail(r, w, f, q);
         }
         chunk(r, i);
     }
 }
-template <int ALIGN>
-__device__ __forceinline__ void few_begin(FewRaw (&raw)[kFewAhead], const FewSpan &f)
+template <int ALIGN, int N>
+__device__ __forceinline__ void few_begin(FewRaw<N> (&raw)[kFewAhead], const FewSpan<N> &f)
 {
     if (f.n >= kFewAhead) {
 #pragma unroll
-        for (int u = 0; u < kFewAhead; ++u) few_fetch<ALIGN>(raw[u], f.row, u);
+        for (int u = 0; u < kFewAhead; ++u) few_fetch<ALIGN, N>(raw[u], f.row, u);
     }
 }
 
@@ -287,25 +294,34 @@ __device__ __forceinline__ void few_mma(float (&d)[4], uint32_t a0, uint32_t a1,
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Two rows' eight k of each lane against those of eight choices.
+// Two rows' eight k of each lane (a, b) against those of eight choices (v).
 template <class T>
-__device__ __forceinline__ void few_products(float (&acc)[4], const FewRaw &r, const uint4 &v)
+__device__ __forceinline__ void few_products(float (&acc)[4], const uint4 &a, const uint4 &b, const uint4 &v)
 {
-    few_mma(acc, r.v[0].x, r.v[1].x, r.v[0].y, r.v[1].y, v.x, v.y, T());
-    few_mma(acc, r.v[0].z, r.v[1].z, r.v[0].w, r.v[1].w, v.z, v.w, T());
+    few_mma(acc, a.x, b.x, a.y, b.y, v.x, v.y, T());
+    few_mma(acc, a.z, b.z, a.w, b.w, v.z, v.w, T());
 }
 
-// The power of two that brings a largest magnitude (bits of an fp32 number) to 2^14 or more, below 2^15, and its inverse; 1 for zero.
-struct FewScale {
-    float scale, inverse;
-};
-__device__ __forceinline__ FewScale few_range(uint32_t bits)
+// The sum of two bf16 that a number is, or is nearest to; pairs of numbers.
+__device__ __forceinline__ void few_two_parts(float a, float b, uint32_t &hi, uint32_t &lo)
 {
-    const int32_t e = static_cast<int32_t>(bits >> 23), up = bits == 0u || e == 255 ? 127 : min(268 - e, 254);
-    FewScale s;
-    s.scale = __uint_as_float(static_cast<uint32_t>(up) << 23);
-    s.inverse = up == 254 ? 0x1p-127f : __uint_as_float(static_cast<uint32_t>(254 - up) << 23);
-    return s;
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    hi = *reinterpret_cast<const uint32_t *>(&h);
+    const float ah = __uint_as_float(hi << 16), bh = __uint_as_float(hi & 0xffff0000u);
+    // infinities and NaN are their first part alone
+    lo = pack_pair(fabsf(ah) < __int_as_float(0x7f800000) ? a - ah : 0.0f, fabsf(bh) < __int_as_float(0x7f800000) ? b - bh : 0.0f, __nv_bfloat16());
+}
+__device__ __forceinline__ void few_two_parts(const uint4 &f16, uint4 &hi, uint4 &lo)
+{
+    const uint32_t w[4] = {f16.x, f16.y, f16.z, f16.w};
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+        few_two_parts(f.x, f.y, h[i], l[i]);
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
 // The chunks of slice s of S: whole runs of four but for the last slice's.
@@ -331,7 +347,6 @@ __device__ __forceinline__ uint4 few_load_x(const uint16_t *row, int32_t k, int3
 }
 
 __device__ __forceinline__ float few_silu(float u) { return u / (1.0f + __expf(-u)); }
-__device__ __forceinline__ float few_finite(float v) { return fabsf(v) < __int_as_float(0x7f800000) ? fabsf(v) : 0.0f; }
 
 // T: the type of x and of the weights.  Dynamic shared memory: the lists, then x.
 template <class T, int ALIGN>
@@ -387,11 +402,11 @@ few_up_kernel(const FewParams p)
     auto span_of = [&](const Work &t, int32_t begin) {
         int32_t first, n;
         few_slice(min(piece, chunks - begin), t.slice, t.slices, first, n);
-        return few_span(p.w, t.expert, t.row0, t.row1, begin + first, __any_sync(0xffffffffu, t.has0) ? n : 0, q);
+        return few_span<2>(p.w, t.expert, t.row0, t.row1, begin + first, __any_sync(0xffffffffu, t.has0) ? n : 0, q);
     };
 
-    FewRaw raw[kFewAhead];
-    FewSpan span{};
+    FewRaw<2> raw[kFewAhead];
+    FewSpan<2> span{};
     if (my_rounds > 0) {
         span = span_of(work_of(0), 0);
         few_begin<ALIGN>(raw, span);
@@ -431,12 +446,12 @@ few_up_kernel(const FewParams p)
                 staged_entry = now.entry;
                 staged_begin = begin;
             }
-            const FewSpan here = span;
+            const FewSpan<2> here = span;
             span.n = 0;
             if (begin + piece < chunks) span = span_of(now, begin + piece);
             else if (round + 1 < my_rounds) span = span_of(work_of(round + 1), 0);
             const uint4 *x = s_x + (here.first - begin) * 32 + lane;
-            few_walk<ALIGN>(raw, p.w, here, span, q, [&](const FewRaw &r, int32_t i) { few_products<T>(acc, r, x[i * 32]); });
+            few_walk<ALIGN>(raw, p.w, here, span, q, [&](const FewRaw<2> &r, int32_t i) { few_products<T>(acc, r.v[0], r.v[1], x[i * 32]); });
             if (here.n < kFewAhead) few_begin<ALIGN>(raw, span);      // nothing was fetched on the way
         }
         if (now.slices > 1) {
@@ -465,13 +480,12 @@ few_up_kernel(const FewParams p)
                 for (int i = 0; i < 2; ++i) {
                     if (i == 1 && p.gated) break;
                     const int32_t k = k0 + 8 * i;
-                    float top = few_finite(v[i]);
-#pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                    if (used && k < p.h_stride) {
-                        p.h[c * p.h_stride + k] = v[i];
-                        if (!std::is_same<T, __nv_bfloat16>::value && m == 0) p.top[(c * p.h_stride + k) >> 3] = top;
-                    }
+                    if (!used || k >= p.h_stride) continue;
+                    uint32_t hi, lo;
+                    few_two_parts(v[i], 0.0f, hi, lo);
+                    uint16_t *dst = reinterpret_cast<uint16_t *>(p.h + c * p.h_stride + k);
+                    dst[0] = static_cast<uint16_t>(hi);
+                    dst[static_cast<int64_t>(p.choices) * p.h_stride] = static_cast<uint16_t>(lo);
                 }
             }
         }
@@ -480,32 +494,19 @@ few_up_kernel(const FewParams p)
 
 // ---- launch 2: y = sum of weight * (W2 h) ------------------------------------------------------------------------------
 
-// The sum of two bf16 that a number is, or is nearest to; pairs of numbers.
-__device__ __forceinline__ void few_two_parts(float a, float b, uint32_t &hi, uint32_t &lo)
-{
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    hi = *reinterpret_cast<const uint32_t *>(&h);
-    const float ah = __uint_as_float(hi << 16), bh = __uint_as_float(hi & 0xffff0000u);
-    // infinities and NaN are their first part alone
-    lo = pack_pair(fabsf(ah) < __int_as_float(0x7f800000) ? a - ah : 0.0f, fabsf(bh) < __int_as_float(0x7f800000) ? b - bh : 0.0f, __nv_bfloat16());
-}
-
-// grid: 16 rows of W2 (outputs) a CTA.  Dynamic shared memory: the lists, the choices' weights, most_slices x choices x 16 sums, then each warp's part of h
-// (p.piece bytes) as the products read it: [choice][chunk][part][4 lanes], choices 64 bytes further apart than they need be.
+// grid: 16 rows of W2 (outputs) a CTA.  Dynamic shared memory: the lists, the choices' weights, most_slices x choices x 16 sums.
 template <class T, int ALIGN>
 __global__ void __launch_bounds__(kFewDownThreads, 1)
 few_down_kernel(const FewParams p)
 {
-    constexpr bool kHalf = std::is_same<T, __half>::value;
-    constexpr int kWarps = kFewDownThreads / 32, kParts = kHalf ? 1 : 2;
+    constexpr int kWarps = kFewDownThreads / 32;
     extern __shared__ __align__(16) uint8_t smem[];
     const FewLists l = few_lists(smem, p);
     float *s_weight = reinterpret_cast<float *>(smem + few_list_bytes(p.experts, p.choices)), *part = s_weight + ((p.choices + 3) & ~3);
-    const int32_t warp = static_cast<int32_t>(threadIdx.x >> 5);
-    uint4 *s_h = reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(part + p.most_slices * p.choices * 16) + warp * p.piece);
     grid_launch_dependents();
     for (int32_t c = static_cast<int32_t>(threadIdx.x); c < p.choices; c += kFewDownThreads) s_weight[c] = p.weights[c];      // inputs of the call: launch 1 has waited for them
     few_make_lists(p, l);
+    const int32_t warp = static_cast<int32_t>(threadIdx.x >> 5);
     const uint32_t lane = threadIdx.x & 31u, q = lane & 3u, m = lane >> 2;
     const int32_t r0 = static_cast<int32_t>(blockIdx.x) * 16 + static_cast<int32_t>(m), chunks = (p.w.depth + kFewChunk - 1) / kFewChunk;
     const int32_t row0 = r0 < p.w.rows ? r0 : 0, row1 = r0 + 8 < p.w.rows ? r0 + 8 : 0;
@@ -515,7 +516,7 @@ few_down_kernel(const FewParams p)
     while (rest_slices * 2 <= p.most_slices && rest * rest_slices * 2 <= kWarps) rest_slices *= 2;
     const int32_t my_rounds = rounds + (warp < rest * rest_slices ? 1 : 0);
     struct Work {
-        int32_t expert, first, count, chunk0, n, slice;
+        int32_t expert, first, count, slice;
     };
     auto work_of = [&](int32_t round) {
         Work t;
@@ -525,94 +526,66 @@ few_down_kernel(const FewParams p)
         t.expert = static_cast<int32_t>(l.entry[2 * entry]);
         t.first = static_cast<int32_t>(l.entry[2 * entry + 1] & 0xffffu);
         t.count = static_cast<int32_t>(l.entry[2 * entry + 1] >> 16);
-        few_slice(chunks, t.slice, whole ? 1 : rest_slices, t.chunk0, t.n);
         return t;
     };
-    // the chunks of h that fit a warp's shared memory (whole runs of four, if it has room for four)
-    auto piece_of = [&](int32_t count) {
-        const int32_t fit = (p.piece / count - 64) / (64 * kParts);
-        return fit >= kFewAhead ? fit & ~(kFewAhead - 1) : fit;
+    auto span_of = [&](int32_t round) {
+        const Work t = work_of(round);
+        int32_t first, n;
+        few_slice(chunks, t.slice, round < rounds ? 1 : rest_slices, first, n);
+        FewSpan<4> f = few_span<4>(p.w, t.expert, row0, row1, first, n, q);
+        const int64_t c = l.list[t.first + min(static_cast<int32_t>(m), t.count - 1)];
+        f.row[2] = reinterpret_cast<const uint8_t *>(p.h + c * p.h_stride) + first * 64 + q * 16;
+        f.row[3] = f.row[2] + static_cast<int64_t>(p.choices) * p.h_stride * 2;
+        return f;
     };
-    auto span_of = [&](const Work &t, int32_t begin) { return few_span(p.w, t.expert, row0, row1, t.chunk0 + begin, min(piece_of(t.count), t.n - begin), q); };
-    FewRaw raw[kFewAhead];
-    FewSpan span{};
+    FewRaw<4> raw[kFewAhead];
+    FewSpan<4> span{};
     if (my_rounds > 0) {
-        span = span_of(work_of(0), 0);
-        few_begin<ALIGN>(raw, span);
+        span = span_of(0);
+        if (span.n >= kFewAhead) {                                // the weights' first chunks: those of h are not there yet
+#pragma unroll
+            for (int u = 0; u < kFewAhead; ++u) {
+                raw[u].v[0] = few_load16<ALIGN>(span.row[0] + u * 64);
+                raw[u].v[1] = few_load16<ALIGN>(span.row[1] + u * 64);
+            }
+        }
     }
     grid_dependency_wait();                                       // h
+    if (my_rounds > 0 && span.n >= kFewAhead) {
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u) {
+            raw[u].v[2] = few_load16<16>(span.row[2] + u * 64);
+            raw[u].v[3] = few_load16<16>(span.row[3] + u * 64);
+        }
+    }
     for (int32_t round = 0; round < my_rounds; ++round) {
         const Work now = work_of(round);
-        const int32_t piece = piece_of(now.count), pitch = (min(piece, now.n) * kParts + 1) * 4;      // 16-byte pieces from a choice to the next
-        FewScale range{1.0f, 1.0f};                               // of choice m, in its four lanes
-        if constexpr (kHalf) {
-            const int64_t c = l.list[now.first + min(static_cast<int32_t>(m), now.count - 1)];
-            const float4 *tops = reinterpret_cast<const float4 *>(p.top + (c * p.h_stride >> 3));      // h_stride / 8 is a multiple of 4
-            float top = 0.0f;
-#pragma unroll 4
-            for (int32_t i = static_cast<int32_t>(q); i < p.h_stride >> 5; i += 4) {
-                const float4 v = tops[i];
-                top = fmaxf(fmaxf(top, v.x), fmaxf(fmaxf(v.y, v.z), v.w));
-            }
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            range = few_range(__float_as_uint(fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2))));
-        }
         float acc[4] = {};
-        for (int32_t begin = 0; begin < now.n; begin += piece) {
-            const FewSpan here = span;
-            // h of the entry's choices: 16-byte pieces, four on their way at a time
-            __syncwarp();
-            const int32_t pieces = min(piece, now.n - begin) * 4;
-            for (int32_t n = 0; n < now.count; ++n) {
-                const float *src = p.h + static_cast<int64_t>(l.list[now.first + n]) * p.h_stride + here.first * kFewChunk;
-                const float s = __shfl_sync(0xffffffffu, range.scale, n * 4);
-                for (int32_t u0 = static_cast<int32_t>(lane); u0 < pieces; u0 += 128) {
-                    float4 v[4][2];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float4 *at = reinterpret_cast<const float4 *>(src + min(u0 + i * 32, pieces - 1) * 8);
-                        v[i][0] = at[0];
-                        v[i][1] = at[1];
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int32_t u = u0 + i * 32;
-                        if (u >= pieces) break;
-                        const float4 a = v[i][0], b = v[i][1];
-                        if constexpr (kHalf) {
-                            s_h[n * pitch + u] = make_uint4(pack_pair(a.x * s, a.y * s, __half()), pack_pair(a.z * s, a.w * s, __half()), pack_pair(b.x * s, b.y * s, __half()),
-                                                            pack_pair(b.z * s, b.w * s, __half()));
-                        } else {
-                            uint4 hi, lo;
-                            few_two_parts(a.x, a.y, hi.x, lo.x);
-                            few_two_parts(a.z, a.w, hi.y, lo.y);
-                            few_two_parts(b.x, b.y, hi.z, lo.z);
-                            few_two_parts(b.z, b.w, hi.w, lo.w);
-                            s_h[n * pitch + (u >> 2) * 8 + (u & 3)] = hi;
-                            s_h[n * pitch + (u >> 2) * 8 + 4 + (u & 3)] = lo;
-                        }
-                    }
-                }
+        const FewSpan<4> here = span;
+        span.n = 0;
+        if (round + 1 < my_rounds) span = span_of(round + 1);
+        few_walk<ALIGN>(raw, p.w, here, span, q, [&](const FewRaw<4> &r, int32_t) {
+            using B = __nv_bfloat16;
+            if constexpr (std::is_same<T, B>::value) {
+                few_products<B>(acc, r.v[0], r.v[1], r.v[2]);
+                few_products<B>(acc, r.v[0], r.v[1], r.v[3]);
+            } else {
+                uint4 a[2], b[2];
+                few_two_parts(r.v[0], a[0], a[1]);
+                few_two_parts(r.v[1], b[0], b[1]);
+                few_products<B>(acc, a[0], b[0], r.v[2]);
+                few_products<B>(acc, a[0], b[0], r.v[3]);
+                few_products<B>(acc, a[1], b[1], r.v[2]);
             }
-            __syncwarp();
-            span.n = 0;
-            if (begin + piece < now.n) span = span_of(now, begin + piece);
-            else if (round + 1 < my_rounds) span = span_of(work_of(round + 1), 0);
-            const uint4 *h = s_h + min(static_cast<int32_t>(m), now.count - 1) * pitch + q;
-            few_walk<ALIGN>(raw, p.w, here, span, q, [&](const FewRaw &r, int32_t i) {
-#pragma unroll
-                for (int k = 0; k < kParts; ++k) few_products<T>(acc, r, h[(i * kParts + k) * 4]);
-            });
-            if (here.n < kFewAhead) few_begin<ALIGN>(raw, span);          // nothing was fetched on the way
-        }
+        });
+        if (here.n < kFewAhead) few_begin<ALIGN>(raw, span);      // nothing was fetched on the way
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int32_t at = static_cast<int32_t>(q) * 2 + j;
-            const float s = __shfl_sync(0xffffffffu, range.inverse, at * 4);
             if (at >= now.count) continue;
             float *dst = part + (now.slice * p.choices + l.list[now.first + at]) * 16;
-            dst[m] = acc[j] * s;
-            dst[m + 8] = acc[2 + j] * s;
+            dst[m] = acc[j];
+            dst[m + 8] = acc[2 + j];
         }
         // an entry that one warp had alone has one sum for each choice: the other slices' are zeros
         if (round < rounds) {

@@ -237,9 +237,8 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
     // No thread reads or writes global memory before the kernels ahead in the stream are complete.
     grid_dependency_wait();
     if (warp == 2 && p.groups > 0) {
-        // the groups' places among the scale tiles, then among the result's tiles
-        scan_groups(p, scale_pre, off, 128, lane);
-        scan_groups(p, pre, off, p.ragged == kRaggedK ? kFp4Unit : p.ragged == kRaggedP ? TP : TQ, lane);
+        // the groups' places among the result's tiles, and among the scale tiles
+        scan_groups(p, pre, off, p.ragged == kRaggedK ? kFp4Unit : p.ragged == kRaggedP ? TP : TQ, lane, scale_pre, 128);
     }
     tc_fence_before_sync();
     __syncthreads();

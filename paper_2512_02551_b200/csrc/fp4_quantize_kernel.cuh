@@ -7,7 +7,7 @@
 // blocks lie in registers again, and the packed columns and their scale tiles leave through shared memory in runs of 64 and 1024 bytes.
 //
 // A value is the nearest 4-bit value of the correctly rounded quotient x / step (step = scale * factor): q = x * r, then one residual step with two
-// multiply-adds (r = 1 / step is correctly rounded, which makes that quotient so).  A plain product with the reciprocal would be off by an ulp where x lies
+// multiply-adds (r = 1 / step is correctly rounded, which makes that quotient so), two values an instruction.  A plain product with the reciprocal would be off by an ulp where x lies
 // halfway between two values, which inputs of few bits often do.  Maxima are taken on the bit patterns: a NaN or an infinity is larger than every number.
 #pragma once
 
@@ -136,12 +136,12 @@ __device__ __forceinline__ BlockStep block_step(float amax, float factor, float 
 template <bool NV>
 __device__ __forceinline__ uint32_t quantize_pair(float a, float b, const BlockStep &s)
 {
-    float x = a * s.inverse, y = b * s.inverse;
-    if constexpr (NV) {
-        x = fmaf(fmaf(-x, s.step, a), s.inverse, x);
-        y = fmaf(fmaf(-y, s.step, b), s.inverse, y);
-    }
-    return __nv_cvt_float2_to_fp4x2(make_float2(x, y), __NV_E2M1, cudaRoundNearest);
+    const uint64_t v = pack_f32x2(__float_as_uint(a), __float_as_uint(b)), r = pack_f32x2(__float_as_uint(s.inverse), __float_as_uint(s.inverse));
+    uint64_t x = mul_f32x2(v, r);
+    if constexpr (NV) x = fma_f32x2(fma_f32x2(x, pack_f32x2(__float_as_uint(-s.step), __float_as_uint(-s.step)), v), r, x);
+    float lo, hi;
+    unpack_f32x2(x, lo, hi);
+    return __nv_cvt_float2_to_fp4x2(make_float2(lo, hi), __NV_E2M1, cudaRoundNearest);
 }
 
 // Eight values in a word.
@@ -189,7 +189,7 @@ __device__ __forceinline__ bool block_of_group(const int32_t *offsets, int32_t g
 
 // MODE: HGEMM_FP4_ROWS (1), COLS (2) or both (3).  grid: x = column tiles (each CTA walks on by gridDim.x), y = row tiles (as many as the padded copy has), z = matrices.
 template <class T, int MODE, bool NV>
-__global__ void __launch_bounds__(kFp4QuantThreads, sizeof(T) == 4 || MODE == 1 ? 3 : 4)
+__global__ void __launch_bounds__(kFp4QuantThreads, sizeof(T) == 4 ? 2 : 3)
 fp4_quantize_kernel(const Fp4QuantParams p)
 {
     constexpr int kBlock = NV ? 16 : 32, kAtom = 4 * kBlock;     // elements of a block; of a scale tile's four
@@ -481,6 +481,39 @@ struct Fp4DequantParams {
     int32_t groups, ragged, rows_ragged, k_capacity;
 };
 
+// 16 elements of each lane (f; row r, columns col ..; active: it has any) to rows that start anywhere: through shared memory (512 elements of a warp), so that lanes store next to
+// each other, four bytes each where the warp's elements lie in one row.
+template <class T>
+__device__ __forceinline__ void store_anywhere(T *buffer, const float (&f)[16], bool active, T *out, int64_t ldo, int64_t r, int64_t col, int64_t cols)
+{
+    const uint32_t lane = lane_id();
+#pragma unroll
+    for (int j = 0; j < 16; ++j) buffer[lane * 16 + j] = narrow_to<T>(f[j]);
+    __syncwarp();
+    const int64_t row0 = __shfl_sync(0xffffffffu, r, 0), col0 = __shfl_sync(0xffffffffu, col, 0);
+    if (sizeof(T) == 2 && __all_sync(0xffffffffu, active && r == row0)) {
+        T *to = out + row0 * ldo + col0;
+        const int32_t n = static_cast<int32_t>(min(static_cast<int64_t>(512), cols - col0)), odd = static_cast<int32_t>(reinterpret_cast<uintptr_t>(to) >> 1) & 1;
+        if (odd && lane == 0) to[0] = buffer[0];
+        const unsigned short *from = reinterpret_cast<const unsigned short *>(buffer);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int32_t e = odd + 2 * (i * 32 + static_cast<int32_t>(lane));
+            if (e + 1 < n) *reinterpret_cast<uint32_t *>(to + e) = from[e] | (static_cast<uint32_t>(from[e + 1]) << 16);
+            else if (e < n) to[e] = buffer[e];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int src = 2 * i + static_cast<int>(lane >> 4), j = static_cast<int>(lane & 15u);
+            const int64_t sr = __shfl_sync(0xffffffffu, r, src), sc = __shfl_sync(0xffffffffu, col, src) + j;
+            const bool there = __shfl_sync(0xffffffffu, static_cast<int>(active), src) != 0;
+            if (there && sc < cols) out[sr * ldo + sc] = buffer[src * 16 + j];
+        }
+    }
+    __syncwarp();
+}
+
 // A thread per 16 elements: 8 bytes of values, one scale.  Dynamic shared memory: 2 (groups + 1) words.
 template <class T, bool NV>
 __global__ void __launch_bounds__(256)
@@ -501,11 +534,15 @@ fp4_dequantize_kernel(const Fp4DequantParams p)
     const uint8_t *q = p.q + matrix * p.rows * p.ldq, *scales = p.scales + matrix * row_tiles * atoms * 512;
     T *out = static_cast<T *>(p.out) + matrix * p.rows * p.ldo;
     const float factor = NV ? p.factor[matrix] : 1.0f;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += step) {
-        const int64_t r = fast_div(static_cast<int32_t>(i), p.fd_chunks), col = (i - r * p.fd_chunks.d) * 16;
+    const uint32_t lane = threadIdx.x & 31u;
+    __shared__ T s_store[8][512];
+    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * blockDim.x + (threadIdx.x & ~31u); i0 < all; i0 += step) {        // whole warps
+        const int64_t i = i0 + lane;
+        bool active = i < all;
+        const int64_t r = active ? fast_div(static_cast<int32_t>(i), p.fd_chunks) : 0, col = active ? (i - r * p.fd_chunks.d) * 16 : 0;
         int64_t place = r;
         if (p.groups > 0) {
-            if (r < off[0] || r >= off[p.groups]) continue;        // a row of no group
+            if (r < off[0] || r >= off[p.groups]) active = false;  // a row of no group
             int32_t lo = 0, hi = p.groups;                         // the last group that starts at or before r
             while (hi - lo > 1) {
                 const int32_t mid = (lo + hi) / 2;
@@ -514,31 +551,35 @@ fp4_dequantize_kernel(const Fp4DequantParams p)
             }
             place = 128ll * pre[lo] + r - off[lo];
         }
-        const uint8_t *src = q + r * p.ldq + col / 2;
-        uint2 v;
-        if (col + 16 <= p.cols) {
-            v = *reinterpret_cast<const uint2 *>(src);             // rows start at multiples of 16 bytes, col / 2 is a multiple of 8
-        } else {
-            v = make_uint2(0u, 0u);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (col + 2 * j < p.cols) (j < 4 ? v.x : v.y) |= static_cast<uint32_t>(src[j]) << (8 * (j & 3));
-        }
-        const int64_t b = col / kBlock;
-        const uint32_t byte = scales[((place >> 7) * atoms + (b >> 2)) * 512 + (place & 31) * 16 + ((place >> 5) & 3) * 4 + (b & 3)];
-        float s;
-        if constexpr (NV) s = __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(byte), __NV_E4M3))) * factor;
-        else s = byte == 0u ? 5.877471754111438e-39f : byte == 255u ? __int_as_float(0x7fffffff) : __uint_as_float(byte << 23);
         float f[16];
+        if (active) {
+            const uint8_t *src = q + r * p.ldq + col / 2;
+            uint2 v;
+            if (col + 16 <= p.cols) {
+                v = *reinterpret_cast<const uint2 *>(src);         // rows start at multiples of 16 bytes, col / 2 is a multiple of 8
+            } else {
+                v = make_uint2(0u, 0u);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(((j < 4 ? v.x : v.y) >> (8 * (j & 3))) & 0xffu), __NV_E2M1);
-            const float2 e = __half22float2(__half2(h));
-            f[2 * j] = e.x * s;
-            f[2 * j + 1] = e.y * s;
+                for (int j = 0; j < 8; ++j)
+                    if (col + 2 * j < p.cols) (j < 4 ? v.x : v.y) |= static_cast<uint32_t>(src[j]) << (8 * (j & 3));
+            }
+            const int64_t b = col / kBlock;
+            const uint32_t byte = scales[((place >> 7) * atoms + (b >> 2)) * 512 + (place & 31) * 16 + ((place >> 5) & 3) * 4 + (b & 3)];
+            float s;
+            if constexpr (NV) s = __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(byte), __NV_E4M3))) * factor;
+            else s = byte == 0u ? 5.877471754111438e-39f : byte == 255u ? __int_as_float(0x7fffffff) : __uint_as_float(byte << 23);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(((j < 4 ? v.x : v.y) >> (8 * (j & 3))) & 0xffu), __NV_E2M1);
+                const float2 e = __half22float2(__half2(h));
+                f[2 * j] = e.x * s;
+                f[2 * j + 1] = e.y * s;
+            }
         }
         T *dst = out + r * p.ldo + col;
-        if (p.vec_ok && col + 16 <= p.cols) {
+        if (!p.vec_ok) {
+            store_anywhere<T>(s_store[threadIdx.x >> 5], f, active, out, p.ldo, r, col, p.cols);
+        } else if (active && col + 16 <= p.cols) {
             if constexpr (sizeof(T) == 4) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) reinterpret_cast<float4 *>(dst)[j] = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
@@ -549,7 +590,7 @@ fp4_dequantize_kernel(const Fp4DequantParams p)
                 reinterpret_cast<uint4 *>(dst)[0] = make_uint4(h[0], h[1], h[2], h[3]);
                 reinterpret_cast<uint4 *>(dst)[1] = make_uint4(h[4], h[5], h[6], h[7]);
             }
-        } else {
+        } else if (active) {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 if (col + j < p.cols) dst[j] = narrow_to<T>(f[j]);

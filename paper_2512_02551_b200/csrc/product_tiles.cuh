@@ -68,38 +68,45 @@ __device__ __forceinline__ ProductTile product_tile(int32_t w, const Params &p, 
     return t;
 }
 
-// Clamped offsets and the prefix sums product_tile reads; one whole warp.
+// Clamped offsets and the prefix sums product_tile reads; one whole warp.  The offsets are fetched first, so that their latencies are one; unit2, pre2 (or nullptr): the prefix
+// sums of another unit.
 template <class Params>
-__device__ __forceinline__ void scan_groups(const Params &p, int32_t *pre, int32_t *off, int32_t unit, uint32_t lane)
+__device__ __forceinline__ void scan_groups(const Params &p, int32_t *pre, int32_t *off, int32_t unit, uint32_t lane, int32_t *pre2 = nullptr, int32_t unit2 = 1)
 {
-    int32_t carry = 0, last = 0;
+    for (int32_t e = static_cast<int32_t>(lane); e <= p.groups; e += 32) off[e] = min(max(p.offsets[e], 0), p.rows_ragged);
+    __syncwarp();
+    int32_t carry = 0, carry2 = 0, last = off[0];
     for (int32_t base = 0; base < p.groups; base += 32) {
         const int32_t e = base + static_cast<int32_t>(lane);
-        int32_t o = p.offsets[min(e, p.groups)];
-        o = min(max(o, 0), p.rows_ragged);
+        int32_t nxt = off[min(e + 1, p.groups)];                 // where group e ends
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {               // non-decreasing whatever the caller's values
-            const int32_t x = __shfl_up_sync(0xffffffffu, o, d);
-            if (static_cast<int32_t>(lane) >= d) o = max(o, x);
+        for (int d = 1; d < 32; d <<= 1) {                       // non-decreasing whatever the caller's values
+            const int32_t x = __shfl_up_sync(0xffffffffu, nxt, d);
+            if (static_cast<int32_t>(lane) >= d) nxt = max(nxt, x);
         }
-        o = max(o, last);
-        int32_t nxt = __shfl_down_sync(0xffffffffu, o, 1);
-        if (lane == 31) nxt = max(o, min(max(p.offsets[min(e + 1, p.groups)], 0), p.rows_ragged));
+        nxt = max(nxt, last);
+        int32_t o = __shfl_up_sync(0xffffffffu, nxt, 1);
+        if (lane == 0) o = last;
         last = __shfl_sync(0xffffffffu, nxt, 31);
-        int32_t n = e < p.groups ? (nxt - o + unit - 1) / unit : 0;
+        const int32_t rows = e < p.groups ? nxt - o : 0;
+        int32_t n = (rows + unit - 1) / unit, n2 = (rows + unit2 - 1) / unit2;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int32_t x = __shfl_up_sync(0xffffffffu, n, d);
-            if (static_cast<int32_t>(lane) >= d) n += x;
+            const int32_t x = __shfl_up_sync(0xffffffffu, n, d), y = __shfl_up_sync(0xffffffffu, n2, d);
+            if (static_cast<int32_t>(lane) >= d) n += x, n2 += y;
         }
         if (e < p.groups) {
-            off[e] = o;
             off[e + 1] = nxt;
             pre[e + 1] = p.ragged == kRaggedK ? min(carry + n, p.k_capacity) : carry + n;
+            if (pre2 != nullptr) pre2[e + 1] = carry2 + n2;
         }
         carry += __shfl_sync(0xffffffffu, n, 31);
+        carry2 += __shfl_sync(0xffffffffu, n2, 31);
     }
-    if (lane == 0) pre[0] = 0;
+    if (lane == 0) {
+        pre[0] = 0;
+        if (pre2 != nullptr) pre2[0] = 0;
+    }
 }
 
 template <class T>

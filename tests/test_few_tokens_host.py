@@ -51,7 +51,7 @@ def test_scratch_and_descriptions():
     L, D = few_tokens.lib(), few_tokens.Description
     good = dict(hidden=100, inner=130, experts=4, top_k=2, weights=16, activation=1, type=2, reserved=0)
     size = lambda tokens, **kw: L.hgemm_few_tokens_scratch(ctypes.byref(D(**{**good, **kw})), tokens)  # noqa: E731
-    assert size(0) == 0 and size(3, weights=2) == 3 * 2 * (160 + 20) * 4
+    assert size(0) == 0 and size(3, weights=2) == 3 * 2 * 160 * 4
     assert 3 * 2 * (8 * 80 + 4 * 260) < size(3) < 1 << 20 and size(64) > size(3) and size(3) % 256 == 0
     for kw in (dict(hidden=0), dict(inner=0), dict(hidden=(1 << 20) + 1), dict(experts=0), dict(experts=1025), dict(top_k=0), dict(top_k=33), dict(weights=0), dict(weights=1), dict(activation=2),
                dict(type=0)):

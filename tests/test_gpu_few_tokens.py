@@ -15,7 +15,7 @@ from paper_2512_02551_b200 import few_tokens, fp4, hgemm, routing  # noqa: E402
 
 DTYPE = {"bf16": torch.bfloat16, "f16": torch.float16}
 #: Bits of h against each kind of weights (None: digits).
-BITS = {"bf16": 16, "f16": 11, "nvfp4": None, "mxfp4": None}
+BITS = {"bf16": 16, "f16": 16, "nvfp4": None, "mxfp4": None}
 KINDS = [("bf16", "bf16"), ("f16", "f16"), ("nvfp4", "bf16"), ("nvfp4", "f16"), ("mxfp4", "bf16"), ("mxfp4", "f16")]
 
 
@@ -66,12 +66,11 @@ def silu(u):
         return u / (1 + np.exp(-u))
 
 
-def formula(x, w1, w2, indices, weights, gated, bits=11):
+def formula(x, w1, w2, indices, weights, gated, bits=16):
     """(y, bound of the error before y's rounding) in 64 bits.
 
-    `bits`: what h is rounded to (2^-bits: a half step, and the factors' products); None: x and h are sums of digits, off by at most 2^-19 of their largest
-    magnitude.  h of an fp16 product is scaled so that its largest magnitude is 2^14 or more: half a step among fp16's smallest numbers, 2^-25, is at most
-    2^-39 of it.  The contraction over `hidden` adds H numbers in 32 bits (2^-23 of their magnitudes each covers truncation; with digits, eight times as many, and
+    `bits`: what h is rounded to (2^-bits: a half step, and the factors' products; an fp16 weight against h loses the product of two second parts, as much
+    again); None: x and h are sums of digits, off by at most 2^-19 of their largest magnitude.  The contraction over `hidden` adds H numbers in 32 bits (2^-23 of their magnitudes each covers truncation; with digits, eight times as many, and
     8 more); silu changes by at most 1.1 times its argument's error, and its exponential is off by 2^-21 (2 + |u|) of itself; then I, and k, numbers are added."""
     digits = bits is None
     many, lost = (8, 2.0 ** -19) if digits else (1, 0.0)
@@ -88,7 +87,7 @@ def formula(x, w1, w2, indices, weights, gated, bits=11):
             g = silu(u[:I])
             dg = 1.1 * du[:I] + np.abs(g) * (2 + np.abs(u[:I])) * 2.0 ** -21
             h, dh = (g * u[I:], np.abs(u[I:]) * dg + (np.abs(g) + dg) * du[I:]) if gated else (g, dg)
-            dh = dh + (lost * np.abs(h).max() if digits else np.abs(h) * 2.0 ** -bits + 2.0 ** -39 * np.abs(h).max()) + 2.0 ** -130
+            dh = dh + (lost * np.abs(h).max() if digits else np.abs(h) * 2.0 ** (1 - bits)) + 2.0 ** -130
             z = w2[e] @ h
             mag = np.abs(w2[e]) @ np.abs(h)
             w = weights[t, j]
