@@ -445,20 +445,19 @@ hgemm_status_t hgemm_fp4_dequantize(hgemm_ctx_t *ctx, int32_t format, int32_t ou
     const int es = type_bytes(out_type);
     if (!q || !scales || !out || !aligned16(q) || !aligned16(scales) || (reinterpret_cast<uintptr_t>(out) % unsigned(es)) != 0) return HGEMM_ERR_INVALID_ARG;
     const int64_t chunks = ceil_div(cols, 16);
-    if (rows * chunks >= (int64_t(1) << 31)) return HGEMM_ERR_UNSUPPORTED;
+    if (rows * chunks >= (int64_t(1) << 31) - 65536 * 256 || ldq > 0x7fffffff || ldo > 0x7fffffff) return HGEMM_ERR_UNSUPPORTED;      // (run numbers are 32 bits wide, a round of all threads beyond the last too)
     hgemm_dev::Fp4DequantParams p;
     std::memset(&p, 0, sizeof(p));
     p.q = static_cast<const uint8_t *>(q);
-    p.ldq = ldq;
+    p.ldq = uint32_t(ldq);
     p.scales = static_cast<const uint8_t *>(scales);
     p.factor = factor;
-    p.rows = rows;
-    p.cols = cols;
-    p.matrices = matrices;
+    p.rows = uint32_t(rows);
+    p.cols = uint32_t(cols);
     p.fd_chunks = hgemm_dev::make_fast_div(uint32_t(chunks));
     p.vec_ok = aligned16(out) && (ldo * es) % 16 == 0 ? 1 : 0;
     p.out = out;
-    p.ldo = ldo;
+    p.ldo = uint32_t(ldo);
     p.offsets = offsets;
     p.groups = groups;
     p.rows_ragged = int32_t(std::min(rows, kMaxDim));

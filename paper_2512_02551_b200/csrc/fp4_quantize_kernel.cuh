@@ -132,23 +132,20 @@ __device__ __forceinline__ BlockStep block_step(float amax, float factor, float 
     return s;
 }
 
-// Two quotients as 4-bit values in one byte.
-template <bool NV>
-__device__ __forceinline__ uint32_t quantize_pair(float a, float b, const BlockStep &s)
-{
-    const uint64_t v = pack_f32x2(__float_as_uint(a), __float_as_uint(b)), r = pack_f32x2(__float_as_uint(s.inverse), __float_as_uint(s.inverse));
-    uint64_t x = mul_f32x2(v, r);
-    if constexpr (NV) x = fma_f32x2(fma_f32x2(x, pack_f32x2(__float_as_uint(-s.step), __float_as_uint(-s.step)), v), r, x);
-    float lo, hi;
-    unpack_f32x2(x, lo, hi);
-    return __nv_cvt_float2_to_fp4x2(make_float2(lo, hi), __NV_E2M1, cudaRoundNearest);
-}
-
-// Eight values in a word.
+// Eight quotients as 4-bit values in a word.
 template <bool NV>
 __device__ __forceinline__ uint32_t quantize8(const float *f, const BlockStep &s)
 {
-    return quantize_pair<NV>(f[0], f[1], s) | (quantize_pair<NV>(f[2], f[3], s) << 8) | (quantize_pair<NV>(f[4], f[5], s) << 16) | (quantize_pair<NV>(f[6], f[7], s) << 24);
+    const uint64_t r = pack_f32x2(__float_as_uint(s.inverse), __float_as_uint(s.inverse)), step = pack_f32x2(__float_as_uint(-s.step), __float_as_uint(-s.step));
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t v = pack_f32x2(__float_as_uint(f[2 * i]), __float_as_uint(f[2 * i + 1]));
+        uint64_t q = mul_f32x2(v, r);
+        if constexpr (NV) q = fma_f32x2(fma_f32x2(q, step, v), r, q);
+        unpack_f32x2(q, x[2 * i], x[2 * i + 1]);
+    }
+    return pack_e2m1(x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]);
 }
 
 // The group that holds block rb (of 128 rows) of the copy laid out per group, and the block's rows: first .. end - 1 of the input (end: the group's).  The offsets are
@@ -222,9 +219,18 @@ fp4_quantize_kernel(const Fp4QuantParams p)
     for (int64_t ct = blockIdx.x; ct < col_tiles; ct += gridDim.x) {
         const int64_t col = ct * 128 + sub * 16;
         Raw16<T> raw[4];
+        // a whole tile of a plain matrix takes its loads and stores without a test per row
+        const bool whole = p.vec_ok && p.row_index == nullptr && row0 + 128 <= row_end && ct * 128 + 128 <= p.cols;
+        const int64_t my_row = row0 + (threadIdx.x >> 3);
+        if (whole) {
+            const T *src = x + my_row * p.ldx + col;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) raw[i] = load16<T>(src + i * 32 * p.ldx, 0, 16, 1);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t r = row0 + (threadIdx.x >> 3) + 32 * i;
+            if (whole) break;
+            const int64_t r = my_row + 32 * i;
             const T *src = nullptr;
             if (r < row_end) {
                 if (p.row_index == nullptr) {
@@ -283,7 +289,9 @@ fp4_quantize_kernel(const Fp4QuantParams p)
                 }
                 const uint2 v = make_uint2(quantize8<NV>(f, s), quantize8<NV>(f + 8, s));
                 const int64_t r = row0 + k;
-                if (r < row_end) {
+                if (whole) {
+                    *reinterpret_cast<uint2 *>(q + my_row * p.ldq + i * 32 * p.ldq + col / 2) = v;
+                } else if (r < row_end) {
                     uint8_t *dst = q + r * p.ldq + col / 2;
                     if (col + 16 <= p.cols) {
                         *reinterpret_cast<uint2 *>(dst) = v;
@@ -468,14 +476,12 @@ fp4_factor_kernel(const T *x0, int64_t ldx, int64_t rows, int64_t cols, int32_t 
 
 struct Fp4DequantParams {
     const uint8_t *q;
-    int64_t ldq;
     const uint8_t *scales;
     const float *factor;
-    int64_t rows, cols, matrices;
+    uint32_t rows, cols, ldq, ldo;
     FastDiv fd_chunks;         // runs of 16 elements in a row
     int32_t vec_ok;            // rows of out start at multiples of 16 bytes
     void *out;
-    int64_t ldo;
     // scan_groups:
     const int32_t *offsets;
     int32_t groups, ragged, rows_ragged, k_capacity;
@@ -484,16 +490,16 @@ struct Fp4DequantParams {
 // 16 elements of each lane (f; row r, columns col ..; active: it has any) to rows that start anywhere: through shared memory (512 elements of a warp), so that lanes store next to
 // each other, four bytes each where the warp's elements lie in one row.
 template <class T>
-__device__ __forceinline__ void store_anywhere(T *buffer, const float (&f)[16], bool active, T *out, int64_t ldo, int64_t r, int64_t col, int64_t cols)
+__device__ __forceinline__ void store_anywhere(T *buffer, const float (&f)[16], bool active, T *out, uint32_t ldo, uint32_t r, uint32_t col, uint32_t cols)
 {
     const uint32_t lane = lane_id();
 #pragma unroll
     for (int j = 0; j < 16; ++j) buffer[lane * 16 + j] = narrow_to<T>(f[j]);
     __syncwarp();
-    const int64_t row0 = __shfl_sync(0xffffffffu, r, 0), col0 = __shfl_sync(0xffffffffu, col, 0);
+    const uint32_t row0 = __shfl_sync(0xffffffffu, r, 0), col0 = __shfl_sync(0xffffffffu, col, 0);
     if (sizeof(T) == 2 && __all_sync(0xffffffffu, active && r == row0)) {
-        T *to = out + row0 * ldo + col0;
-        const int32_t n = static_cast<int32_t>(min(static_cast<int64_t>(512), cols - col0)), odd = static_cast<int32_t>(reinterpret_cast<uintptr_t>(to) >> 1) & 1;
+        T *to = out + static_cast<uint64_t>(row0) * ldo + col0;
+        const int32_t n = static_cast<int32_t>(min(512u, cols - col0)), odd = static_cast<int32_t>(reinterpret_cast<uintptr_t>(to) >> 1) & 1;
         if (odd && lane == 0) to[0] = buffer[0];
         const unsigned short *from = reinterpret_cast<const unsigned short *>(buffer);
 #pragma unroll
@@ -506,9 +512,9 @@ __device__ __forceinline__ void store_anywhere(T *buffer, const float (&f)[16], 
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int src = 2 * i + static_cast<int>(lane >> 4), j = static_cast<int>(lane & 15u);
-            const int64_t sr = __shfl_sync(0xffffffffu, r, src), sc = __shfl_sync(0xffffffffu, col, src) + j;
+            const uint32_t sr = __shfl_sync(0xffffffffu, r, src), sc = __shfl_sync(0xffffffffu, col, src) + j;
             const bool there = __shfl_sync(0xffffffffu, static_cast<int>(active), src) != 0;
-            if (there && sc < cols) out[sr * ldo + sc] = buffer[src * 16 + j];
+            if (there && sc < cols) out[static_cast<uint64_t>(sr) * ldo + sc] = buffer[src * 16 + j];
         }
     }
     __syncwarp();
@@ -527,56 +533,57 @@ fp4_dequantize_kernel(const Fp4DequantParams p)
         if (threadIdx.x < 32) scan_groups(p, pre, off, 128, threadIdx.x);
         __syncthreads();
     }
-    constexpr int kBlock = NV ? 16 : 32, kAtom = 4 * kBlock;
-    const int64_t atoms = (p.cols + kAtom - 1) / kAtom, row_tiles = (p.rows + 127) / 128;
-    const int64_t all = p.rows * p.fd_chunks.d, step = static_cast<int64_t>(gridDim.x) * blockDim.x;     // one matrix: below 2^31, checked by the host
-    const int64_t matrix = blockIdx.y;
+    constexpr uint32_t kAtom = NV ? 64 : 128;
+    const uint32_t atoms = (p.cols + kAtom - 1) / kAtom, row_tiles = (p.rows + 127) / 128;
+    const uint32_t all = p.rows * p.fd_chunks.d, step = gridDim.x * blockDim.x;          // of one matrix: below 2^31, checked by the host
+    const uint64_t matrix = blockIdx.y;
     const uint8_t *q = p.q + matrix * p.rows * p.ldq, *scales = p.scales + matrix * row_tiles * atoms * 512;
     T *out = static_cast<T *>(p.out) + matrix * p.rows * p.ldo;
     const float factor = NV ? p.factor[matrix] : 1.0f;
     const uint32_t lane = threadIdx.x & 31u;
     __shared__ T s_store[8][512];
-    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * blockDim.x + (threadIdx.x & ~31u); i0 < all; i0 += step) {        // whole warps
-        const int64_t i = i0 + lane;
-        bool active = i < all;
-        const int64_t r = active ? fast_div(static_cast<int32_t>(i), p.fd_chunks) : 0, col = active ? (i - r * p.fd_chunks.d) * 16 : 0;
-        int64_t place = r;
+    for (uint32_t i0 = blockIdx.x * blockDim.x + (threadIdx.x & ~31u); i0 < all; i0 += step) {        // whole warps
+        const uint32_t i = min(i0 + lane, all - 1), r = static_cast<uint32_t>(fast_div(static_cast<int32_t>(i), p.fd_chunks)), run = i - r * p.fd_chunks.d, col = run * 16;
+        bool active = i0 + lane < all;
+        uint32_t place = r;
         if (p.groups > 0) {
-            if (r < off[0] || r >= off[p.groups]) active = false;  // a row of no group
+            if (static_cast<int32_t>(r) < off[0] || static_cast<int32_t>(r) >= off[p.groups]) active = false;      // a row of no group
             int32_t lo = 0, hi = p.groups;                         // the last group that starts at or before r
             while (hi - lo > 1) {
                 const int32_t mid = (lo + hi) / 2;
-                if (off[mid] <= r) lo = mid;
+                if (off[mid] <= static_cast<int32_t>(r)) lo = mid;
                 else hi = mid;
             }
-            place = 128ll * pre[lo] + r - off[lo];
+            place = static_cast<uint32_t>(128 * pre[lo] + static_cast<int32_t>(r) - off[lo]);
         }
         float f[16];
         if (active) {
-            const uint8_t *src = q + r * p.ldq + col / 2;
+            const uint8_t *src = q + static_cast<uint64_t>(r) * p.ldq + run * 8;
             uint2 v;
             if (col + 16 <= p.cols) {
-                v = *reinterpret_cast<const uint2 *>(src);         // rows start at multiples of 16 bytes, col / 2 is a multiple of 8
+                v = *reinterpret_cast<const uint2 *>(src);         // rows start at multiples of 16 bytes
             } else {
                 v = make_uint2(0u, 0u);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (uint32_t j = 0; j < 8; ++j)
                     if (col + 2 * j < p.cols) (j < 4 ? v.x : v.y) |= static_cast<uint32_t>(src[j]) << (8 * (j & 3));
             }
-            const int64_t b = col / kBlock;
-            const uint32_t byte = scales[((place >> 7) * atoms + (b >> 2)) * 512 + (place & 31) * 16 + ((place >> 5) & 3) * 4 + (b & 3)];
+            const uint32_t b = NV ? run : run >> 1;               // the block
+            const uint32_t byte = scales[static_cast<uint64_t>((place >> 7) * atoms + (b >> 2)) * 512 + (place & 31u) * 16 + ((place >> 5) & 3u) * 4 + (b & 3u)];
             float s;
             if constexpr (NV) s = __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(byte), __NV_E4M3))) * factor;
             else s = byte == 0u ? 5.877471754111438e-39f : byte == 255u ? __int_as_float(0x7fffffff) : __uint_as_float(byte << 23);
+            uint32_t h[8];
+            unpack_e2m1(v.x, reinterpret_cast<uint32_t(&)[4]>(h[0]));
+            unpack_e2m1(v.y, reinterpret_cast<uint32_t(&)[4]>(h[4]));
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(((j < 4 ? v.x : v.y) >> (8 * (j & 3))) & 0xffu), __NV_E2M1);
-                const float2 e = __half22float2(__half2(h));
-                f[2 * j] = e.x * s;
-                f[2 * j + 1] = e.y * s;
+                float lo, hi;
+                two_floats(h[j], lo, hi, __half());
+                unpack_f32x2(mul_f32x2(pack_f32x2(__float_as_uint(lo), __float_as_uint(hi)), pack_f32x2(__float_as_uint(s), __float_as_uint(s))), f[2 * j], f[2 * j + 1]);
             }
         }
-        T *dst = out + r * p.ldo + col;
+        T *dst = out + static_cast<uint64_t>(r) * p.ldo + col;
         if (!p.vec_ok) {
             store_anywhere<T>(s_store[threadIdx.x >> 5], f, active, out, p.ldo, r, col, p.cols);
         } else if (active && col + 16 <= p.cols) {
@@ -592,7 +599,7 @@ fp4_dequantize_kernel(const Fp4DequantParams p)
             }
         } else if (active) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
+            for (uint32_t j = 0; j < 16; ++j)
                 if (col + j < p.cols) dst[j] = narrow_to<T>(f[j]);
         }
     }
