@@ -117,7 +117,7 @@ typedef struct {
 
 hgemm_status_t hgemm_fp4_plan_get_config(const hgemm_fp4_plan_t *plan, hgemm_fp4_config_t *out);
 hgemm_status_t hgemm_fp4_plan_set_config(hgemm_fp4_plan_t *plan, const hgemm_fp4_config_t *cfg);
-/* What the planner would choose (host only). */
+/* What the planner would choose for 16-bit results (host only). */
 hgemm_status_t hgemm_fp4_planned_config(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups, int32_t num_sms, hgemm_fp4_config_t *out);
 
 #ifdef __cplusplus

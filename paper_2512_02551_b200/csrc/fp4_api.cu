@@ -61,9 +61,11 @@ int64_t tiles_of(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups, 
     return (std::min<int64_t>(groups, M) + M / bt) * ceil_div(outs, bo);
 }
 
-// Estimated time of a configuration in microseconds: a start-up, then rounds of tiles over the SMs, each stage (256 of the contraction) and each tile's
-// end at their measured cost (B200, operands in L2).
-double estimate_us(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups, int32_t num_sms, const hgemm_fp4_config_t &c)
+// Estimated time of a configuration in microseconds: a start (launch, first loads, last stores), the first round's stages (256 of the contraction), then rounds of
+// tiles over the SMs, whose stages share L2 with the other SMs' and whose ends cost what the epilogue does not hide.  Measured (B200, bf16 results, operands in
+// L2): 256 x 4096 x 4096: pairs of 256 columns 9.6 us, of 128 columns 7.1, single CTAs of 64 rows 8.5, of 128 rows 10.7; 4096^3: 28.0, 29.6, 53.8, 44.1;
+// 16 x 4096 x 4096: 64 rows by one, two, four CTAs a tile 7.1, 6.5, 6.7; 16 x 1024 x 4096: by four, eight 5.3, 5.1.
+double estimate_us(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups, int32_t num_sms, int32_t out_bytes, const hgemm_fp4_config_t &c)
 {
     const bool wgrad = form == HGEMM_FP8_WEIGHT_GRAD, pair = c.cta_group == 2;
     const int64_t outs = form == HGEMM_FP8_FORWARD ? N : K;
@@ -79,20 +81,25 @@ double estimate_us(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups
         tiles = of_rows * double(ceil_div(outs, bo));
         stages = double(ceil_div(form == HGEMM_FP8_FORWARD ? K : N, 256));
     }
-    const double stage_us = pair ? (c.block_q == 256 ? 0.36 : 0.25) : c.block_q == 64 ? 0.16 : 0.25;
+    struct Cost {
+        double start, first, stage, end;
+    };
+    const Cost t = pair ? (c.block_q == 256 ? Cost{5.2, 0.27, 0.37, 0.5} : Cost{4.6, 0.15, 0.21, 0.45}) : c.block_q == 64 ? Cost{4.9, 0.17, 0.17, 1.7} : Cost{7.0, 0.20, 0.20, 3.2};
+    const double widen = out_bytes == 4 ? 1.6 : 1.0;                           // fp32 results: twice the bytes at a tile's end
     const int units = std::max(1, num_sms / (pair ? 2 : c.split_k));
-    const double rounds = std::ceil(tiles / units);
-    const double shared_us = c.split_k == 1 ? 0.0 : c.split_k == 2 ? 1.0 : c.split_k == 4 ? 1.2 : 1.7;
-    const double tile_us = (pair ? 0.3 : 0.3) + (c.split_k > 1 ? 3.0 : 0.0);   // CTAs that share a tile do not go on to another: each round starts anew
-    return 4.0 + rounds * (std::ceil(stages / c.split_k) * stage_us) + std::max(0.0, rounds - 1.0) * tile_us + (pair ? 1.6 : 0.8) + shared_us;
+    const double rounds = std::ceil(tiles / units), own = std::ceil(stages / c.split_k);
+    const double shared = c.split_k == 1 ? 0.0 : c.split_k == 2 ? 0.5 : c.split_k == 4 ? 0.6 : 0.8;
+    const double thin = pair && groups == 0 && !wgrad && M <= 32 ? 1.0 : 0.0;       // (1 x 8192 x 2048: pairs 7.8 us, 64 rows 6.1; with 128 rows 6.0 and 7.1)
+    const double again = t.end * widen + (c.split_k > 1 ? 3.0 : 0.0);          // CTAs that share a tile do not go on to another: each round starts anew
+    return t.start + thin + own * t.first + shared + (rounds - 1.0) * (own * t.stage + again);
 }
 
-hgemm_fp4_config_t choose(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups, int32_t num_sms)
+hgemm_fp4_config_t choose(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups, int32_t num_sms, int32_t out_bytes)
 {
     hgemm_fp4_config_t best{2, 256, 1, 0};
-    double least = estimate_us(form, M, N, K, groups, num_sms, best);
+    double least = estimate_us(form, M, N, K, groups, num_sms, out_bytes, best);
     auto consider = [&](const hgemm_fp4_config_t &c) {
-        const double t = estimate_us(form, M, N, K, groups, num_sms, c);
+        const double t = estimate_us(form, M, N, K, groups, num_sms, out_bytes, c);
         if (t < least) {
             least = t;
             best = c;
@@ -475,7 +482,7 @@ hgemm_status_t hgemm_fp4_planned_config(int32_t form, int64_t M, int64_t N, int6
 {
     if (!out || num_sms < 1) return HGEMM_ERR_INVALID_ARG;
     if (!legal_shape(form, M, N, K, groups)) return HGEMM_ERR_INVALID_ARG;
-    *out = choose(form, M, N, K, groups, num_sms);
+    *out = choose(form, M, N, K, groups, num_sms, 2);
     return HGEMM_OK;
 }
 
@@ -499,7 +506,7 @@ hgemm_status_t hgemm_fp4_plan(hgemm_ctx_t *ctx, int32_t form, int64_t M, int64_t
     pl->groups = groups;
     pl->format = format;
     pl->out_type = out_type;
-    pl->cfg = choose(form, M, N, K, groups, ctx->num_sms);
+    pl->cfg = choose(form, M, N, K, groups, ctx->num_sms, type_bytes(out_type));
     try {
         ctx->fp4_plans.push_back(pl);
     } catch (const std::bad_alloc &) {
