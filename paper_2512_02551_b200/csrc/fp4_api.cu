@@ -451,31 +451,32 @@ hgemm_status_t hgemm_fp4_dequantize(hgemm_ctx_t *ctx, int32_t format, int32_t ou
     if (rows == 0) return HGEMM_OK;
     const int es = type_bytes(out_type);
     if (!q || !scales || !out || !aligned16(q) || !aligned16(scales) || (reinterpret_cast<uintptr_t>(out) % unsigned(es)) != 0) return HGEMM_ERR_INVALID_ARG;
-    const int64_t chunks = ceil_div(cols, 16);
-    if (rows * chunks >= (int64_t(1) << 31) - 65536 * 256 || ldq > 0x7fffffff || ldo > 0x7fffffff) return HGEMM_ERR_UNSUPPORTED;      // (run numbers are 32 bits wide, a round of all threads beyond the last too)
+    const int64_t col_tiles = ceil_div(cols, 128), row_tiles = ceil_div(offsets ? hgemm_fp8_padded_rows(rows, groups) : rows, 128);
+    // As in the quantiser: one tile a CTA, several of one row tile where it walks the offsets first.
+    const int64_t walkers = offsets ? std::min(col_tiles, std::max<int64_t>(1, int64_t(ctx->num_sms) * 8 / row_tiles)) : col_tiles;
+    if (row_tiles * walkers > 0x7fffffff) return HGEMM_ERR_UNSUPPORTED;       // (a grid's limit)
     hgemm_dev::Fp4DequantParams p;
     std::memset(&p, 0, sizeof(p));
     p.q = static_cast<const uint8_t *>(q);
-    p.ldq = uint32_t(ldq);
+    p.ldq = ldq;
     p.scales = static_cast<const uint8_t *>(scales);
     p.factor = factor;
-    p.rows = uint32_t(rows);
-    p.cols = uint32_t(cols);
-    p.fd_chunks = hgemm_dev::make_fast_div(uint32_t(chunks));
+    p.rows = rows;
+    p.cols = cols;
+    p.row_tiles = row_tiles;
+    p.walkers = int32_t(walkers);
     p.vec_ok = aligned16(out) && (ldo * es) % 16 == 0 ? 1 : 0;
     p.out = out;
-    p.ldo = uint32_t(ldo);
+    p.ldo = ldo;
     p.offsets = offsets;
     p.groups = groups;
-    p.rows_ragged = int32_t(std::min(rows, kMaxDim));
     using namespace hgemm_dev;
     const bool nv = format == HGEMM_FP4_NV;
     const void *fn = out_type == HGEMM_TYPE_F32   ? (nv ? reinterpret_cast<const void *>(fp4_dequantize_kernel<float, true>) : reinterpret_cast<const void *>(fp4_dequantize_kernel<float, false>))
                      : out_type == HGEMM_TYPE_F16 ? (nv ? reinterpret_cast<const void *>(fp4_dequantize_kernel<__half, true>) : reinterpret_cast<const void *>(fp4_dequantize_kernel<__half, false>))
                                                   : (nv ? reinterpret_cast<const void *>(fp4_dequantize_kernel<__nv_bfloat16, true>) : reinterpret_cast<const void *>(fp4_dequantize_kernel<__nv_bfloat16, false>));
-    const int64_t ctas = std::min<int64_t>(ceil_div(rows * chunks, 256), std::max<int64_t>(1, int64_t(ctx->num_sms) * 32 / matrices));
     void *args[1] = {&p};
-    return launch(ctx, fn, dim3(unsigned(ctas), unsigned(matrices), 1), 256, groups > 0 ? 8 * (groups + 1) : 0, 1, args, stream);
+    return launch(ctx, fn, dim3(unsigned(row_tiles * walkers), unsigned(matrices), 1), kFp4DequantThreads, 0, 1, args, stream);
 }
 
 hgemm_status_t hgemm_fp4_planned_config(int32_t form, int64_t M, int64_t N, int64_t K, int32_t groups, int32_t num_sms, hgemm_fp4_config_t *out)

@@ -478,129 +478,165 @@ struct Fp4DequantParams {
     const uint8_t *q;
     const uint8_t *scales;
     const float *factor;
-    uint32_t rows, cols, ldq, ldo;
-    FastDiv fd_chunks;         // runs of 16 elements in a row
+    int64_t rows, cols, ldq, ldo;
+    int64_t row_tiles;         // of 128 rows (per group: as many as the padded copy has)
+    int32_t walkers;           // CTAs that share a row tile's column tiles
     int32_t vec_ok;            // rows of out start at multiples of 16 bytes
     void *out;
-    // scan_groups:
     const int32_t *offsets;
-    int32_t groups, ragged, rows_ragged, k_capacity;
+    int32_t groups;
 };
 
-// 16 elements of each lane (f; row r, columns col ..; active: it has any) to rows that start anywhere: through shared memory (512 elements of a warp), so that lanes store next to
-// each other, four bytes each where the warp's elements lie in one row.
-template <class T>
-__device__ __forceinline__ void store_anywhere(T *buffer, const float (&f)[16], bool active, T *out, uint32_t ldo, uint32_t r, uint32_t col, uint32_t cols)
+constexpr int kFp4DequantThreads = 256;
+
+// A row of a tile, whose pieces 8 lanes hold (v; the lanes of four rows a warp), to a place `to` that starts anywhere: each lane stores the 16 bytes from the next multiple
+// of 16 bytes on, its own piece's end and the next piece's start; what the first piece has before that and the last behind it, a piece together, leave by the
+// element.  n: elements of the row (0: none); edge: room for a piece.  Whole warps.
+template <class T, int PIECES>
+__device__ __forceinline__ void store_anywhere(const uint32_t (&v)[PIECES][4], T *to, int32_t n, T *edge)
 {
-    const uint32_t lane = lane_id();
+    constexpr int32_t kPiece = 16 / static_cast<int32_t>(sizeof(T));
+    const int32_t sub = static_cast<int32_t>(lane_id() & 7u), s = static_cast<int32_t>((0u - static_cast<uint32_t>(reinterpret_cast<uintptr_t>(to))) & 15u) / static_cast<int32_t>(sizeof(T));      // elements up to the first such place
+    const int32_t words = s * static_cast<int32_t>(sizeof(T)) / 4;
+    const uint32_t pick = sizeof(T) == 2 && (s & 1) ? 0x5432u : 0x3210u;
+    const int src = static_cast<int>((lane_id() & 24u) | ((lane_id() + 1u) & 7u));
+    uint32_t after[PIECES][4];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) buffer[lane * 16 + j] = narrow_to<T>(f[j]);
-    __syncwarp();
-    const uint32_t row0 = __shfl_sync(0xffffffffu, r, 0), col0 = __shfl_sync(0xffffffffu, col, 0);
-    if (sizeof(T) == 2 && __all_sync(0xffffffffu, active && r == row0)) {
-        T *to = out + static_cast<uint64_t>(row0) * ldo + col0;
-        const int32_t n = static_cast<int32_t>(min(512u, cols - col0)), odd = static_cast<int32_t>(reinterpret_cast<uintptr_t>(to) >> 1) & 1;
-        if (odd && lane == 0) to[0] = buffer[0];
-        const unsigned short *from = reinterpret_cast<const unsigned short *>(buffer);
+    for (int u = 0; u < PIECES; ++u)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int32_t e = odd + 2 * (i * 32 + static_cast<int32_t>(lane));
-            if (e + 1 < n) *reinterpret_cast<uint32_t *>(to + e) = from[e] | (static_cast<uint32_t>(from[e + 1]) << 16);
-            else if (e < n) to[e] = buffer[e];
+        for (int k = 0; k < 4; ++k) after[u][k] = __shfl_sync(0xffffffffu, v[u][k], src);
+    __syncwarp();                                                 // (the edges of the call before)
+#pragma unroll
+    for (int u = 0; u < PIECES; ++u) {
+        uint32_t x[8], y[5], z[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            x[k] = v[u][k];
+            x[4 + k] = sub == 7 ? after[(u + 1) % PIECES][k] : after[u][k];      // (the last piece's next is the first)
         }
-    } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int src = 2 * i + static_cast<int>(lane >> 4), j = static_cast<int>(lane & 15u);
-            const uint32_t sr = __shfl_sync(0xffffffffu, r, src), sc = __shfl_sync(0xffffffffu, col, src) + j;
-            const bool there = __shfl_sync(0xffffffffu, static_cast<int>(active), src) != 0;
-            if (there && sc < cols) out[static_cast<uint64_t>(sr) * ldo + sc] = buffer[src * 16 + j];
+        for (int k = 0; k < 6; ++k) x[k] = words & 2 ? x[k + 2] : x[k];
+#pragma unroll
+        for (int k = 0; k < 5; ++k) y[k] = words & 1 ? x[k + 1] : x[k];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z[k] = __byte_perm(y[k], y[k + 1], pick);
+        const uint4 out = make_uint4(z[0], z[1], z[2], z[3]);
+        const int32_t e = (u * 8 + sub) * kPiece + s;
+        if (u == PIECES - 1 && sub == 7) {
+            *reinterpret_cast<uint4 *>(edge) = out;
+        } else if (e + kPiece <= n) {
+            *reinterpret_cast<uint4 *>(to + e) = out;
+        } else if (e < n) {
+#pragma unroll
+            for (int j = 0; j < kPiece; ++j) {
+                if (e + j >= n) continue;
+                if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t *>(to)[e + j] = z[j];
+                else reinterpret_cast<unsigned short *>(to)[e + j] = static_cast<unsigned short>(z[j / 2] >> (16 * (j & 1)));
+            }
         }
     }
     __syncwarp();
+    const int32_t at = sub < kPiece - s ? 128 - kPiece + s + sub : sub - (kPiece - s);
+    if (sub < kPiece && at < n) to[at] = edge[sub];
 }
 
-// A thread per 16 elements: 8 bytes of values, one scale.  Dynamic shared memory: 2 (groups + 1) words.
+// A tile of 128 x 128 elements, as the quantiser's: 8 lanes hold a row's 16-byte pieces of the result, so that their stores fill whole sectors, and a
+// thread's four rows (32 apart) have their scales in the same 16 bytes of a scale tile.  (One run of 16 elements per thread, its scale fetched by the byte
+// and its result stored in two halves or through shared memory: 8191 x 4096 bf16 21 us along rows, 28 along columns.)
 template <class T, bool NV>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kFp4DequantThreads)
 fp4_dequantize_kernel(const Fp4DequantParams p)
 {
-    extern __shared__ int32_t s_groups[];
-    int32_t *pre = s_groups, *off = pre + p.groups + 1;
+    constexpr int kAtom = NV ? 64 : 128, kAtoms = 128 / kAtom;
+    constexpr int kPiece = 16 / static_cast<int>(sizeof(T)), kPieces = 16 / kPiece;      // elements of a lane's piece; its pieces of a row
+    __shared__ int32_t s_place[3];
+    __shared__ __align__(16) T s_edge[kFp4DequantThreads / 8][kPiece];
     grid_launch_dependents();
     grid_dependency_wait();
-    if (p.groups > 0) {
-        if (threadIdx.x < 32) scan_groups(p, pre, off, 128, threadIdx.x);
+    const int64_t rb = static_cast<int64_t>(blockIdx.x) / p.walkers;
+    int64_t row0 = rb * 128, row_end = p.rows;
+    if (p.offsets != nullptr) {
+        if (threadIdx.x < 32) {
+            int32_t first = 0, end = 0;
+            const bool found = block_of_group(p.offsets, p.groups, static_cast<int32_t>(p.rows), static_cast<int32_t>(rb), threadIdx.x, first, end);
+            if (threadIdx.x == 0) { s_place[0] = found; s_place[1] = first; s_place[2] = end; }
+        }
         __syncthreads();
+        if (!s_place[0]) return;                                  // beyond the last group (block-uniform)
+        row0 = s_place[1];
+        row_end = s_place[2];
     }
-    constexpr uint32_t kAtom = NV ? 64 : 128;
-    const uint32_t atoms = (p.cols + kAtom - 1) / kAtom, row_tiles = (p.rows + 127) / 128;
-    const uint32_t all = p.rows * p.fd_chunks.d, step = gridDim.x * blockDim.x;          // of one matrix: below 2^31, checked by the host
-    const uint64_t matrix = blockIdx.y;
-    const uint8_t *q = p.q + matrix * p.rows * p.ldq, *scales = p.scales + matrix * row_tiles * atoms * 512;
+    const int64_t matrix = blockIdx.y, atoms = (p.cols + kAtom - 1) / kAtom, col_tiles = (p.cols + 127) / 128;
+    const uint8_t *q = p.q + matrix * p.rows * p.ldq, *scales = p.scales + (matrix * p.row_tiles + rb) * atoms * 512;
     T *out = static_cast<T *>(p.out) + matrix * p.rows * p.ldo;
     const float factor = NV ? p.factor[matrix] : 1.0f;
-    const uint32_t lane = threadIdx.x & 31u;
-    __shared__ T s_store[8][512];
-    for (uint32_t i0 = blockIdx.x * blockDim.x + (threadIdx.x & ~31u); i0 < all; i0 += step) {        // whole warps
-        const uint32_t i = min(i0 + lane, all - 1), r = static_cast<uint32_t>(fast_div(static_cast<int32_t>(i), p.fd_chunks)), run = i - r * p.fd_chunks.d, col = run * 16;
-        bool active = i0 + lane < all;
-        uint32_t place = r;
-        if (p.groups > 0) {
-            if (static_cast<int32_t>(r) < off[0] || static_cast<int32_t>(r) >= off[p.groups]) active = false;      // a row of no group
-            int32_t lo = 0, hi = p.groups;                         // the last group that starts at or before r
-            while (hi - lo > 1) {
-                const int32_t mid = (lo + hi) / 2;
-                if (off[mid] <= static_cast<int32_t>(r)) lo = mid;
-                else hi = mid;
-            }
-            place = static_cast<uint32_t>(128 * pre[lo] + static_cast<int32_t>(r) - off[lo]);
+    const uint32_t sub = threadIdx.x & 7u, line = threadIdx.x >> 3;
+    const int64_t my_row = row0 + line;
+    const int32_t rows = static_cast<int32_t>(min(row_end - row0, static_cast<int64_t>(128)));       // of this tile
+    for (int64_t ct = static_cast<int64_t>(blockIdx.x) % p.walkers; ct < col_tiles; ct += p.walkers) {
+        const int64_t col0 = ct * 128;
+        const int32_t cols = static_cast<int32_t>(min(p.cols - col0, static_cast<int64_t>(128)));
+        const bool whole = rows == 128 && cols == 128;            // its loads and stores need no test of their own
+        uint32_t sc[kAtoms][4];
+#pragma unroll
+        for (int a = 0; a < kAtoms; ++a) {
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (a == 0 || ct * kAtoms + a < atoms) v = *reinterpret_cast<const uint4 *>(scales + (ct * kAtoms + a) * 512 + line * 16);
+            sc[a][0] = v.x, sc[a][1] = v.y, sc[a][2] = v.z, sc[a][3] = v.w;
         }
-        float f[16];
-        if (active) {
-            const uint8_t *src = q + static_cast<uint64_t>(r) * p.ldq + run * 8;
-            uint2 v;
-            if (col + 16 <= p.cols) {
-                v = *reinterpret_cast<const uint2 *>(src);         // rows start at multiples of 16 bytes
-            } else {
-                v = make_uint2(0u, 0u);
+        uint32_t w[4][2];                                         // 8 elements each: a piece, or two
 #pragma unroll
-                for (uint32_t j = 0; j < 8; ++j)
-                    if (col + 2 * j < p.cols) (j < 4 ? v.x : v.y) |= static_cast<uint32_t>(src[j]) << (8 * (j & 3));
-            }
-            const uint32_t b = NV ? run : run >> 1;               // the block
-            const uint32_t byte = scales[static_cast<uint64_t>((place >> 7) * atoms + (b >> 2)) * 512 + (place & 31u) * 16 + ((place >> 5) & 3u) * 4 + (b & 3u)];
-            float s;
-            if constexpr (NV) s = __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(byte), __NV_E4M3))) * factor;
-            else s = byte == 0u ? 5.877471754111438e-39f : byte == 255u ? __int_as_float(0x7fffffff) : __uint_as_float(byte << 23);
-            uint32_t h[8];
-            unpack_e2m1(v.x, reinterpret_cast<uint32_t(&)[4]>(h[0]));
-            unpack_e2m1(v.y, reinterpret_cast<uint32_t(&)[4]>(h[4]));
+        for (int i = 0; i < 4; ++i) {
+            const uint8_t *src = q + my_row * p.ldq + col0 / 2 + i * 32 * p.ldq;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float lo, hi;
-                two_floats(h[j], lo, hi, __half());
-                unpack_f32x2(mul_f32x2(pack_f32x2(__float_as_uint(lo), __float_as_uint(hi)), pack_f32x2(__float_as_uint(s), __float_as_uint(s))), f[2 * j], f[2 * j + 1]);
+            for (int u = 0; u < kPieces; ++u) {
+                const uint32_t at = u * 4 * kPiece + sub * (kPiece / 2);                  // bytes of the tile's row
+                uint32_t v = 0u;
+                if (whole || (static_cast<int32_t>(line) + 32 * i < rows && static_cast<int32_t>(2 * at) + kPiece <= cols)) {
+                    if constexpr (kPiece == 8) v = *reinterpret_cast<const uint32_t *>(src + at);
+                    else v = *reinterpret_cast<const unsigned short *>(src + at);
+                } else if (static_cast<int32_t>(line) + 32 * i < rows) {
+#pragma unroll
+                    for (int j = 0; j < kPiece / 2; ++j)
+                        if (static_cast<int32_t>(2 * (at + j)) < cols) v |= static_cast<uint32_t>(src[at + j]) << (8 * j);
+                }
+                if (kPiece == 8 || u % 2 == 0) w[i][u * kPiece / 8] = v;
+                else w[i][u / 2] |= v << 16;
             }
         }
-        T *dst = out + static_cast<uint64_t>(r) * p.ldo + col;
-        if (!p.vec_ok) {
-            store_anywhere<T>(s_store[threadIdx.x >> 5], f, active, out, p.ldo, r, col, p.cols);
-        } else if (active && col + 16 <= p.cols) {
-            if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) reinterpret_cast<float4 *>(dst)[j] = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
-            } else {
-                uint32_t h[8];
+        for (int i = 0; i < 4; ++i) {
+            if (32 * i >= rows) break;
+            T *dst = out + my_row * p.ldo + col0 + i * 32 * p.ldo;
+            uint32_t h[4], v[kPieces][4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) h[j] = pack_pair(f[2 * j], f[2 * j + 1], T());
-                reinterpret_cast<uint4 *>(dst)[0] = make_uint4(h[0], h[1], h[2], h[3]);
-                reinterpret_cast<uint4 *>(dst)[1] = make_uint4(h[4], h[5], h[6], h[7]);
+            for (int u = 0; u < kPieces; ++u) {
+                if (kPiece == 8 || u % 2 == 0) unpack_e2m1(w[i][u * kPiece / 8], h);
+                const uint32_t e0 = u * 8 * kPiece + sub * kPiece, b = NV ? (e0 & 63u) >> 4 : e0 >> 5;
+                const uint32_t byte = (sc[NV ? u * 8 * kPiece / 64 : 0][i] >> (8u * b)) & 0xffu;
+                float s;
+                if constexpr (NV) s = __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(byte), __NV_E4M3))) * factor;
+                else s = byte == 0u ? 5.877471754111438e-39f : byte == 255u ? __int_as_float(0x7fffffff) : __uint_as_float(byte << 23);
+                float f[kPiece];
+#pragma unroll
+                for (int j = 0; j < kPiece / 2; ++j) {
+                    float lo, hi;
+                    two_floats(h[(u * kPiece / 2 + j) & 3], lo, hi, __half());
+                    unpack_f32x2(mul_f32x2(pack_f32x2(__float_as_uint(lo), __float_as_uint(hi)), pack_f32x2(__float_as_uint(s), __float_as_uint(s))), f[2 * j], f[2 * j + 1]);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if constexpr (sizeof(T) == 4) v[u][k] = __float_as_uint(f[k]);
+                    else v[u][k] = pack_pair(f[2 * k], f[2 * k + 1], T());
+                }
             }
-        } else if (active) {
+            if (p.vec_ok && cols == 128) {
+                if (static_cast<int32_t>(line) + 32 * i >= rows) continue;
 #pragma unroll
-            for (uint32_t j = 0; j < 16; ++j)
-                if (col + j < p.cols) dst[j] = narrow_to<T>(f[j]);
+                for (int u = 0; u < kPieces; ++u) *reinterpret_cast<uint4 *>(dst + (u * 8 + sub) * kPiece) = make_uint4(v[u][0], v[u][1], v[u][2], v[u][3]);
+            } else {
+                store_anywhere<T>(v, dst, static_cast<int32_t>(line) + 32 * i < rows ? cols : 0, s_edge[line]);
+            }
         }
     }
 }

@@ -714,6 +714,7 @@ __device__ __forceinline__ uint32_t pack_e2m1(float a, float b, float c, float d
 }
 
 // The values of eight e2m1 codes as pairs of fp16.
+// (Give it words all of which hold values: with a 16-bit load for w, its upper half known to be zero, everything came out as zeros.)
 __device__ __forceinline__ void unpack_e2m1(uint32_t w, uint32_t (&d)[4])
 {
     asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"

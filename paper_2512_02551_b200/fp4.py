@@ -103,11 +103,11 @@ def _format(format: str) -> int:
 
 
 def _values_shape(shape):
-    return torch.Size((*shape[:-1], _up(shape[-1], 2)))
+    return (*shape[:-1], -(-shape[-1] // 2))
 
 
 def _scales_shape(shape, format):
-    return torch.Size((*shape[:-2], _up(shape[-2], TILE_ROWS), _up(shape[-1], 4 * BLOCK[format]), TILE_BYTES))
+    return (*shape[:-2], -(-shape[-2] // TILE_ROWS), -(-shape[-1] // (4 * BLOCK[format])), TILE_BYTES)
 
 
 def _col_shape(shape, groups):
@@ -182,7 +182,9 @@ def tensor_factor(ctx, x, factor, stream=None) -> None:
     """factor (1,), or (matrices,) for a stack: the "nvfp4" factor of x (fp32, fp16 or bf16), max |x| / 2688 rounded up to a power of two."""
     n, R, C, ld = _matrix(x)
     f = _dense(factor, (n,), torch.float32, "factor")
-    _check(lib().hgemm_fp4_tensor_factor(ctx._h, TYPES[x.dtype], n, R, C, x.data_ptr(), ld, f, _stream(ctx, stream)), f"hgemm_fp4_tensor_factor({tuple(x.shape)})")
+    st = lib().hgemm_fp4_tensor_factor(ctx._h, TYPES[x.dtype], n, R, C, x.data_ptr(), ld, f, _stream(ctx, stream))
+    if st != OK:
+        raise HgemmError(st, f"hgemm_fp4_tensor_factor({tuple(x.shape)})")
 
 
 def _quantize(ctx, x, row_copy, col_copy, factor, format, rows, offsets, stream):
@@ -203,7 +205,9 @@ def _quantize(ctx, x, row_copy, col_copy, factor, format, rows, offsets, stream)
     qc, ldqc, sc = (None, 0, None) if col_copy is None else _copy(*col_copy, cols, cols, format, "q_cols")
     d = Quantize((ROWS if row_copy is not None else 0) | (COLS if col_copy is not None else 0), TYPES[x.dtype], fmt, n, R, C, ld, x.data_ptr(),
                  None if rows is None else rows.data_ptr(), x.shape[-2], None if offsets is None else offsets.data_ptr(), groups, 0, f, q, ldq, s, qc, ldqc, sc)
-    _check(lib().hgemm_fp4_quantize(ctx._h, ctypes.byref(d), _stream(ctx, stream)), f"hgemm_fp4_quantize(blocks={d.blocks}, {R}x{C})")
+    st = lib().hgemm_fp4_quantize(ctx._h, ctypes.byref(d), _stream(ctx, stream))
+    if st != OK:
+        raise HgemmError(st, f"hgemm_fp4_quantize(blocks={d.blocks}, {R}x{C})")
 
 
 def quantize_rows(ctx, x, q, scales, factor=None, format: str = "nvfp4", rows=None, offsets=None, stream=None) -> None:
@@ -233,8 +237,10 @@ def dequantize(ctx, q, scales, out, factor=None, format: str = "nvfp4", offsets=
     if groups and out.dim() == 3:
         raise ValueError("a stack has no offsets")
     v, ld, s = _copy(q, scales, shape, (padded_rows(shape[0], groups), shape[1]) if groups else shape, format, "q")
-    _check(lib().hgemm_fp4_dequantize(ctx._h, fmt, TYPES[out.dtype], n, shape[-2], shape[-1], v, ld, s, _factor_of(factor, n, format), None if offsets is None else offsets.data_ptr(),
-                                      groups, out.data_ptr(), ldo, _stream(ctx, stream)), f"hgemm_fp4_dequantize({tuple(shape)})")
+    st = lib().hgemm_fp4_dequantize(ctx._h, fmt, TYPES[out.dtype], n, shape[-2], shape[-1], v, ld, s, _factor_of(factor, n, format), None if offsets is None else offsets.data_ptr(),
+                                    groups, out.data_ptr(), ldo, _stream(ctx, stream))
+    if st != OK:
+        raise HgemmError(st, f"hgemm_fp4_dequantize({tuple(shape)})")
 
 
 # ---- products ------------------------------------------------------------------------------------
