@@ -1,7 +1,8 @@
 // A layer of experts with 16-bit weights for a few tokens: W1 and the activation in one launch, W2 and the weighted sum over a token's choices in another.
 // (4-bit weights: few_digits_kernel.cuh.)
 //
-// Bound by the chosen experts' weights, read once from memory for a handful of multiply-adds.  They go from memory to registers (16 bytes a lane, four
+// Bound by the chosen experts' weights, read once from memory for a handful of multiply-adds (5 tokens, 4 of 32 experts, 2048 -> 1000 -> 2048, bf16: 34 us, 3.7 TB/s; a
+// launch's start, its list of choices and its last tiles take some 6 us each).  They go from memory to registers (16 bytes a lane, four
 // chunks of two rows in flight at any time) and from there to mma.sync: a warp's 16 rows of a weight matrix are the operand that fills the instruction's
 // rows, up to 8 choices of the expert are its columns.  A lane takes 16 consecutive bytes of its row, four lanes 64 (a chunk): which k a lane holds is free as
 // long as both operands agree.  (Tensor memory and a ring of shared-memory stages would lengthen the way of rows that start anywhere: tensor copies

@@ -347,8 +347,10 @@ hgemm_status_t fp4_digits_product(hgemm_ctx_s *ctx, int32_t format, int64_t choi
     plan.groups = groups;
     plan.format = format;
     plan.out_type = HGEMM_TYPE_F32;
-    // 8 or 16 rows a tile, by what an expert has on average; CTAs that share a contraction where tiles leave SMs without work
-    plan.cfg = {1, choices > 8 * std::min<int64_t>(groups, choices) ? 128 : 64, 1, 0};
+    // 8 choices a tile (64 columns) while there are few, 16 beyond (2048 -> 1024 -> 2048, SwiGLU, the whole layer: 8 choices of 64 experts 25.4 against 27.5 us;
+    // 32: 38.1 and 37.6; 512: 73.8 and 72.0; 512 of 16 experts, two or three tiles an expert instead of four: 56.2 and 50.2).  CTAs that share a contraction only where
+    // tiles leave SMs without work: each round of them starts anew (8 choices of 64 experts, tiles for every SM, shared by two: 37.5 us).
+    plan.cfg = {1, choices > 16 || choices > 8 * groups ? 128 : 64, 1, 0};
     while (plan.cfg.split_k < 8 && digits_tiles(choices, N, groups, plan.cfg) * plan.cfg.split_k * 2 <= ctx->num_sms && ceil_div(K, 256) >= 2 * plan.cfg.split_k * 2) plan.cfg.split_k *= 2;
     const cudaError_t e = cudaFuncSetAttribute(digits_kernel_of(plan.cfg, format), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemOptIn);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
@@ -373,9 +375,9 @@ hgemm_status_t hgemm_fp4_tensor_factor(hgemm_ctx_t *ctx, int32_t x_type, int64_t
     const int es = type_bytes(x_type);
     if (rows > 0 && (!x || (reinterpret_cast<uintptr_t>(x) % unsigned(es)) != 0)) return HGEMM_ERR_INVALID_ARG;
     int32_t vec = aligned16(x) && (ldx * es) % 16 == 0 ? 1 : 0;
-    // Up to 2^19 elements a matrix: eight CTAs (a cluster) have all of it, and one launch does; beyond that the GPU is wider than a cluster, and the factors,
-    // set to zero first, are raised to the maximum.
-    const bool cluster = rows * cols <= (int64_t(1) << 19);
+    // Up to 2 MB a matrix: eight CTAs (a cluster) have all of it, and one launch does; beyond that the GPU is wider than a cluster, and the factors,
+    // set to zero first, are raised to the maximum (bf16, 4096 columns: 24 rows 2.4 against 5.8 us, 256 rows 4.5 and 5.8, 512 rows 6.8 and 5.9).
+    const bool cluster = rows * cols * es <= (int64_t(1) << 21);
     if (!cluster) {
         const cudaError_t e = cudaMemsetAsync(factor, 0, size_t(matrices) * 4, static_cast<cudaStream_t>(stream));
         if (e != cudaSuccess) return cuda_fail(ctx, e);
@@ -428,7 +430,8 @@ hgemm_status_t hgemm_fp4_quantize(hgemm_ctx_t *ctx, const hgemm_fp4_quantize_t *
     p.col_rows = col_rows;
     p.row_tiles = ceil_div(d->rows, 128);
     const int64_t col_tiles = ceil_div(d->cols, 128), row_tiles = ceil_div(col_rows, 128);      // (per group: as many as the copy has room for)
-    // A CTA walks the offsets before its first tile; where that is worth sharing, it takes several tiles of its 128 rows.
+    // A CTA walks the offsets before its first tile; where that is worth sharing, it takes several tiles of its 128 rows: eight CTAs an SM in all (16384 x 2048 bf16, both copies;
+    // two an SM, eight, one a tile: 32 groups 83, 38, 34 us; 256 groups 102, 72, 90; 1024 groups 251, 251, 497).
     const int64_t per_row = d->offsets ? std::min(col_tiles, std::max<int64_t>(1, int64_t(ctx->num_sms) * 8 / row_tiles)) : col_tiles;
     const void *fn = d->x_type == HGEMM_TYPE_F32 ? quantize_kernel<float>(d->blocks, d->format) : d->x_type == HGEMM_TYPE_F16 ? quantize_kernel<__half>(d->blocks, d->format)
                                                                                                                              : quantize_kernel<__nv_bfloat16>(d->blocks, d->format);
@@ -452,7 +455,7 @@ hgemm_status_t hgemm_fp4_dequantize(hgemm_ctx_t *ctx, int32_t format, int32_t ou
     const int es = type_bytes(out_type);
     if (!q || !scales || !out || !aligned16(q) || !aligned16(scales) || (reinterpret_cast<uintptr_t>(out) % unsigned(es)) != 0) return HGEMM_ERR_INVALID_ARG;
     const int64_t col_tiles = ceil_div(cols, 128), row_tiles = ceil_div(offsets ? hgemm_fp8_padded_rows(rows, groups) : rows, 128);
-    // As in the quantiser: one tile a CTA, several of one row tile where it walks the offsets first.
+    // As in the quantiser: one tile a CTA, several of one row tile where it walks the offsets first (32, 256, 1024 groups: 17, 22, 57 us; one a tile 16, 39, 225).
     const int64_t walkers = offsets ? std::min(col_tiles, std::max<int64_t>(1, int64_t(ctx->num_sms) * 8 / row_tiles)) : col_tiles;
     if (row_tiles * walkers > 0x7fffffff) return HGEMM_ERR_UNSUPPORTED;       // (a grid's limit)
     hgemm_dev::Fp4DequantParams p;
