@@ -86,6 +86,19 @@ __device__ __forceinline__ uint32_t magnitude_max(uint32_t m, uint32_t w)
     if constexpr (sizeof(T) == 4) return max(m, w & 0x7fffffffu);
     else return __vmaxu2(m, w & 0x7fff7fffu);
 }
+// The largest magnitudes of N registers of pairs (an even number).  Numbers without sign find the largest of the negative ones (their sign bits are the highest), numbers with
+// sign that of the others; three at a time.
+template <int N>
+__device__ __forceinline__ uint32_t pair_magnitudes(const uint32_t *w)
+{
+    uint32_t below = 0u, above = 0u;
+#pragma unroll
+    for (int j = 0; j < N; j += 2) {
+        below = __vimax3_u16x2(below, w[j], w[j + 1]);
+        above = __vimax3_s16x2(above, w[j], w[j + 1]);
+    }
+    return __vmaxu2(below & 0x7fff7fffu, above);
+}
 // The larger of a register's two 16-bit magnitudes, as the type's bit pattern.
 __device__ __forceinline__ uint32_t larger16(uint32_t m) { return max(m & 0xffffu, m >> 16); }
 
@@ -188,7 +201,7 @@ __device__ __forceinline__ bool block_of_group(const int32_t *offsets, int32_t g
 
 // MODE: HGEMM_FP4_ROWS (1), COLS (2) or both (3).  grid: x = column tiles (each CTA walks on by gridDim.x), y = row tiles (as many as the padded copy has), z = matrices.
 template <class T, int MODE, bool NV>
-__global__ void __launch_bounds__(kFp4QuantThreads, sizeof(T) == 4 ? 2 : 3)
+__global__ void __launch_bounds__(kFp4QuantThreads, sizeof(T) == 4 ? 2 : NV ? 3 : 4)
 fp4_quantize_kernel(const Fp4QuantParams p)
 {
     constexpr int kBlock = NV ? 16 : 32, kAtom = 4 * kBlock;     // elements of a block; of a scale tile's four
@@ -269,9 +282,12 @@ fp4_quantize_kernel(const Fp4QuantParams p)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t m = 0u;
+                if constexpr (sizeof(T) == 2) {
+                    m = larger16(pair_magnitudes<8>(raw[i].w));
+                } else {
 #pragma unroll
-                for (int j = 0; j < static_cast<int>(4 * sizeof(T)); ++j) m = magnitude_max<T>(m, raw[i].w[j]);
-                if constexpr (sizeof(T) == 2) m = larger16(m);
+                    for (int j = 0; j < 16; ++j) m = magnitude_max<T>(m, raw[i].w[j]);
+                }
                 if constexpr (!NV) m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
                 const BlockStep s = block_step<NV>(magnitude_of(m, T()), factor, g);
                 // the scales of four blocks make a word
@@ -307,34 +323,38 @@ fp4_quantize_kernel(const Fp4QuantParams p)
         }
         if constexpr (MODE != 1) {
             __syncthreads();
-            // 32 rows (part of the tile's four) of a column, or of two: blocks, values, scales
-            auto column = [&](const float (&f)[32], const uint32_t (&m)[2], uint32_t c, uint32_t part) {
-                uint4 v;
-                if constexpr (NV) {
-                    const BlockStep s0 = block_step<NV>(magnitude_of(m[0], T()), factor, g), s1 = block_step<NV>(magnitude_of(m[1], T()), factor, g);
-                    v = make_uint4(quantize8<NV>(f, s0), quantize8<NV>(f + 8, s0), quantize8<NV>(f + 16, s1), quantize8<NV>(f + 24, s1));
-                    *reinterpret_cast<unsigned short *>(s_scale + (part >> 1) * 512u + (c & 31u) * 16u + (c >> 5) * 4u + (part & 1u) * 2u) = static_cast<unsigned short>(s0.byte | (s1.byte << 8));
-                } else {
-                    const BlockStep s = block_step<NV>(magnitude_of(max(m[0], m[1]), T()), factor, g);
-                    v = make_uint4(quantize8<NV>(f, s), quantize8<NV>(f + 8, s), quantize8<NV>(f + 16, s), quantize8<NV>(f + 24, s));
-                    s_scale[(c & 31u) * 16u + (c >> 5) * 4u + part] = static_cast<uint8_t>(s.byte);
-                }
-                *reinterpret_cast<uint4 *>(s_out + c * kOutPitch + part * 16u) = v;
+            // 32 rows (part of the tile's four) of a column, or of two: blocks, values, scales.  A part of a block, 16 rows, at a time
+            auto put = [&](const uint2 (&v)[2], uint32_t c, uint32_t part, uint32_t b0, uint32_t b1) {
+                *reinterpret_cast<uint4 *>(s_out + c * kOutPitch + part * 16u) = make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
+                if constexpr (NV) *reinterpret_cast<unsigned short *>(s_scale + (part >> 1) * 512u + (c & 31u) * 16u + (c >> 5) * 4u + (part & 1u) * 2u) = static_cast<unsigned short>(b0 | (b1 << 8));
+                else s_scale[(c & 31u) * 16u + (c >> 5) * 4u + part] = static_cast<uint8_t>(b0);
             };
             if constexpr (sizeof(T) == 2) {
                 const uint32_t pair = threadIdx.x & 63u, part = threadIdx.x >> 6;
-                uint32_t w[32], m[2] = {0u, 0u};
+                const uint8_t *src = s_raw + part * 32u * kPitch + pair * 4u;
+                uint32_t w[32];
+                uint2 lo[2], hi[2];
+                uint32_t byte_lo[2], byte_hi[2];
+                BlockStep s_lo, s_hi;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    w[j] = *reinterpret_cast<const uint32_t *>(s_raw + (part * 32u + j) * kPitch + pair * 4u);
-                    m[j / 16] = magnitude_max<T>(m[j / 16], w[j]);
+                for (int k = 0; k < 2; ++k) {
+                    if (NV || k == 0) {
+#pragma unroll
+                        for (int j = 0; j < (NV ? 16 : 32); ++j) w[16 * k + j] = *reinterpret_cast<const uint32_t *>(src + (16 * k + j) * kPitch);
+                        const uint32_t m = pair_magnitudes<NV ? 16 : 32>(w + 16 * k);
+                        s_lo = block_step<NV>(magnitude_of(m & 0xffffu, T()), factor, g);
+                        s_hi = block_step<NV>(magnitude_of(m >> 16, T()), factor, g);
+                    }
+                    float f[16], h[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) two_floats(w[16 * k + j], f[j], h[j], T());
+                    lo[k] = make_uint2(quantize8<NV>(f, s_lo), quantize8<NV>(f + 8, s_lo));
+                    hi[k] = make_uint2(quantize8<NV>(h, s_hi), quantize8<NV>(h + 8, s_hi));
+                    byte_lo[k] = s_lo.byte;
+                    byte_hi[k] = s_hi.byte;
                 }
-                float f[32], h[32];
-#pragma unroll
-                for (int j = 0; j < 32; ++j) two_floats(w[j], f[j], h[j], T());
-                const uint32_t lo[2] = {m[0] & 0xffffu, m[1] & 0xffffu}, hi[2] = {m[0] >> 16, m[1] >> 16};
-                column(f, lo, 2u * pair, part);
-                column(h, hi, 2u * pair + 1u, part);
+                put(lo, 2u * pair, part, byte_lo[0], byte_lo[1]);
+                put(hi, 2u * pair + 1u, part, byte_hi[0], byte_hi[1]);
             } else {
 #pragma unroll 1
                 for (uint32_t i = 0; i < 2; ++i) {
@@ -347,7 +367,16 @@ fp4_quantize_kernel(const Fp4QuantParams p)
                         m[j / 16] = magnitude_max<T>(m[j / 16], w);
                         f[j] = __uint_as_float(w);
                     }
-                    column(f, m, c, part);
+                    if constexpr (!NV) m[0] = m[1] = max(m[0], m[1]);
+                    uint2 v[2];
+                    uint32_t byte[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const BlockStep s = block_step<NV>(magnitude_of(m[k], T()), factor, g);
+                        v[k] = make_uint2(quantize8<NV>(f + 16 * k, s), quantize8<NV>(f + 16 * k + 8, s));
+                        byte[k] = s.byte;
+                    }
+                    put(v, c, part, byte[0], byte[1]);
                 }
             }
             __syncthreads();
