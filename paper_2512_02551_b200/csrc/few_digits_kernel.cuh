@@ -28,7 +28,7 @@
 
 namespace hgemm_dev {
 
-constexpr int kDigitThreads = 512, kDigitKeep = 4;      // runs of four elements that a thread keeps between its two looks at them
+constexpr int kDigitThreads = 512;
 constexpr int kCombineThreads = 128;
 constexpr int kDigits = 8;
 
@@ -43,10 +43,8 @@ struct DigitParams {
     int32_t depth, top_k, experts, choices;
     const int32_t *indices;
     // written by the kernel that reads x, read by the others
-    int32_t *offsets;          // 8 times the experts' first positions, experts + 1
     int32_t *position;         // of a choice; -1: of no expert
     int32_t *place;            // row of the scale tiles of a choice's first digit
-    float *one;                // 1
     // the digits
     uint8_t *q;
     int64_t ldq;
@@ -159,7 +157,7 @@ __device__ __forceinline__ void digit_write(const DigitParams &p, float (&f)[4],
         if ((lane & (kAtomLanes - 1)) < kDigits && (r & ~(kAtomLanes - 1)) < runs) *reinterpret_cast<uint32_t *>(scales + static_cast<int64_t>(r / kAtomLanes) * 512 + d * 16) = word;
     }
     uint8_t *dst = q + r * 2;
-#pragma unroll
+#pragma unroll 1                                                  // (see few_digits_kernel: short code)
     for (int32_t d = 0; d < kDigits; ++d, dst += p.ldq) {
         const bool some = e > 0;
         const float step = some ? __uint_as_float(static_cast<uint32_t>(min(e, 253)) << 23) : 0.0f, back = some ? __uint_as_float(static_cast<uint32_t>(254 - min(e, 253)) << 23) : 0.0f;
@@ -179,8 +177,7 @@ __device__ __forceinline__ void digit_write(const DigitParams &p, float (&f)[4],
     }
 }
 
-// One CTA per choice.  FIRST: the kernel that reads x; it finds the choices' places (dynamic shared memory: a word for each expert), and its last CTA
-// writes the experts' offsets.  (Fetching the next product's weights to L2 meanwhile was tried: the launch then ends with the last of them, 1 token 25 -> 31 us.)
+// One CTA per choice.  The code is short rather than unrolled: a launch of a few microseconds fetches its instructions anew.  FIRST: the kernel that reads x; it finds the choices' places (dynamic shared memory: a word for each expert).  (Fetching the next product's weights to L2 meanwhile was tried: the launch then ends with the last of them, 1 token 25 -> 31 us.)
 template <bool NV, bool FIRST>
 __global__ void __launch_bounds__(kDigitThreads)
 few_digits_kernel(const DigitParams p)
@@ -189,17 +186,13 @@ few_digits_kernel(const DigitParams p)
     extern __shared__ int32_t s_count[];
     __shared__ int32_t s_sums[3];
     __shared__ uint32_t s_top;
-    grid_launch_dependents();
     const int32_t c = static_cast<int32_t>(blockIdx.x), me = static_cast<int32_t>(threadIdx.x);
     grid_dependency_wait();
+    grid_launch_dependents();                                     // from here on the product may read the call's inputs (fp4_digits_product)
     const int32_t runs = p.atoms * (kAtom / 4);                   // of four elements, those that fill the last scale tile among them
-    const uint16_t *x = FIRST ? static_cast<const uint16_t *>(p.x) + static_cast<int64_t>(min(c, p.choices - 1) / p.top_k) * p.ldx : nullptr;
-    float f[kDigitKeep][4];
-    if constexpr (FIRST) {
-#pragma unroll
-        for (int i = 0; i < kDigitKeep; ++i)
-            if ((me & ~31) + i * kDigitThreads < runs) digit_load(p, x, nullptr, 1.0f, min(me + i * kDigitThreads, runs) * 4, f[i]);      // (run number `runs`: beyond the depth)
-    }
+    const uint16_t *x = FIRST ? static_cast<const uint16_t *>(p.x) + static_cast<int64_t>(c / p.top_k) * p.ldx : nullptr;
+    float f[4];                                                   // the first run, kept between the two looks at it
+    if constexpr (FIRST) digit_load(p, x, nullptr, 1.0f, min(me, runs) * 4, f);                      // (run number `runs`: beyond the depth)
     int32_t position, place;
     if (me == 0) {
         s_sums[0] = s_sums[1] = s_sums[2] = 0;
@@ -208,7 +201,7 @@ few_digits_kernel(const DigitParams p)
     if constexpr (FIRST) {
         for (int32_t e = me; e < p.experts; e += kDigitThreads) s_count[e] = 0;
         __syncthreads();
-        const int32_t mine = c < p.choices ? p.indices[c] : -1;
+        const int32_t mine = p.indices[c];
         int32_t ahead = 0;                                        // choices of the same expert ahead of this one
         for (int32_t i = me; i < p.choices; i += kDigitThreads) {
             const int32_t e = p.indices[i];
@@ -218,27 +211,6 @@ few_digits_kernel(const DigitParams p)
             }
         }
         __syncthreads();
-        if (c == p.choices) {                                     // the offsets
-            if (me < 32) {
-                int32_t carry = 0;
-                for (int32_t base = 0; base < p.experts; base += 32) {
-                    const int32_t e = base + me;
-                    int32_t sum = e < p.experts ? s_count[e] : 0;
-#pragma unroll
-                    for (int d = 1; d < 32; d <<= 1) {
-                        const int32_t v = __shfl_up_sync(0xffffffffu, sum, d);
-                        if (me >= d) sum += v;
-                    }
-                    if (e < p.experts) p.offsets[e + 1] = kDigits * (carry + sum);
-                    carry += __shfl_sync(0xffffffffu, sum, 31);
-                }
-                if (me == 0) {
-                    p.offsets[0] = 0;
-                    *p.one = 1.0f;
-                }
-            }
-            return;
-        }
         if (mine < 0 || mine >= p.experts) {
             if (me == 0) p.position[c] = -1;
             return;
@@ -263,11 +235,7 @@ few_digits_kernel(const DigitParams p)
     }
     const float *u = FIRST ? nullptr : p.u + position * p.ldu;
     const float u_factor = FIRST ? 1.0f : p.u_factor[position];
-    if constexpr (!FIRST) {
-#pragma unroll
-        for (int i = 0; i < kDigitKeep; ++i)
-            if ((me & ~31) + i * kDigitThreads < runs) digit_load(p, nullptr, u, u_factor, min(me + i * kDigitThreads, runs) * 4, f[i]);
-    }
+    if constexpr (!FIRST) digit_load(p, nullptr, u, u_factor, min(me, runs) * 4, f);
     float inverse = 1.0f;
     if constexpr (NV) {
         uint32_t top = 0u;
@@ -278,10 +246,9 @@ few_digits_kernel(const DigitParams p)
                 if (b < 0x7f800000u) top = max(top, b);
             }
         };
-#pragma unroll
-        for (int i = 0; i < kDigitKeep; ++i)
-            if ((me & ~31) + i * kDigitThreads < runs) look(f[i]);
-        for (int32_t r = me + kDigitKeep * kDigitThreads; r < runs; r += kDigitThreads) {
+        look(f);
+#pragma unroll 1
+        for (int32_t r = me + kDigitThreads; r < runs; r += kDigitThreads) {
             float v[4];
             digit_load(p, x, u, u_factor, r * 4, v);
             look(v);
@@ -299,12 +266,10 @@ few_digits_kernel(const DigitParams p)
     uint8_t *q = p.q + static_cast<int64_t>(position) * kDigits * p.ldq;
     uint8_t *scales = p.scales + static_cast<int64_t>(place >> 7) * p.atoms * 512 + (place & 31) * 16 + ((place >> 5) & 3) * 4;      // a choice's rows never cross 32
     const int32_t base = me & ~31, lane = me & 31;
-#pragma unroll
-    for (int i = 0; i < kDigitKeep; ++i)
-        if (base + i * kDigitThreads < runs) digit_write<NV>(p, f[i], inverse, base + i * kDigitThreads + lane, runs, q, scales);
-    for (int32_t r0 = base + kDigitKeep * kDigitThreads; r0 < runs; r0 += kDigitThreads) {
-        digit_load(p, x, u, u_factor, min(r0 + lane, runs) * 4, f[0]);
-        digit_write<NV>(p, f[0], inverse, r0 + lane, runs, q, scales);
+#pragma unroll 1
+    for (int32_t r0 = base; r0 < runs; r0 += kDigitThreads) {
+        if (r0 != base) digit_load(p, x, u, u_factor, min(r0 + lane, runs) * 4, f);
+        digit_write<NV>(p, f, inverse, r0 + lane, runs, q, scales);
     }
 }
 

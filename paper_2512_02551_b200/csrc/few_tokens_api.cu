@@ -147,7 +147,7 @@ hgemm_status_t run16(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &
 // Scratch memory: where its parts begin (multiples of 256 bytes).  Both products' digits share a place, and so do both products' results: each is used up before
 // the second's is written.
 struct Layout {
-    int64_t offsets, position, place, one, x_factor, h_factor, digits, scales, results, bytes;
+    int64_t position, place, x_factor, h_factor, digits, scales, results, bytes;
     int64_t ld_x, ld_h;        // bytes between digit rows
     int64_t ld_u, ld_z;        // results' rows, in numbers
 };
@@ -166,10 +166,8 @@ Layout layout_of(const hgemm_few_tokens_t &d, int64_t choices)
     l.ld_u = up_to(up_rows(d), 4);
     l.ld_z = up_to(d.hidden, 4);
     const int64_t rows = hgemm_fp8_padded_rows(choices * kDigits, d.experts);
-    l.offsets = part(4 * (d.experts + 1));
     l.position = part(4 * choices);
     l.place = part(4 * choices);
-    l.one = part(4);
     l.x_factor = part(4 * choices);
     l.h_factor = part(4 * choices);
     l.digits = part(choices * kDigits * std::max(l.ld_x, l.ld_h));
@@ -186,8 +184,7 @@ hgemm_status_t run4(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c
     const Layout l = layout_of(d, choices);
     const bool nv = d.weights == HGEMM_WEIGHTS_NVFP4;
     const int32_t format = format_of(d), gated = d.activation == HGEMM_ACT_SWIGLU ? 1 : 0;
-    float *one = reinterpret_cast<float *>(c.scratch + l.one), *results = reinterpret_cast<float *>(c.scratch + l.results);
-    int32_t *offsets = reinterpret_cast<int32_t *>(c.scratch + l.offsets);
+    float *results = reinterpret_cast<float *>(c.scratch + l.results);
 
     // x as digits
     DigitParams p;
@@ -201,20 +198,24 @@ hgemm_status_t run4(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c
     p.experts = d.experts;
     p.choices = int32_t(choices);
     p.indices = c.indices;
-    p.offsets = offsets;
     p.position = reinterpret_cast<int32_t *>(c.scratch + l.position);
     p.place = reinterpret_cast<int32_t *>(c.scratch + l.place);
-    p.one = one;
     p.q = c.scratch + l.digits;
     p.ldq = l.ld_x;
     p.scales = c.scratch + l.scales;
     p.atoms = int32_t(ceil_div(d.hidden, nv ? 64 : 128));
     p.factor = reinterpret_cast<float *>(c.scratch + l.x_factor);
-    hgemm_status_t st = launch(ctx, nv ? reinterpret_cast<const void *>(few_digits_kernel<true, true>) : reinterpret_cast<const void *>(few_digits_kernel<false, true>), dim3(unsigned(choices + 1)),
+    const void *first = nv ? reinterpret_cast<const void *>(few_digits_kernel<true, true>) : reinterpret_cast<const void *>(few_digits_kernel<false, true>);
+    const void *second = nv ? reinterpret_cast<const void *>(few_digits_kernel<true, false>) : reinterpret_cast<const void *>(few_digits_kernel<false, false>);
+    for (const void *fn : {first, second}) {                 // an SM that runs them can take a CTA of the product, which needs nearly all of its shared memory
+        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        if (e != cudaSuccess) return cuda_fail(ctx, e);
+    }
+    hgemm_status_t st = launch(ctx, first, dim3(unsigned(choices)),
                                kDigitThreads, 4 * d.experts, &p, c.stream);
     if (st != HGEMM_OK) return st;
-    st = hgemm_host::fp4_digits_product(ctx, format, choices, up_rows(d), d.hidden, d.experts, p.q, l.ld_x, p.scales, w1.values, w1.ld, w1.scales, nv ? one : nullptr, w1.factor, results, l.ld_u,
-                                        offsets, c.stream);
+    st = hgemm_host::fp4_digits_product(ctx, format, choices, up_rows(d), d.hidden, d.experts, p.q, l.ld_x, p.scales, w1.values, w1.ld, w1.scales, w1.factor, results, l.ld_u, c.indices,
+                                        c.stream);
     if (st != HGEMM_OK) return st;
 
     // h as digits
@@ -228,10 +229,10 @@ hgemm_status_t run4(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c
     p.ldq = l.ld_h;
     p.atoms = int32_t(ceil_div(d.inner, nv ? 64 : 128));
     p.factor = reinterpret_cast<float *>(c.scratch + l.h_factor);
-    st = launch(ctx, nv ? reinterpret_cast<const void *>(few_digits_kernel<true, false>) : reinterpret_cast<const void *>(few_digits_kernel<false, false>), dim3(unsigned(choices)),
+    st = launch(ctx, second, dim3(unsigned(choices)),
                 kDigitThreads, 0, &p, c.stream);
     if (st != HGEMM_OK) return st;
-    st = hgemm_host::fp4_digits_product(ctx, format, choices, d.hidden, d.inner, d.experts, p.q, l.ld_h, p.scales, w2.values, w2.ld, w2.scales, nv ? one : nullptr, w2.factor, results, l.ld_z, offsets,
+    st = hgemm_host::fp4_digits_product(ctx, format, choices, d.hidden, d.inner, d.experts, p.q, l.ld_h, p.scales, w2.values, w2.ld, w2.scales, w2.factor, results, l.ld_z, c.indices,
                                         c.stream);
     if (st != HGEMM_OK) return st;
 

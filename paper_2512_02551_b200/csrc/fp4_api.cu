@@ -117,10 +117,10 @@ hgemm_fp4_config_t choose(int32_t form, int64_t M, int64_t N, int64_t K, int32_t
     return best;
 }
 
-int stages_of(const hgemm_fp4_config_t &c, bool nv, int32_t groups)
+int stages_of(const hgemm_fp4_config_t &c, bool nv, int32_t groups, int smem)
 {
     const int fixed = 1024 + (c.cta_group == 2 ? 8 * hgemm_dev::kFp4StagingPerWarp : 0) + hgemm_dev::kFp4CtrlBytes + 12 * (groups + 1);
-    return std::min((kSmemOptIn - fixed) / hgemm_dev::fp4_stage_bytes(c.cta_group, c.block_q, nv), hgemm_dev::kFp4MaxStages);
+    return std::min((smem - fixed) / hgemm_dev::fp4_stage_bytes(c.cta_group, c.block_q, nv), hgemm_dev::kFp4MaxStages);
 }
 
 template <bool NV>
@@ -224,10 +224,13 @@ int64_t digits_tiles(int64_t choices, int64_t N, int32_t groups, const hgemm_fp4
     return (std::min<int64_t>(groups, choices) + choices * kDigits / c.block_q) * ceil_div(N, 128);
 }
 
+// Shared memory of a CTA; DIGITS: with room beside it for one that makes digits, so that the weights are on their way before those end (all of it: 1 token 24.5 us, 16 tokens 57.5).
+constexpr int product_smem(bool digits) { return digits ? kSmemOptIn - 8192 : kSmemOptIn; }
+
 // The forward product of rows that are written as sums of eight 4-bit rows each (DIGITS: M counts those), or any product of a plan.
 template <bool DIGITS>
 hgemm_status_t run_product(const hgemm_fp4_plan_s &plan, const void *A, int64_t lda, const void *a_scales, const float *a_factor, const void *B, int64_t ldb, const void *b_scales,
-                           const float *b_factor, void *C, int64_t ldc, const int32_t *offsets, int32_t accumulate, void *stream)
+                           const float *b_factor, void *C, int64_t ldc, const int32_t *offsets, int32_t accumulate, void *stream, const int32_t *indices = nullptr)
 {
     hgemm_ctx_s *ctx = plan.ctx;
     const int32_t form = plan.form, groups = plan.groups;
@@ -235,7 +238,7 @@ hgemm_status_t run_product(const hgemm_fp4_plan_s &plan, const void *A, int64_t 
     const bool wgrad = form == HGEMM_FP8_WEIGHT_GRAD, nv = plan.format == HGEMM_FP4_NV;
     const int64_t out_cols = form == HGEMM_FP8_FORWARD ? N : K;
     const int64_t depth = wgrad ? (groups > 0 ? hgemm_fp8_padded_rows(M, groups) : M) : form == HGEMM_FP8_FORWARD ? K : N;       // contracted elements of the copies
-    if ((groups > 0) != (offsets != nullptr) || accumulate < 0 || accumulate > 1 || (accumulate && plan.out_type != HGEMM_TYPE_F32)) return HGEMM_ERR_INVALID_ARG;
+    if ((groups > 0) != ((DIGITS ? indices : offsets) != nullptr) || accumulate < 0 || accumulate > 1 || (accumulate && plan.out_type != HGEMM_TYPE_F32)) return HGEMM_ERR_INVALID_ARG;
     if (lda < ceil_div(depth, 2) || ldb < ceil_div(depth, 2) || ldc < out_cols || (lda & 15) != 0 || (ldb & 15) != 0) return HGEMM_ERR_INVALID_ARG;
     const int es = type_bytes(plan.out_type);
     if (M == 0 && !wgrad) return HGEMM_OK;
@@ -246,17 +249,19 @@ hgemm_status_t run_product(const hgemm_fp4_plan_s &plan, const void *A, int64_t 
         return e == cudaSuccess ? HGEMM_OK : cuda_fail(ctx, e);
     }
     if (!A || !B || !a_scales || !b_scales || !aligned16(A) || !aligned16(B) || !aligned16(a_scales) || !aligned16(b_scales) || !aligned4(offsets)) return HGEMM_ERR_INVALID_ARG;
-    if (nv != (a_factor != nullptr) || nv != (b_factor != nullptr) || !aligned4(a_factor) || !aligned4(b_factor)) return HGEMM_ERR_INVALID_ARG;
+    if ((nv && !DIGITS) != (a_factor != nullptr) || nv != (b_factor != nullptr) || !aligned4(a_factor) || !aligned4(b_factor)) return HGEMM_ERR_INVALID_ARG;
 
     const hgemm_fp4_config_t &c = plan.cfg;
     const bool swap = c.cta_group == 1;                      // the kernel's P operand is the caller's B
     Fp4Params p;
     std::memset(&p, 0, sizeof(p));
-    p.stages = stages_of(c, nv, groups);
+    p.stages = stages_of(c, nv, groups, product_smem(DIGITS));
     if (p.stages < 2) return HGEMM_ERR_UNSUPPORTED;
     p.split = c.split_k;
     p.groups = groups;
     p.offsets = offsets;
+    p.indices = indices;
+    p.choices = DIGITS ? int32_t(M / kDigits) : 0;
     p.rows_ragged = int32_t(M);
     p.kblocks = int32_t(ceil_div(depth, 128));
     p.k_capacity = int32_t(ceil_div(depth, 128));
@@ -326,7 +331,7 @@ hgemm_status_t run_product(const hgemm_fp4_plan_s &plan, const void *A, int64_t 
     const int64_t units = c.split_k > 1 ? tiles : std::min<int64_t>(tiles, std::max(1, ctx->num_sms / per_unit));
     if (units * per_unit > 0x7fffffff) return HGEMM_ERR_UNSUPPORTED;
     void *args[6] = {&map_p, &map_q, &map_sp, &map_sq, &map_c, &p};
-    return launch(ctx, DIGITS ? digits_kernel_of(c, plan.format) : kernel_of(c, plan.format), dim3(unsigned(units * per_unit), 1, 1), hgemm_dev::kFp4Threads, kSmemOptIn, per_unit, args, stream);
+    return launch(ctx, DIGITS ? digits_kernel_of(c, plan.format) : kernel_of(c, plan.format), dim3(unsigned(units * per_unit), 1, 1), hgemm_dev::kFp4Threads, product_smem(DIGITS), per_unit, args, stream);
 }
 
 } // namespace
@@ -336,7 +341,7 @@ namespace hgemm_host {
 int status_slot_of(const hgemm_fp4_plan_s *plan) { return plan->status_slot; }
 
 hgemm_status_t fp4_digits_product(hgemm_ctx_s *ctx, int32_t format, int64_t choices, int64_t N, int64_t K, int32_t groups, const void *digits, int64_t ld, const void *digit_scales, const void *B,
-                                  int64_t ldb, const void *b_scales, const float *one, const float *b_factor, float *C, int64_t ldc, const int32_t *offsets, void *stream)
+                                  int64_t ldb, const void *b_scales, const float *b_factor, float *C, int64_t ldc, const int32_t *indices, void *stream)
 {
     hgemm_fp4_plan_s plan;
     plan.ctx = ctx;
@@ -352,9 +357,9 @@ hgemm_status_t fp4_digits_product(hgemm_ctx_s *ctx, int32_t format, int64_t choi
     // tiles leave SMs without work: each round of them starts anew (8 choices of 64 experts, tiles for every SM, shared by two: 37.5 us).
     plan.cfg = {1, choices > 16 || choices > 8 * groups ? 128 : 64, 1, 0};
     while (plan.cfg.split_k < 8 && digits_tiles(choices, N, groups, plan.cfg) * plan.cfg.split_k * 2 <= ctx->num_sms && ceil_div(K, 256) >= 2 * plan.cfg.split_k * 2) plan.cfg.split_k *= 2;
-    const cudaError_t e = cudaFuncSetAttribute(digits_kernel_of(plan.cfg, format), cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemOptIn);
+    const cudaError_t e = cudaFuncSetAttribute(digits_kernel_of(plan.cfg, format), cudaFuncAttributeMaxDynamicSharedMemorySize, product_smem(true));
     if (e != cudaSuccess) return cuda_fail(ctx, e);
-    return run_product<true>(plan, digits, ld, digit_scales, one, B, ldb, b_scales, b_factor, C, ldc, offsets, 0, stream);
+    return run_product<true>(plan, digits, ld, digit_scales, nullptr, B, ldb, b_scales, b_factor, C, ldc, nullptr, 0, stream, indices);
 }
 
 } // namespace hgemm_host

@@ -67,6 +67,8 @@ struct Fp4Params {
     FastDiv fd_other, fd_group, fd_sweep, fd_raster, fd_last;   // divisors of the tile numbering: see product_tile
     int32_t groups, ragged, rows_ragged, k_capacity;   // rows_ragged: clamp of the offsets; k_capacity: units the padded copy has
     const int32_t *offsets;
+    const int32_t *indices;        // DIGITS: the group of each of `choices` rows of the caller's, instead of offsets
+    int32_t choices;
     int32_t sp_group, sq_group;    // scale tiles (along the rows) between the matrices of an operand with one per group
     const float *fp, *fq;          // tensor factors (nullptr: 1), one, or one per group where f*_group is 1
     int32_t fp_group, fq_group;
@@ -177,7 +179,8 @@ __device__ __forceinline__ void fp4_store_one(const Fp4Params &p, int64_t at, fl
 }
 
 // CG: CTAs per tile.  BN: rows of Q per tile.  NV: e4m3 scales of 16 elements, else powers of two of 32.  CG == 2 stores by rows, CG == 1 transposed.
-// DIGITS (CG == 1): each eight rows of Q are one row of the caller's, written as a sum of eight; the result has their sums.
+// DIGITS (CG == 1): each eight rows of Q are one row of the caller's, written as a sum of eight; the result has their sums.  The kernel ahead in the stream makes those
+// rows; P, its scales and factors and the rows' groups are older (that kernel starts this one when all before it is complete), and the first tile's P is fetched meanwhile.
 template <int CG, int BN, bool NV, bool DIGITS = false>
 __global__ void __launch_bounds__(kFp4Threads, 1)
 fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_sp,
@@ -239,11 +242,38 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         prefetch_tensormap(&tmap_sq);
     }
     if (warp == 1) tmem_alloc<CG>(smem_addr(const_cast<uint32_t *>(tmem_slot)), 512);
-    // No thread reads or writes global memory before the kernels ahead in the stream are complete.
-    grid_dependency_wait();
-    if (warp == 2 && p.groups > 0) {
-        // the groups' places among the result's tiles, and among the scale tiles
-        scan_groups(p, pre, off, p.ragged == kRaggedK ? kFp4Unit : p.ragged == kRaggedP ? TP : TQ, lane, scale_pre, 128);
+    if constexpr (DIGITS) {
+        // the groups' rows from the choices, then their places as below
+        for (int32_t e = static_cast<int32_t>(threadIdx.x); e <= p.groups; e += kFp4Threads) off[e] = 0;
+        __syncthreads();
+        for (int32_t c = static_cast<int32_t>(threadIdx.x); c < p.choices; c += kFp4Threads) {
+            const int32_t e = p.indices[c];
+            if (e >= 0 && e < p.groups) atomicAdd(&off[e + 1], kDigits);
+        }
+        __syncthreads();
+        if (warp == 2) {
+            int32_t carry = 0;
+            for (int32_t base = 1; base <= p.groups; base += 32) {
+                const int32_t e = base + static_cast<int32_t>(lane);
+                int32_t n = e <= p.groups ? off[e] : 0;
+#pragma unroll
+                for (int d = 1; d < 32; d <<= 1) {
+                    const int32_t x = __shfl_up_sync(0xffffffffu, n, d);
+                    if (static_cast<int32_t>(lane) >= d) n += x;
+                }
+                n += carry;
+                if (e <= p.groups) off[e] = n;
+                carry = __shfl_sync(0xffffffffu, n, 31);
+            }
+            scan_groups<false>(p, pre, off, TQ, lane, scale_pre, 128);
+        }
+    } else {
+        // No thread reads or writes global memory before the kernels ahead in the stream are complete.
+        grid_dependency_wait();
+        if (warp == 2 && p.groups > 0) {
+            // the groups' places among the result's tiles, and among the scale tiles
+            scan_groups(p, pre, off, p.ragged == kRaggedK ? kFp4Unit : p.ragged == kRaggedP ? TP : TQ, lane, scale_pre, 128);
+        }
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -273,6 +303,20 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         uint32_t ph = 0;
         const uint32_t full_leader = CG == 2 ? mapa(bar_full, 0) : bar_full;
         bool ok = true;
+        int32_t ahead = 0;                                        // contracted elements of the first tile whose P is on its way, in units
+        if constexpr (DIGITS) {
+            if (unit < total) {
+                const ProductTile t = tile_of(unit);
+                ahead = min(t.kbn, 2 * p.stages);
+                for (int32_t kb = 0; kb < ahead; kb += 2) {
+                    const uint32_t fb = bar_full + 4 * kb, p_dst = smem_base + static_cast<uint32_t>(kb / 2) * kOperandBytes, sp_dst = scale_base + static_cast<uint32_t>(kb / 2) * (kSpBytes + kSqBytes);
+                    mbar_arrive_expect_tx_elect(fb, kStageBytes);
+                    tma_load_3d_elect(p_dst, &tmap_p, (t.kb0 + kb) * (kFp4Unit / 2), t.p0, t.group, fb);
+                    tma_load_3d_elect(sp_dst, &tmap_sp, 0, (t.kb0 + kb) * (kAtoms / 2), t.group * p.sp_group + (t.p0 >> 7), fb);
+                }
+            }
+            grid_dependency_wait();                               // in every CTA, with a tile or without: this kernel's end says that the one ahead has ended
+        }
         for (int32_t w = unit; ok && w < total; w += units) {
             const ProductTile t = tile_of(w);
             const int32_t prow = t.p0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * 128, qrow = t.q0 + static_cast<int32_t>(CG == 2 ? rank : 0u) * (BN / CG);
@@ -287,10 +331,12 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                 const int32_t k0 = (t.kb0 + kb) * (kFp4Unit / 2), a0 = (t.kb0 + kb) * (kAtoms / 2);
                 const uint32_t fb = full_leader + 8 * s;
                 if constexpr (CG == 1) {
-                    mbar_arrive_expect_tx_elect(bar_full + 8 * s, kStageBytes);
-                    tma_load_3d_elect(p_dst, &tmap_p, k0, prow, pz, fb);
+                    if (!DIGITS || w != unit || kb >= ahead) {
+                        mbar_arrive_expect_tx_elect(bar_full + 8 * s, kStageBytes);
+                        tma_load_3d_elect(p_dst, &tmap_p, k0, prow, pz, fb);
+                        tma_load_3d_elect(sp_dst, &tmap_sp, 0, a0, sp, fb);
+                    }
                     tma_load_3d_elect(q_dst, &tmap_q, k0, qrow, qz, fb);
-                    tma_load_3d_elect(sp_dst, &tmap_sp, 0, a0, sp, fb);
                     tma_load_3d_elect(sq_dst, &tmap_sq, 0, a0, sq, fb);
                 } else {
                     if (is_leader) mbar_arrive_expect_tx_elect(bar_full + 8 * s, kStageBytes);

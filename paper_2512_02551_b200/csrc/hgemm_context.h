@@ -42,10 +42,11 @@ struct hgemm_ctx_s {
 namespace hgemm_host {
 int status_slot_of(const hgemm_fp8_plan_s *plan);   // the plan's word in the context's status array
 int status_slot_of(const hgemm_fp4_plan_s *plan);
-// C[c][n] (fp32) = sum of the products of choice c's eight digit rows (8 c .. 8 c + 7 of `digits`, sorted by group) with row n of the group's matrix of B; offsets: 8 times
-// the choices'.  one: a factor of 1 on the device (NV).  Reports to the context's own status word.
+// C[i][n] (fp32) = sum of the products of the eight digit rows 8 i .. 8 i + 7 with row n of their group's matrix of B, i = the place of a choice among all, sorted by
+// group; indices: the choices' groups (outside [0, groups): no row).  The kernel ahead in the stream makes the digits; everything else that is read is older: it is read
+// before that kernel ends, so that one lets this one start only when all before it is complete.  Reports to the context's own status word.
 hgemm_status_t fp4_digits_product(hgemm_ctx_s *ctx, int32_t format, int64_t choices, int64_t N, int64_t K, int32_t groups, const void *digits, int64_t ld, const void *digit_scales, const void *B,
-                                  int64_t ldb, const void *b_scales, const float *one, const float *b_factor, float *C, int64_t ldc, const int32_t *offsets, void *stream);
+                                  int64_t ldb, const void *b_scales, const float *b_factor, float *C, int64_t ldc, const int32_t *indices, void *stream);
 // Synchronises the device, reads a status word and clears it: HGEMM_OK, or what the word stands for.
 hgemm_status_t take_status_word(hgemm_ctx_s *ctx, int slot, uint32_t *code);
 // One small kernel whose only wait is on a barrier that nothing signals; it reports to the slot.

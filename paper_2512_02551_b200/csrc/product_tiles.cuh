@@ -69,11 +69,12 @@ __device__ __forceinline__ ProductTile product_tile(int32_t w, const Params &p, 
 }
 
 // Clamped offsets and the prefix sums product_tile reads; one whole warp.  The offsets are fetched first, so that their latencies are one; unit2, pre2 (or nullptr): the prefix
-// sums of another unit.
-template <class Params>
+// sums of another unit.  FETCH = false: off has the offsets already.
+template <bool FETCH = true, class Params>
 __device__ __forceinline__ void scan_groups(const Params &p, int32_t *pre, int32_t *off, int32_t unit, uint32_t lane, int32_t *pre2 = nullptr, int32_t unit2 = 1)
 {
-    for (int32_t e = static_cast<int32_t>(lane); e <= p.groups; e += 32) off[e] = min(max(p.offsets[e], 0), p.rows_ragged);
+    if constexpr (FETCH)
+        for (int32_t e = static_cast<int32_t>(lane); e <= p.groups; e += 32) off[e] = min(max(p.offsets[e], 0), p.rows_ragged);
     __syncwarp();
     int32_t carry = 0, carry2 = 0, last = off[0];
     for (int32_t base = 0; base < p.groups; base += 32) {
