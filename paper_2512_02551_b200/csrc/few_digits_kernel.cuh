@@ -187,13 +187,19 @@ few_digits_kernel(const DigitParams p)
     __shared__ int32_t s_sums[3];
     __shared__ uint32_t s_top;
     const int32_t c = static_cast<int32_t>(blockIdx.x), me = static_cast<int32_t>(threadIdx.x);
+    int32_t position = 0, place = 0;
+    float u_factor = 1.0f;
+    if constexpr (!FIRST) {                                       // the first kernel's, which the product has waited for
+        position = p.position[c];
+        place = p.place[c];
+        if (position >= 0) u_factor = p.u_factor[position];
+    }
     grid_dependency_wait();
     grid_launch_dependents();                                     // from here on the product may read the call's inputs (fp4_digits_product)
     const int32_t runs = p.atoms * (kAtom / 4);                   // of four elements, those that fill the last scale tile among them
     const uint16_t *x = FIRST ? static_cast<const uint16_t *>(p.x) + static_cast<int64_t>(c / p.top_k) * p.ldx : nullptr;
     float f[4];                                                   // the first run, kept between the two looks at it
     if constexpr (FIRST) digit_load(p, x, nullptr, 1.0f, min(me, runs) * 4, f);                      // (run number `runs`: beyond the depth)
-    int32_t position, place;
     if (me == 0) {
         s_sums[0] = s_sums[1] = s_sums[2] = 0;
         s_top = 0u;
@@ -228,13 +234,10 @@ few_digits_kernel(const DigitParams p)
             p.place[c] = place;
         }
     } else {
-        position = p.position[c];
-        place = p.place[c];
         if (position < 0) return;
         __syncthreads();
     }
     const float *u = FIRST ? nullptr : p.u + position * p.ldu;
-    const float u_factor = FIRST ? 1.0f : p.u_factor[position];
     if constexpr (!FIRST) digit_load(p, nullptr, u, u_factor, min(me, runs) * 4, f);
     float inverse = 1.0f;
     if constexpr (NV) {
@@ -292,8 +295,7 @@ few_combine_kernel(const CombineParams p)
 {
     grid_launch_dependents();
     const int32_t n = (static_cast<int32_t>(blockIdx.x) * kCombineThreads + static_cast<int32_t>(threadIdx.x)) * 4, t = static_cast<int32_t>(blockIdx.y);
-    grid_dependency_wait();
-    // lane j has choice j's row and factor
+    // lane j has choice j's row and factor: the digits' kernels', which the product has waited for
     const int32_t lane = static_cast<int32_t>(threadIdx.x & 31u);
     int32_t mine = -1;
     float w = 0.0f;
@@ -302,6 +304,7 @@ few_combine_kernel(const CombineParams p)
         w = p.weights[t * p.top_k + lane];
     }
     const float s = mine >= 0 ? p.factor[mine] : 0.0f;
+    grid_dependency_wait();
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int32_t j0 = 0; j0 < p.top_k; j0 += 8) {
         float4 z[8];

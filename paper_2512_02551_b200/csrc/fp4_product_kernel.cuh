@@ -223,7 +223,12 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
     const int32_t unit = static_cast<int32_t>(blockIdx.x) / per_unit, units = static_cast<int32_t>(gridDim.x) / per_unit;
     WaitCtl ctl{abort_flag, p.status, p.wait_budget};
 
-    grid_launch_dependents();
+    int32_t mine = -1;                                            // a choice's group, on its way during the set-up
+    if constexpr (DIGITS) {
+        if (static_cast<int32_t>(threadIdx.x) < p.choices) mine = p.indices[threadIdx.x];
+    } else {
+        grid_launch_dependents();
+    }
     if (threadIdx.x == 0) {
         *abort_flag = 0u;
         for (int s = 0; s < p.stages; ++s) {
@@ -247,7 +252,7 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         for (int32_t e = static_cast<int32_t>(threadIdx.x); e <= p.groups; e += kFp4Threads) off[e] = 0;
         __syncthreads();
         for (int32_t c = static_cast<int32_t>(threadIdx.x); c < p.choices; c += kFp4Threads) {
-            const int32_t e = p.indices[c];
+            const int32_t e = c < kFp4Threads ? mine : p.indices[c];
             if (e >= 0 && e < p.groups) atomicAdd(&off[e + 1], kDigits);
         }
         __syncthreads();
@@ -316,6 +321,7 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                 }
             }
             grid_dependency_wait();                               // in every CTA, with a tile or without: this kernel's end says that the one ahead has ended
+            grid_launch_dependents();                             // and its results may be read by the next from here on
         }
         for (int32_t w = unit; ok && w < total; w += units) {
             const ProductTile t = tile_of(w);
