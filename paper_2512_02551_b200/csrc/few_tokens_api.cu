@@ -177,9 +177,28 @@ Layout layout_of(const hgemm_few_tokens_t &d, int64_t choices)
     return l;
 }
 
+// Once a context: an SM that makes digits can take a CTA of the product too, which needs nearly all of its shared memory.
+hgemm_status_t prepare4(hgemm_ctx_s *ctx)
+{
+    using namespace hgemm_dev;
+    const void *const kernels[4] = {reinterpret_cast<const void *>(few_digits_kernel<true, true>), reinterpret_cast<const void *>(few_digits_kernel<true, false>),
+                                    reinterpret_cast<const void *>(few_digits_kernel<false, true>), reinterpret_cast<const void *>(few_digits_kernel<false, false>)};
+    for (const void *fn : kernels) {
+        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+        if (e != cudaSuccess) return cuda_fail(ctx, e);
+    }
+    const hgemm_status_t st = hgemm_host::fp4_digits_prepare(ctx);
+    if (st == HGEMM_OK) ctx->few_ready = true;
+    return st;
+}
+
 hgemm_status_t run4(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c, const hgemm_expert_weights_t &w1, const hgemm_expert_weights_t &w2)
 {
     using namespace hgemm_dev;
+    if (!ctx->few_ready) {
+        const hgemm_status_t st = prepare4(ctx);
+        if (st != HGEMM_OK) return st;
+    }
     const int64_t choices = c.tokens * d.top_k;
     const Layout l = layout_of(d, choices);
     const bool nv = d.weights == HGEMM_WEIGHTS_NVFP4;
@@ -207,10 +226,6 @@ hgemm_status_t run4(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c
     p.factor = reinterpret_cast<float *>(c.scratch + l.x_factor);
     const void *first = nv ? reinterpret_cast<const void *>(few_digits_kernel<true, true>) : reinterpret_cast<const void *>(few_digits_kernel<false, true>);
     const void *second = nv ? reinterpret_cast<const void *>(few_digits_kernel<true, false>) : reinterpret_cast<const void *>(few_digits_kernel<false, false>);
-    for (const void *fn : {first, second}) {                 // an SM that runs them can take a CTA of the product, which needs nearly all of its shared memory
-        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-        if (e != cudaSuccess) return cuda_fail(ctx, e);
-    }
     hgemm_status_t st = launch(ctx, first, dim3(unsigned(choices)),
                                kDigitThreads, 4 * d.experts, &p, c.stream);
     if (st != HGEMM_OK) return st;

@@ -224,7 +224,8 @@ int64_t digits_tiles(int64_t choices, int64_t N, int32_t groups, const hgemm_fp4
     return (std::min<int64_t>(groups, choices) + choices * kDigits / c.block_q) * ceil_div(N, 128);
 }
 
-// Shared memory of a CTA; DIGITS: with room beside it for one that makes digits, so that the weights are on their way before those end (all of it: 1 token 24.5 us, 16 tokens 57.5).
+// Shared memory of a CTA; DIGITS: with room beside it for one that makes digits, so that the first weights are on their way before those end (16 tokens of 8 among
+// 64 experts: 47.6 us; with all of it 53.0).
 constexpr int product_smem(bool digits) { return digits ? kSmemOptIn - 8192 : kSmemOptIn; }
 
 // The forward product of rows that are written as sums of eight 4-bit rows each (DIGITS: M counts those), or any product of a plan.
@@ -340,6 +341,17 @@ namespace hgemm_host {
 
 int status_slot_of(const hgemm_fp4_plan_s *plan) { return plan->status_slot; }
 
+hgemm_status_t fp4_digits_prepare(hgemm_ctx_s *ctx)
+{
+    for (const int32_t format : {HGEMM_FP4_NV, HGEMM_FP4_MX}) {
+        for (const int32_t width : {64, 128}) {
+            const cudaError_t e = cudaFuncSetAttribute(digits_kernel_of({1, width, 1, 0}, format), cudaFuncAttributeMaxDynamicSharedMemorySize, product_smem(true));
+            if (e != cudaSuccess) return cuda_fail(ctx, e);
+        }
+    }
+    return HGEMM_OK;
+}
+
 hgemm_status_t fp4_digits_product(hgemm_ctx_s *ctx, int32_t format, int64_t choices, int64_t N, int64_t K, int32_t groups, const void *digits, int64_t ld, const void *digit_scales, const void *B,
                                   int64_t ldb, const void *b_scales, const float *b_factor, float *C, int64_t ldc, const int32_t *indices, void *stream)
 {
@@ -352,13 +364,11 @@ hgemm_status_t fp4_digits_product(hgemm_ctx_s *ctx, int32_t format, int64_t choi
     plan.groups = groups;
     plan.format = format;
     plan.out_type = HGEMM_TYPE_F32;
-    // 8 choices a tile (64 columns) while there are few, 16 beyond (2048 -> 1024 -> 2048, SwiGLU, the whole layer: 8 choices of 64 experts 25.4 against 27.5 us;
-    // 32: 38.1 and 37.6; 512: 73.8 and 72.0; 512 of 16 experts, two or three tiles an expert instead of four: 56.2 and 50.2).  CTAs that share a contraction only where
-    // tiles leave SMs without work: each round of them starts anew (8 choices of 64 experts, tiles for every SM, shared by two: 37.5 us).
-    plan.cfg = {1, choices > 16 || choices > 8 * groups ? 128 : 64, 1, 0};
+    // 8 choices a tile (64 columns), or 16 where experts have more than 6 on average (2048 -> 1024 -> 2048, SwiGLU, the whole layer: 8 choices of 64 experts 16.6 against
+    // 18.4 us; 256: 52.3 and 55.3; 512: 62.8 and 60.7; 512 of 16 experts: 49.0 and 41.8).  CTAs that share a contraction only where tiles leave SMs without
+    // work: each round of them starts anew (8 choices of 64 experts, tiles for every SM, shared by two: 32.9 us).
+    plan.cfg = {1, choices > 8 && choices > 6 * groups ? 128 : 64, 1, 0};
     while (plan.cfg.split_k < 8 && digits_tiles(choices, N, groups, plan.cfg) * plan.cfg.split_k * 2 <= ctx->num_sms && ceil_div(K, 256) >= 2 * plan.cfg.split_k * 2) plan.cfg.split_k *= 2;
-    const cudaError_t e = cudaFuncSetAttribute(digits_kernel_of(plan.cfg, format), cudaFuncAttributeMaxDynamicSharedMemorySize, product_smem(true));
-    if (e != cudaSuccess) return cuda_fail(ctx, e);
     return run_product<true>(plan, digits, ld, digit_scales, nullptr, B, ldb, b_scales, b_factor, C, ldc, nullptr, 0, stream, indices);
 }
 

@@ -1,6 +1,7 @@
 // The library's context object, shared by the translation units that implement the C ABI.
 #pragma once
 
+#include <atomic>
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -30,6 +31,7 @@ struct hgemm_ctx_s {
     encode_tiled_fn encode = nullptr;
     int last_cuda_error = 0;
     bool dependent_launch = true;
+    std::atomic<bool> few_ready{false};            // the few-token kernels' attributes are set
     bool tma_3d = true;
     std::vector<hgemm_plan_s *> plans;
     std::vector<hgemm_fp8_plan_s *> fp8_plans;
@@ -42,6 +44,8 @@ struct hgemm_ctx_s {
 namespace hgemm_host {
 int status_slot_of(const hgemm_fp8_plan_s *plan);   // the plan's word in the context's status array
 int status_slot_of(const hgemm_fp4_plan_s *plan);
+// What fp4_digits_product's kernels need once on a context's device.
+hgemm_status_t fp4_digits_prepare(hgemm_ctx_s *ctx);
 // C[i][n] (fp32) = sum of the products of the eight digit rows 8 i .. 8 i + 7 with row n of their group's matrix of B, i = the place of a choice among all, sorted by
 // group; indices: the choices' groups (outside [0, groups): no row).  The kernel ahead in the stream makes the digits; everything else that is read is older: it is read
 // before that kernel ends, so that one lets this one start only when all before it is complete.  Reports to the context's own status word.

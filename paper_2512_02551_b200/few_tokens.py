@@ -12,7 +12,7 @@ import ctypes
 import torch
 
 from . import fp4, hgemm
-from .fp8 import TYPES, _check, _dense, _ld, _stream
+from .fp8 import TYPES, _dense, _ld, _stream
 
 WEIGHTS = {"f16": 1, "bf16": 2, "nvfp4": 16, "mxfp4": 17}
 ACTIVATIONS = {"silu": 0, "swiglu": 1}
@@ -65,10 +65,11 @@ class Layer:
             raise ValueError(f"weights is one of {', '.join(WEIGHTS)}, activation one of {', '.join(ACTIVATIONS)}")
         if dtype not in (torch.float16, torch.bfloat16):
             raise ValueError("x and y are float16 or bfloat16")
-        self.ctx, self.dtype, self.weights = ctx, dtype, weights
+        self.ctx, self.dtype, self.weights, self._types = ctx, dtype, weights, (dtype,)
         self.hidden, self.inner, self.experts, self.top_k = int(hidden), int(inner), int(experts), int(top_k)
         self._desc = Description(self.hidden, self.inner, self.experts, self.top_k, WEIGHTS[weights], ACTIVATIONS[activation], TYPES[dtype], 0)
         self._ref = ctypes.byref(self._desc)
+        self._call = lib().hgemm_few_tokens
         if lib().hgemm_few_tokens_scratch(self._ref, 0) < 0:
             raise ValueError(f"not a layer that can be run: {[getattr(self._desc, n) for n, _ in Description._fields_]}")
         self._w1 = torch.Size((self.experts, self.inner * (2 if activation == "swiglu" else 1), self.hidden))
@@ -92,16 +93,23 @@ class Layer:
         if len(w) not in (2, 3):
             raise ValueError(f"{name} must be (values, scale tiles, factors)")
         values, tiles = self._shapes[i]
+        v = w[0]
+        st = v.stride()
+        if len(st) == 3 and st[2] == 1 and st[1] >= values[2] > 1 and st[1] % 16 == 0 and st[0] == values[1] * st[1] and v.shape == values and v.dtype == torch.uint8 and v.is_cuda:
+            ld = st[1]                                            # matrices one after the other, as fp4.empty_rows makes them
+        else:
+            ld = fp4._ld_bytes(v, values, name)
         factor = fp4._factor_of(w[2] if len(w) == 3 else None, self.experts, self.weights, f"{name} factors")
-        return Weights(w[0].data_ptr(), fp4._ld_bytes(w[0], values, name), _dense(w[1], tiles, torch.uint8, f"{name} scales"), factor)
+        return Weights(v.data_ptr(), ld, _dense(w[1], tiles, torch.uint8, name), factor)
 
     def run(self, x, w1, w2, indices, weights, y, scratch, stream=None) -> None:
         """y (T, hidden) = the layer on x (T, hidden); indices (T, top_k) int32 and weights (T, top_k) fp32 are a router's."""
         T = x.shape[0]
-        shape = (T, self.hidden)
-        ldx, ldy = _ld(x, shape, (self.dtype,), "x"), _ld(y, shape, (self.dtype,), "y")
-        i, w = _dense(indices, (T, self.top_k), torch.int32, "indices"), _dense(weights, (T, self.top_k), torch.float32, "weights")
+        shape, chosen = (T, self.hidden), (T, self.top_k)
+        ldx, ldy = _ld(x, shape, self._types, "x"), _ld(y, shape, self._types, "y")
+        i, w = _dense(indices, chosen, torch.int32, "indices"), _dense(weights, chosen, torch.float32, "weights")
         s = _dense(scratch, scratch.shape, torch.uint8, "scratch")
         a, b = self._weights(w1, 0, "w1"), self._weights(w2, 1, "w2")
-        _check(lib().hgemm_few_tokens(self.ctx._h, self._ref, T, x.data_ptr(), ldx, ctypes.byref(a), ctypes.byref(b), i, w, y.data_ptr(), ldy, s, scratch.numel(), _stream(self.ctx, stream)),
-               f"hgemm_few_tokens({T} tokens, {self.weights})")
+        st = self._call(self.ctx._h, self._ref, T, x.data_ptr(), ldx, ctypes.byref(a), ctypes.byref(b), i, w, y.data_ptr(), ldy, s, scratch.numel(), _stream(self.ctx, stream))
+        if st != hgemm.OK:
+            raise hgemm.HgemmError(st, f"hgemm_few_tokens({T} tokens, {self.weights})")
