@@ -13,8 +13,8 @@
 //
 // Work.  Launch 1: a warp has a tile of 16 rows (SWIGLU: 8 rows of each half, whose products meet in one lane), a CTA eight tiles of one expert, whose
 // tokens it lays out in shared memory as the instruction wants them.  As many rounds as give every CTA the same; the groups of tiles that are left over are
-// shared by up to eight CTAs each, whose warps split the contraction.  Launch 2: one CTA for 16 outputs of all tokens; its warps take the chosen
-// experts in turn (those left over by several warps each), so that every sum over a token's choices stays in a CTA and has a fixed order.  Every CTA makes
+// shared by up to eight CTAs each, whose warps split the contraction.  Launch 2: one CTA, or a cluster, for 16 outputs of all tokens; its warps take the chosen
+// experts in turn (those left over by several warps each), so that every sum over a token's choices stays in a cluster and has a fixed order.  Every CTA makes
 // the list of the experts' choices for itself; launch 2 does so, and fetches its first weights, before launch 1 ends (both are inputs of the call,
 // which launch 1 has waited for).  A column of the instruction that has no choice computes with whatever is there; its sums are not used.
 #pragma once
@@ -59,6 +59,7 @@ struct FewParams {
     FastDiv fd_groups;
     int32_t piece;             // launch 1: bytes of shared memory for x
     int32_t most_slices;       // warps that may share a contraction
+    int32_t ranks;             // launch 2: CTAs (a cluster) that share 16 outputs
 };
 
 constexpr int kFewChunk = 32;                     // k of a chunk: 64 bytes of a row
@@ -495,7 +496,7 @@ few_up_kernel(const FewParams p)
 
 // ---- launch 2: y = sum of weight * (W2 h) ------------------------------------------------------------------------------
 
-// grid: 16 rows of W2 (outputs) a CTA.  Dynamic shared memory: the lists, the choices' weights, most_slices x choices x 16 sums.
+// grid: 16 rows of W2 (outputs) a cluster of `ranks` CTAs, which take the entries in turn (entry i: CTA i % ranks).  Dynamic shared memory: the lists, the choices' weights, most_slices x choices x 16 sums.
 template <class T, int ALIGN>
 __global__ void __launch_bounds__(kFewDownThreads, 1)
 few_down_kernel(const FewParams p)
@@ -509,20 +510,21 @@ few_down_kernel(const FewParams p)
     few_make_lists(p, l);
     const int32_t warp = static_cast<int32_t>(threadIdx.x >> 5);
     const uint32_t lane = threadIdx.x & 31u, q = lane & 3u, m = lane >> 2;
-    const int32_t r0 = static_cast<int32_t>(blockIdx.x) * 16 + static_cast<int32_t>(m), chunks = (p.w.depth + kFewChunk - 1) / kFewChunk;
+    const int32_t rank = p.ranks > 1 ? static_cast<int32_t>(cluster_ctarank()) : 0, out0 = static_cast<int32_t>(blockIdx.x) / p.ranks * 16;
+    const int32_t r0 = out0 + static_cast<int32_t>(m), chunks = (p.w.depth + kFewChunk - 1) / kFewChunk;
     const int32_t row0 = r0 < p.w.rows ? r0 : 0, row1 = r0 + 8 < p.w.rows ? r0 + 8 : 0;
     // rounds of an entry per warp; those left over are shared by several warps
-    const int32_t entries = *l.total, rounds = entries / kWarps, rest = entries - rounds * kWarps;
+    const int32_t entries = *l.total, all = kWarps * p.ranks, rounds = entries / all, rest = entries - rounds * all;
     int32_t rest_slices = 1;
-    while (rest_slices * 2 <= p.most_slices && rest * rest_slices * 2 <= kWarps) rest_slices *= 2;
-    const int32_t my_rounds = rounds + (warp < rest * rest_slices ? 1 : 0);
+    while (rest_slices * 2 <= p.most_slices && (rest + p.ranks - 1) / p.ranks * rest_slices * 2 <= kWarps) rest_slices *= 2;
+    const int32_t my_rounds = rounds + (warp / rest_slices * p.ranks + rank < rest ? 1 : 0);
     struct Work {
         int32_t expert, first, count, slice;
     };
     auto work_of = [&](int32_t round) {
         Work t;
         const bool whole = round < rounds;
-        const int32_t entry = whole ? round * kWarps + warp : rounds * kWarps + warp / rest_slices;
+        const int32_t entry = (whole ? round * all + warp * p.ranks : rounds * all + warp / rest_slices * p.ranks) + rank;
         t.slice = whole ? 0 : warp % rest_slices;
         t.expert = static_cast<int32_t>(l.entry[2 * entry]);
         t.first = static_cast<int32_t>(l.entry[2 * entry + 1] & 0xffffu);
@@ -595,19 +597,51 @@ few_down_kernel(const FewParams p)
             }
         }
     }
+    // places are not needed any more: whose sums a choice has
+    for (int32_t i = static_cast<int32_t>(threadIdx.x); i < entries; i += kFewDownThreads) {
+        const uint32_t e = l.entry[2 * i + 1];
+        for (uint32_t k = 0; k < e >> 16; ++k) l.rank[l.list[(e & 0xffffu) + k]] = static_cast<uint16_t>(i % p.ranks);
+    }
     __syncthreads();
-    for (int32_t o = static_cast<int32_t>(threadIdx.x); o < p.tokens * 16; o += kFewDownThreads) {
-        const int32_t t = o >> 4, r = o & 15, row = static_cast<int32_t>(blockIdx.x) * 16 + r;
+    if (rest_slices > 1) {                                        // the slices of this CTA's own
+        for (int32_t i = static_cast<int32_t>(threadIdx.x); i < p.choices * 16; i += kFewDownThreads) {
+            if (l.expert[i >> 4] == kFewNone || l.rank[i >> 4] != rank) continue;
+            float v = part[i];
+            for (int32_t s = 1; s < rest_slices; ++s) v += part[s * p.choices * 16 + i];
+            part[i] = v;
+        }
+        __syncthreads();
+    }
+    if (p.ranks > 1) {
+        cluster_arrive();
+        cluster_wait();
+    }
+    for (int32_t o = rank * kFewDownThreads + static_cast<int32_t>(threadIdx.x); o < p.tokens * 16; o += p.ranks * kFewDownThreads) {
+        const int32_t t = o >> 4, r = o & 15, row = out0 + r;
         if (row >= p.w.rows) continue;
         float sum = 0.0f;
-        for (int32_t j = 0; j < p.top_k; ++j) {
-            const int32_t c = t * p.top_k + j;
-            if (l.expert[c] == kFewNone) continue;
-            float v = 0.0f;
-            for (int32_t s = 0; s < rest_slices; ++s) v += part[(s * p.choices + c) * 16 + r];
-            sum = fmaf(s_weight[c], v, sum);
+        for (int32_t j0 = 0; j0 < p.top_k; j0 += 4) {
+            float v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int32_t c = t * p.top_k + min(j0 + j, p.top_k - 1);
+                const bool there = j0 + j < p.top_k && l.expert[c] != kFewNone;
+                v[j] = 0.0f;
+                if (there && p.ranks > 1) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[j]) : "r"(mapa(smem_addr(part + c * 16 + r), l.rank[c])) : "memory");
+                else if (there) v[j] = part[c * 16 + r];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int32_t c = t * p.top_k + min(j0 + j, p.top_k - 1);
+                if (j0 + j < p.top_k && l.expert[c] != kFewNone) sum = fmaf(s_weight[c], v[j], sum);
+            }
         }
         static_cast<T *>(p.y)[t * p.ldy + row] = narrow_to<T>(sum);
+    }
+    __syncwarp();
+    if (p.ranks > 1) {                                            // no CTA leaves while another reads its sums
+        cluster_arrive();
+        cluster_wait();
     }
 }
 

@@ -70,8 +70,8 @@ def formula(x, w1, w2, indices, weights, gated, bits=16):
     """(y, bound of the error before y's rounding) in 64 bits.
 
     `bits`: what h is rounded to (2^-bits: a half step, and the factors' products; an fp16 weight against h loses the product of two second parts, as much
-    again); None: x and h are sums of digits, off by at most 2^-19 of their largest magnitude.  The contraction over `hidden` adds H numbers in 32 bits (2^-23 of their magnitudes each covers truncation; with digits, eight times as many, and
-    8 more); silu changes by at most 1.1 times its argument's error, and its exponential is off by 2^-21 (2 + |u|) of itself; then I, and k, numbers are added."""
+    again); None: x and h are sums of digits, off by at most 2^-19 of their largest magnitude.  The contraction over `hidden` adds H numbers in 32
+    bits (2^-23 of their magnitudes each covers truncation; with digits, eight times as many, and 8 more); silu changes by at most 1.1 times its argument's error, and its exponential is off by 2^-21 (2 + |u|) of itself; then I, and k, numbers are added."""
     digits = bits is None
     many, lost = (8, 2.0 ** -19) if digits else (1, 0.0)
     T, H = x.shape
@@ -161,6 +161,16 @@ def test_choices_outside_twice_and_none(ctx, kind, dtype):
 def test_most_choices(ctx, kind, dtype):
     case(ctx, kind, dtype, 64, 64, 48, 40, 32, True)
     case(ctx, kind, dtype, 64, 48, 40, 1, 32, False, indices=np.zeros((64, 32), np.int64))
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("T,k,E,H,I", [(1, 3, 5, 40, 300), (2, 1, 4, 24, 500), (61, 7, 50, 24, 200), (64, 5, 9, 600, 33), (20, 6, 40, 1200, 65)])
+def test_few_outputs_for_many_choices(ctx, kind, dtype, T, k, E, H, I):
+    """Outputs that several CTAs share, by one choice each and by more than their warps take at once; numbers of choices that are not multiples of
+    anything, some of them of no expert."""
+    r = rng("few outputs", T, k, E)
+    indices = np.where(r.random((T, k)) < 0.1, -1, r.integers(0, E, (T, k)))
+    case(ctx, kind, dtype, T, H, I, E, k, False, indices=indices)
 
 
 def test_many_experts_and_rounds(ctx):
