@@ -273,6 +273,44 @@ def test_captured_replayed_and_at_once(ctx):
         assert torch.equal(got[0], ys[0]) and torch.equal(got[1], ys[0])
 
 
+@pytest.mark.parametrize("kind", ["nvfp4", "mxfp4", "bf16"])
+def test_steps_in_a_row(ctx, kind):
+    """The router's choices, the weights and x are overwritten right ahead of each step and right behind it, by kernels that start before the ones ahead of them end:
+    the bits of steps that wait for each other."""
+    T, H, I, E, k, N = 16, 512, 256, 16, 4, 12
+    g = torch.Generator(device="cuda").manual_seed(5)
+    draw = lambda *s: torch.randn(*s, generator=g, device="cuda")  # noqa: E731
+    w1s, w2s, ls, xs = [draw(E, 2 * I, H) * H ** -0.5 for _ in range(3)], [draw(E, H, I) * I ** -0.5 for _ in range(3)], [draw(T, E) for _ in range(N)], [draw(T, H).bfloat16() for _ in range(N)]
+    if kind == "bf16":
+        held = [torch.empty(E, 2 * I, H, dtype=torch.bfloat16, device="cuda"), torch.empty(E, H, I, dtype=torch.bfloat16, device="cuda")]
+    else:
+        held = [(*fp4.empty_rows(*s, format=kind), torch.ones(E, device="cuda") if kind == "nvfp4" else None) for s in ((E, 2 * I, H), (E, H, I))]
+    router, layer = routing.Router(ctx, E, k, score="softmax", renormalize=True), few_tokens.Layer(ctx, H, I, E, k, weights=kind)
+    weights, indices, x, scratch = torch.empty(T, k, device="cuda"), torch.empty(T, k, dtype=torch.int32, device="cuda"), torch.empty(T, H, dtype=torch.bfloat16, device="cuda"), layer.empty_scratch(T)
+
+    def step(n, y, wait):
+        for w, h in ((w1s[n % 3], held[0]), (w2s[n % 3], held[1])):
+            if kind == "bf16":
+                h.copy_(w)
+            else:
+                fp4.quantize_rows(ctx, w, h[0], h[1], factor=h[2], format=kind)
+        x.copy_(xs[n])
+        wait()
+        router.forward(ls[n], weights, indices)
+        wait()
+        layer.run(x, *held, indices, weights, y, scratch)
+        wait()
+
+    ys, zs = [torch.empty_like(x) for _ in range(N)], [torch.empty_like(x) for _ in range(N)]
+    for n in range(N):
+        step(n, ys[n], torch.cuda.synchronize)
+    for _ in range(5):
+        for n in range(N):
+            step(n, zs[n], lambda: None)
+        assert all(torch.equal(a, b) for a, b in zip(ys, zs))
+    assert ctx.last_device_status()[0] == hgemm.OK
+
+
 def test_no_tokens(ctx):
     layer = few_tokens.Layer(ctx, 64, 64, 2, 1, weights="bf16", dtype=torch.bfloat16, activation="silu")
     w = torch.zeros(2, 64, 64, dtype=torch.bfloat16, device="cuda")
