@@ -125,6 +125,7 @@ constexpr uint32_t kMantissa6 = 0x400000u, kMantissa2688 = 0x280000u;        // 
 struct BlockStep {
     uint32_t byte;             // the scale
     float step, inverse;       // what values are divided by, and its reciprocal (0 where values are 0)
+    bool far;                  // the block's largest quotient is beyond fp32 (NV: a factor much smaller than the block's values ask for)
 };
 
 // amax: NaN for a block with a NaN or an infinity.  g = 1 / factor (NV).
@@ -138,13 +139,29 @@ __device__ __forceinline__ BlockStep block_step(float amax, float factor, float 
         const float step = __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(s.byte), __NV_E4M3))) * factor;
         s.step = step > 0.0f ? step : 0.0f;                      // (a NaN: the block's zeros stay zeros)
         s.inverse = step > 0.0f ? __frcp_rn(step) : 0.0f;
+        s.far = amax * s.inverse > 3.402823466e38f;
     } else {
         const int32_t e = min(max(power_above(amax, 2, kMantissa6), 0), 254);
         s.byte = amax != amax ? 255u : static_cast<uint32_t>(e);
         s.step = 0.0f;
         s.inverse = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);   // 2^(127 - e), exactly (e = 254: below the smallest normal number; no finite block has it)
+        s.far = false;
     }
     return s;
+}
+
+// 16 elements of a block that has quotients beyond fp32: those would be infinities, of which the residual step makes NaN, whose sign is lost.  What lies beyond 8 steps has
+// the value of 8 steps: the largest, with its sign.
+template <bool NV>
+__device__ __forceinline__ void bring_near(float (&f)[16], const BlockStep &s)
+{
+    if constexpr (NV) {
+        if (s.far) {
+            const float most = 8.0f * s.step;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) f[i] = fminf(fmaxf(f[i], -most), most);
+        }
+    }
 }
 
 // Eight quotients as 4-bit values in a word.
@@ -305,6 +322,7 @@ fp4_quantize_kernel(const Fp4QuantParams p)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) two_floats(raw[i].w[j], f[2 * j], f[2 * j + 1], T());
                 }
+                bring_near<NV>(f, s);
                 const uint2 v = make_uint2(quantize8<NV>(f, s), quantize8<NV>(f + 8, s));
                 const int64_t r = row0 + k;
                 if (whole) {
@@ -348,6 +366,8 @@ fp4_quantize_kernel(const Fp4QuantParams p)
                     float f[16], h[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) two_floats(w[16 * k + j], f[j], h[j], T());
+                    bring_near<NV>(f, s_lo);
+                    bring_near<NV>(h, s_hi);
                     lo[k] = make_uint2(quantize8<NV>(f, s_lo), quantize8<NV>(f + 8, s_lo));
                     hi[k] = make_uint2(quantize8<NV>(h, s_hi), quantize8<NV>(h + 8, s_hi));
                     byte_lo[k] = s_lo.byte;
@@ -359,13 +379,13 @@ fp4_quantize_kernel(const Fp4QuantParams p)
 #pragma unroll 1
                 for (uint32_t i = 0; i < 2; ++i) {
                     const uint32_t c = threadIdx.x & 127u, part = (threadIdx.x >> 7) + 2u * i;
-                    float f[32];
+                    float f[2][16];
                     uint32_t m[2] = {0u, 0u};
 #pragma unroll
                     for (int j = 0; j < 32; ++j) {
                         const uint32_t w = *reinterpret_cast<const uint32_t *>(s_raw + (part * 32u + j) * kPitch + c * 4u);
                         m[j / 16] = magnitude_max<T>(m[j / 16], w);
-                        f[j] = __uint_as_float(w);
+                        f[j / 16][j % 16] = __uint_as_float(w);
                     }
                     if constexpr (!NV) m[0] = m[1] = max(m[0], m[1]);
                     uint2 v[2];
@@ -373,7 +393,8 @@ fp4_quantize_kernel(const Fp4QuantParams p)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
                         const BlockStep s = block_step<NV>(magnitude_of(m[k], T()), factor, g);
-                        v[k] = make_uint2(quantize8<NV>(f + 16 * k, s), quantize8<NV>(f + 16 * k + 8, s));
+                        bring_near<NV>(f[k], s);
+                        v[k] = make_uint2(quantize8<NV>(f[k], s), quantize8<NV>(f[k] + 8, s));
                         byte[k] = s.byte;
                     }
                     put(v, c, part, byte[0], byte[1]);

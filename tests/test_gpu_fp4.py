@@ -415,6 +415,22 @@ def test_quantise_extremes(ctx):
             check_copy(q, s, x.numpy(), fmt, factor, what=f"{fmt} {factor}")
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("factor", [2.0 ** -100, 2.0 ** -60, 1.5 * 2.0 ** -80])
+def test_quantise_far_beyond_the_factor(ctx, dtype, factor):
+    """A factor kept from smaller values: quotients beyond fp32 are 6 with their own sign, and the small values of such a block what they are elsewhere."""
+    r = rng(str(dtype), factor)
+    big = r.choice([-1e38, -1e25, -1e12, 1e12, 1e25, 1e38, -float(torch.finfo(torch.bfloat16).max)], (150, 200))
+    small = r.choice([-7.0, -6.0, -5.0, -2.5, -0.25, 0.0, 0.25, 0.75, 1.75, 3.5, 9.0], (150, 200)) * 448.0 * np.float32(factor)
+    x = torch.from_numpy(np.where(r.random((150, 200)) < 0.5, big, small)).to(dtype)
+    x64 = ref.f64(x)
+    f = torch.tensor([factor], dtype=torch.float32, device="cuda")
+    both = empty_copy((150, 200), (150, 200), "nvfp4"), empty_copy((200, 150), (200, 150), "nvfp4")
+    fp4.quantize_both(ctx, x.cuda(), *both[0], *both[1], factor=f)
+    check_copy(*both[0], x64.astype(np.float32), "nvfp4", factor, what="rows")
+    check_copy(*both[1], np.ascontiguousarray(x64.T).astype(np.float32), "nvfp4", factor, what="columns")
+
+
 @pytest.mark.parametrize("dtype", OUTS, ids=str)
 def test_tensor_factor(ctx, dtype):
     for rows, cols, n in ((1, 1, 1), (7, 77, 1), (24, 4096, 1), (300, 128, 5), (1500, 1000, 1), (2048, 512, 3)):
