@@ -85,7 +85,7 @@ struct Fp4Params {
 // swizzled as TMA reads them: conflict-free), which leaves as a tensor store while the warp goes on.  A warp whose rows end inside its 32
 // (a group's end) stores 16 bytes a lane; rows of C that are not multiples of 16 bytes, and C +=, take ordinary stores of 4 bytes a lane.
 template <class T>
-__device__ __forceinline__ void fp4_store_box(const uint32_t *v, float alpha, uint32_t staging, const Fp4Params &p, const CUtensorMap *tmap_c, const ProductTile &t, int32_t row0,
+__device__ __forceinline__ void fp4_store_box(const uint32_t *v, float2 alpha, uint32_t staging, const Fp4Params &p, const CUtensorMap *tmap_c, const ProductTile &t, int32_t row0,
                                               int32_t col, uint32_t lane)
 {
     constexpr int kSize = static_cast<int>(sizeof(T));
@@ -98,8 +98,8 @@ __device__ __forceinline__ void fp4_store_box(const uint32_t *v, float alpha, ui
         uint32_t h[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if constexpr (kSize == 4) h[i] = __float_as_uint(__uint_as_float(v[4 * j + i]) * alpha);
-            else h[i] = pack_pair(__uint_as_float(v[8 * j + 2 * i]) * alpha, __uint_as_float(v[8 * j + 2 * i + 1]) * alpha, T());
+            if constexpr (kSize == 4) h[i] = __float_as_uint(__uint_as_float(v[4 * j + i]) * alpha.x * alpha.y);
+            else h[i] = pack_pair(__uint_as_float(v[8 * j + 2 * i]) * alpha.x * alpha.y, __uint_as_float(v[8 * j + 2 * i + 1]) * alpha.x * alpha.y, T());
         }
         st_shared_v4(mine + ((j ^ swz) * 16u), h[0], h[1], h[2], h[3]);
     }
@@ -163,6 +163,15 @@ __device__ __forceinline__ void fp4_store_box(const uint32_t *v, float alpha, ui
             }
         }
     }
+}
+
+// The operands' factors: 1 and their product, or, where that is no normal number of fp32 (the result may be one all the same: sums reach from 2^-20 to 2^43), the larger one
+// and the smaller.  Sums are multiplied by one after the other.
+__device__ __forceinline__ float2 fp4_factors(const Fp4Params &p, int32_t group)
+{
+    const float a = p.fp ? p.fp[p.fp_group ? group : 0] : 1.0f, b = p.fq ? p.fq[p.fq_group ? group : 0] : 1.0f, both = a * b;
+    if (fabsf(both) >= 1.17549435e-38f && fabsf(both) <= 3.402823466e38f) return make_float2(1.0f, both);
+    return fabsf(a) > fabsf(b) ? make_float2(a, b) : make_float2(b, a);
 }
 
 // One element of a result of type out_type.
@@ -419,7 +428,7 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         for (int32_t w = unit; w < total; w += units) {
             const ProductTile t = tile_of(w);
             const int32_t kbn = __shfl_sync(0xffffffffu, t.kbn, 0);
-            const float alpha = (p.fp ? p.fp[p.fp_group ? t.group : 0] : 1.0f) * (p.fq ? p.fq[p.fq_group ? t.group : 0] : 1.0f);
+            const float2 alpha = fp4_factors(p, t.group);
             const uint32_t d = n & 1u;
             if (kbn > 0) {
                 if (!mbar_wait_warp(bar_tfull + 8 * d, (n >> 1) & 1u, ctl, status_code(kRoleFp4Store, 0, d))) break;
@@ -476,7 +485,7 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
                     o[j] = __uint_as_float(v[j * kDigits]);
 #pragma unroll
                     for (int i = 1; i < kDigits; ++i) o[j] += __uint_as_float(v[j * kDigits + i]);
-                    o[j] *= alpha;
+                    o[j] = o[j] * alpha.x * alpha.y;
                 }
                 if (p.split > 1) {
                     // this slice's part where the operand stages were (every MMA that read them is complete): columns of 128 rows, 132 words apart

@@ -155,6 +155,33 @@ def test_several_waves_of_tiles(ctx, fmt):
             assert torch.equal(out, want.to(out_dtype)), (config, out_dtype)
 
 
+@pytest.mark.parametrize("config", [(2, 256, 1), (2, 128, 1), (1, 64, 1), (1, 128, 4)], ids=str)
+@pytest.mark.parametrize("fa,fb,small", [(-80, -80, False), (-99, -40, False), (-40, -99, False), (70, 60, True), (60, 70, True), (125, -126, False)])
+def test_factors_whose_product_leaves_fp32(ctx, config, fa, fb, small):
+    """Results are numbers where the product of the factors alone is none; rows of zeros stay zeros."""
+    M, N, K = 140, 200, 390
+    r = rng(config, fa, fb)
+    a, b = Operand(r, (M, K), "nvfp4", integers=True), Operand(r, (N, K), "nvfp4", integers=True)
+    scale = 1 if small else 0x7E                                    # 2^-9, or 448
+    values = []
+    for o, rows, e in ((a, M, fa), (b, N, fb)):
+        code = np.where(r.random((rows, 1)) < 0.1, 0, r.integers(0, 16, (rows, K))).astype(np.uint8)
+        o.q = on_gpu(ref.pack(code), 16, 0x77)
+        o.tiles = torch.from_numpy(ref.tiles_from(np.full((rows, ref.blocks(K, "nvfp4")), scale, np.uint8), "nvfp4")).cuda()
+        factor = np.float32(1.1) * np.float32(2.0) ** np.float32(e)
+        o.factor = torch.tensor([factor], device="cuda")
+        values.append(ref.decode(code) * ref.E4M3[scale] * float(factor))
+    for out_dtype in (torch.float32, torch.bfloat16):
+        buf, out = guarded((M, N), out_dtype)
+        with fp4.Plan(ctx, M, N, K, out_dtype=out_dtype) as plan:
+            plan.set_config(*config)
+            plan.run(a.q, a.tiles, b.q, b.tiles, out, a_factor=a.factor, b_factor=b.factor)
+            assert plan.last_device_status()[0] == hgemm.OK
+        untouched(buf, out)
+        ref.check_product(out, *values, f"{config} 2^{fa} 2^{fb}")
+        assert bool((out != 0).any())
+
+
 def test_launches_in_a_row_and_at_once(ctx):
     """Launches that follow one another without a pause, and two streams at once: the same bits each time."""
     M, N, K = 70, 500, 640
