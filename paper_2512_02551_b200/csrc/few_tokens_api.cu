@@ -69,7 +69,7 @@ const void *down_kernel(int align)
 
 hgemm_status_t launch(hgemm_ctx_s *ctx, const void *fn, dim3 grid, int threads, int smem, void *params, void *stream, int cluster = 1)
 {
-    if (smem > 48 * 1024) {
+    if (smem > 40 * 1024) {                      // what a kernel may have unasked, 48 KB, counts its static shared memory too (few_up_kernel: 4160 bytes)
         const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return cuda_fail(ctx, e);
     }

@@ -2,6 +2,9 @@
 
 Results sit inside guard bands, x's and the weights' rows inside NaN; the tolerance follows from the arithmetic (see ``check``)."""
 import ctypes
+import os
+import subprocess
+import sys
 import zlib
 
 import numpy as np
@@ -177,6 +180,25 @@ def test_many_experts_and_rounds(ctx):
     """More tiles than warps: every warp walks on to further experts."""
     case(ctx, "nvfp4", "bf16", 24, 512, 1024, 96, 8, True)
     case(ctx, "f16", "f16", 24, 512, 1024, 64, 4, False)
+
+
+FIRST_CALL = """
+import sys
+sys.path[:0] = %r
+import test_gpu_few_tokens as few
+from paper_2512_02551_b200 import hgemm
+with hgemm.Context(0) as ctx:
+    few.case(ctx, *%r)
+"""
+
+
+@pytest.mark.parametrize("kind,T,k,E,H", [("bf16", 1, 2, 4, 2688), ("f16", 1, 2, 4, 2700), ("bf16", 2, 3, 5, 2816), ("bf16", 1, 1, 1, 2880), ("f16", 1, 2, 4, 2944), ("bf16", 16, 8, 128, 2624)])
+def test_a_process_first_call(kind, T, k, E, H):
+    """Sizes around the shared memory that a kernel has without asking, each as the first call of a process: nothing has raised the limit before."""
+    args = (kind, kind, T, H, 24, E, k, False)
+    here = os.path.dirname(os.path.abspath(__file__))
+    done = subprocess.run([sys.executable, "-c", FIRST_CALL % ([here, os.path.dirname(here)], args)], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
 
 
 def test_infinite_and_nan_inputs_stay_in_their_token(ctx):
