@@ -69,10 +69,6 @@ const void *down_kernel(int align)
 
 hgemm_status_t launch(hgemm_ctx_s *ctx, const void *fn, dim3 grid, int threads, int smem, void *params, void *stream, int cluster = 1)
 {
-    if (smem > 40 * 1024) {                      // what a kernel may have unasked, 48 KB, counts its static shared memory too (few_up_kernel: 4160 bytes)
-        const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return cuda_fail(ctx, e);
-    }
     cudaLaunchConfig_t lc;
     std::memset(&lc, 0, sizeof(lc));
     lc.gridDim = grid;
@@ -112,9 +108,32 @@ struct Call {
     void *stream;
 };
 
+// Shared memory of the second launch: lists, the choices' weights, slices of 16 sums a choice.
+constexpr int down_smem(int experts, int choices, int slices) { return hgemm_dev::few_list_bytes(experts, choices) + 4 * ((choices + 3) & ~3) + slices * choices * 64; }
+
+// Once a context and type: the shared memory that any call may ask for.  The limit is the kernel's, whoever launches it: it is never lowered, so that a call on another thread is not
+// refused.  (What a kernel may have unasked, 48 KB, counts its static shared memory too.)
+template <class T>
+hgemm_status_t prepare16(hgemm_ctx_s *ctx)
+{
+    constexpr int kLists = hgemm_dev::few_list_bytes(1024, hgemm_dev::kFewMaxChoices), kDown = down_smem(1024, hgemm_dev::kFewMaxChoices, 1);
+    static_assert(kLists + kMaxX <= 100 * 1024 && kDown <= 224 * 1024, "shared memory of a CTA");
+    for (const int align : {16, 4, 2}) {
+        cudaError_t e = cudaFuncSetAttribute(up_kernel<T>(align), cudaFuncAttributeMaxDynamicSharedMemorySize, kLists + kMaxX);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(down_kernel<T>(align), cudaFuncAttributeMaxDynamicSharedMemorySize, kDown);
+        if (e != cudaSuccess) return cuda_fail(ctx, e);
+    }
+    ctx->few16_ready[std::is_same<T, __half>::value ? 0 : 1] = true;
+    return HGEMM_OK;
+}
+
 hgemm_status_t run16(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &c, const hgemm_expert_weights_t &w1, const hgemm_expert_weights_t &w2)
 {
     const bool half = d.type == HGEMM_TYPE_F16;
+    if (!ctx->few16_ready[half ? 0 : 1]) {
+        const hgemm_status_t st = half ? prepare16<__half>(ctx) : prepare16<__nv_bfloat16>(ctx);
+        if (st != HGEMM_OK) return st;
+    }
     FewParams p;
     std::memset(&p, 0, sizeof(p));
     p.gated = d.activation == HGEMM_ACT_SWIGLU ? 1 : 0;
@@ -155,7 +174,7 @@ hgemm_status_t run16(hgemm_ctx_s *ctx, const hgemm_few_tokens_t &d, const Call &
     p.ranks = 1;
     while (p.ranks < 8 && tiles * p.ranks * 2 <= ctx->num_sms && p.ranks * 4 <= p.choices) p.ranks *= 2;
     return launch(ctx, half ? down_kernel<__half>(p.w.align) : down_kernel<__nv_bfloat16>(p.w.align), dim3(unsigned(tiles * p.ranks)), hgemm_dev::kFewDownThreads,
-                  lists + 4 * ((p.choices + 3) & ~3) + p.most_slices * p.choices * 64, &p, c.stream, p.ranks);
+                  down_smem(p.experts, p.choices, p.most_slices), &p, c.stream, p.ranks);
 }
 
 // ---- 4-bit weights -------------------------------------------------------------------------------------------------

@@ -31,7 +31,8 @@ struct hgemm_ctx_s {
     encode_tiled_fn encode = nullptr;
     int last_cuda_error = 0;
     bool dependent_launch = true;
-    std::atomic<bool> few_ready{false};            // the few-token kernels' attributes are set
+    std::atomic<bool> few_ready{false};            // the few-token kernels' attributes are set: 4-bit weights
+    std::atomic<bool> few16_ready[2] = {};         // fp16, bf16 weights
     bool tma_3d = true;
     std::vector<hgemm_plan_s *> plans;
     std::vector<hgemm_fp8_plan_s *> fp8_plans;

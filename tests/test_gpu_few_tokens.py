@@ -5,6 +5,7 @@ import ctypes
 import os
 import subprocess
 import sys
+import threading
 import zlib
 
 import numpy as np
@@ -199,6 +200,36 @@ def test_a_process_first_call(kind, T, k, E, H):
     here = os.path.dirname(os.path.abspath(__file__))
     done = subprocess.run([sys.executable, "-c", FIRST_CALL % ([here, os.path.dirname(here)], args)], capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, done.stderr[-2000:]
+
+
+def test_threads_with_contexts_of_their_own():
+    """Calls of different sizes from two threads, each with its own context, stream and scratch memory: none changes what the other's launch may have."""
+    H, I, E, k, N = 64, 32, 16, 8, 20000
+    m1, m2 = (torch.randn(*s, device="cuda").bfloat16() for s in ((E, I, H), (E, H, I)))
+    torch.cuda.synchronize()
+    refused, gate = [], threading.Barrier(2)
+
+    def decode(T):
+        stream = torch.cuda.Stream()
+        with hgemm.Context(0) as own, torch.cuda.stream(stream):
+            layer = few_tokens.Layer(own, H, I, E, k, weights="bf16", activation="silu")
+            x, scratch = torch.ones(T, H, device="cuda").bfloat16(), layer.empty_scratch(T)
+            idx, w, y = (torch.arange(T * k, device="cuda") % E).int().view(T, k), torch.ones(T, k, device="cuda"), torch.empty_like(x)
+            p = ctypes.c_void_p
+            ws = [few_tokens.Weights(m.data_ptr(), m.stride(1), None, None) for m in (m1, m2)]
+            args = [own._h, ctypes.byref(layer._desc), ctypes.c_int64(T), p(x.data_ptr()), ctypes.c_int64(H), ctypes.byref(ws[0]), ctypes.byref(ws[1]), p(idx.data_ptr()), p(w.data_ptr()),
+                    p(y.data_ptr()), ctypes.c_int64(H), p(scratch.data_ptr()), ctypes.c_int64(scratch.numel()), p(stream.cuda_stream)]
+            call = few_tokens.lib().hgemm_few_tokens               # the calls themselves, so that they meet
+            gate.wait()
+            refused.append(sum(call(*args) != hgemm.OK for _ in range(N)))
+            stream.synchronize()
+
+    threads = [threading.Thread(target=decode, args=(T,)) for T in (16, 32)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert refused == [0, 0], f"refused calls of {N} each: {refused}"
 
 
 def test_infinite_and_nan_inputs_stay_in_their_token(ctx):
