@@ -191,9 +191,9 @@ few_digits_kernel(const DigitParams p)
     int32_t position = 0, place = 0;
     float u_factor = 1.0f;
     if constexpr (!FIRST) {                                       // the first kernel's, which the product has waited for
-        position = p.position[c];
-        place = p.place[c];
-        if (position >= 0) u_factor = p.u_factor[position];
+        position = ld_older(p.position + c);
+        place = ld_older(p.place + c);
+        if (position >= 0) u_factor = ld_older(p.u_factor + position);
     }
     grid_dependency_wait();
     grid_launch_dependents();                                     // from here on the product may read the call's inputs (fp4_digits_product)
@@ -301,10 +301,10 @@ few_combine_kernel(const CombineParams p)
     int32_t mine = -1;
     float w = 0.0f;
     if (lane < p.top_k) {
-        mine = p.position[t * p.top_k + lane];
-        w = p.weights[t * p.top_k + lane];
+        mine = ld_older(p.position + t * p.top_k + lane);
+        w = ld_older(p.weights + t * p.top_k + lane);
     }
-    const float s = mine >= 0 ? p.factor[mine] : 0.0f;
+    const float s = mine >= 0 ? ld_older(p.factor + mine) : 0.0f;
     grid_dependency_wait();
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int32_t j0 = 0; j0 < p.top_k; j0 += 8) {

@@ -99,7 +99,7 @@ __device__ __forceinline__ void few_make_lists(const FewParams &p, const FewList
     const int32_t threads = static_cast<int32_t>(blockDim.x), me = static_cast<int32_t>(threadIdx.x);
     for (int32_t e = me; e < p.experts; e += threads) l.count[e] = 0u;
     for (int32_t c = me; c < ((p.choices + 7) & ~7); c += threads) {
-        const int32_t e = c < p.choices ? p.indices[c] : -1;
+        const int32_t e = c < p.choices ? ld_older(p.indices + c) : -1;
         l.expert[c] = static_cast<uint16_t>(e >= 0 && e < p.experts ? e : kFewNone);
     }
     __syncthreads();
@@ -206,6 +206,26 @@ __device__ __forceinline__ uint4 few_load16(const uint8_t *p)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             asm volatile("{\n\t.reg .b16 a, b;\n\tld.global.u16 a, [%1];\n\tld.global.u16 b, [%1 + 2];\n\tmov.b32 %0, {a, b};\n\t}" : "=r"(w[i]) : "l"(p + 4 * i));
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return v;
+}
+
+// The same ahead of the kernel's own wait (see ld_older).
+template <int ALIGN>
+__device__ __forceinline__ uint4 few_load16_older(const uint8_t *p)
+{
+    uint4 v;
+    if constexpr (ALIGN == 16) {
+        asm volatile("ld.relaxed.gpu.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    } else if constexpr (ALIGN == 4) {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(p);
+        v = make_uint4(ld_older(w), ld_older(w + 1), ld_older(w + 2), ld_older(w + 3));
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            asm volatile("{\n\t.reg .b16 a, b;\n\tld.relaxed.gpu.global.u16 a, [%1];\n\tld.relaxed.gpu.global.u16 b, [%1 + 2];\n\tmov.b32 %0, {a, b};\n\t}" : "=r"(w[i]) : "l"(p + 4 * i) : "memory");
         v = make_uint4(w[0], w[1], w[2], w[3]);
     }
     return v;
@@ -506,7 +526,7 @@ few_down_kernel(const FewParams p)
     const FewLists l = few_lists(smem, p);
     float *s_weight = reinterpret_cast<float *>(smem + few_list_bytes(p.experts, p.choices)), *part = s_weight + ((p.choices + 3) & ~3);
     grid_launch_dependents();
-    for (int32_t c = static_cast<int32_t>(threadIdx.x); c < p.choices; c += kFewDownThreads) s_weight[c] = p.weights[c];      // inputs of the call: launch 1 has waited for them
+    for (int32_t c = static_cast<int32_t>(threadIdx.x); c < p.choices; c += kFewDownThreads) s_weight[c] = ld_older(p.weights + c);      // inputs of the call: launch 1 has waited for them
     few_make_lists(p, l);
     const int32_t warp = static_cast<int32_t>(threadIdx.x >> 5);
     const uint32_t lane = threadIdx.x & 31u, q = lane & 3u, m = lane >> 2;
@@ -548,8 +568,8 @@ few_down_kernel(const FewParams p)
         if (span.n >= kFewAhead) {                                // the weights' first chunks: those of h are not there yet
 #pragma unroll
             for (int u = 0; u < kFewAhead; ++u) {
-                raw[u].v[0] = few_load16<ALIGN>(span.row[0] + u * 64);
-                raw[u].v[1] = few_load16<ALIGN>(span.row[1] + u * 64);
+                raw[u].v[0] = few_load16_older<ALIGN>(span.row[0] + u * 64);
+                raw[u].v[1] = few_load16_older<ALIGN>(span.row[1] + u * 64);
             }
         }
     }

@@ -169,7 +169,7 @@ __device__ __forceinline__ void fp4_store_box(const uint32_t *v, float2 alpha, u
 // and the smaller.  Sums are multiplied by one after the other.
 __device__ __forceinline__ float2 fp4_factors(const Fp4Params &p, int32_t group)
 {
-    const float a = p.fp ? p.fp[p.fp_group ? group : 0] : 1.0f, b = p.fq ? p.fq[p.fq_group ? group : 0] : 1.0f, both = a * b;
+    const float a = p.fp ? ld_older(p.fp + (p.fp_group ? group : 0)) : 1.0f, b = p.fq ? ld_older(p.fq + (p.fq_group ? group : 0)) : 1.0f, both = a * b;
     if (fabsf(both) >= 1.17549435e-38f && fabsf(both) <= 3.402823466e38f) return make_float2(1.0f, both);
     return fabsf(a) > fabsf(b) ? make_float2(a, b) : make_float2(b, a);
 }
@@ -234,7 +234,7 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
 
     int32_t mine = -1;                                            // a choice's group, on its way during the set-up
     if constexpr (DIGITS) {
-        if (static_cast<int32_t>(threadIdx.x) < p.choices) mine = p.indices[threadIdx.x];
+        if (static_cast<int32_t>(threadIdx.x) < p.choices) mine = ld_older(p.indices + threadIdx.x);
     } else {
         grid_launch_dependents();
     }
@@ -261,7 +261,7 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
         for (int32_t e = static_cast<int32_t>(threadIdx.x); e <= p.groups; e += kFp4Threads) off[e] = 0;
         __syncthreads();
         for (int32_t c = static_cast<int32_t>(threadIdx.x); c < p.choices; c += kFp4Threads) {
-            const int32_t e = c < kFp4Threads ? mine : p.indices[c];
+            const int32_t e = c < kFp4Threads ? mine : ld_older(p.indices + c);
             if (e >= 0 && e < p.groups) atomicAdd(&off[e + 1], kDigits);
         }
         __syncthreads();
@@ -322,6 +322,7 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             if (unit < total) {
                 const ProductTile t = tile_of(unit);
                 ahead = min(t.kbn, 2 * p.stages);
+                fence_proxy_async_all();
                 for (int32_t kb = 0; kb < ahead; kb += 2) {
                     const uint32_t fb = bar_full + 4 * kb, p_dst = smem_base + static_cast<uint32_t>(kb / 2) * kOperandBytes, sp_dst = scale_base + static_cast<uint32_t>(kb / 2) * (kSpBytes + kSqBytes);
                     mbar_arrive_expect_tx_elect(fb, kStageBytes);
@@ -433,6 +434,7 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
             if (kbn > 0) {
                 if (!mbar_wait_warp(bar_tfull + 8 * d, (n >> 1) & 1u, ctl, status_code(kRoleFp4Store, 0, d))) break;
                 tc_fence_after_sync();
+                if (DIGITS && n == 0) grid_dependency_wait();     // before the first store; the kernel ahead is complete (it made what this tile was computed from)
                 ++n;
             }
             const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + d * kAccStep;
@@ -510,6 +512,7 @@ fp4_product_kernel(const __grid_constant__ CUtensorMap tmap_p, const __grid_cons
     // ---- sum over the slices of a tile (one tile per cluster: gridDim.x = split * tiles) --------------------------
     __syncwarp();
     if (CG == 1 && p.split > 1) {
+        if constexpr (DIGITS) grid_dependency_wait();             // (as above)
         cluster_arrive();
         cluster_wait();
         if (unit < total && !*abort_flag) {

@@ -213,6 +213,20 @@ __device__ __forceinline__ void grid_dependency_wait()
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
+// Reading ahead of one's own wait.  Kernel k + 2 may read what kernel k (or one before it) wrote ahead of its own grid_dependency_wait, if kernel k + 1 starts it only after its
+// wait for k.  The wait alone is documented to make writes visible, so what this rests on: when that wait returns, k has completed and its writes are visible to all of
+// k + 1, whichever SM its CTAs are on, so they are performed at the GPU's scope; k + 2 starts later; and it reads at that scope, by the loads below or by TMA after a
+// proxy fence, so that no line which an earlier kernel left in the SM's L1 answers.  (A few-token layer with all such reads behind the waits: 1 token 20.4 -> 25.7 us, 16 tokens
+// 48 -> 58; with a fence at the GPU's scope ahead of the start, which would order nothing but the starting CTA's own accesses, 50.)
+__device__ __forceinline__ uint32_t ld_older(const uint32_t *p)
+{
+    uint32_t v;
+    asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ int32_t ld_older(const int32_t *p) { return static_cast<int32_t>(ld_older(reinterpret_cast<const uint32_t *>(p))); }
+__device__ __forceinline__ float ld_older(const float *p) { return __uint_as_float(ld_older(reinterpret_cast<const uint32_t *>(p))); }
+
 // ---- cluster --------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t cluster_ctarank()

@@ -364,6 +364,46 @@ def test_steps_in_a_row(ctx, kind):
     assert ctx.last_device_status()[0] == hgemm.OK
 
 
+@pytest.mark.parametrize("kind", ["nvfp4", "mxfp4", "bf16", "f16"])
+@pytest.mark.parametrize("T,k", [(1, 1), (1, 4), (3, 2)])
+def test_steps_of_few_ctas(ctx, kind, T, k):
+    """Steps of launches that leave most SMs without a CTA, so that an SM sees the same places of memory again after steps that it had no part in: choices, weights and x change with
+    every step, launched one by one and replayed from a graph; the bits of steps that wait for each other."""
+    H, I, E, N = 72, 40, 16, 60
+    r = rng("few ctas", kind, T, k)
+    dt = torch.float16 if kind == "f16" else torch.bfloat16
+    w1, _ = weights_of(r, (E, 2 * I, H), kind)
+    w2, _ = weights_of(r, (E, H, I), kind)
+    layer = few_tokens.Layer(ctx, H, I, E, k, weights=kind, dtype=dt)
+    xs, ws = torch.from_numpy(r.standard_normal((N, T, H))).to(dt).cuda(), torch.from_numpy(r.random((N, T, k)).astype(np.float32)).cuda()
+    ids = torch.from_numpy(r.integers(-1, E, (N, T, k)).astype(np.int32)).cuda()
+    x, w, idx, scratch = torch.empty_like(xs[0]), torch.empty_like(ws[0]), torch.empty_like(ids[0]), layer.empty_scratch(T)
+    y = torch.empty_like(x)
+
+    def steps(launch, wait):
+        out = torch.empty_like(xs)
+        for n in range(N):
+            x.copy_(xs[n])
+            w.copy_(ws[n])
+            idx.copy_(ids[n])
+            wait()
+            launch()
+            wait()
+            out[n].copy_(y)
+        torch.cuda.synchronize()
+        return out
+
+    run = lambda: layer.run(x, w1, w2, idx, w, y, scratch)  # noqa: E731
+    want = steps(run, torch.cuda.synchronize)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for launch in (run, graph.replay):
+        for _ in range(3):
+            assert torch.equal(steps(launch, lambda: None), want)
+    assert ctx.last_device_status()[0] == hgemm.OK
+
+
 def test_no_tokens(ctx):
     layer = few_tokens.Layer(ctx, 64, 64, 2, 1, weights="bf16", dtype=torch.bfloat16, activation="silu")
     w = torch.zeros(2, 64, 64, dtype=torch.bfloat16, device="cuda")
