@@ -727,15 +727,6 @@ __device__ __forceinline__ uint32_t pack_e2m1(float a, float b, float c, float d
     return w;
 }
 
-// The values of eight e2m1 codes as pairs of fp16.
-// (Give it words all of which hold values: with a 16-bit load for w, its upper half known to be zero, everything came out as zeros.)
-__device__ __forceinline__ void unpack_e2m1(uint32_t w, uint32_t (&d)[4])
-{
-    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\tcvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
-        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3]) : "r"(w));
-}
-
 // ---- small helpers ------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t pack_half2_rn(uint32_t a_f32_bits, uint32_t b_f32_bits)

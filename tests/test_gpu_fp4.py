@@ -3,6 +3,7 @@
 Bytes that nothing may read hold patterns that would show (rows' ends, rows of other groups: the value 6 with scales of NaN), results sit inside
 guard bands; the quantiser is checked bit for bit, products by bounds that follow from the arithmetic (fp4_reference.product_bound) or exactly."""
 import ctypes
+import subprocess
 import zlib
 
 import numpy as np
@@ -12,7 +13,7 @@ import torch
 pytestmark = pytest.mark.gpu
 
 import fp4_reference as ref  # noqa: E402
-from paper_2512_02551_b200 import fp4, hgemm  # noqa: E402
+from paper_2512_02551_b200 import build, fp4, hgemm  # noqa: E402
 
 OUTS = [torch.float32, torch.float16, torch.bfloat16]
 FORMATS = ["nvfp4", "mxfp4"]
@@ -456,6 +457,42 @@ def test_quantise_far_beyond_the_factor(ctx, dtype, factor):
     fp4.quantize_both(ctx, x.cuda(), *both[0], *both[1], factor=f)
     check_copy(*both[0], x64.astype(np.float32), "nvfp4", factor, what="rows")
     check_copy(*both[1], np.ascontiguousarray(x64.T).astype(np.float32), "nvfp4", factor, what="columns")
+
+
+UNPACK = """
+#include "fp4_quantize_kernel.cuh"
+template <class T>
+__global__ void unpack(const T *in, uint32_t *out)
+{
+    constexpr int kBytes = static_cast<int>(sizeof(T));
+    uint32_t d[4];
+    hgemm_dev::unpack_e2m1(in[threadIdx.x], d);
+    for (int i = 0; i < kBytes; ++i) out[kBytes * threadIdx.x + i] = d[i];
+}
+extern "C" int run(int bytes, const void *in, uint32_t *out)
+{
+    if (bytes == 1) unpack<<<1, 256>>>(static_cast<const uint8_t *>(in), out);
+    else if (bytes == 2) unpack<<<1, 256>>>(static_cast<const uint16_t *>(in), out);
+    else unpack<<<1, 256>>>(static_cast<const uint32_t *>(in), out);
+    return cudaDeviceSynchronize();
+}
+"""
+
+
+def test_unpacking_words_of_which_a_part_is_known(tmp_path):
+    """Codes to values from loads of 8, 16 and 32 bits, as many values as were loaded: what the compiler knows about the rest of a word changes nothing."""
+    src, lib = tmp_path / "unpack.cu", tmp_path / "unpack.so"
+    src.write_text(UNPACK)
+    subprocess.run([build._nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-shared", "-Xcompiler", "-fPIC", "-I", build.CSRC, "-o", str(lib), str(src)], check=True)
+    fn = ctypes.CDLL(str(lib)).run
+    fn.argtypes = [ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p]
+    for n, dtype in ((1, np.uint8), (2, np.uint16), (4, np.uint32)):
+        words = rng("unpack", n).integers(0, 1 << (8 * n), 256).astype(dtype)
+        code = np.stack([(words.astype(np.uint64) >> np.uint64(4 * i)) & np.uint64(15) for i in range(2 * n)], -1).astype(np.uint8)
+        out = torch.empty(256, 2 * n, dtype=torch.float16, device="cuda")
+        given = torch.from_numpy(words.view(np.uint8).copy()).cuda()
+        assert fn(n, given.data_ptr(), out.data_ptr()) == 0
+        assert np.array_equal(ref.f64(out), ref.decode(code)), n
 
 
 @pytest.mark.parametrize("dtype", OUTS, ids=str)
