@@ -9,9 +9,11 @@
  * choices.  Weights are fp16 or bf16, of x's type, or 4-bit row copies with block scales (hgemm_fp4.h) with x of either type.
  *
  * All sums are in fp32, and the result is rounded once; a token's choices are added up in their order, so that results do not depend on scheduling.
- *     16-bit weights    two launches; x and the weights enter the products as they are, h to 16 bits of mantissa
- *     4-bit weights     five launches; the weights enter the products as they are, x and h as sums of 4-bit digits: off by at most 2^-19 of the token's (the
- *                       choice's) largest magnitude.  A NaN or an infinity in x makes its token's results NaN
+ *     16-bit weights    two launches; x and the weights enter the products as they are, h to 16 bits of mantissa (against fp16 weights too: the products of both second parts, 2^-16
+ *                       of the whole, are left out).  An infinity in x or in a weight makes the results that it reaches infinite or NaN
+ *     4-bit weights     five launches; the weights enter the products as they are, x and h as sums of 4-bit digits: off by at most 2^-19 (NVFP4) or 2^-22 (MXFP4) of the token's
+ *                       (the choice's) largest magnitude, or by 2^-127 where that is more.  With NVFP4 small elements beside a large one keep fewer bits: e4m3 scales
+ *                       end at 2^-9; MXFP4's lose no more than 2^-22 of their block's largest.  A NaN or an infinity in x makes its token's results NaN
  *
  * Choices with an index outside [0, experts) count as zero.  A token may choose an expert twice.
  *

@@ -7,9 +7,10 @@
 //     s_1 = the smallest power of two with max |v| <= 6 s_1 in the block;  digit d = e2m1(r_d / s_d);  r_{d+1} = r_d - digit * s_d
 //     s_2 = s_1 / 4 (|r_2| <= s_1: half the step below 6),  s_{d+1} = s_d / 8 (|r| <= s_d / 2: half the step below 4)
 //
-// Every step is exact, so that what is missing is the last remainder: at most s_8 / 2 = s_1 2^-21 (MX).  NV scales are e4m3, whose smallest is 2^-9, the last that a
-// block's digits have: values are scaled by a power of two for each choice, so that its largest s_1 is at most 2^8 and its largest magnitude above
-// 768; the remainder is at most 2^-10, less than 2^-19 of that.
+// Every step is exact, so that what is missing is the last remainder: at most s_8 / 2 = s_1 2^-21 (MX), less than 2^-22 of the block's largest magnitude, which is above 3 s_1.  NV scales
+// are e4m3, whose smallest is 2^-9, the last that a block's digits have: values are scaled by a power of two for each choice, so that its largest s_1 is 2^8 and its largest
+// magnitude above 768; the remainder is at most 2^-10, less than 2^-19 of that.  (So a block far below the largest has fewer digits, the largest seven.)  Where numbers near
+// fp32's smallest stop the scales (MX: 2^-126) or that power of two (NV: 2^-126), the remainder is at most 2^-127 and 2^-136.
 //
 // Choices are sorted by expert; choice number c lies at position[c], its digits in rows 8 position[c] .. + 7, their scales in tiles that begin anew for each
 // expert.  One CTA per choice makes its digits: from x, or from the first product by way of the activation.  Latency bounds these kernels: a few thousand elements each.

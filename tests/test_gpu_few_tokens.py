@@ -232,6 +232,88 @@ def test_threads_with_contexts_of_their_own():
     assert refused == [0, 0], f"refused calls of {N} each: {refused}"
 
 
+#: What is lost of x and h, as a part of their largest magnitude (digits: the remainder, see the header) or, for h of 16-bit weights, of itself (two roundings to bf16).
+LOST = {"nvfp4": 2.0 ** -19, "mxfp4": 2.0 ** -22, "bf16": 2.0 ** -16, "f16": 2.0 ** -16}
+
+
+def simple_weights(w, kind):
+    """What the call takes of a stack of -1, 0 and 1."""
+    if kind in DTYPE:
+        return torch.from_numpy(w).to(DTYPE[kind]).cuda()
+    packed = ref.pack(np.where(w < 0, 10, np.where(w > 0, 2, 0)).astype(np.uint8))
+    n = packed.shape[-1]
+    q = torch.from_numpy(np.pad(packed, ((0, 0), (0, 0), (0, -n % 16 + 16)))).cuda()[..., :n]
+    one = np.full((*w.shape[:-1], ref.blocks(w.shape[-1], kind)), 0x38 if kind == "nvfp4" else 127, np.uint8)
+    return (q, torch.from_numpy(ref.tiles_from(one, kind)).cuda(), *([torch.ones(w.shape[0], device="cuda")] if kind == "nvfp4" else []))
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+def test_neighbouring_values_keep_their_difference(ctx, kind, dtype):
+    """Results that are the small differences of nearly equal values of h, so that the last digits of h are all there is.  u = 1.5 + m 2^-16 with m < 16 is exact (one large and one
+    small element of x, weights of 1), and the gate the same throughout, so that h differs by silu(1.5) times u's differences but for a rounding of each (2^-24) and what is lost of
+    it; a common error of silu (2^-21 (2 + 1.5), see ``formula``) is one of the difference.  The sums are exact: two digits each, multiples of the last digit's step."""
+    r = rng("neighbours", kind, dtype)
+    H, I, T = 64, 96, 3
+    x = np.zeros((T, H))
+    x[:, 0] = 1.5
+    x[:, 32:] = r.integers(1, 16, (T, H - 32)) * 2.0 ** -16
+    w1, w2 = np.zeros((1, 2 * I, H)), np.zeros((1, H, I))
+    w1[0, :, 0] = 1
+    w1[0, np.arange(I, 2 * I), r.integers(32, H, I)] = 1
+    for n in range(H):
+        a, b = r.permutation(I)[:2]
+        w2[0, n, a], w2[0, n, b] = 1, -1
+    xs = torch.from_numpy(x).to(DTYPE[dtype])
+    assert np.array_equal(ref.f64(xs), x)
+    layer = few_tokens.Layer(ctx, H, I, 1, 1, weights=kind, dtype=DTYPE[dtype])
+    y = torch.empty(T, H, dtype=DTYPE[dtype], device="cuda")
+    layer.run(xs.cuda(), simple_weights(w1, kind), simple_weights(w2, kind), torch.zeros(T, 1, dtype=torch.int32, device="cuda"), torch.ones(T, 1, device="cuda"), y, layer.empty_scratch(T))
+    h = silu(1.5) * (x @ w1[0, I:].T)
+    want = h @ w2[0].T
+    check(y, want, 2 * (LOST[kind] + 2.0 ** -24) * np.abs(h).max() + 3.5 * 2.0 ** -21 * np.abs(want), f"{kind} {dtype}")
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("large", [2.0 ** 4, 2.0 ** 8, 2.0 ** 11])
+def test_small_values_beside_a_large_channel(ctx, kind, dtype, large):
+    """One element of x far larger than the others, which half of the rows of W1 do not look at: what the others keep."""
+    r = rng("large channel", kind, dtype, large)
+    T, H, I = 3, 192, 80
+    x = r.standard_normal((T, H))
+    x[:, 5] = large * (1 + r.random(T))
+    x = torch.from_numpy(x).to(DTYPE[dtype])
+    w1 = np.where(r.random((1, 2 * I, H)) < 0.3, r.choice([-1.0, 1.0], (1, 2 * I, H)), 0.0)
+    w1[0, :, 5] = r.random(2 * I) < 0.02
+    w2 = r.choice([-1.0, 0.0, 1.0], (1, H, I))
+    layer = few_tokens.Layer(ctx, H, I, 1, 1, weights=kind, dtype=DTYPE[dtype])
+    y = torch.empty(T, H, dtype=DTYPE[dtype], device="cuda")
+    weight = np.full((T, 1), 2.0 ** -8)
+    layer.run(x.cuda(), simple_weights(w1, kind), simple_weights(w2, kind), torch.zeros(T, 1, dtype=torch.int32, device="cuda"), torch.full((T, 1), 2.0 ** -8, device="cuda"), y,
+              layer.empty_scratch(T))
+    check(y, *formula(ref.f64(x), w1, w2, np.zeros((T, 1), int), weight, True, BITS[kind]), f"{kind} {dtype} {large}")
+
+
+@pytest.mark.parametrize("kind", ["nvfp4", "mxfp4"])
+@pytest.mark.parametrize("e", [100, 112, 118, 122])
+def test_digits_of_the_smallest_numbers(ctx, kind, e):
+    """Magnitudes near fp32's smallest: what is lost of x is at most 2^-127 where that is more than its part of the largest; the weights bring the results back."""
+    r = rng("smallest", kind, e)
+    T, H, I = 4, 80, 48
+    x = torch.from_numpy(r.standard_normal((T, H)) * 2.0 ** -e).bfloat16()
+    w1, w2 = r.choice([-1.0, 0.0, 1.0], (1, I, H)), r.choice([-1.0, 0.0, 1.0], (1, H, I))
+    m1 = list(simple_weights(w1, kind))
+    if kind == "nvfp4":
+        m1[2] = m1[2] * 2.0 ** 60
+    else:
+        m1[1] = torch.where(m1[1] == 127, 187, m1[1])               # scales of 2^60
+    layer = few_tokens.Layer(ctx, H, I, 1, 1, weights=kind, activation="silu")
+    y = torch.empty(T, H, dtype=torch.bfloat16, device="cuda")
+    layer.run(x.cuda(), tuple(m1), simple_weights(w2, kind), torch.zeros(T, 1, dtype=torch.int32, device="cuda"), torch.ones(T, 1, device="cuda"), y, layer.empty_scratch(T))
+    want, err = formula(ref.f64(x), w1 * 2.0 ** 60, w2, np.zeros((T, 1), int), np.ones((T, 1)), False, None)
+    err = err + 1.1 * 2.0 ** (60 - 127) * (np.abs(w2[0]) @ np.abs(w1[0]).sum(1)) * (e > 100)
+    check(y, want, err, f"{kind} 2^-{e}")
+
+
 def test_infinite_and_nan_inputs_stay_in_their_token(ctx):
     for kind, dtype in KINDS:
         r = rng(kind, dtype)
