@@ -183,6 +183,33 @@ def test_many_experts_and_rounds(ctx):
     case(ctx, "f16", "f16", 24, 512, 1024, 64, 4, False)
 
 
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("H", [4097, 4128, 4224, 5120, 8193])
+def test_long_hidden(ctx, kind, dtype, H):
+    """x in more pieces than one (16-bit weights: 4096 elements at a time, the last piece of less than a run of chunks among them), and longer than a pass of the threads that make digits."""
+    case(ctx, kind, dtype, 3, H, 72, 3, 2, H % 2 == 0)
+    case(ctx, kind, dtype, 10, H, 40, 2, 1, H % 2 == 1, *((1, 0), (2, 0), (8, 8))[H % 3])
+
+
+@pytest.mark.parametrize("kind,dtype,gated", [("bf16", "bf16", True), ("f16", "f16", False)])
+def test_long_hidden_in_several_rounds(ctx, kind, dtype, gated):
+    """More groups of rows than CTAs, in pieces: from round to round of one expert's tokens, on to the next's, and the rest shared."""
+    case(ctx, kind, dtype, 64, 4232, 640 if gated else 1280, 4, 4, gated, indices=rng("rounds", kind).integers(0, 4, (64, 4)))
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS[::2])
+def test_as_many_experts_as_there_may_be(ctx, kind, dtype):
+    r = rng("experts", kind)
+    case(ctx, kind, dtype, 64, 48, 24, 1024, 32, True, indices=r.integers(0, 1024, (64, 32)))
+    case(ctx, kind, dtype, 2, 48, 24, 1024, 3, False, indices=np.array([[1023, 0, 1023], [-1, 1022, 1024]]))
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS[::2])
+@pytest.mark.parametrize("H,I", [(5120, 1536), (7168, 512)])
+def test_widths_of_large_layers(ctx, kind, dtype, H, I):
+    case(ctx, kind, dtype, 4, H, I, 3, 2, True)
+
+
 FIRST_CALL = """
 import sys
 sys.path[:0] = %r
