@@ -56,6 +56,16 @@ class _Weights:
                 self.factor = torch.empty(w.shape[0], device="cuda")
         self.half = None
 
+    def __iter__(self):
+        """The copy that the forward product reads, as a call takes it: ``plan.run(*x, *weights, y)``."""
+        return iter(self.rows)
+
+    def __getitem__(self, i):
+        return self.rows[i]
+
+    def __len__(self) -> int:
+        return len(self.rows)
+
     def quantize(self, w) -> None:
         if self.operands == "fp8":
             fp8.quantize_tiles(self.ctx, w, *self.rows)
@@ -77,7 +87,7 @@ class _Weights:
 
 class ExpertLayer:
     """y[t] = sum over the chosen experts e of w[t,e] * silu(x[t] W1[e]^T) W2[e]^T, with buffers and plans for one number of tokens (``close``
-    give the plans back).  operands: "fp8", "nvfp4" or "mxfp4"."""
+    gives the plans back).  operands: "fp8", "nvfp4" or "mxfp4"."""
 
     def __init__(self, ctx, tokens: int, hidden: int, inner: int, experts: int, top_k: int, seed: int = 0, operands: str = "fp8"):
         if operands not in OPERANDS:
@@ -108,6 +118,9 @@ class ExpertLayer:
         self.da, self.dx_rows = new(R, I, dtype=bf16), new(R, H, dtype=bf16)
         self.dw1, self.dw2, self.dlogits = new(E, I, H), new(E, H, I), new(T, E, dtype=torch.float16)
         self.xq, self.aq, self.dyq, self.dhq = (_Copies(ctx, R, n, E, operands) for n in (H, I, H, I))
+        if operands == "fp8":                                                     # the 8-bit copies by names of their own: by rows and, per expert, by columns
+            self.x8, self.a8, self.dy8, self.dh8 = (c.rows for c in (self.xq, self.aq, self.dyq, self.dhq))
+            self.x8c, self.a8c, self.dy8c, self.dh8c = (c.cols for c in (self.xq, self.aq, self.dyq, self.dhq))
         self.few = few_tokens.Layer(ctx, H, I, E, top_k, weights="f16" if operands == "fp8" else operands, activation="silu", dtype=torch.float16)
         self.decode_plans, self.scratch = {}, None                                # made by the first decoding step
 

@@ -140,3 +140,19 @@ def test_refusals(ctx):
         with pytest.raises(ValueError):
             layer.decode(torch.zeros(65, 128, dtype=torch.float16, device="cuda"))
         assert layer.decode(torch.zeros(0, 128, dtype=torch.float16, device="cuda")).shape == (0, 128)
+
+
+def test_eight_bit_copies_by_their_names(ctx):
+    """The 8-bit copies and the weights' tiles as a program hands them to products of its own."""
+    x, dy = inputs()
+    with ExpertLayer(ctx, T, H, I, E, K, seed=5) as layer:
+        layer.forward(x)
+        layer.backward(dy)
+        h, dx_rows, dw2 = torch.empty_like(layer.h), torch.empty_like(layer.dx_rows), torch.empty_like(layer.dw2)
+        layer.up.run(*layer.x8, *layer.q1, h, offsets=layer.offsets)
+        layer.up_dx.run(*layer.dh8, *layer.q1, dx_rows, offsets=layer.offsets)
+        layer.down_dw.run(*layer.dy8c, *layer.a8c, dw2, offsets=layer.offsets)
+        assert torch.equal(h, layer.h) and torch.equal(dx_rows, layer.dx_rows) and torch.equal(dw2, layer.dw2)
+        values, scales = layer.q2
+        assert len(layer.q2) == 2 and layer.q2[0] is values and values.shape == (E, H, I)
+        assert all(len(c) == 2 for c in (layer.a8, layer.dy8, layer.x8c, layer.dh8c))
