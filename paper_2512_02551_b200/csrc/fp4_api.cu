@@ -445,9 +445,10 @@ hgemm_status_t hgemm_fp4_quantize(hgemm_ctx_t *ctx, const hgemm_fp4_quantize_t *
     p.col_rows = col_rows;
     p.row_tiles = ceil_div(d->rows, 128);
     const int64_t col_tiles = ceil_div(d->cols, 128), row_tiles = ceil_div(col_rows, 128);      // (per group: as many as the copy has room for)
-    // A CTA walks the offsets before its first tile; where that is worth sharing, it takes several tiles of its 128 rows: eight CTAs an SM in all (16384 x 2048 bf16, both copies;
-    // two an SM, eight, one a tile: 32 groups 83, 38, 34 us; 256 groups 102, 72, 90; 1024 groups 251, 251, 497).
-    const int64_t per_row = d->offsets ? std::min(col_tiles, std::max<int64_t>(1, int64_t(ctx->num_sms) * 8 / row_tiles)) : col_tiles;
+    // A CTA walks the offsets before its first tile.  Beyond 64 groups that is worth sharing: it takes several tiles of its 128 rows, eight CTAs an SM in all.  Up to there one CTA a tile,
+    // whose rounds end more evenly (both copies in nvfp4, bf16; eight an SM against one a tile: 16384 x 2048, 32 groups 42.5 and 38.6 us, 64 47.5 and 44.0, 128 53.2 and 55.9,
+    // 256 76 and 93, 1024 269 and 505; 8192 x 7168, 32 groups 78 and 72, 96 93 and 101; 2048 x 4096, 32 groups 21.8 and 17.9, 96 53 and 51, 256 127 and 150).
+    const int64_t per_row = d->groups > 64 ? std::min(col_tiles, std::max<int64_t>(1, int64_t(ctx->num_sms) * 8 / row_tiles)) : col_tiles;
     const void *fn = d->x_type == HGEMM_TYPE_F32 ? quantize_kernel<float>(d->blocks, d->format) : d->x_type == HGEMM_TYPE_F16 ? quantize_kernel<__half>(d->blocks, d->format)
                                                                                                                              : quantize_kernel<__nv_bfloat16>(d->blocks, d->format);
     const int smem = hgemm_dev::fp4_quant_smem(es, nv, by_cols);
@@ -470,7 +471,8 @@ hgemm_status_t hgemm_fp4_dequantize(hgemm_ctx_t *ctx, int32_t format, int32_t ou
     const int es = type_bytes(out_type);
     if (!q || !scales || !out || !aligned16(q) || !aligned16(scales) || (reinterpret_cast<uintptr_t>(out) % unsigned(es)) != 0) return HGEMM_ERR_INVALID_ARG;
     const int64_t col_tiles = ceil_div(cols, 128), row_tiles = ceil_div(offsets ? hgemm_fp8_padded_rows(rows, groups) : rows, 128);
-    // As in the quantiser: one tile a CTA, several of one row tile where it walks the offsets first (32, 256, 1024 groups: 17, 22, 57 us; one a tile 16, 39, 225).
+    // One tile a CTA; several of one row tile where it walks the offsets first, eight CTAs an SM in all (16384 x 2048, eight an SM against one a tile: 1 group 16.1 and 16.5 us, 16
+    // 16.3 and 17.3, 32 17.7 and 17.6, 128 22 and 26, 256 26 and 43, 1024 60 and 230; 2048 x 4096, 32 groups 8.4 and 7.7, 64 10.7 and 12.3).
     const int64_t walkers = offsets ? std::min(col_tiles, std::max<int64_t>(1, int64_t(ctx->num_sms) * 8 / row_tiles)) : col_tiles;
     if (row_tiles * walkers > 0x7fffffff) return HGEMM_ERR_UNSUPPORTED;       // (a grid's limit)
     hgemm_dev::Fp4DequantParams p;

@@ -580,6 +580,35 @@ def test_quantise_per_group(ctx, fmt, dtype, offsets):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("E", [64, 65, 100])
+def test_quantise_many_groups_of_wide_rows(ctx, fmt, E):
+    """More column tiles than CTAs share a row tile: with many groups each walks on to further ones."""
+    M, C = 1300, 2700
+    r = rng(fmt, E, "many")
+    x = source(r, M, C, torch.bfloat16, odd=False)
+    x32 = ref.f64(x).astype(np.float32)
+    off = np.concatenate([[0], np.sort(r.integers(0, M + 1, E - 1)), [M]])
+    start, room = starts_of(off), fp4.padded_rows(M, E)
+    f, factor = (torch.tensor([0.5], device="cuda"), 0.5) if fmt == "nvfp4" else (None, None)
+    given = torch.tensor(off, dtype=torch.int32, device="cuda")
+    row, col = empty_copy((M, C), (room, C), fmt), empty_copy((C, room), (C, room), fmt)
+    fp4.quantize_both(ctx, x.cuda(), *row, *col, factor=f, format=fmt, offsets=given)
+    atoms = 4 * ref.BLOCK[fmt]
+    for g in range(E):
+        n = off[g + 1] - off[g]
+        if n:
+            end = start[g] + (n + 127) // 128 * 128
+            check_copy(row[0][off[g]:off[g + 1]], row[1][start[g] // 128:end // 128], x32[off[g]:off[g + 1]], fmt, factor, what=f"rows of group {g}")
+            wide = np.zeros((C, end - start[g]), np.float32)
+            wide[:, :n] = x32[off[g]:off[g + 1]].T
+            check_copy(col[0][:, start[g] // 2:end // 2], col[1][:, start[g] // atoms:end // atoms], wide, fmt, factor, what=f"columns of group {g}")
+    out = torch.empty(M, C, device="cuda")
+    fp4.dequantize(ctx, *row, out, factor=f, format=fmt, offsets=given)
+    places = np.concatenate([start[g] + np.arange(off[g + 1] - off[g]) for g in range(E)])
+    assert np.array_equal(ref.f64(out), ref.values(row[0], row[1], C, fmt, 0.5 if factor else 1.0, places))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_stacks(ctx, fmt):
     """A stack of weights: each matrix with its own factor; copies, and back."""
     G, R, C = 5, 130, 72
