@@ -204,6 +204,37 @@ def test_as_many_experts_as_there_may_be(ctx, kind, dtype):
     case(ctx, kind, dtype, 2, 48, 24, 1024, 3, False, indices=np.array([[1023, 0, 1023], [-1, 1022, 1024]]))
 
 
+@pytest.mark.parametrize("kind", ["bf16", "nvfp4", "mxfp4"])
+def test_stacks_beyond_32_bits(ctx, kind):
+    """Stacks of more than 2^31 elements (16-bit) or bytes (4-bit); the last experts, the first and one between are chosen."""
+    E, H, I, k, gated = (600, 2048, 1800, 3, False) if kind == "bf16" else (1024, 2048, 1100, 3, True)
+    chosen = np.array([[E - 1, 0, E // 2], [E - 2, E - 1, 1]])
+    g = torch.Generator(device="cuda").manual_seed(3)
+    held, values = [], []
+    for shape in ((E, 2 * I if gated else I, H), (E, H, I)):
+        K = shape[-1]
+        if kind == "bf16":
+            w = torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+            for e in np.unique(chosen):
+                w[e] = (torch.randn(shape[1:], generator=g, device="cuda") * K ** -0.5).bfloat16()
+            held.append(w)
+            values.append({e: ref.f64(w[e]) for e in np.unique(chosen)})
+        else:
+            n = -(-K // 2)
+            q = torch.randint(0, 256, (*shape[:-1], -(-n // 16) * 16), dtype=torch.uint8, generator=g, device="cuda")[..., :n]
+            tiles = torch.randint(*((0x28, 0x40) if kind == "nvfp4" else (118, 124)), fp4._scales_shape(shape, kind), dtype=torch.uint8, generator=g, device="cuda")
+            held.append((q, tiles, torch.full((E,), 0.0625, device="cuda")) if kind == "nvfp4" else (q, tiles))
+            values.append({e: ref.values(q[e], tiles[e], K, kind, 0.0625 if kind == "nvfp4" else 1.0) for e in np.unique(chosen)})
+        assert max(t.numel() for t in ([held[-1]] if kind == "bf16" else held[-1][:1])) > (1 << 31 if len(held) == 1 else 1 << 30)
+    x = torch.randn(2, H, generator=g, device="cuda").bfloat16()
+    weights = torch.rand(2, k, generator=g, device="cuda")
+    layer = few_tokens.Layer(ctx, H, I, E, k, weights=kind, activation="swiglu" if gated else "silu")
+    y = torch.empty_like(x)
+    layer.run(x, *held, torch.tensor(chosen, dtype=torch.int32, device="cuda"), weights, y, layer.empty_scratch(2))
+    order = np.unique(chosen)                                      # the formula on the chosen ones alone
+    check(y, *formula(ref.f64(x), np.stack([values[0][e] for e in order]), np.stack([values[1][e] for e in order]), np.searchsorted(order, chosen), ref.f64(weights), gated, BITS[kind]), kind)
+
+
 @pytest.mark.parametrize("kind,dtype", KINDS[::2])
 @pytest.mark.parametrize("H,I", [(5120, 1536), (7168, 512)])
 def test_widths_of_large_layers(ctx, kind, dtype, H, I):
