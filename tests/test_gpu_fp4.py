@@ -768,6 +768,72 @@ def test_large_stacks_of_weights(ctx):
             ref.check_product(out, a.values, w.values)
 
 
+def test_large_results(ctx):
+    """Results of more than 2^31 elements: a matrix, and a stack of gradients whose last ones have rows."""
+    M, N, K = 70000, 40008, 64
+    r = rng("large result")
+    a, b = Operand(r, (M, K), "nvfp4"), Operand(r, (N, K), "nvfp4")
+    out = torch.full((M, N), float("nan"), dtype=torch.bfloat16, device="cuda")
+    at = np.concatenate([np.arange(3), r.integers(0, M, 20), np.arange(M - 40, M)])
+    for config in ((2, 256, 1), (2, 128, 1), (1, 128, 1)):
+        with fp4.Plan(ctx, M, N, K) as plan:
+            plan.set_config(*config)
+            plan.run(a.q, a.tiles, b.q, b.tiles, out, a_factor=a.factor, b_factor=b.factor)
+            assert plan.last_device_status()[0] == hgemm.OK
+        ref.check_product(out[torch.from_numpy(at).cuda()], a.values[at], b.values, str(config))
+        assert not bool(torch.isnan(out).any())
+        out.fill_(float("nan"))
+    del out
+    E, N, K = 600, 2000, 2056
+    counts = np.zeros(E, np.int64)
+    counts[[0, 1, 598, 599]] = 5, 130, 100, 70
+    offsets = np.concatenate([[0], np.cumsum(counts)])
+    M, start = int(offsets[-1]), starts_of(offsets)
+    room = fp4.padded_rows(M, E)
+    a, b = Operand(r, (N, room), "mxfp4"), Operand(r, (K, room), "mxfp4")
+    own = np.zeros(room, bool)
+    for e in np.flatnonzero(counts):
+        own[start[e]:start[e] + counts[e]] = True
+    for o in (a, b):                                               # columns of no row: zeros with scales of their own
+        c = ref.codes(o.q, room).copy()
+        c[:, ~own] = 0
+        o.q, o.values = on_gpu(ref.pack(c), 16), o.values * own
+    out = torch.full((E, N, K), float("nan"), dtype=torch.bfloat16, device="cuda")
+    for config in ((2, 256, 1), (1, 64, 1)):
+        with fp4.Plan(ctx, M, N, K, form="weight_grad", groups=E, format="mxfp4") as plan:
+            plan.set_config(*config)
+            plan.run(a.q, a.tiles, b.q, b.tiles, out, offsets=torch.tensor(offsets, dtype=torch.int32, device="cuda"))
+            assert plan.last_device_status()[0] == hgemm.OK
+        for e in (0, 1, 598, 599):
+            at = slice(start[e], start[e] + counts[e])
+            ref.check_product(out[e], a.values[:, at], b.values[:, at], f"{config} {e}")
+        assert float(out[2:598].abs().max()) == 0
+        out.fill_(float("nan"))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_quantise_beyond_32_bits(ctx, fmt):
+    """A matrix of more than 2^31 elements, both ways; its corners."""
+    R, C = 66000, 33000
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn(R, C, dtype=torch.bfloat16, generator=g, device="cuda")
+    f = torch.full((1,), 2.0 ** -8, device="cuda") if fmt == "nvfp4" else None
+    factor = 2.0 ** -8 if fmt == "nvfp4" else None
+    row, col = fp4.empty_rows(R, C, format=fmt), fp4.empty_cols(R, C, format=fmt)
+    fp4.quantize_both(ctx, x, *row, *col, factor=f, format=fmt)
+    top, left = R // 128 * 128, C // 128 * 128                      # where the last tiles begin
+    check_copy(row[0][top:], row[1][top // 128:], ref.f64(x[top:]).astype(np.float32), fmt, factor)
+    check_copy(col[0][left:], col[1][left // 128:], ref.f64(x[:, left:].t().contiguous()).astype(np.float32), fmt, factor)
+    back = torch.empty_like(x)
+    fp4.dequantize(ctx, *row, back, factor=f, format=fmt)
+    want = ref.values(row[0][top:], row[1][top // 128:], C, fmt, 1.0 if factor is None else factor)
+    assert np.array_equal(ref.f64(back[top:]), ref.f64(torch.from_numpy(want).bfloat16()))
+    if f is not None:
+        x[-1, -1] = 3000.0
+        fp4.tensor_factor(ctx, x, f)
+        assert f.item() == 2.0
+
+
 # ---- refusals ----------------------------------------------------------------------------------------
 
 def test_refusals(ctx):
