@@ -14,9 +14,9 @@
 //
 // Choices are sorted by expert; choice number c lies at position[c], its digits in rows 8 position[c] .. + 7, their scales in tiles that begin anew for each
 // expert.  One CTA per choice makes its digits: from x, or from the first product by way of the activation.  Latency bounds these kernels: a few thousand elements each.
-// The products start beside them and fetch their first weights meanwhile.  Measured (2048 -> 1024 -> 2048, SwiGLU, nvfp4, 8 of 64 experts): 1 token 16.5 us, of which the digits
+// The products start beside them and fetch their first weights meanwhile.  Measured (2048 -> 1024 -> 2048, SwiGLU, nvfp4, 8 of 64 experts): 1 token 16.9 us in a graph, of which the digits
 // of x take 3.6, the first product's rest 3.7, the digits of h 2.5, the second product's rest 3.4, the sum 1.1, and 1 passes between one's end and the next's reading; 16 tokens
-// 47.5 us, 4.2 TB/s.  With all their runs of four elements unrolled the digits took 5.7 and 2.7 us: a launch fetches its instructions anew.
+// 48.2 us, 4.1 TB/s.  With all their runs of four elements unrolled the digits took 5.7 and 2.7 us: a launch fetches its instructions anew.
 #pragma once
 
 #include <cuda_bf16.h>

@@ -1,15 +1,16 @@
 // A layer of experts with 16-bit weights for a few tokens: W1 and the activation in one launch, W2 and the weighted sum over a token's choices in another.
 // (4-bit weights: few_digits_kernel.cuh.)
 //
-// Bound by the chosen experts' weights, read once from memory for a handful of multiply-adds (5 tokens, 4 of 32 experts, 2048 -> 1000 -> 2048, bf16: 34 us, 3.7 TB/s; a
+// Bound by the chosen experts' weights, read once from memory for a handful of multiply-adds (5 tokens, 4 of 32 experts, 2048 -> 1000 -> 2048, bf16: 34.4 us in a graph, 3.7 TB/s, 35-38 a call; a
 // launch's start, its list of choices and its last tiles take some 6 us each).  They go from memory to registers (16 bytes a lane, four
 // chunks of two rows in flight at any time) and from there to mma.sync: a warp's 16 rows of a weight matrix are the operand that fills the instruction's
 // rows, up to 8 choices of the expert are its columns.  A lane takes 16 consecutive bytes of its row, four lanes 64 (a chunk): which k a lane holds is free as
 // long as both operands agree.  (Tensor memory and a ring of shared-memory stages would lengthen the way of rows that start anywhere: tensor copies
 // need rows at multiples of 16 bytes.)
 //
-// h is the sum of two bf16 (16 bits of mantissa, in bf16's range).  Against it an fp16 weight is the sum of two bf16 too, and of the four products that of both
-// second parts, 2^-16 of the whole, is left out.
+// h is the sum of two bf16 (16 bits of mantissa, in bf16's range: fp16 would not hold every h, one bf16 would round it as coarsely as y).  What that loses, 2^-16 of each h, is small beside
+// y's own rounding (2^-8 or 2^-11), and a third part would be half as much again to write, read and multiply.  Against h an fp16 weight is the sum of two bf16 too, and of the
+// four products that of both second parts, 2^-16 of the whole, is left out for the same reason.
 //
 // Work.  Launch 1: a warp has a tile of 16 rows (SWIGLU: 8 rows of each half, whose products meet in one lane), a CTA eight tiles of one expert, whose
 // tokens it lays out in shared memory as the instruction wants them.  As many rounds as give every CTA the same; the groups of tiles that are left over are

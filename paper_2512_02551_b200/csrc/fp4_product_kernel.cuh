@@ -19,10 +19,11 @@
 // Products over groups: see product_tiles.cuh.  A group's scale tiles start at a tile boundary wherever its rows start.  Weight gradients contract
 // over a group's rows, which the column copy pads with zeros to multiples of 128; a stage's second half is left out where the group ends.
 //
-// What it reaches (B200, bf16 results, nvfp4): 8192^3 190-197 us, 5.6-5.8 PFLOP/s; 1000 x 4096 x 4096 (mxfp4) 10.0 us, one round of 64 tiles, of which 5 are start and
-// end; a gradient of 4096 x 2000 weights over 8000 rows 38-44 us (128 tiles on 74 pairs, fp32 stores); 7 x 8192 x 4096 7.3 us and 512 rows over 64 experts
-// (2048 x 1024 each way) 28.5 us, 5.4 TB/s of weights. At 8192^3 the tensor
-// pipe is active 80 % of the time at 1.5 GHz (the power cap); small calls are bound by their start and end, about 5 us.
+// What it reaches (B200, bf16 results, nvfp4): 8192^3 225 us in calls one after the other, 4.9 PFLOP/s, and 192 in bursts of 24 launches, before the power cap takes hold;
+// 1000 x 4096 x 4096 (mxfp4) 10.3 us, one round of 64 tiles, of which 5 are start and end; a gradient of 4096 x 2000 weights over 8000 rows 37-42 us (128 tiles on 74 pairs: two
+// rounds for 1.7 rounds' work); 7 x 8192 x 4096 7.3 us and 512 rows over 64 experts (2048 x 2048 each) 28.5-30 us, 5.1-5.4 TB/s of weights.  At 8192^3 the tensor pipe is
+// active 80 % of the time at 1.5 GHz; small calls are bound by their start and end, about 5 us; short contractions by the ends of their tiles (a gradient of 2048 x 2048 weights over
+// 1024 rows for each of 32 experts, bf16: 83 us, 3 a tile of four stages, for which the tensor pipe needs 1.1).
 //
 // Every mbarrier wait is bounded (see hgemm_device.cuh): a wait that runs out raises the status word and the CTA's abort flag, and
 // every role falls through to the common teardown.

@@ -1,9 +1,10 @@
 // 4-bit quantisation with one scale per block of 16 (e4m3, and a factor for the tensor) or 32 (a power of two) along rows, along columns, or both
 // in one pass; the tensor's factor; and the way back.
 //
-// Bytes: 2 or 4 read and a half (both copies: one) written per element; what bounds it is instructions, ten per quantised element (8191 x 4096 bf16, both copies:
-// 34 us, 3.1 TB/s, 61 % of the issue slots; the factor before it 14 us, 4.8 TB/s; back to bf16 16 us along rows, 5.4 TB/s, and 23 us along columns,
-// whose rows of 8191 start at every second byte).  256 threads own a tile of 128 x 128 elements.  As it is
+// Bytes: 2 or 4 read and a half (both copies: one) written per element.  Ten instructions per quantised element, and too few warps to issue them at every cycle: three CTAs of 77 registers
+// an SM keep 34 % of its warps, and 61 % of the issue slots are used (8191 x 4096 bf16, both copies: 35 us, 3.0 TB/s; 2048 tiles are 4.6 rounds; four CTAs an SM spilled).  The
+// factor before it takes 14 us, 4.8 TB/s, waiting for loads; back to bf16 17 us along rows, 5.1 TB/s, and 25 us along columns,
+// whose rows of 8191 start at every second byte.  256 threads own a tile of 128 x 128 elements.  As it is
 // loaded, 8 lanes hold a row's 128 elements, 16 each: a block, or half of one, whose maximum needs at most one shuffle.  For the column copy
 // the tile goes to shared memory as it came; there a thread takes 32 rows of two columns (16-bit types) or of one (fp32, twice), so that
 // blocks lie in registers again, and the packed columns and their scale tiles leave through shared memory in runs of 64 and 1024 bytes.
